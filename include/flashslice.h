@@ -261,6 +261,65 @@ fs_status fs_coupling_bwd(const fs_shape* s, const void* x_mid, const void* fx,
                           float* dW, float* dbias, float* dtau, float* dM, int accumulate,
                           void* ws, size_t ws_bytes, fs_stream_t stream);
 
+/* ---- Layer norm and 8-bit checkpoints of point features ----------------------------------
+ *
+ * The original layer normalises the residual stream before the coupling's projections
+ * (Sec. 2 "The Transolver layer"), and a training step keeps its activations for the
+ * backward pass.  These calls work on `rows` rows of C channels (the B*N points' C = H*d
+ * features; or the B*H*G tokens' d channels), dense and row-major, in the dtype of the
+ * fs_rows; gamma, beta, mean, rstd and their gradients are fp32.
+ *
+ * An 8-bit checkpoint of x [rows, C] is q8 [rows, C] (int8) with e8 [rows, ceil(C / 32)]
+ * (uint8): each block of 32 channels of a row (the last one may be shorter) is kept as
+ * x ~ q 2^s with e8 = s + 127, where s >= -126 is the smallest that brings the block's
+ * largest magnitude to at most 127; q is rounded to nearest, ties to even, so each value is
+ * off by at most half a step, 2^(s-1) <= 2^-6.99 of the block's largest magnitude (or 2^-127).
+ * A block that holds NaN or infinity has e8 = 255 and restores to NaN.  The values are exact
+ * in both dtypes.
+ *
+ * Supported: rows >= 1, C in [1, 8192], rows*C < 2^40.  Pointers as above: device,
+ * 16-byte aligned, asynchronous on `stream`.  Outputs may not share a byte with an input or
+ * another output, except where a call says so (FS_ERR_INVALID). */
+typedef struct fs_rows {
+  int64_t rows;  /* >= 1 */
+  int32_t C;     /* channels of a row, 1..8192 */
+  int32_t dtype; /* fs_dtype of the rows */
+} fs_rows;
+
+/* Layer norm of v = x + res over each row's channels:
+ *   y = (v - mean) rstd gamma + beta,  rstd = 1 / sqrt(var + eps)  (var over C, biased)
+ *   res: NULL for v = x.  With it v is rounded to the dtype, and that value is normalised.
+ *   sum: NULL, or receives v (only with res; may be x or res itself: the stream in place).
+ *   gamma, beta [C]: NULL stands for 1 and 0.  mean, rstd [rows]: NULL to leave them out.
+ *   q8, e8: both NULL, or receive v's 8-bit checkpoint.
+ * One kernel: each input is read once, each output written once. */
+fs_status fs_norm_fwd(const fs_rows* s, const void* x, const void* res, const float* gamma,
+                      const float* beta, float eps, void* sum, void* y, float* mean, float* rstd,
+                      int8_t* q8, uint8_t* e8, fs_stream_t stream);
+
+/* Backward of fs_norm_fwd given dy: with xh = (v - mean) rstd and g = dy gamma,
+ *   dv = rstd (g - avg_c(g) - xh avg_c(g xh)) + dres,  dgamma = sum_rows dy xh,
+ *   dbeta = sum_rows dy.
+ *   v: the normalised rows, or NULL and their checkpoint q8, e8 (xh is then formed from the
+ *   values that it stands for).  mean, rstd: the forward's.
+ *   dres: NULL, or the gradient that reaches v along the residual stream.
+ *   dv may be dy or dres itself.  dv is the gradient of x and of res.
+ *   dgamma, dbeta: both NULL, or written (accumulate == 0) or added to (accumulate != 0).
+ * ws: fs_norm_workspace_bytes(s). */
+fs_status fs_norm_bwd(const fs_rows* s, const void* v, const int8_t* q8, const uint8_t* e8,
+                      const float* gamma, const float* mean, const float* rstd, const void* dy,
+                      const void* dres, void* dv, float* dgamma, float* dbeta, int accumulate,
+                      void* ws, size_t ws_bytes, fs_stream_t stream);
+
+/* Bytes of scratch that fs_norm_bwd needs on the current device; 0 for invalid or
+ * unsupported rows. */
+size_t fs_norm_workspace_bytes(const fs_rows* s);
+
+/* x into its 8-bit checkpoint (q8, e8), and back into the values that it stands for. */
+fs_status fs_ckpt_pack(const fs_rows* s, const void* x, int8_t* q8, uint8_t* e8, fs_stream_t stream);
+fs_status fs_ckpt_unpack(const fs_rows* s, const int8_t* q8, const uint8_t* e8, void* x,
+                         fs_stream_t stream);
+
 /* Fixed-scratch variant of fs_slice_fwd.  The paper has no counterpart.
  *
  * For callers that cannot give the library device memory at the call site: a

@@ -1,12 +1,12 @@
 // C ABI of the library: host-side validation, workspace layout, kernel dispatch.
 // Declarations and the contract of every entry point: include/flashslice.h.
+#include "fs_check.h"
 #include "fs_simt_tiles.h"
 #include "fs_tc.h"
 
 #include <algorithm>
 #include <cmath>
 #include <cstring>
-#include <initializer_list>
 
 namespace fs {
 
@@ -63,30 +63,6 @@ bool supported_shape(const fs_shape* s) {
 }
 
 Shape to_shape(const fs_shape* s) { return Shape{s->B, s->N, s->H, s->d, s->G, s->dtype, s->eps, s->dot}; }
-
-bool aligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
-// A byte range [p, p + n) of a caller buffer.
-struct Span {
-  const void* p;
-  size_t n;
-};
-// True when two ranges share a byte.
-bool overlap(Span a, Span b) {
-  const uintptr_t a0 = reinterpret_cast<uintptr_t>(a.p), b0 = reinterpret_cast<uintptr_t>(b.p);
-  return a.n && b.n && a0 < b0 + b.n && b0 < a0 + a.n;
-}
-// The out-of-place calls (the mixes and their backward) read every input while
-// they write: no output may share a byte with an input or with another output.
-bool disjoint(std::initializer_list<Span> ins, std::initializer_list<Span> outs) {
-  for (const Span& o : outs) {
-    for (const Span& i : ins)
-      if (overlap(o, i)) return false;
-    for (const Span& o2 : outs)
-      if (&o2 != &o && overlap(o, o2)) return false;
-  }
-  return true;
-}
 
 // Byte sizes of the regions each op places in `ws` (each 256-byte aligned).
 struct Regions {
@@ -181,8 +157,6 @@ fs_status check_ws(const Shape& s, int op, void* ws, size_t ws_bytes) {
   return FS_OK;
 }
 
-fs_status cuda_status(cudaError_t e) { return e == cudaSuccess ? FS_OK : FS_ERR_CUDA; }
-
 // Every ws-using call writes its status word anew: the first of its kernels that knows the
 // temperatures does (`reset`), so that no memset breaks the chain of kernels.
 
@@ -216,17 +190,6 @@ cudaError_t backward_stats(const Shape& sh, const void* x_mid, const float* W_sl
   do {                                                  \
     if (!valid_shape(s)) return FS_ERR_INVALID;         \
     if (!supported_shape(s)) return FS_ERR_UNSUPPORTED; \
-  } while (0)
-
-#define FS_CHECK_PTR(p)                                      \
-  do {                                                       \
-    if (!(p) || !aligned(p)) return FS_ERR_INVALID;          \
-  } while (0)
-
-#define FS_CUDA(call)                                          \
-  do {                                                         \
-    cudaError_t e_ = (call);                                   \
-    if (e_ != cudaSuccess) return FS_ERR_CUDA;                 \
   } while (0)
 
 }  // namespace

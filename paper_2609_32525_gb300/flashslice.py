@@ -35,12 +35,17 @@ EXPORTED = ("fs_workspace_bytes", "fs_slice_fwd", "fs_slice_finalize", "fs_mix",
             "fs_deslice_bwd", "fs_mix_bwd", "fs_slice_bwd", "fs_device_status", "fs_status_string",
             "fs_path_for_shape", "fs_backward_path_for_shape", "fs_forward_launch_count", "fs_backward_launch_count",
             "fs_slice_fwd_noalloc", "fs_slice_fwd_lse", "fs_mix_channels", "fs_mix_channels_bwd", "fs_stats",
-            "fs_coupling_bwd", "fs_coupling_bwd_launch_count")
+            "fs_coupling_bwd", "fs_coupling_bwd_launch_count", "fs_norm_fwd", "fs_norm_bwd",
+            "fs_norm_workspace_bytes", "fs_ckpt_pack", "fs_ckpt_unpack")
 
 
 class fs_shape(ctypes.Structure):
     _fields_ = [("B", ctypes.c_int64), ("N", ctypes.c_int64), ("H", ctypes.c_int32), ("d", ctypes.c_int32),
                 ("G", ctypes.c_int32), ("dtype", ctypes.c_int32), ("eps", ctypes.c_float), ("dot", ctypes.c_int32)]
+
+
+class fs_rows(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("C", ctypes.c_int32), ("dtype", ctypes.c_int32)]
 
 
 class FlashSliceError(RuntimeError):
@@ -53,6 +58,8 @@ _P = ctypes.c_void_p
 _S = ctypes.POINTER(fs_shape)
 _I = ctypes.c_int
 _Z = ctypes.c_size_t
+_F = ctypes.c_float
+_R = ctypes.POINTER(fs_rows)
 _sig = {
     "fs_workspace_bytes": (_Z, [_S, _I]),
     "fs_slice_fwd": (_I, [_S, _P, _P, _P, _P, _P, _P, _P, _P, _I, _P, _Z, _P]),
@@ -74,6 +81,11 @@ _sig = {
     "fs_backward_launch_count": (_I, [_S, _I]),
     "fs_coupling_bwd_launch_count": (_I, [_S, _I]),
     "fs_coupling_bwd": (_I, [_S] + [_P] * 11 + [_P] * 8 + [_I, _P, _Z, _P]),
+    "fs_norm_fwd": (_I, [_R] + [_P] * 4 + [_F] + [_P] * 7),
+    "fs_norm_bwd": (_I, [_R] + [_P] * 11 + [_I, _P, _Z, _P]),
+    "fs_norm_workspace_bytes": (_Z, [_R]),
+    "fs_ckpt_pack": (_I, [_R, _P, _P, _P, _P]),
+    "fs_ckpt_unpack": (_I, [_R, _P, _P, _P, _P]),
     "fs_slice_fwd_noalloc": (_I, [_S, _P, _P, _P, _P, _P, _P, _P, _P, _I, ctypes.POINTER(_P), _P]),
 }
 for _name, (_res, _args) in _sig.items():
@@ -246,6 +258,113 @@ def fs_slice_fwd_noalloc(shape, x_mid, fx, W_slice, bias, tau, tokens, wsum, lse
 def device_status_at(addr: int, stream=None) -> int:
     """fs_device_status of a scratch given by its device address."""
     return int(_lib.fs_device_status(_P(addr), _stream(stream)))
+
+
+# ---- layer norm and 8-bit checkpoints -----------------------------------------------------
+#
+# These calls know the size and type of every argument, so they check each tensor here: a
+# wrong one raises ValueError before the library sees a pointer.
+
+
+def _arg(fn, name, t, dtype, numel, stream, optional=False):
+    if t is None:
+        if optional:
+            return None
+        raise ValueError(f"{fn}: {name} is missing")
+    if t.dtype != dtype or t.numel() != numel:
+        raise ValueError(f"{fn}: {name} has {t.numel()} values of {t.dtype}, expected {numel} of {dtype}")
+    if not t.is_contiguous():
+        raise ValueError(f"{fn}: {name} must be contiguous")
+    if not t.is_cuda or t.device.index != torch.cuda.current_device() or (
+            stream is not None and stream.device != t.device):
+        raise ValueError(f"{fn}: {name} is on {t.device}, the call on the current device and its stream")
+    return ctypes.c_void_p(t.data_ptr())
+
+
+def make_rows(rows, C, dtype=FS_F32) -> fs_rows:
+    """rows rows of C channels in dtype (a torch.dtype or FS_F32 / FS_BF16)."""
+    if isinstance(dtype, torch.dtype):
+        if dtype not in (torch.float32, torch.bfloat16):
+            raise ValueError(f"rows are float32 or bfloat16, not {dtype}")
+        dtype = FS_BF16 if dtype == torch.bfloat16 else FS_F32
+    return fs_rows(int(rows), int(C), int(dtype))
+
+
+def rows_of(x: torch.Tensor, C=None) -> fs_rows:
+    """The rows of x: its last dimension's channels, or C of them (the last dimensions together)."""
+    C = x.shape[-1] if C is None else C
+    return make_rows(x.numel() // C, C, x.dtype)
+
+
+def _row_sizes(r):
+    dt = torch.bfloat16 if r.dtype == FS_BF16 else torch.float32
+    return dt, r.rows * r.C, r.rows * ((r.C + 31) // 32)
+
+
+def checkpoint(rows: fs_rows, device="cuda"):
+    """Buffers (q8, e8) of an 8-bit checkpoint of these rows."""
+    return (torch.empty(rows.rows, rows.C, dtype=torch.int8, device=device),
+            torch.empty(rows.rows, (rows.C + 31) // 32, dtype=torch.uint8, device=device))
+
+
+def norm_workspace_bytes(rows: fs_rows) -> int:
+    return int(_lib.fs_norm_workspace_bytes(ctypes.byref(rows)))
+
+
+def norm_workspace(rows: fs_rows, device="cuda") -> torch.Tensor:
+    """Scratch for fs_norm_bwd."""
+    ws = torch.empty(max(16, norm_workspace_bytes(rows)), dtype=torch.uint8, device=device)
+    ws[:16].zero_()
+    return ws
+
+
+def fs_norm_fwd(rows, x, res, gamma, beta, eps, sum, y, mean, rstd, q8=None, e8=None, stream=None):
+    fn, f32 = "fs_norm_fwd", torch.float32
+    dt, n, nb = _row_sizes(rows)
+
+    def a(name, t, d, k, optional=True):
+        return _arg(fn, name, t, d, k, stream, optional)
+
+    st = _lib.fs_norm_fwd(ctypes.byref(rows), a("x", x, dt, n, False), a("res", res, dt, n),
+                          a("gamma", gamma, f32, rows.C), a("beta", beta, f32, rows.C), float(eps),
+                          a("sum", sum, dt, n), a("y", y, dt, n, False), a("mean", mean, f32, rows.rows),
+                          a("rstd", rstd, f32, rows.rows), a("q8", q8, torch.int8, n), a("e8", e8, torch.uint8, nb),
+                          _stream(stream))
+    _check(fn, st)
+
+
+def fs_norm_bwd(rows, v, q8, e8, gamma, mean, rstd, dy, dres, dv, dgamma, dbeta, accumulate, ws, stream=None):
+    fn, f32 = "fs_norm_bwd", torch.float32
+    dt, n, nb = _row_sizes(rows)
+
+    def a(name, t, d, k, optional=True):
+        return _arg(fn, name, t, d, k, stream, optional)
+
+    st = _lib.fs_norm_bwd(ctypes.byref(rows), a("v", v, dt, n), a("q8", q8, torch.int8, n),
+                          a("e8", e8, torch.uint8, nb), a("gamma", gamma, f32, rows.C),
+                          a("mean", mean, f32, rows.rows, False), a("rstd", rstd, f32, rows.rows, False),
+                          a("dy", dy, dt, n, False), a("dres", dres, dt, n), a("dv", dv, dt, n, False),
+                          a("dgamma", dgamma, f32, rows.C), a("dbeta", dbeta, f32, rows.C), int(bool(accumulate)),
+                          a("ws", ws, torch.uint8, ws.numel(), False), ws.numel(), _stream(stream))
+    _check(fn, st)
+
+
+def fs_ckpt_pack(rows, x, q8, e8, stream=None):
+    fn = "fs_ckpt_pack"
+    dt, n, nb = _row_sizes(rows)
+    st = _lib.fs_ckpt_pack(ctypes.byref(rows), _arg(fn, "x", x, dt, n, stream),
+                           _arg(fn, "q8", q8, torch.int8, n, stream), _arg(fn, "e8", e8, torch.uint8, nb, stream),
+                           _stream(stream))
+    _check(fn, st)
+
+
+def fs_ckpt_unpack(rows, q8, e8, x, stream=None):
+    fn = "fs_ckpt_unpack"
+    dt, n, nb = _row_sizes(rows)
+    st = _lib.fs_ckpt_unpack(ctypes.byref(rows), _arg(fn, "q8", q8, torch.int8, n, stream),
+                             _arg(fn, "e8", e8, torch.uint8, nb, stream), _arg(fn, "x", x, dt, n, stream),
+                             _stream(stream))
+    _check(fn, st)
 
 
 # ---- convenience: one coupling, buffers allocated through torch ----------------------------
