@@ -261,6 +261,74 @@ fs_status fs_coupling_bwd(const fs_shape* s, const void* x_mid, const void* fx,
                           float* dW, float* dbias, float* dtau, float* dM, int accumulate,
                           void* ws, size_t ws_bytes, fs_stream_t stream);
 
+/* ---- Self-attention of the slice tokens --------------------------------------------------
+ *
+ * The token operation of the original layer (Sec. 2, "The Transolver layer"; the "baseline"
+ * of the Sec. 3 variants table), in place of fs_mix: the core of Eq. (1) depends on the
+ * tokens.  q, k, v are the tokens' projections (fs_mix_channels makes them).  Per batch b
+ * and head h, with key head h / (H / Hkv), query i and key j:
+ *
+ *   s_ij = scale q_i . k_j
+ *   c_ij = cap tanh(s_ij / cap)  if cap > 0, else s_ij           capped scores
+ *   a_ij = c_ij - slopes[h] |pos_q[b,i] - pos_k[b,j]|            distance bias
+ *   a masked pair has weight 0
+ *   lse_i = log sum_j exp(a_ij),  p_ij = exp(a_ij - lse_i),  out_i = sum_j p_ij v_j
+ *
+ * Masks (a pair is seen if every mask in use allows it):
+ *   documents: doc_q[b,i] == doc_k[b,j] and doc_k[b,j] >= 0.  Tokens of several bodies or
+ *     samples share a batch entry this way, in any order; a negative number marks a token
+ *     that is not in use (a slot that no point fills).
+ *   FS_MASK_PREFIX: key j <= i + (Gk - Gq), or j < prefix[b] (NULL: 0, each query sees its
+ *     own and earlier keys).  The queries are the last Gq of the Gk tokens; Gq <= Gk.
+ * A query that sees no key (or only keys with a score of -infinity) has out = 0, lse =
+ * -infinity and gradients 0.  What masked tokens hold, NaN and infinities included, reaches
+ * no result of a query or key that does not see them.
+ *
+ * Everything is fp32: [B, H, Gq, d] for q, out, dout, dq; [B, Hkv, Gk, d] for k, v, dk, dv;
+ * lse [B, H, Gq].  The products run on the tensor cores with every operand split into two
+ * tf32 parts (2^-22 relative), accumulation is fp32.  Hkv divides H; heads that share a key
+ * head have their dk and dv summed.  Supported: d in {16, 32, 64}; Gk and (H / Hkv) Gq up to
+ * 2^20; B*H <= 65535; B*H*max(Gq, Gk)*d < 2^40.  No output may share a byte with an input or
+ * another output (FS_ERR_INVALID). */
+typedef enum fs_mask { FS_MASK_NONE = 0, FS_MASK_PREFIX = 1 } fs_mask;
+
+typedef struct fs_attn_shape {
+  int64_t B;    /* batch size, >= 1 */
+  int32_t H;    /* query heads */
+  int32_t Hkv;  /* key and value heads, divides H */
+  int32_t Gq;   /* queries per head */
+  int32_t Gk;   /* keys per head */
+  int32_t d;    /* head width, 16, 32 or 64 */
+  int32_t mask; /* fs_mask */
+  float scale;  /* finite */
+  float cap;    /* >= 0; 0: scores are not capped */
+} fs_attn_shape;
+
+/* Device pointers, each may be NULL; the struct itself is read on the host during the call. */
+typedef struct fs_attn_mask {
+  const float* slopes;  /* [H]: the distance bias; constants, no gradient */
+  const float* pos_q;   /* [B, Gq], with slopes and pos_k only; NULL: i + (Gk - Gq) */
+  const float* pos_k;   /* [B, Gk]; NULL: j */
+  const int32_t* doc_q; /* [B, Gq], together with doc_k */
+  const int32_t* doc_k; /* [B, Gk] */
+  const int32_t* prefix; /* [B], under FS_MASK_PREFIX only */
+} fs_attn_mask;
+
+/* mask may be NULL (no bias, no documents).  ws: fs_attn_workspace_bytes(s, 0). */
+fs_status fs_attn_fwd(const fs_attn_shape* s, const float* q, const float* k, const float* v,
+                      const fs_attn_mask* mask, float* out, float* lse, void* ws, size_t ws_bytes,
+                      fs_stream_t stream);
+
+/* Gradients for dout, with out and lse of the forward; all overwritten.
+ * ws: fs_attn_workspace_bytes(s, 1). */
+fs_status fs_attn_bwd(const fs_attn_shape* s, const float* q, const float* k, const float* v,
+                      const fs_attn_mask* mask, const float* out, const float* lse,
+                      const float* dout, float* dq, float* dk, float* dv, void* ws,
+                      size_t ws_bytes, fs_stream_t stream);
+
+/* Bytes of scratch on the current device; 0 for an invalid or unsupported shape. */
+size_t fs_attn_workspace_bytes(const fs_attn_shape* s, int backward);
+
 /* ---- Layer norm and 8-bit checkpoints of point features ----------------------------------
  *
  * The original layer normalises the residual stream before the coupling's projections

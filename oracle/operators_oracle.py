@@ -96,6 +96,8 @@ def attention(q, k, v, scale, cap=0.0, slopes=None, pos_q=None, pos_k=None, doc_
                     pk = at.astype(np.float64) if pos_k is None else pos_k[b, at].astype(np.float64)
                     a = a - float(slopes[h]) * np.abs(pq - pk)
                 top = a.max()
+                if top == -np.inf:  # no key has any weight
+                    continue
                 p = np.exp(a - top) if np.isfinite(top) else np.full(len(at), np.nan)
                 lse[b, h, i] = top + np.log(p.sum())
                 p = p / p.sum()

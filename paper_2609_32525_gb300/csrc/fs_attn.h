@@ -1,0 +1,42 @@
+// Attention of the slice tokens (internal declarations).
+#pragma once
+
+#include <cuda_runtime.h>
+#include <cstdint>
+
+namespace fs {
+
+// One call, in the kernels' terms.  The heads that share a key head form a unit (b, kv head);
+// their query rows lie one after another in memory, so a unit has rows = (H / Hkv) Gq rows and
+// row r is query r % Gq of the unit's head r / Gq.
+struct AttnArgs {
+  const float *q, *k, *v;        // [units, rows, d], [units, Gk, d]
+  const float *slopes;           // [H] or null
+  const float *pos_q, *pos_k;    // [B, Gq], [B, Gk] or null
+  const int *doc_q, *doc_k;      // [B, Gq], [B, Gk] or null
+  const int *prefix;             // [B] or null (0)
+  float *out, *lse;              // forward: written; backward: read
+  const float *dout;
+  float *dq, *dk, *dv;
+  float *delta;                  // [units, rows]
+  float *part;                   // partial results of the splits
+  float *part_kv;
+  uint32_t *status;
+  int B, H, Hkv, Gq, Gk, rows, units;
+  int causal;                    // the prefix mask
+  int warps;                     // per block: 16 rows each
+  int splits, splits_kv;         // of the keys (forward, dq), of the rows (dk, dv)
+  float scale, cap;
+};
+
+// Warps per block and splits (of the keys; of the query rows for dk and dv) for a shape on the
+// current device.
+struct AttnPlan {
+  int warps, splits, splits_kv;
+};
+AttnPlan attn_plan(int64_t units, int64_t rows, int64_t Gk, int d, bool backward);
+
+cudaError_t attn_fwd(const AttnArgs& a, int d, cudaStream_t st);
+cudaError_t attn_bwd(const AttnArgs& a, int d, cudaStream_t st);
+
+}  // namespace fs

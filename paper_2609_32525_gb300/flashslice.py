@@ -29,6 +29,7 @@ FS_OK, FS_ERR_INVALID, FS_ERR_UNSUPPORTED, FS_ERR_CUDA, FS_ERR_TIMEOUT, FS_ERR_B
 FS_NOALLOC_SCRATCH_BYTES = 16 << 20
 FS_F32, FS_BF16 = 0, 1
 FS_DOT_BF16, FS_DOT_BF16X2 = 0, 1
+FS_MASK_NONE, FS_MASK_PREFIX = 0, 1
 FS_OP_SLICE_FWD, FS_OP_DESLICE_FWD, FS_OP_DESLICE_BWD, FS_OP_SLICE_BWD, FS_OP_STATS, FS_OP_COUPLING_BWD = range(6)
 
 EXPORTED = ("fs_workspace_bytes", "fs_slice_fwd", "fs_slice_finalize", "fs_mix", "fs_deslice_fwd",
@@ -36,7 +37,8 @@ EXPORTED = ("fs_workspace_bytes", "fs_slice_fwd", "fs_slice_finalize", "fs_mix",
             "fs_path_for_shape", "fs_backward_path_for_shape", "fs_forward_launch_count", "fs_backward_launch_count",
             "fs_slice_fwd_noalloc", "fs_slice_fwd_lse", "fs_mix_channels", "fs_mix_channels_bwd", "fs_stats",
             "fs_coupling_bwd", "fs_coupling_bwd_launch_count", "fs_norm_fwd", "fs_norm_bwd",
-            "fs_norm_workspace_bytes", "fs_ckpt_pack", "fs_ckpt_unpack")
+            "fs_norm_workspace_bytes", "fs_ckpt_pack", "fs_ckpt_unpack", "fs_attn_fwd", "fs_attn_bwd",
+            "fs_attn_workspace_bytes")
 
 
 class fs_shape(ctypes.Structure):
@@ -46,6 +48,15 @@ class fs_shape(ctypes.Structure):
 
 class fs_rows(ctypes.Structure):
     _fields_ = [("rows", ctypes.c_int64), ("C", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+
+class fs_attn_shape(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int64)] + [(n, ctypes.c_int32) for n in ("H", "Hkv", "Gq", "Gk", "d", "mask")] + [
+        ("scale", ctypes.c_float), ("cap", ctypes.c_float)]
+
+
+class fs_attn_mask(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("slopes", "pos_q", "pos_k", "doc_q", "doc_k", "prefix")]
 
 
 class FlashSliceError(RuntimeError):
@@ -60,6 +71,8 @@ _I = ctypes.c_int
 _Z = ctypes.c_size_t
 _F = ctypes.c_float
 _R = ctypes.POINTER(fs_rows)
+_A = ctypes.POINTER(fs_attn_shape)
+_M = ctypes.POINTER(fs_attn_mask)
 _sig = {
     "fs_workspace_bytes": (_Z, [_S, _I]),
     "fs_slice_fwd": (_I, [_S, _P, _P, _P, _P, _P, _P, _P, _P, _I, _P, _Z, _P]),
@@ -81,6 +94,9 @@ _sig = {
     "fs_backward_launch_count": (_I, [_S, _I]),
     "fs_coupling_bwd_launch_count": (_I, [_S, _I]),
     "fs_coupling_bwd": (_I, [_S] + [_P] * 11 + [_P] * 8 + [_I, _P, _Z, _P]),
+    "fs_attn_fwd": (_I, [_A, _P, _P, _P, _M, _P, _P, _P, _Z, _P]),
+    "fs_attn_bwd": (_I, [_A, _P, _P, _P, _M, _P, _P, _P, _P, _P, _P, _P, _Z, _P]),
+    "fs_attn_workspace_bytes": (_Z, [_A, _I]),
     "fs_norm_fwd": (_I, [_R] + [_P] * 4 + [_F] + [_P] * 7),
     "fs_norm_bwd": (_I, [_R] + [_P] * 11 + [_I, _P, _Z, _P]),
     "fs_norm_workspace_bytes": (_Z, [_R]),
@@ -260,9 +276,9 @@ def device_status_at(addr: int, stream=None) -> int:
     return int(_lib.fs_device_status(_P(addr), _stream(stream)))
 
 
-# ---- layer norm and 8-bit checkpoints -----------------------------------------------------
+# ---- argument checks ----------------------------------------------------------------------
 #
-# These calls know the size and type of every argument, so they check each tensor here: a
+# The calls below know the size and type of every argument, so they check each tensor here: a
 # wrong one raises ValueError before the library sees a pointer.
 
 
@@ -278,7 +294,81 @@ def _arg(fn, name, t, dtype, numel, stream, optional=False):
     if not t.is_cuda or t.device.index != torch.cuda.current_device() or (
             stream is not None and stream.device != t.device):
         raise ValueError(f"{fn}: {name} is on {t.device}, the call on the current device and its stream")
-    return ctypes.c_void_p(t.data_ptr())
+    return t.data_ptr()
+
+
+# ---- token attention ----------------------------------------------------------------------
+
+
+def make_attn_shape(B, H, G, d, Hkv=None, Gk=None, scale=None, cap=0.0, prefix=False) -> fs_attn_shape:
+    """G query tokens and Gk (default G) key tokens per head; Hkv (default H) key heads; scale
+    defaults to 1 / sqrt(d); cap 0 for none; prefix: the prefix mask (FS_MASK_PREFIX)."""
+    return fs_attn_shape(int(B), int(H), int(H if Hkv is None else Hkv), int(G), int(G if Gk is None else Gk), int(d),
+                         FS_MASK_PREFIX if prefix else FS_MASK_NONE,
+                         float(d ** -0.5 if scale is None else scale), float(cap))
+
+
+class attn_mask:
+    """The optional tensors of an attention call: slopes [H], pos_q [B, Gq] and pos_k [B, Gk] (float32);
+    doc_q, doc_k, prefix [B] (int32)."""
+
+    def __init__(self, slopes=None, pos_q=None, pos_k=None, doc_q=None, doc_k=None, prefix=None):
+        self.slopes, self.pos_q, self.pos_k = slopes, pos_q, pos_k
+        self.doc_q, self.doc_k, self.prefix = doc_q, doc_k, prefix
+
+
+def _attn_mask(fn, s, m, stream):
+    if m is None:
+        return None
+    f, i, nq, nk = torch.float32, torch.int32, s.B * s.Gq, s.B * s.Gk
+
+    def a(name, d, n):
+        return _arg(fn, name, getattr(m, name), d, n, stream, True)
+
+    return ctypes.byref(fs_attn_mask(a("slopes", f, s.H), a("pos_q", f, nq), a("pos_k", f, nk), a("doc_q", i, nq),
+                                     a("doc_k", i, nk), a("prefix", i, s.B)))
+
+
+def attn_workspace_bytes(shape: fs_attn_shape, backward=False) -> int:
+    return int(_lib.fs_attn_workspace_bytes(ctypes.byref(shape), int(bool(backward))))
+
+
+def attn_workspace(shape: fs_attn_shape, backward=False, device="cuda") -> torch.Tensor:
+    """Scratch of fs_attn_fwd, or of fs_attn_bwd."""
+    ws = torch.empty(max(16, attn_workspace_bytes(shape, backward)), dtype=torch.uint8, device=device)
+    ws[:16].zero_()
+    return ws
+
+
+def fs_attn_fwd(shape, q, k, v, mask, out, lse, ws, stream=None):
+    """mask: an attn_mask, or None."""
+    fn, s = "fs_attn_fwd", shape
+    nq, nk = s.B * s.H * s.Gq, s.B * s.Hkv * s.Gk * s.d
+
+    def a(name, t, n):
+        return _arg(fn, name, t, torch.float32, n, stream)
+
+    st = _lib.fs_attn_fwd(ctypes.byref(s), a("q", q, nq * s.d), a("k", k, nk), a("v", v, nk),
+                          _attn_mask(fn, s, mask, stream), a("out", out, nq * s.d), a("lse", lse, nq),
+                          _arg(fn, "ws", ws, torch.uint8, ws.numel(), stream), ws.numel(), _stream(stream))
+    _check(fn, st)
+
+
+def fs_attn_bwd(shape, q, k, v, mask, out, lse, dout, dq, dk, dv, ws, stream=None):
+    fn, s = "fs_attn_bwd", shape
+    nq, nk = s.B * s.H * s.Gq, s.B * s.Hkv * s.Gk * s.d
+
+    def a(name, t, n):
+        return _arg(fn, name, t, torch.float32, n, stream)
+
+    st = _lib.fs_attn_bwd(ctypes.byref(s), a("q", q, nq * s.d), a("k", k, nk), a("v", v, nk),
+                          _attn_mask(fn, s, mask, stream), a("out", out, nq * s.d), a("lse", lse, nq),
+                          a("dout", dout, nq * s.d), a("dq", dq, nq * s.d), a("dk", dk, nk), a("dv", dv, nk),
+                          _arg(fn, "ws", ws, torch.uint8, ws.numel(), stream), ws.numel(), _stream(stream))
+    _check(fn, st)
+
+
+# ---- layer norm and 8-bit checkpoints -----------------------------------------------------
 
 
 def make_rows(rows, C, dtype=FS_F32) -> fs_rows:
