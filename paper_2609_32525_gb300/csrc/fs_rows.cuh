@@ -77,6 +77,13 @@ __device__ __forceinline__ RawV<T, VE> from_float(const float (&f)[VE]) {
 template <int TPR>
 __host__ __device__ constexpr int block_threads() { return TPR <= 32 ? 256 : TPR; }
 
+// Rows whose loads a thread issues before it uses the first.
+template <int K>
+__host__ __device__ constexpr int rows_ahead() { return K == 1 ? 2 : 1; }
+// Blocks of the backward on an SM: by its registers, for narrow threads.
+template <int TPR, int N>
+__host__ __device__ constexpr int bwd_blocks_per_sm() { return TPR <= 32 && N <= 8 ? 3 : 1; }
+
 // The sum over a row's TPR threads, in every one of them, in a fixed order.
 template <int TPR>
 __device__ __forceinline__ float row_sum(float v, float* red) {
@@ -110,40 +117,192 @@ __device__ __forceinline__ float inverse_scale_of(uint32_t byte) {  // 2^-s; 0 f
   return __uint_as_float(byte == 255u ? 0u : (254u - byte) << 23);
 }
 
-// Quantises a vector of a row; the 32 / VE neighbouring lanes that share a block agree on its
-// scale.  All lanes of the warp call it.
-template <int VE>
-__device__ __forceinline__ void quantise(const float (&f)[VE], uint32_t& byte, RawV<uint8_t, VE>& q) {
-  uint32_t top = 0;
-#pragma unroll
-  for (int i = 0; i < VE; i++) top = max(top, __float_as_uint(f[i]) & 0x7fffffffu);
-#pragma unroll
-  for (int o = kCkptBlock / VE / 2; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-  byte = scale_byte(top);
-  const float inv = inverse_scale_of(byte);
-  uint8_t b[VE];
-#pragma unroll
-  for (int i = 0; i < VE; i++) b[i] = (uint8_t)(int8_t)__float2int_rn(byte == 255u ? 0.f : f[i] * inv);
-  memcpy(&q, b, sizeof(q));
+// Two fp32 values in one instruction: these passes are close to the issue rate.
+struct F2 {
+  unsigned long long v;
+};
+__device__ __forceinline__ F2 pair(float a, float b) {
+  F2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b));
+  return r;
 }
+__device__ __forceinline__ void split(F2 x, float& a, float& b) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(x.v));
+}
+__device__ __forceinline__ F2 operator+(F2 a, F2 b) {
+  F2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+__device__ __forceinline__ F2 operator*(F2 a, F2 b) {
+  F2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+__device__ __forceinline__ F2 fma(F2 a, F2 b, F2 c) {
+  F2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+  return r;
+}
+__device__ __forceinline__ float total(F2 x) {
+  float a, b;
+  split(x, a, b);
+  return a + b;
+}
+
+// A thread's N channels of a row as pairs; an odd last one is paired with 0.
+template <int N>
+struct Vals {
+  static constexpr int P = (N + 1) / 2;
+  F2 p[P];
+};
+template <typename T, int VE, int K>
+__device__ __forceinline__ Vals<K * VE> vals_of(const RawV<T, VE> (&r)[K]) {
+  Vals<K * VE> o;
+  float f[K * VE + 1];
+  f[K * VE] = 0.f;
+#pragma unroll
+  for (int k = 0; k < K; k++) to_float<T, VE>(r[k], *reinterpret_cast<float(*)[VE]>(f + k * VE));
+#pragma unroll
+  for (int i = 0; i < o.P; i++) o.p[i] = pair(f[2 * i], f[2 * i + 1]);
+  return o;
+}
+template <int N>
+__device__ __forceinline__ void floats_of(const Vals<N>& v, float (&f)[2 * Vals<N>::P]) {
+#pragma unroll
+  for (int i = 0; i < v.P; i++) split(v.p[i], f[2 * i], f[2 * i + 1]);
+}
+
+// |a|, |b|, |c|: the largest; NaN if one is.
+__device__ __forceinline__ float max_abs(float a, float b, float c) {
+  float r;
+  asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+
+// Quantises a vector of a row; the 32 / VE neighbouring lanes that share a block agree on its
+// scale.  All lanes of the warp call it.  Adding 1.5 2^23 rounds to whole numbers, ties to
+// even, and leaves them in the low byte.
+template <int VE>
+__device__ __forceinline__ void quantise(const float* f, uint32_t& byte, RawV<uint8_t, VE>& q) {
+  float m = 0.f;
+#pragma unroll
+  for (int i = 0; i < VE; i += 2) m = max_abs(m, f[i], VE > 1 ? f[i + 1] : 0.f);
+#pragma unroll
+  for (int o = kCkptBlock / VE / 2; o > 0; o >>= 1) m = max_abs(m, __shfl_xor_sync(0xffffffffu, m, o), 0.f);
+  byte = scale_byte(__float_as_uint(m));
+  const float inv = inverse_scale_of(byte);
+  uint32_t u[VE];
+#pragma unroll
+  for (int i = 0; i < VE; i++)
+    u[i] = byte == 255u ? 0u : __float_as_uint(fmaf(f[i], inv, 12582912.f));
+  if constexpr (VE >= 4) {
+    uint32_t w[VE / 4];
+#pragma unroll
+    for (int i = 0; i < VE / 4; i++)
+      w[i] = __byte_perm(__byte_perm(u[4 * i], u[4 * i + 1], 0x0040), __byte_perm(u[4 * i + 2], u[4 * i + 3], 0x0040),
+                         0x5410);
+    memcpy(&q, w, sizeof(q));
+  } else {
+    uint8_t b[VE];
+#pragma unroll
+    for (int i = 0; i < VE; i++) b[i] = (uint8_t)u[i];
+    memcpy(&q, b, sizeof(q));
+  }
+}
+// A byte with its sign bit flipped is q + 128; as the low byte of 2^23 it is exact in fp32.
 template <int VE>
 __device__ __forceinline__ void restore(const RawV<uint8_t, VE>& q, uint32_t byte, float (&f)[VE]) {
   const float size = scale_of(byte);
-  int8_t b[VE];
-  memcpy(b, &q, sizeof(q));
+  if constexpr (VE >= 4) {
+    uint32_t w[VE / 4];
+    memcpy(w, &q, sizeof(q));
 #pragma unroll
-  for (int i = 0; i < VE; i++) f[i] = (float)b[i] * size;
+    for (int i = 0; i < VE; i++) {
+      const uint32_t u = w[i / 4] ^ 0x80808080u;
+      f[i] = (__uint_as_float(__byte_perm(u, 0x4b000000u, 0x7440 + i % 4)) - 8388736.f) * size;
+    }
+  } else {
+    int8_t b[VE];
+    memcpy(b, &q, sizeof(q));
+#pragma unroll
+    for (int i = 0; i < VE; i++) f[i] = (float)b[i] * size;
+  }
 }
 
-// Rows in flight per thread: four vectors' loads are issued before the first is used.
-template <int K>
-__host__ __device__ constexpr int rows_ahead() { return K >= 4 ? 1 : 4 / K; }
+// ---- rows on their way -------------------------------------------------------------------------
+//
+// What bounds these passes is memory bandwidth, and what keeps them from it is latency: a row's
+// two sums depend on its loads, one on the other.  So every thread fetches the vectors of its
+// next rows with cp.async into slots of shared memory that it alone reads: several rows are on
+// their way at no cost in registers, and no barrier is needed.  (With the next rows in
+// registers instead, 118 of them, 1,048,576 rows of 256 bf16 channels took 315 us in the plain
+// forward, against 270 us with one row at a time.)
+
+// N bytes from global to this thread's slot, zeros where !ok (src is then any valid address).
+template <int N>
+__device__ __forceinline__ void fetch(void* dst, const void* src, bool ok) {
+  if constexpr (N >= 4) {
+    const uint32_t d = (uint32_t)__cvta_generic_to_shared(dst);
+    const int n = ok ? N : 0;
+    if constexpr (N == 16)
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(d), "l"(src), "r"(n) : "memory");
+    else
+      asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(d), "l"(src), "n"(N), "r"(n) : "memory");
+  } else {  // below cp.async's smallest size
+    using R = typename Raw<N>::type;
+    *static_cast<R*>(dst) = ok ? *static_cast<const R*>(src) : R(0);
+  }
+}
+__device__ __forceinline__ void fetch_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void fetch_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// A thread's slots for one stage: element (k, thread) of a [K][THREADS] array of R.
+template <typename R, int THREADS>
+__device__ __forceinline__ R* slot(char* base, int k) {
+  return reinterpret_cast<R*>(base) + k * THREADS + threadIdx.x;
+}
+// Stages: up to 64 KB of slots per block (8 stages of bf16 rows of 256 channels: plain forward
+// 181 us, 4 stages 189 us), two at least.
+template <int BYTES, int THREADS>
+__host__ __device__ constexpr int stages() {
+  constexpr int fit = 65536 / (BYTES * THREADS);
+  return fit >= 8 ? 8 : fit <= 2 ? 2 : fit;
+}
+
+// gamma or beta of a thread's channels; `none` where it is null and past C.
+template <int N, int VE, int TPR>
+__device__ __forceinline__ Vals<N> channels_of(const float* p, int C, int t, float none) {
+  Vals<N> o;
+  float f[N + 1];
+  f[N] = none;
+#pragma unroll
+  for (int i = 0; i < N; i++) {
+    const int c = (i / VE * TPR + t) * VE + i % VE;
+    f[i] = p && c < C ? p[c] : none;
+  }
+#pragma unroll
+  for (int i = 0; i < o.P; i++) o.p[i] = pair(f[2 * i], f[2 * i + 1]);
+  return o;
+}
 
 // kNorm: the layer norm, with the residual sum and the checkpoint where asked; else the
 // checkpoint alone.
 template <typename T, int VE, int TPR, int K, bool kNorm>
+struct Fwd {
+  static constexpr int THREADS = block_threads<TPR>(), NB = VE * (int)sizeof(T);
+  static constexpr int BYTES = K * NB * (kNorm ? 2 : 1);  // a thread's slots of a stage
+  static constexpr int S = stages<BYTES, THREADS>();
+  static constexpr size_t SMEM = (size_t)BYTES * THREADS * S;
+};
+
+template <typename T, int VE, int TPR, int K, bool kNorm>
 __global__ void __launch_bounds__(block_threads<TPR>()) k_rows_fwd(const RowsArgs args) {
-  constexpr int RPB = block_threads<TPR>() / TPR, RU = rows_ahead<K>();
+  using F = Fwd<T, VE, TPR, K, kNorm>;
+  constexpr int THREADS = F::THREADS, RPB = THREADS / TPR, S = F::S;
+  using R = RawV<T, VE>;
+  extern __shared__ __align__(16) char slots[];
   __shared__ float red[32];
   RowsArgs a = args;
   grid_begin(a.x, a.res, a.gamma, a.beta);
@@ -151,96 +310,116 @@ __global__ void __launch_bounds__(block_threads<TPR>()) k_rows_fwd(const RowsArg
   const T* res = static_cast<const T*>(a.res);
   const int t = threadIdx.x % TPR, rb = threadIdx.x / TPR;
   const int C = a.C, nb = (C + kCkptBlock - 1) / kCkptBlock;
-  float gm[K][VE], bt[K][VE];
-  if constexpr (kNorm) {
+  const int64_t groups = (a.rows + RPB - 1) / RPB;
+  auto issue = [&](int64_t group, int stage) {
+    const int64_t row = group * RPB + rb;
+    char* base = slots + (size_t)stage * F::BYTES * THREADS;
 #pragma unroll
-    for (int k = 0; k < K; k++)
-#pragma unroll
-      for (int i = 0; i < VE; i++) {
-        const int c = (k * TPR + t) * VE + i;
-        gm[k][i] = a.gamma && c < C ? a.gamma[c] : 1.f;
-        bt[k][i] = a.beta && c < C ? a.beta[c] : 0.f;
-      }
-  }
-  const float invC = 1.f / (float)C;
-  for (int64_t r0 = (int64_t)blockIdx.x * (RPB * RU); r0 < a.rows; r0 += (int64_t)gridDim.x * (RPB * RU)) {
-    RawV<T, VE> xr[RU][K], rr[RU][K];
-#pragma unroll
-    for (int u = 0; u < RU; u++) {
-      const int64_t row = r0 + u * RPB + rb;
-#pragma unroll
-      for (int k = 0; k < K; k++) {
-        const int c = (k * TPR + t) * VE;
-        const bool ok = row < a.rows && c < C;
-        xr[u][k] = ok ? *reinterpret_cast<const RawV<T, VE>*>(x + row * C + c) : raw_zero<RawV<T, VE>>();
-        if (kNorm && res)
-          rr[u][k] = ok ? *reinterpret_cast<const RawV<T, VE>*>(res + row * C + c) : raw_zero<RawV<T, VE>>();
-      }
+    for (int k = 0; k < K; k++) {
+      const int c = (k * TPR + t) * VE;
+      const bool ok = row < a.rows && c < C;
+      const int64_t at = ok ? row * C + c : 0;
+      fetch<F::NB>(slot<R, THREADS>(base, k), x + at, ok);
+      if (kNorm && res) fetch<F::NB>(slot<R, THREADS>(base, K + k), res + at, ok);
     }
+  };
+  int64_t next = blockIdx.x;
 #pragma unroll
-    for (int u = 0; u < RU; u++) {
-      const int64_t row = r0 + u * RPB + rb;
-      const bool here = row < a.rows;
-      float v[K][VE];
-      float s = 0.f;
+  for (int s = 0; s < S - 1; s++, next += gridDim.x) {
+    if (next < groups) issue(next, s);
+    fetch_commit();
+  }
+  constexpr int N = K * VE, P = Vals<N>::P;
+  const Vals<N> gm = channels_of<N, VE, TPR>(kNorm ? a.gamma : nullptr, C, t, 1.f);
+  const Vals<N> bt = channels_of<N, VE, TPR>(kNorm ? a.beta : nullptr, C, t, 0.f);
+  const bool whole = N % 2 == 0 && ((K - 1) * TPR + t) * VE < C;
+  const float invC = 1.f / (float)C;
+  int stage = 0;
+  for (int64_t group = blockIdx.x; group < groups; group += gridDim.x, next += gridDim.x) {
+    if (next < groups) issue(next, stage == 0 ? S - 1 : stage - 1);
+    fetch_commit();
+    fetch_wait<S - 1>();
+    char* base = slots + (size_t)stage * F::BYTES * THREADS;
+    stage = stage == S - 1 ? 0 : stage + 1;
+    const int64_t row = group * RPB + rb;
+    const bool here = row < a.rows;
+    R raw[K];
 #pragma unroll
-      for (int k = 0; k < K; k++) {
-        const int c = (k * TPR + t) * VE;
-        to_float<T, VE>(xr[u][k], v[k]);
-        if (kNorm && res) {
-          float r[VE];
-          to_float<T, VE>(rr[u][k], r);
+    for (int k = 0; k < K; k++) raw[k] = *slot<R, THREADS>(base, k);
+    Vals<N> v = vals_of<T, VE, K>(raw);
+    if (kNorm && res) {
 #pragma unroll
-          for (int i = 0; i < VE; i++) r[i] += v[k][i];
-          // the stream is kept in its own type, and what is kept is what is normalised
-          const RawV<T, VE> w = from_float<T, VE>(r);
-          to_float<T, VE>(w, v[k]);
-          if (a.sum && here && c < C)
-            *reinterpret_cast<RawV<T, VE>*>(static_cast<T*>(a.sum) + row * C + c) = w;
-        }
-        if constexpr (kNorm) {
+      for (int k = 0; k < K; k++) raw[k] = *slot<R, THREADS>(base, K + k);
+      const Vals<N> r = vals_of<T, VE, K>(raw);
 #pragma unroll
-          for (int i = 0; i < VE; i++) s += v[k][i];  // channels past C hold 0
-        }
-      }
-      if (!kNorm || a.q8) {
+      for (int i = 0; i < P; i++) v.p[i] = v.p[i] + r.p[i];
+      float f[2 * P];
+      floats_of(v, f);
+      // the stream is kept in its own type, and what is kept is what is normalised
+#pragma unroll
+      for (int k = 0; k < K; k++) raw[k] = from_float<T, VE>(*reinterpret_cast<float(*)[VE]>(f + k * VE));
+      v = vals_of<T, VE, K>(raw);
+      if (a.sum && here) {
 #pragma unroll
         for (int k = 0; k < K; k++) {
           const int c = (k * TPR + t) * VE;
-          uint32_t byte;
-          RawV<uint8_t, VE> q;
-          quantise<VE>(v[k], byte, q);
-          if (here && c < C) {
-            *reinterpret_cast<RawV<uint8_t, VE>*>(reinterpret_cast<uint8_t*>(a.q8) + row * C + c) = q;
-            if (c % kCkptBlock == 0) a.e8[row * nb + c / kCkptBlock] = (uint8_t)byte;
-          }
+          if (c < C) *reinterpret_cast<R*>(static_cast<T*>(a.sum) + row * C + c) = raw[k];
         }
       }
-      if constexpr (kNorm) {
-        const float mean = row_sum<TPR>(s, red) * invC;
-        float d2 = 0.f;
+    }
+    if (!kNorm || a.q8) {
+      float f[2 * P];
+      floats_of(v, f);
+#pragma unroll
+      for (int k = 0; k < K; k++) {
+        const int c = (k * TPR + t) * VE;
+        uint32_t byte;
+        RawV<uint8_t, VE> q;
+        quantise<VE>(f + k * VE, byte, q);
+        if (here && c < C) {
+          *reinterpret_cast<RawV<uint8_t, VE>*>(reinterpret_cast<uint8_t*>(a.q8) + row * C + c) = q;
+          if (c % kCkptBlock == 0) a.e8[row * nb + c / kCkptBlock] = (uint8_t)byte;
+        }
+      }
+    }
+    if constexpr (kNorm) {
+      F2 s = v.p[0];  // channels past C hold 0
+#pragma unroll
+      for (int i = 1; i < P; i++) s = s + v.p[i];
+      const float mean = row_sum<TPR>(total(s), red) * invC;
+      const F2 minus = pair(-mean, -mean);
+      float f[2 * P], d2 = 0.f;
+#pragma unroll
+      for (int i = 0; i < P; i++) v.p[i] = v.p[i] + minus;
+      if (whole) {  // every vector of the thread lies inside C
+        F2 q = v.p[0] * v.p[0];
+#pragma unroll
+        for (int i = 1; i < P; i++) q = fma(v.p[i], v.p[i], q);
+        d2 = total(q);
+      } else {
+        floats_of(v, f);
 #pragma unroll
         for (int k = 0; k < K; k++)
 #pragma unroll
-          for (int i = 0; i < VE; i++) {
-            const int c = (k * TPR + t) * VE + i;
-            v[k][i] -= mean;
-            if (c < C) d2 += v[k][i] * v[k][i];
-          }
-        const float rstd = 1.f / sqrtf(row_sum<TPR>(d2, red) * invC + a.eps);
-        if (here) {
+          for (int i = 0; i < VE; i++)
+            if ((k * TPR + t) * VE < C) d2 += f[k * VE + i] * f[k * VE + i];
+      }
+      const float rstd = rsqrtf(row_sum<TPR>(d2, red) * invC + a.eps);
+      const F2 r2 = pair(rstd, rstd);
 #pragma unroll
-          for (int k = 0; k < K; k++) {
-            const int c = (k * TPR + t) * VE;
-            float o[VE];
+      for (int i = 0; i < P; i++) v.p[i] = fma(v.p[i] * r2, gm.p[i], bt.p[i]);
+      floats_of(v, f);
+      if (here) {
 #pragma unroll
-            for (int i = 0; i < VE; i++) o[i] = v[k][i] * rstd * gm[k][i] + bt[k][i];
-            if (c < C) *reinterpret_cast<RawV<T, VE>*>(static_cast<T*>(a.y) + row * C + c) = from_float<T, VE>(o);
-          }
-          if (t == 0) {
-            if (a.mean) a.mean[row] = mean;
-            if (a.rstd) a.rstd[row] = rstd;
-          }
+        for (int k = 0; k < K; k++) {
+          const int c = (k * TPR + t) * VE;
+          if (c < C)
+            *reinterpret_cast<R*>(static_cast<T*>(a.y) + row * C + c) =
+                from_float<T, VE>(*reinterpret_cast<float(*)[VE]>(f + k * VE));
+        }
+        if (t == 0) {
+          if (a.mean) a.mean[row] = mean;
+          if (a.rstd) a.rstd[row] = rstd;
         }
       }
     }
@@ -249,7 +428,7 @@ __global__ void __launch_bounds__(block_threads<TPR>()) k_rows_fwd(const RowsArg
 
 template <typename T, int VE, int TPR, int K>
 __global__ void __launch_bounds__(block_threads<TPR>()) k_ckpt_unpack(const RowsArgs args) {
-  constexpr int RPB = block_threads<TPR>() / TPR, RU = rows_ahead<K>();
+  constexpr int RPB = block_threads<TPR>() / TPR, RU = K >= 4 ? 1 : 4 / K;  // no sums: loads stay in registers
   RowsArgs a = args;
   grid_begin(a.q8, a.e8);
   const int t = threadIdx.x % TPR, rb = threadIdx.x / TPR;
@@ -286,13 +465,18 @@ __global__ void __launch_bounds__(block_threads<TPR>()) k_ckpt_unpack(const Rows
   }
 }
 
-// kCkpt: v comes from its checkpoint.
+// kCkpt: v comes from its checkpoint.  Rows on their way stay in registers here, two at a time
+// with three blocks of 256 threads on an SM (1,048,576 rows of 256 bf16 channels: 306 us from
+// rows, 360 us from the checkpoint with dres; four rows and 126 registers took 467 and 520 us).
 template <typename T, int VE, int TPR, int K, bool kCkpt>
-__global__ void __launch_bounds__(block_threads<TPR>()) k_norm_bwd(const RowsArgs args) {
+__global__ void __launch_bounds__(block_threads<TPR>(), bwd_blocks_per_sm<TPR, K * VE>()) k_norm_bwd(const RowsArgs args) {
   constexpr int THREADS = block_threads<TPR>();
   constexpr int RPB = THREADS / TPR, RU = rows_ahead<K>();
   constexpr int W = TPR <= 32 ? THREADS / 32 : 1;  // warps with their own sums of the same channels
   constexpr int WC = TPR * K * VE;                 // channels a row group covers
+  constexpr int N = K * VE, P = Vals<N>::P;
+  using R = RawV<T, VE>;
+  using Q = RawV<uint8_t, VE>;
   __shared__ float red[32];
   __shared__ float acc[W > 1 ? W * WC : 1];
   RowsArgs a = args;
@@ -304,19 +488,14 @@ __global__ void __launch_bounds__(block_threads<TPR>()) k_norm_bwd(const RowsArg
   const uint8_t* q8 = reinterpret_cast<const uint8_t*>(a.q8);
   const int t = threadIdx.x % TPR, rb = threadIdx.x / TPR;
   const int C = a.C, nb = (C + kCkptBlock - 1) / kCkptBlock;
-  float gm[K][VE], dg[K][VE], db[K][VE];
+  const Vals<N> gm = channels_of<N, VE, TPR>(a.gamma, C, t, 1.f);
+  Vals<N> dg, db;
 #pragma unroll
-  for (int k = 0; k < K; k++)
-#pragma unroll
-    for (int i = 0; i < VE; i++) {
-      const int c = (k * TPR + t) * VE + i;
-      gm[k][i] = a.gamma && c < C ? a.gamma[c] : 1.f;
-      dg[k][i] = db[k][i] = 0.f;
-    }
+  for (int i = 0; i < P; i++) dg.p[i] = db.p[i] = pair(0.f, 0.f);
   const float invC = 1.f / (float)C;
   for (int64_t r0 = (int64_t)blockIdx.x * (RPB * RU); r0 < a.rows; r0 += (int64_t)gridDim.x * (RPB * RU)) {
-    RawV<T, VE> xr[RU][K], yr[RU][K], rr[RU][K];
-    RawV<uint8_t, VE> q[RU][K];
+    R xr[RU][K], yr[RU][K], rr[RU][K];
+    Q q[RU][K];
     uint32_t e[RU][K];
     float mean[RU], rstd[RU];
 #pragma unroll
@@ -330,52 +509,63 @@ __global__ void __launch_bounds__(block_threads<TPR>()) k_norm_bwd(const RowsArg
         const bool ok = row < a.rows && c < C;
         const int64_t at = row * C + c;
         if constexpr (kCkpt) {
-          q[u][k] = ok ? *reinterpret_cast<const RawV<uint8_t, VE>*>(q8 + at) : raw_zero<RawV<uint8_t, VE>>();
+          q[u][k] = ok ? *reinterpret_cast<const Q*>(q8 + at) : raw_zero<Q>();
           e[u][k] = ok ? a.e8[row * nb + c / kCkptBlock] : 0u;
         } else {
-          xr[u][k] = ok ? *reinterpret_cast<const RawV<T, VE>*>(x + at) : raw_zero<RawV<T, VE>>();
+          xr[u][k] = ok ? *reinterpret_cast<const R*>(x + at) : raw_zero<R>();
         }
-        yr[u][k] = ok ? *reinterpret_cast<const RawV<T, VE>*>(dy + at) : raw_zero<RawV<T, VE>>();
-        if (dres) rr[u][k] = ok ? *reinterpret_cast<const RawV<T, VE>*>(dres + at) : raw_zero<RawV<T, VE>>();
+        yr[u][k] = ok ? *reinterpret_cast<const R*>(dy + at) : raw_zero<R>();
+        if (dres) rr[u][k] = ok ? *reinterpret_cast<const R*>(dres + at) : raw_zero<R>();
       }
     }
 #pragma unroll
     for (int u = 0; u < RU; u++) {
       const int64_t row = r0 + u * RPB + rb;
-      float xh[K][VE], g[K][VE];
-      float s1 = 0.f, s2 = 0.f;
+      Vals<N> xh;
+      if constexpr (kCkpt) {
+        float f[N + 1];
+        f[N] = 0.f;
 #pragma unroll
-      for (int k = 0; k < K; k++) {
-        if constexpr (kCkpt) restore<VE>(q[u][k], e[u][k], xh[k]);
-        else to_float<T, VE>(xr[u][k], xh[k]);
-        float d[VE];
-        to_float<T, VE>(yr[u][k], d);
+        for (int k = 0; k < K; k++) restore<VE>(q[u][k], e[u][k], *reinterpret_cast<float(*)[VE]>(f + k * VE));
 #pragma unroll
-        for (int i = 0; i < VE; i++) {
-          const bool in = VE > 1 || (k * TPR + t) * VE + i < C;  // vectors lie whole inside or outside C
-          xh[k][i] = (xh[k][i] - mean[u]) * rstd[u];
-          // past C, dy is 0: nothing is added there
-          db[k][i] += d[i];
-          dg[k][i] += d[i] * xh[k][i];
-          g[k][i] = d[i] * gm[k][i];
-          s1 += in ? g[k][i] : 0.f;
-          s2 += in ? g[k][i] * xh[k][i] : 0.f;
-        }
+        for (int i = 0; i < P; i++) xh.p[i] = pair(f[2 * i], f[2 * i + 1]);
+      } else {
+        xh = vals_of<T, VE, K>(xr[u]);
       }
-      s1 = row_sum<TPR>(s1, red) * invC;
-      s2 = row_sum<TPR>(s2, red) * invC;
+      Vals<N> g = vals_of<T, VE, K>(yr[u]);
+      const F2 minus = pair(-mean[u], -mean[u]), r2 = pair(rstd[u], rstd[u]);
+      F2 t1 = pair(0.f, 0.f), t2 = t1;
+#pragma unroll
+      for (int i = 0; i < P; i++) {  // past C, dy is 0: nothing is added there
+        xh.p[i] = (xh.p[i] + minus) * r2;
+        db.p[i] = db.p[i] + g.p[i];
+        dg.p[i] = fma(g.p[i], xh.p[i], dg.p[i]);
+        g.p[i] = g.p[i] * gm.p[i];
+        t1 = t1 + g.p[i];
+        t2 = fma(g.p[i], xh.p[i], t2);
+      }
+      const float s1 = row_sum<TPR>(total(t1), red) * invC;
+      const float s2 = row_sum<TPR>(total(t2), red) * invC;
+      const F2 m1 = pair(-s1, -s1), m2 = pair(-s2, -s2);
+#pragma unroll
+      for (int i = 0; i < P; i++) g.p[i] = fma(xh.p[i], m2, g.p[i] + m1);
+      if (dres) {
+        const Vals<N> r = vals_of<T, VE, K>(rr[u]);
+#pragma unroll
+        for (int i = 0; i < P; i++) g.p[i] = fma(g.p[i], r2, r.p[i]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < P; i++) g.p[i] = g.p[i] * r2;
+      }
       if (row < a.rows) {
+        float f[2 * P];
+        floats_of(g, f);
 #pragma unroll
         for (int k = 0; k < K; k++) {
           const int c = (k * TPR + t) * VE;
-          float o[VE], r[VE];
-          if (dres) to_float<T, VE>(rr[u][k], r);
-#pragma unroll
-          for (int i = 0; i < VE; i++) {
-            o[i] = (g[k][i] - s1 - xh[k][i] * s2) * rstd[u];
-            if (dres) o[i] += r[i];
-          }
-          if (c < C) *reinterpret_cast<RawV<T, VE>*>(static_cast<T*>(a.y) + row * C + c) = from_float<T, VE>(o);
+          if (c < C)
+            *reinterpret_cast<R*>(static_cast<T*>(a.y) + row * C + c) =
+                from_float<T, VE>(*reinterpret_cast<float(*)[VE]>(f + k * VE));
         }
       }
     }
@@ -384,22 +574,19 @@ __global__ void __launch_bounds__(block_threads<TPR>()) k_norm_bwd(const RowsArg
   float* part = a.part + (int64_t)blockIdx.x * 2 * C;
 #pragma unroll
   for (int which = 0; which < 2; which++) {
-    float(&sum)[K][VE] = which ? db : dg;
+    float sum[2 * P];
+    floats_of(which ? db : dg, sum);
     if constexpr (TPR < 32) {  // row groups of a warp
 #pragma unroll
       for (int o = TPR; o < 32; o <<= 1)
 #pragma unroll
-        for (int k = 0; k < K; k++)
-#pragma unroll
-          for (int i = 0; i < VE; i++) sum[k][i] += __shfl_xor_sync(0xffffffffu, sum[k][i], o);
+        for (int i = 0; i < N; i++) sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], o);
     }
     if constexpr (W > 1) {
       __syncthreads();
       if ((threadIdx.x & 31) < TPR) {
 #pragma unroll
-        for (int k = 0; k < K; k++)
-#pragma unroll
-          for (int i = 0; i < VE; i++) acc[(threadIdx.x >> 5) * WC + (k * TPR + t) * VE + i] = sum[k][i];
+        for (int i = 0; i < N; i++) acc[(threadIdx.x >> 5) * WC + (i / VE * TPR + t) * VE + i % VE] = sum[i];
       }
       __syncthreads();
       for (int c = threadIdx.x; c < C; c += THREADS) {
@@ -410,14 +597,18 @@ __global__ void __launch_bounds__(block_threads<TPR>()) k_norm_bwd(const RowsArg
       }
     } else {
 #pragma unroll
-      for (int k = 0; k < K; k++)
-#pragma unroll
-        for (int i = 0; i < VE; i++) {
-          const int c = (k * TPR + t) * VE + i;
-          if (c < C) part[which * C + c] = sum[k][i];
-        }
+      for (int i = 0; i < N; i++) {
+        const int c = (i / VE * TPR + t) * VE + i % VE;
+        if (c < C) part[which * C + c] = sum[i];
+      }
     }
   }
+}
+
+template <typename Kernel>
+cudaError_t allow_smem(Kernel kernel, size_t bytes) {
+  if (bytes <= 24576) return cudaSuccess;  // with the static arrays within the default limit
+  return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
 }
 
 // ---- choice of the plan ----------------------------------------------------------------------
@@ -447,60 +638,55 @@ auto with_lanes(int C, F f) {
   if constexpr (KM >= 8) if (slots <= 4096) return f(Int<VE>(), Int<512>(), Int<8>());
   return f(Int<VE>(), Int<512>(), Int<KM>());
 }
-// Vectors of 16 bytes where every row starts on one; else pairs of bf16, else single channels.
+// Vectors of 16 bytes where every row starts on one; else pairs of channels, else single ones.
 template <typename T, typename F>
 auto with_plan(int C, F f) {
   constexpr int V16 = 16 / sizeof(T);
   if (C % V16 == 0) return with_lanes<T, V16>(C, f);
-  if constexpr (sizeof(T) == 2)
-    if (C % 2 == 0) return with_lanes<T, 2>(C, f);
+  if (C % 2 == 0) return with_lanes<T, 2>(C, f);
   return with_lanes<T, 1>(C, f);
 }
 
+// ahead: rows that a block's row group takes at a time.
 template <typename V, typename TPR, typename K>
-int64_t rows_per_block() { return (int64_t)(block_threads<TPR::value>() / TPR::value) * rows_ahead<K::value>(); }
-template <typename V, typename TPR, typename K>
-dim3 grid_of(int64_t rows, int per_sm) {
-  const int64_t per = rows_per_block<V, TPR, K>();
+dim3 grid_of(int64_t rows, int per_sm, int ahead) {
+  const int64_t per = (int64_t)(block_threads<TPR::value>() / TPR::value) * ahead;
   const int64_t most = (int64_t)num_sms() * per_sm * 256 / block_threads<TPR::value>();
   const int64_t want = (rows + per - 1) / per;
   return dim3((unsigned)(want < most ? want : (most < 1 ? 1 : most)));
 }
-constexpr int kFwdPerSm = 8, kBwdPerSm = 4;  // blocks of 256 threads per SM, by their registers
+constexpr int kFwdPerSm = 24, kBwdPerSm = 9;  // blocks of 256 threads per SM: several waves, which even out
 
 }  // namespace rows
 
 template <typename T>
 int64_t norm_bwd_blocks(int64_t rows, int C) {
   return rows::with_plan<T>(C, [&](auto v, auto l, auto k) {
-    return (int64_t)rows::grid_of<decltype(v), decltype(l), decltype(k)>(rows, rows::kBwdPerSm).x;
+    return (int64_t)rows::grid_of<decltype(v), decltype(l), decltype(k)>(rows, rows::kBwdPerSm, rows::rows_ahead<decltype(k)::value>()).x;
   });
 }
 
-template <typename T>
-cudaError_t norm_fwd(const RowsArgs& a, cudaStream_t st) {
+template <typename T, bool kNorm>
+cudaError_t rows_fwd(const RowsArgs& a, cudaStream_t st) {
   return rows::with_plan<T>(a.C, [&](auto v, auto l, auto k) {
     using V = decltype(v); using L = decltype(l); using K = decltype(k);
-    return launch(rows::k_rows_fwd<T, V::value, L::value, K::value, true>,
-                  rows::grid_of<V, L, K>(a.rows, rows::kFwdPerSm), dim3(rows::block_threads<L::value>()), 0, st, a);
+    using F = rows::Fwd<T, V::value, L::value, K::value, kNorm>;
+    auto kernel = rows::k_rows_fwd<T, V::value, L::value, K::value, kNorm>;
+    if (cudaError_t e = rows::allow_smem(kernel, F::SMEM)) return e;
+    return launch(kernel, rows::grid_of<V, L, K>(a.rows, rows::kFwdPerSm, 1), dim3(F::THREADS), F::SMEM, st, a);
   });
 }
-
 template <typename T>
-cudaError_t ckpt_pack(const RowsArgs& a, cudaStream_t st) {
-  return rows::with_plan<T>(a.C, [&](auto v, auto l, auto k) {
-    using V = decltype(v); using L = decltype(l); using K = decltype(k);
-    return launch(rows::k_rows_fwd<T, V::value, L::value, K::value, false>,
-                  rows::grid_of<V, L, K>(a.rows, rows::kFwdPerSm), dim3(rows::block_threads<L::value>()), 0, st, a);
-  });
-}
+cudaError_t norm_fwd(const RowsArgs& a, cudaStream_t st) { return rows_fwd<T, true>(a, st); }
+template <typename T>
+cudaError_t ckpt_pack(const RowsArgs& a, cudaStream_t st) { return rows_fwd<T, false>(a, st); }
 
 template <typename T>
 cudaError_t ckpt_unpack(const RowsArgs& a, cudaStream_t st) {
   return rows::with_plan<T>(a.C, [&](auto v, auto l, auto k) {
     using V = decltype(v); using L = decltype(l); using K = decltype(k);
     return launch(rows::k_ckpt_unpack<T, V::value, L::value, K::value>,
-                  rows::grid_of<V, L, K>(a.rows, rows::kFwdPerSm), dim3(rows::block_threads<L::value>()), 0, st, a);
+                  rows::grid_of<V, L, K>(a.rows, rows::kFwdPerSm, 1), dim3(rows::block_threads<L::value>()), 0, st, a);
   });
 }
 

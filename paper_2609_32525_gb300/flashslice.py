@@ -282,19 +282,30 @@ def device_status_at(addr: int, stream=None) -> int:
 # wrong one raises ValueError before the library sees a pointer.
 
 
-def _arg(fn, name, t, dtype, numel, stream, optional=False):
+def _arg(fn, name, t, dtype, numel, dev, optional=False):
     if t is None:
         if optional:
             return None
         raise ValueError(f"{fn}: {name} is missing")
-    if t.dtype != dtype or t.numel() != numel:
+    if t.dtype is dtype and t.numel() == numel and t.get_device() == dev and t.is_contiguous():
+        return t.data_ptr()
+    if t.dtype is not dtype or t.numel() != numel:
         raise ValueError(f"{fn}: {name} has {t.numel()} values of {t.dtype}, expected {numel} of {dtype}")
     if not t.is_contiguous():
         raise ValueError(f"{fn}: {name} must be contiguous")
-    if not t.is_cuda or t.device.index != torch.cuda.current_device() or (
-            stream is not None and stream.device != t.device):
-        raise ValueError(f"{fn}: {name} is on {t.device}, the call on the current device and its stream")
-    return t.data_ptr()
+    raise ValueError(f"{fn}: {name} is on {t.device}, the call on the current device and its stream")
+
+
+def _where(fn, first, stream):
+    """The current device, and the raw stream of the call."""
+    if not isinstance(first, torch.Tensor) or not first.is_cuda:  # nothing to ask a device for
+        return -2, None
+    dev = torch.cuda.current_device()
+    if stream is None:
+        stream = torch.cuda.current_stream(dev)
+    elif stream.device_index != dev:
+        raise ValueError(f"{fn}: the stream is on cuda:{stream.device_index}, the current device is cuda:{dev}")
+    return dev, stream.cuda_stream
 
 
 # ---- token attention ----------------------------------------------------------------------
@@ -317,16 +328,14 @@ class attn_mask:
         self.doc_q, self.doc_k, self.prefix = doc_q, doc_k, prefix
 
 
-def _attn_mask(fn, s, m, stream):
+def _attn_mask(fn, s, m, dev):
     if m is None:
         return None
     f, i, nq, nk = torch.float32, torch.int32, s.B * s.Gq, s.B * s.Gk
-
-    def a(name, d, n):
-        return _arg(fn, name, getattr(m, name), d, n, stream, True)
-
-    return ctypes.byref(fs_attn_mask(a("slopes", f, s.H), a("pos_q", f, nq), a("pos_k", f, nk), a("doc_q", i, nq),
-                                     a("doc_k", i, nk), a("prefix", i, s.B)))
+    return ctypes.byref(fs_attn_mask(
+        _arg(fn, "slopes", m.slopes, f, s.H, dev, True), _arg(fn, "pos_q", m.pos_q, f, nq, dev, True),
+        _arg(fn, "pos_k", m.pos_k, f, nk, dev, True), _arg(fn, "doc_q", m.doc_q, i, nq, dev, True),
+        _arg(fn, "doc_k", m.doc_k, i, nk, dev, True), _arg(fn, "prefix", m.prefix, i, s.B, dev, True)))
 
 
 def attn_workspace_bytes(shape: fs_attn_shape, backward=False) -> int:
@@ -342,30 +351,26 @@ def attn_workspace(shape: fs_attn_shape, backward=False, device="cuda") -> torch
 
 def fs_attn_fwd(shape, q, k, v, mask, out, lse, ws, stream=None):
     """mask: an attn_mask, or None."""
-    fn, s = "fs_attn_fwd", shape
-    nq, nk = s.B * s.H * s.Gq, s.B * s.Hkv * s.Gk * s.d
-
-    def a(name, t, n):
-        return _arg(fn, name, t, torch.float32, n, stream)
-
-    st = _lib.fs_attn_fwd(ctypes.byref(s), a("q", q, nq * s.d), a("k", k, nk), a("v", v, nk),
-                          _attn_mask(fn, s, mask, stream), a("out", out, nq * s.d), a("lse", lse, nq),
-                          _arg(fn, "ws", ws, torch.uint8, ws.numel(), stream), ws.numel(), _stream(stream))
-    _check(fn, st)
+    fn, s, f = "fs_attn_fwd", shape, torch.float32
+    dev, st = _where(fn, q, stream)
+    nr, nk = s.B * s.H * s.Gq, s.B * s.Hkv * s.Gk * s.d
+    nq, nw = nr * s.d, 0 if ws is None else ws.numel()
+    _check(fn, _lib.fs_attn_fwd(
+        s, _arg(fn, "q", q, f, nq, dev), _arg(fn, "k", k, f, nk, dev), _arg(fn, "v", v, f, nk, dev),
+        _attn_mask(fn, s, mask, dev), _arg(fn, "out", out, f, nq, dev), _arg(fn, "lse", lse, f, nr, dev),
+        _arg(fn, "ws", ws, torch.uint8, nw, dev), nw, st))
 
 
 def fs_attn_bwd(shape, q, k, v, mask, out, lse, dout, dq, dk, dv, ws, stream=None):
-    fn, s = "fs_attn_bwd", shape
-    nq, nk = s.B * s.H * s.Gq, s.B * s.Hkv * s.Gk * s.d
-
-    def a(name, t, n):
-        return _arg(fn, name, t, torch.float32, n, stream)
-
-    st = _lib.fs_attn_bwd(ctypes.byref(s), a("q", q, nq * s.d), a("k", k, nk), a("v", v, nk),
-                          _attn_mask(fn, s, mask, stream), a("out", out, nq * s.d), a("lse", lse, nq),
-                          a("dout", dout, nq * s.d), a("dq", dq, nq * s.d), a("dk", dk, nk), a("dv", dv, nk),
-                          _arg(fn, "ws", ws, torch.uint8, ws.numel(), stream), ws.numel(), _stream(stream))
-    _check(fn, st)
+    fn, s, f = "fs_attn_bwd", shape, torch.float32
+    dev, st = _where(fn, q, stream)
+    nr, nk = s.B * s.H * s.Gq, s.B * s.Hkv * s.Gk * s.d
+    nq, nw = nr * s.d, 0 if ws is None else ws.numel()
+    _check(fn, _lib.fs_attn_bwd(
+        s, _arg(fn, "q", q, f, nq, dev), _arg(fn, "k", k, f, nk, dev), _arg(fn, "v", v, f, nk, dev),
+        _attn_mask(fn, s, mask, dev), _arg(fn, "out", out, f, nq, dev), _arg(fn, "lse", lse, f, nr, dev),
+        _arg(fn, "dout", dout, f, nq, dev), _arg(fn, "dq", dq, f, nq, dev), _arg(fn, "dk", dk, f, nk, dev),
+        _arg(fn, "dv", dv, f, nk, dev), _arg(fn, "ws", ws, torch.uint8, nw, dev), nw, st))
 
 
 # ---- layer norm and 8-bit checkpoints -----------------------------------------------------
@@ -409,52 +414,45 @@ def norm_workspace(rows: fs_rows, device="cuda") -> torch.Tensor:
 
 
 def fs_norm_fwd(rows, x, res, gamma, beta, eps, sum, y, mean, rstd, q8=None, e8=None, stream=None):
-    fn, f32 = "fs_norm_fwd", torch.float32
+    fn, f, r, C = "fs_norm_fwd", torch.float32, rows.rows, rows.C
     dt, n, nb = _row_sizes(rows)
-
-    def a(name, t, d, k, optional=True):
-        return _arg(fn, name, t, d, k, stream, optional)
-
-    st = _lib.fs_norm_fwd(ctypes.byref(rows), a("x", x, dt, n, False), a("res", res, dt, n),
-                          a("gamma", gamma, f32, rows.C), a("beta", beta, f32, rows.C), float(eps),
-                          a("sum", sum, dt, n), a("y", y, dt, n, False), a("mean", mean, f32, rows.rows),
-                          a("rstd", rstd, f32, rows.rows), a("q8", q8, torch.int8, n), a("e8", e8, torch.uint8, nb),
-                          _stream(stream))
-    _check(fn, st)
+    dev, st = _where(fn, x, stream)
+    _check(fn, _lib.fs_norm_fwd(
+        rows, _arg(fn, "x", x, dt, n, dev), _arg(fn, "res", res, dt, n, dev, True),
+        _arg(fn, "gamma", gamma, f, C, dev, True), _arg(fn, "beta", beta, f, C, dev, True), eps,
+        _arg(fn, "sum", sum, dt, n, dev, True), _arg(fn, "y", y, dt, n, dev), _arg(fn, "mean", mean, f, r, dev, True),
+        _arg(fn, "rstd", rstd, f, r, dev, True), _arg(fn, "q8", q8, torch.int8, n, dev, True),
+        _arg(fn, "e8", e8, torch.uint8, nb, dev, True), st))
 
 
 def fs_norm_bwd(rows, v, q8, e8, gamma, mean, rstd, dy, dres, dv, dgamma, dbeta, accumulate, ws, stream=None):
-    fn, f32 = "fs_norm_bwd", torch.float32
+    fn, f, r, C = "fs_norm_bwd", torch.float32, rows.rows, rows.C
     dt, n, nb = _row_sizes(rows)
-
-    def a(name, t, d, k, optional=True):
-        return _arg(fn, name, t, d, k, stream, optional)
-
-    st = _lib.fs_norm_bwd(ctypes.byref(rows), a("v", v, dt, n), a("q8", q8, torch.int8, n),
-                          a("e8", e8, torch.uint8, nb), a("gamma", gamma, f32, rows.C),
-                          a("mean", mean, f32, rows.rows, False), a("rstd", rstd, f32, rows.rows, False),
-                          a("dy", dy, dt, n, False), a("dres", dres, dt, n), a("dv", dv, dt, n, False),
-                          a("dgamma", dgamma, f32, rows.C), a("dbeta", dbeta, f32, rows.C), int(bool(accumulate)),
-                          a("ws", ws, torch.uint8, ws.numel(), False), ws.numel(), _stream(stream))
-    _check(fn, st)
+    dev, st = _where(fn, dy, stream)
+    nw = 0 if ws is None else ws.numel()
+    _check(fn, _lib.fs_norm_bwd(
+        rows, _arg(fn, "v", v, dt, n, dev, True), _arg(fn, "q8", q8, torch.int8, n, dev, True),
+        _arg(fn, "e8", e8, torch.uint8, nb, dev, True), _arg(fn, "gamma", gamma, f, C, dev, True),
+        _arg(fn, "mean", mean, f, r, dev), _arg(fn, "rstd", rstd, f, r, dev), _arg(fn, "dy", dy, dt, n, dev),
+        _arg(fn, "dres", dres, dt, n, dev, True), _arg(fn, "dv", dv, dt, n, dev),
+        _arg(fn, "dgamma", dgamma, f, C, dev, True), _arg(fn, "dbeta", dbeta, f, C, dev, True), int(bool(accumulate)),
+        _arg(fn, "ws", ws, torch.uint8, nw, dev), nw, st))
 
 
 def fs_ckpt_pack(rows, x, q8, e8, stream=None):
     fn = "fs_ckpt_pack"
     dt, n, nb = _row_sizes(rows)
-    st = _lib.fs_ckpt_pack(ctypes.byref(rows), _arg(fn, "x", x, dt, n, stream),
-                           _arg(fn, "q8", q8, torch.int8, n, stream), _arg(fn, "e8", e8, torch.uint8, nb, stream),
-                           _stream(stream))
-    _check(fn, st)
+    dev, st = _where(fn, x, stream)
+    _check(fn, _lib.fs_ckpt_pack(rows, _arg(fn, "x", x, dt, n, dev), _arg(fn, "q8", q8, torch.int8, n, dev),
+                                 _arg(fn, "e8", e8, torch.uint8, nb, dev), st))
 
 
 def fs_ckpt_unpack(rows, q8, e8, x, stream=None):
     fn = "fs_ckpt_unpack"
     dt, n, nb = _row_sizes(rows)
-    st = _lib.fs_ckpt_unpack(ctypes.byref(rows), _arg(fn, "q8", q8, torch.int8, n, stream),
-                             _arg(fn, "e8", e8, torch.uint8, nb, stream), _arg(fn, "x", x, dt, n, stream),
-                             _stream(stream))
-    _check(fn, st)
+    dev, st = _where(fn, x, stream)
+    _check(fn, _lib.fs_ckpt_unpack(rows, _arg(fn, "q8", q8, torch.int8, n, dev),
+                                   _arg(fn, "e8", e8, torch.uint8, nb, dev), _arg(fn, "x", x, dt, n, dev), st))
 
 
 # ---- convenience: one coupling, buffers allocated through torch ----------------------------
