@@ -29,9 +29,11 @@ struct AttnArgs {
   float scale, cap;
 };
 
-// Warps per block and splits (of the keys; of the query rows for dk and dv) for a shape on the
-// current device.
+// How a call is run on the current device: on tcgen05 (fs_attn_tc.cu) or with warps' own
+// products (fs_attn.cu), there with so many warps per block; splits of the keys, and of the
+// query rows for dk and dv.
 struct AttnPlan {
+  bool tc;
   int warps, splits, splits_kv;
 };
 AttnPlan attn_plan(int64_t units, int64_t rows, int64_t Gk, int d, bool backward);

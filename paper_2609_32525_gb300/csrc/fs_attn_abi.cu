@@ -1,6 +1,7 @@
 // Entry points of the token attention: host checks, workspace layout, dispatch.  Contract:
 // include/flashslice.h.
 #include "fs_attn.h"
+#include "fs_attn_tc.h"
 #include "fs_check.h"
 #include "fs_internal.h"
 
@@ -39,12 +40,17 @@ Dims dims(const fs_attn_shape* s) {
 }
 
 struct Layout {
+  AttnPlan plan;
   size_t delta, part, part_kv, total;
+  // of the tensor-core kernels: images by tensor (k, v, q, dout), of rows and of columns
+  size_t row_img[4], col_img[4], k_pos, k_doc, k_range, q_info, q_tok, q_range;
+  int64_t rows_pad, k_pad;
 };
 Layout layout(const fs_attn_shape* s, bool backward) {
   const Dims n = dims(s);
-  const AttnPlan p = attn_plan(n.units, n.rows, s->Gk, s->d, backward);
   Layout l{};
+  l.plan = attn_plan(n.units, n.rows, s->Gk, s->d, backward);
+  const AttnPlan& p = l.plan;
   size_t off = kAlign;  // the status word
   auto take = [&](int64_t floats) {
     const size_t o = off;
@@ -57,6 +63,24 @@ Layout layout(const fs_attn_shape* s, bool backward) {
     l.part_kv = take(p.splits_kv > 1 ? p.splits_kv * 2 * n.nk : 0);
   } else {
     l.part = take(p.splits > 1 ? p.splits * (n.nq + 2 * n.units * n.rows) : 0);
+  }
+  if (p.tc) {
+    l.k_pad = (s->Gk + 63) / 64 * 64;
+    l.rows_pad = (n.rows + 63) / 64 * 64;
+    // forward: rows of k, columns of v; backward: rows of all four, columns of k, q and dout
+    for (int t = 0; t < (backward ? 4 : 2); t++) {
+      const int64_t img = 2 * n.units * (t < 2 ? l.k_pad : l.rows_pad) * 32;
+      l.row_img[t] = backward || t == 0 ? take(img) : 0;
+      l.col_img[t] = backward == (t != 1) ? take(img) : 0;
+    }
+    l.k_pos = take(s->B * l.k_pad);
+    l.k_doc = take(s->B * l.k_pad);
+    l.k_range = take(2 * s->B * (l.k_pad / 32));
+    if (backward) {
+      l.q_info = take(4 * n.units * l.rows_pad);
+      l.q_tok = take(2 * n.units * l.rows_pad);
+      l.q_range = take(2 * n.units * (l.rows_pad / 32));
+    }
   }
   l.total = off;
   return l;
@@ -86,7 +110,7 @@ bool apart(const fs_attn_shape* s, const fs_attn_mask& m, std::initializer_list<
 AttnArgs args_of(const fs_attn_shape* s, const fs_attn_mask& m, const float* q, const float* k, const float* v,
                  void* ws, const Layout& l, bool backward) {
   const Dims n = dims(s);
-  const AttnPlan p = attn_plan(n.units, n.rows, s->Gk, s->d, backward);
+  const AttnPlan& p = l.plan;
   AttnArgs a{};
   a.q = q; a.k = k; a.v = v;
   a.slopes = m.slopes; a.pos_q = m.pos_q; a.pos_k = m.pos_k;
@@ -103,6 +127,25 @@ AttnArgs args_of(const fs_attn_shape* s, const fs_attn_mask& m, const float* q, 
     a.part_kv = at(ws, l.part_kv);
   }
   return a;
+}
+
+cudaError_t run(const fs_attn_shape* s, const AttnArgs& a, void* ws, const Layout& l, bool backward, cudaStream_t st) {
+  if (!l.plan.tc) return backward ? attn_bwd(a, s->d, st) : attn_fwd(a, s->d, st);
+  AttnTcArgs t{};
+  t.a = a;
+  for (int i = 0; i < 4; i++) {
+    t.row_img[i] = l.row_img[i] ? reinterpret_cast<uint8_t*>(at(ws, l.row_img[i])) : nullptr;
+    t.col_img[i] = l.col_img[i] ? reinterpret_cast<uint8_t*>(at(ws, l.col_img[i])) : nullptr;
+  }
+  t.k_pos = at(ws, l.k_pos);
+  t.k_doc = reinterpret_cast<int*>(at(ws, l.k_doc));
+  t.k_range = reinterpret_cast<int2*>(at(ws, l.k_range));
+  t.q_info = at(ws, l.q_info);
+  t.q_tok = reinterpret_cast<int*>(at(ws, l.q_tok));
+  t.q_range = reinterpret_cast<int2*>(at(ws, l.q_range));
+  t.rows_pad = (int)l.rows_pad;
+  t.k_pad = (int)l.k_pad;
+  return attn_tc(t, backward, st);
 }
 
 }  // namespace
@@ -137,7 +180,7 @@ fs_status fs_attn_fwd(const fs_attn_shape* s, const float* q, const float* k, co
   if (!apart(s, m, {{q, qb}, {k, kb}, {v, kb}}, {{out, qb}, {lse, rb}, {ws, l.total}})) return FS_ERR_INVALID;
   AttnArgs a = args_of(s, m, q, k, v, ws, l, false);
   a.out = out; a.lse = lse;
-  return cuda_status(attn_fwd(a, s->d, reinterpret_cast<cudaStream_t>(stream)));
+  return cuda_status(run(s, a, ws, l, false, reinterpret_cast<cudaStream_t>(stream)));
 }
 
 fs_status fs_attn_bwd(const fs_attn_shape* s, const float* q, const float* k, const float* v,
@@ -158,7 +201,7 @@ fs_status fs_attn_bwd(const fs_attn_shape* s, const float* q, const float* k, co
   AttnArgs a = args_of(s, m, q, k, v, ws, l, true);
   a.out = const_cast<float*>(out); a.lse = const_cast<float*>(lse); a.dout = dout;
   a.dq = dq; a.dk = dk; a.dv = dv;
-  return cuda_status(attn_bwd(a, s->d, reinterpret_cast<cudaStream_t>(stream)));
+  return cuda_status(run(s, a, ws, l, true, reinterpret_cast<cudaStream_t>(stream)));
 }
 
 }  // extern "C"

@@ -1,0 +1,726 @@
+// Self-attention of the slice tokens on tcgen05 (d = 32): the same results as fs_attn.cu's
+// kernels, for calls with enough rows to fill tiles of 128.
+//
+// A block owns 128 rows (queries; for dk and dv keys) and streams the other side in tiles.  Own
+// rows lie in TMEM as the first operand, split into tf32 parts; the streamed side comes as
+// images that one preparation kernel lays out per call, rows of 32 channels and their
+// transposes, both parts, in the 128-byte swizzle, so that plain bulk copies bring them and
+// every operand is K-major.  Per tile
+//
+//   S = X0 Y0^T (and dP = X1 Y1^T)   first operand TMEM, 3 products of parts, into TMEM
+//   weights (and score gradients)    a warpgroup, one own row per thread, registers
+//   parts of them back into TMEM     in place of S and dP
+//   acc = P Y^T (and dS Y^T)         first operand TMEM
+//
+// and each thread adds its row of acc to fp32 registers: the tensor core cuts its accumulator
+// towards zero at every step, and one tile is as long as a chain may get (within it the small
+// products come first).
+//
+// Two warpgroups take alternate tiles, each with its own TMEM buffers and its own issuing warp,
+// so that one's products run under the other's exponentials.  First operands in TMEM are what
+// lets products 32 columns wide run at the tensor rate: from shared memory the 128 own rows
+// would be read again for each of them, 4 KB against 1 KB of the tile's.
+//
+// Warps: 0 loads, 1 and 2 issue, 4 to 11 are the two warpgroups.
+#include "fs_attn.cuh"
+#include "fs_attn_tc.h"
+#include "fs_tc_ptx.cuh"
+
+#include <algorithm>
+
+namespace fs {
+namespace {
+
+using namespace tc;
+
+constexpr int kThreads = 384, kOwn = 128, kD = 32;
+constexpr int kListMost = kAttnTcTiles;  // tiles of one block's range
+constexpr size_t kMostSmem = 232448;
+
+enum Mode { kFwd, kDq, kDkv };
+
+// ---- images ------------------------------------------------------------------------------------
+
+// Row image: rows of 128 bytes (32 channels); column image: per 32 rows a block of 32 channel
+// rows of 128 bytes.  Both 128-byte swizzled, 4 KB per 32 rows.
+__device__ __forceinline__ uint32_t image_at(int row, int col4) {  // 16-byte piece col4 of a row
+  return (uint32_t)(row * 128 + ((col4 ^ (row & 7)) << 4));
+}
+
+__global__ void __launch_bounds__(256) k_attn_prep(const __grid_constant__ AttnTcArgs args) {
+  __shared__ float tile[32][33];
+  __shared__ float dot[32];
+  const int64_t zero = grid_begin();
+  const AttnArgs& a = args.a;
+  const int job = blockIdx.y, tid = threadIdx.x + (int)zero;
+  const bool of_q = job >= 2;  // jobs: k, v, q, dout
+  if (job == 0 && blockIdx.x == 0 && tid == 0) *a.status = kDevOk;
+  const int n = of_q ? a.rows : a.Gk, pad = of_q ? args.rows_pad : args.k_pad, atoms = pad / 32;
+  const int unit = blockIdx.x / atoms, atom = blockIdx.x - unit * atoms;
+  if (unit >= a.units) return;
+  const float* src = (job == 0 ? a.k : job == 1 ? a.v : job == 2 ? a.q : a.dout) + (int64_t)unit * n * kD;
+  const int b = unit / a.Hkv, tokens = of_q ? a.Gq : a.Gk;
+  const int* docs = of_q ? (a.doc_q ? a.doc_q + (int64_t)b * a.Gq : nullptr)
+                         : (a.doc_k ? a.doc_k + (int64_t)b * a.Gk : nullptr);
+  const int r = tid >> 3, c4 = tid & 7, row = atom * 32 + r;
+  bool ok = row < n;
+  if (ok && docs) ok = docs[row % tokens] >= 0;  // tokens that nothing sees are zeros
+  float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (ok) v = *reinterpret_cast<const float4*>(src + (int64_t)row * kD + 4 * c4);
+  const size_t base = (size_t)unit * pad * 128 + (size_t)atom * 4096;
+  uint8_t* rows_hi = args.row_img[job];
+  uint8_t* cols_hi = args.col_img[job];
+  const size_t lo_off = (size_t)a.units * pad * 128;
+  if (rows_hi) {
+    const Split s0 = split(v.x), s1 = split(v.y), s2 = split(v.z), s3 = split(v.w);
+    const size_t at = base + image_at(r, c4);
+    *reinterpret_cast<uint4*>(rows_hi + at) = make_uint4(s0.hi, s1.hi, s2.hi, s3.hi);
+    *reinterpret_cast<uint4*>(rows_hi + lo_off + at) = make_uint4(s0.lo, s1.lo, s2.lo, s3.lo);
+  }
+  if (cols_hi) {
+    tile[r][4 * c4] = v.x; tile[r][4 * c4 + 1] = v.y; tile[r][4 * c4 + 2] = v.z; tile[r][4 * c4 + 3] = v.w;
+    __syncthreads();
+    const Split s0 = split(tile[4 * c4][r]), s1 = split(tile[4 * c4 + 1][r]), s2 = split(tile[4 * c4 + 2][r]),
+                s3 = split(tile[4 * c4 + 3][r]);
+    const size_t at = base + image_at(r, c4);  // channel r, rows 4 c4 ..
+    *reinterpret_cast<uint4*>(cols_hi + at) = make_uint4(s0.hi, s1.hi, s2.hi, s3.hi);
+    *reinterpret_cast<uint4*>(cols_hi + lo_off + at) = make_uint4(s0.lo, s1.lo, s2.lo, s3.lo);
+  }
+  if (job == 3) {  // D = dout . out
+    float s = 0.f;
+    if (ok) {
+      const float4 o = *reinterpret_cast<const float4*>(a.out + ((int64_t)unit * n + row) * kD + 4 * c4);
+      s = v.x * o.x + v.y * o.y + v.z * o.z + v.w * o.w;
+    }
+#pragma unroll
+    for (int m = 4; m > 0; m >>= 1) s += __shfl_xor_sync(0xffffffffu, s, m);
+    if (c4 == 0) dot[r] = s;
+    __syncthreads();
+  }
+  if (tid >= 32 || (job != 0 && job != 3) || (job == 0 && unit % a.Hkv != 0)) return;
+  const int mine = atom * 32 + tid, tok = mine % tokens;
+  const bool in = mine < n;
+  const int doc = docs && in ? docs[tok] : -1;
+  int lo = doc >= 0 ? doc : INT_MAX, hi = doc;
+#pragma unroll
+  for (int m = 16; m > 0; m >>= 1) {
+    lo = min(lo, __shfl_xor_sync(0xffffffffu, lo, m));
+    hi = max(hi, __shfl_xor_sync(0xffffffffu, hi, m));
+  }
+  if (job == 0) {
+    const int64_t at = (int64_t)b * pad + mine;
+    if (a.slopes) args.k_pos[at] = !in ? 0.f : a.pos_k ? a.pos_k[(int64_t)b * a.Gk + tok] : (float)tok;
+    if (docs) {
+      args.k_doc[at] = doc;
+      if (tid == 0) args.k_range[(int64_t)b * atoms + atom] = make_int2(lo, hi);
+    }
+    return;
+  }
+  const int64_t at = (int64_t)unit * pad + mine, all = (int64_t)a.units * pad;
+  const int first = a.Gk - a.Gq, h = (unit % a.Hkv) * (a.H / a.Hkv) + (in ? mine / a.Gq : 0);
+  args.q_info[at] = in ? lse2_of(a.lse[(int64_t)unit * n + mine]) : INFINITY;  // weight 0 past the last row
+  args.q_info[all + at] = in ? dot[tid] : 0.f;
+  if (in) a.delta[(int64_t)unit * n + mine] = dot[tid];
+  if (a.slopes) {
+    args.q_info[2 * all + at] = in ? a.slopes[h] * kLog2e : 0.f;
+    args.q_info[3 * all + at] = !in ? 0.f : a.pos_q ? a.pos_q[(int64_t)b * a.Gq + tok] : (float)(first + tok);
+  }
+  if (docs) {
+    args.q_tok[at] = doc;
+    if (tid == 0) args.q_range[(int64_t)unit * atoms + atom] = make_int2(lo, hi);
+  }
+  if (a.causal) args.q_tok[all + at] = first + tok;
+}
+
+// ---- tensor-core pieces -------------------------------------------------------------------------
+
+constexpr uint32_t kHiWord = sdesc_hi(1024, kSw128);
+constexpr uint32_t idesc_tf32(int N) {
+  return (1u << 4) | (2u << 7) | (2u << 10) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(kOwn >> 4) << 24);
+}
+// D (+)= A B^T with A in TMEM (tf32), one lane of a converged warp issues.
+__device__ __forceinline__ void mma_tf32(uint32_t d, uint32_t a, uint32_t b_lo, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n .reg .pred p, e;\n .reg .b64 b;\n mov.b64 b, {%2, %3};\n"
+      " setp.ne.b32 p, %5, 0;\n elect.sync _|e, 0xffffffff;\n"
+      " @e tcgen05.mma.cta_group::1.kind::tf32 [%0], [%1], b, %4, p;\n}\n" ::"r"(d),
+      "r"(a), "r"(b_lo), "n"(kHiWord), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+// d = X Y^T over 32 channels: X's parts in TMEM, Y's N rows in shared memory.
+template <int N>
+__device__ __forceinline__ void issue_rows(uint32_t d, uint32_t x_hi, uint32_t x_lo, uint32_t y_hi, uint32_t y_lo) {
+  constexpr uint32_t id = idesc_tf32(N);
+#pragma unroll
+  for (int k = 0; k < 4; k++) {
+    mma_tf32(d, x_lo + 8 * k, y_hi + 2 * k, id, k > 0);
+    mma_tf32(d, x_hi + 8 * k, y_lo + 2 * k, id, 1);
+  }
+#pragma unroll
+  for (int k = 0; k < 4; k++) mma_tf32(d, x_hi + 8 * k, y_hi + 2 * k, id, 1);
+}
+// d = P Y over TN streamed rows: P's parts in TMEM, Y's column image in shared memory.
+template <int TN>
+__device__ __forceinline__ void issue_cols(uint32_t d, uint32_t p_hi, uint32_t p_lo, uint32_t y_hi, uint32_t y_lo) {
+  constexpr uint32_t id = idesc_tf32(kD);
+#pragma unroll
+  for (int k = 0; k < TN / 8; k++) {
+    const uint32_t at = (k >> 2) * 256 + (k & 3) * 2;
+    mma_tf32(d, p_lo + 8 * k, y_hi + at, id, k > 0);
+    mma_tf32(d, p_hi + 8 * k, y_lo + at, id, 1);
+  }
+#pragma unroll
+  for (int k = 0; k < TN / 8; k++) mma_tf32(d, p_hi + 8 * k, y_hi + (k >> 2) * 256 + (k & 3) * 2, id, 1);
+}
+
+// Columns of a pair's TMEM: S, dP (written over by parts of the weights and score gradients),
+// low parts, accumulators; the own rows' parts before both pairs.
+template <Mode M>
+struct Map {
+  static constexpr int TN = M == kDkv ? 32 : 64;
+  static constexpr int ROWS = M == kFwd ? 1 : 2, COLS = M == kDkv ? 2 : 1;  // images of a stage
+  static constexpr uint32_t IMG = TN * 128;                                // bytes of one part
+  static constexpr uint32_t INFO = (ROWS + COLS) * 2 * IMG, STAGE = INFO + 1024;
+  static constexpr int ST = M == kFwd ? 6 : 4;
+  static constexpr uint32_t S = 0, DP = TN, PLO = 64, DSLO = 96, ACC0 = 128, ACC1 = 160;
+  static constexpr size_t SMEM = (size_t)ST * STAGE + 1024 + kListMost * 4 + 512;
+};
+static_assert(Map<kFwd>::SMEM <= kMostSmem && Map<kDq>::SMEM <= kMostSmem && Map<kDkv>::SMEM <= kMostSmem, "");
+constexpr uint32_t kX0 = 0, kX1 = 64, kPair = 128, kPairCols = 192;
+
+// Parts of N values into N columns each.
+template <int N>
+__device__ __forceinline__ void store_parts(uint32_t hi_at, uint32_t lo_at, const float (&p)[N]) {
+#pragma unroll
+  for (int j = 0; j < N; j += 16) {
+    uint32_t h[16], l[16];
+#pragma unroll
+    for (int i = 0; i < 16; i++) {
+      const Split s = split(p[j + i]);
+      h[i] = s.hi;
+      l[i] = s.lo;
+    }
+    tmem_st16(hi_at + j, h);
+    tmem_st16(lo_at + j, l);
+  }
+}
+
+// What a thread knows of its own row.
+struct Row {
+  int index, doc, prefix;
+  float pos, slope2, lse2, delta;
+};
+
+template <Mode M>
+struct Info {  // of a stage's streamed rows
+  const float *lse2, *delta, *slope2, *pos;
+  const int *doc, *index;
+  __device__ __forceinline__ explicit Info(uint8_t* p) {
+    constexpr int TN = Map<M>::TN;
+    const float* f = reinterpret_cast<const float*>(p + Map<M>::INFO);
+    if (M == kDkv) {
+      lse2 = f; delta = f + TN; slope2 = f + 2 * TN; pos = f + 3 * TN;
+      doc = reinterpret_cast<const int*>(f + 4 * TN);
+      index = reinterpret_cast<const int*>(f + 5 * TN);
+    } else {
+      lse2 = delta = slope2 = nullptr;
+      index = nullptr;
+      pos = f;
+      doc = reinterpret_cast<const int*>(f + TN);
+    }
+  }
+};
+
+// Whether own row `o` and streamed row j (of the stage; at k0 + j among the keys) see each other.
+template <Mode M>
+__device__ __forceinline__ bool pair_ok(const AttnArgs& a, const Row& o, const Info<M>& f, int k0, int j) {
+  if (M == kDkv) return sees(a, o.prefix, a.causal ? f.index[j] : 0, o.index, a.doc_q ? f.doc[j] : 0, o.doc);
+  return k0 + j < a.Gk && sees(a, o.prefix, o.index, k0 + j, o.doc, a.doc_q ? f.doc[j] : 0);
+}
+
+// Scores of 32 columns in base-2 units, in place.
+template <bool kPlain, bool kMask>
+__device__ __forceinline__ void forward_scores(const AttnArgs& a, const Row& o, const Info<kFwd>& f, int k0, int j0,
+                                               float (&s)[32]) {
+  const float f2 = a.scale * kLog2e;
+#pragma unroll
+  for (int j = 0; j < 32; j++) {
+    if (kPlain) s[j] *= f2;
+    else s[j] = score_of(a, s[j], o.slope2, a.slopes ? fabsf(o.pos - f.pos[j0 + j]) : 0.f).a;
+    if (kMask && !pair_ok<kFwd>(a, o, f, k0, j0 + j)) s[j] = -INFINITY;
+  }
+}
+// Weights and score gradients of 16 columns from scores and dP, in place.
+template <Mode M, bool kPlain, bool kMask>
+__device__ __forceinline__ void backward_scores(const AttnArgs& a, const Row& o, const Info<M>& f, int k0, int j0,
+                                                float (&s)[16], float (&d)[16]) {
+  const float f2 = a.scale * kLog2e;
+#pragma unroll
+  for (int j = 0; j < 16; j++) {
+    const float lse2 = M == kDkv ? f.lse2[j0 + j] : o.lse2, delta = M == kDkv ? f.delta[j0 + j] : o.delta;
+    float p, slope = a.scale;
+    if (kPlain) {
+      p = exp2_fast(fmaf(s[j], f2, -lse2));
+    } else {
+      const float s2 = M == kDkv ? (a.slopes ? f.slope2[j0 + j] : 0.f) : o.slope2;
+      const Score c = score_of(a, s[j], s2, a.slopes ? fabsf(o.pos - f.pos[j0 + j]) : 0.f);
+      p = exp2_fast(c.a - lse2);
+      slope = c.slope;
+    }
+    const bool ok = !kMask || pair_ok<M>(a, o, f, k0, j0 + j);
+    s[j] = ok ? p : 0.f;
+    d[j] = ok ? p * slope * (d[j] - delta) : 0.f;
+  }
+}
+
+// ---- a block --------------------------------------------------------------------------------------
+
+template <Mode M>
+__device__ __forceinline__ void block_of(const AttnTcArgs& args, int block, int sp, uint8_t* smem) {
+  using C = Map<M>;
+  constexpr int TN = C::TN, ST = C::ST;
+  AttnArgs a = args.a;
+  int* list = reinterpret_cast<int*>(smem + (size_t)ST * C::STAGE);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(list + kListMost);
+  uint64_t *full = bars, *empty = full + ST, *x_ready = empty + ST, *s_full = x_ready + 1, *p_ready = s_full + 2,
+           *done = p_ready + 2, *drain = done + 2;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 2);
+  int* count = reinterpret_cast<int*>(tmem_slot + 1);
+  Abort* ab = reinterpret_cast<Abort*>(count + 1);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < ST; s++) {
+      mbar_init(&full[s], 1);
+      mbar_init(&empty[s], 1);
+    }
+    mbar_init(x_ready, 8);
+    for (int w = 0; w < 2; w++) {
+      mbar_init(&s_full[w], 1);
+      mbar_init(&p_ready[w], 4);
+      mbar_init(&done[w], 1);
+      mbar_init(&drain[w], 1);
+    }
+    ab->flag = 0;
+    fence_mbar_init();
+  }
+  if (warp == 1) tmem_alloc(tmem_slot, 512);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  grid_trigger();
+  grid_wait(a.q, a.k, a.v, a.slopes, a.pos_q, a.pos_k, a.doc_q, a.doc_k, a.prefix, a.lse, a.dout, a.delta);
+  uint32_t* status = a.status;
+
+  const bool own_keys = M == kDkv;
+  const int n_own = own_keys ? a.Gk : a.rows, n_str = own_keys ? a.rows : a.Gk;
+  const int pad = own_keys ? args.rows_pad : args.k_pad;
+  const int splits = own_keys ? a.splits_kv : a.splits;
+  const int blocks = (n_own + kOwn - 1) / kOwn;
+  const int unit = block / blocks, r_blk = (block - unit * blocks) * kOwn;
+  const Unit u = unit_of(a, unit, kD);
+  const Side& own_s = own_keys ? u.k : u.q;
+  const int ntiles = (n_str + TN - 1) / TN;
+  const int tile0 = (int)((int64_t)ntiles * sp / splits), tile1 = (int)((int64_t)ntiles * (sp + 1) / splits);
+  const Own own = own_range(a, own_s, r_blk, r_blk + kOwn);
+
+  // The tiles of this block's range that may hold a visible pair, in order.
+  if (warp == 0) {
+    int n = 0;
+    for (int t0 = tile0; t0 < tile1; t0 += 32) {
+      const int tile = t0 + lane, s0 = tile * TN, s1 = min(s0 + TN, n_str);
+      bool see = tile < tile1;
+      if (see && a.causal) {
+        if (!own_keys) {
+          see = s0 <= own.last || s0 < u.prefix;
+        } else {
+          const int f = u.q.token(s0), l = u.q.token(s1 - 1);
+          const int last = u.q.first + (s1 - s0 > l - f + 1 ? a.Gq - 1 : l);
+          see = own.first <= last || own.first < u.prefix;
+        }
+      }
+      if (see && a.doc_q) {
+        bool any = false;
+        for (int i = s0 / 32; i * 32 < s1; i++) {
+          const int2 r = own_keys ? args.q_range[(int64_t)unit * (pad / 32) + i]
+                                  : args.k_range[(int64_t)u.b * (pad / 32) + i];
+          any |= r.x <= own.doc_hi && r.y >= own.doc_lo;
+        }
+        see = any;
+      }
+      const uint32_t m = __ballot_sync(0xffffffffu, see);
+      if (see) list[n + __popc(m & ((1u << lane) - 1u))] = tile;
+      n += __popc(m);
+    }
+    if (lane == 0) *count = n;
+  }
+  __syncthreads();
+  const int n = *count;
+  const int pairs_n[2] = {(n + 1) / 2, n / 2};  // tiles of each pair
+
+  float acc0[32], acc1[M == kDkv ? 32 : 1];
+  float top = -INFINITY, sum = 0.f;
+#pragma unroll
+  for (int i = 0; i < 32; i++) {
+    acc0[i] = 0.f;
+    if (M == kDkv) acc1[i] = 0.f;
+  }
+  const int wg = (warp - 4) >> 2, wq = warp & 3, own_row = r_blk + wq * 32 + lane;
+
+  if (warp == 0) {
+    if (lane == 0) {
+      const uint8_t *row0, *row1 = nullptr, *col0, *col1 = nullptr;
+      const size_t at = (size_t)unit * pad * 128, lo_off = (size_t)a.units * pad * 128;
+      row0 = args.row_img[M == kDkv ? 2 : 0] + at;
+      if (M != kFwd) row1 = args.row_img[M == kDkv ? 3 : 1] + at;
+      col0 = args.col_img[M == kFwd ? 1 : M == kDq ? 0 : 2] + at;
+      if (M == kDkv) col1 = args.col_img[3] + at;
+      const int64_t all = (int64_t)a.units * pad, qat = (int64_t)unit * pad, kat = (int64_t)u.b * pad;
+      uint32_t bytes = (C::ROWS + C::COLS) * 2 * C::IMG;
+      if (M == kDkv) bytes += TN * 4 * (2 + (a.slopes ? 2 : 0) + (a.doc_q ? 1 : 0) + (a.causal ? 1 : 0));
+      else bytes += TN * 4 * ((a.slopes ? 1 : 0) + (a.doc_q ? 1 : 0));
+      int i = 0;
+      for (; i < n; i++) {
+        const int s = i % ST;
+        if (i >= ST && !mbar_wait(&empty[s], (uint32_t)((i / ST - 1) & 1), ab, status)) break;
+        uint8_t* st = smem + (size_t)s * C::STAGE;
+        const int64_t r0 = (int64_t)list[i] * TN;
+        uint64_t* bar = &full[s];
+        mbar_expect_tx(bar, bytes);
+        auto image = [&](int k, const uint8_t* src) {
+          bulk_load(st + (2 * k) * C::IMG, src + r0 * 128, C::IMG, bar);
+          bulk_load(st + (2 * k + 1) * C::IMG, src + lo_off + r0 * 128, C::IMG, bar);
+        };
+        image(0, row0);
+        if (M != kFwd) image(1, row1);
+        image(C::ROWS, col0);
+        if (M == kDkv) image(C::ROWS + 1, col1);
+        uint8_t* info = st + C::INFO;
+        auto part = [&](int k, const void* src) { bulk_load(info + k * TN * 4, src, TN * 4, bar); };
+        if (M == kDkv) {
+          part(0, args.q_info + qat + r0);
+          part(1, args.q_info + all + qat + r0);
+          if (a.slopes) {
+            part(2, args.q_info + 2 * all + qat + r0);
+            part(3, args.q_info + 3 * all + qat + r0);
+          }
+          if (a.doc_q) part(4, args.q_tok + qat + r0);
+          if (a.causal) part(5, args.q_tok + all + qat + r0);
+        } else {
+          if (a.slopes) part(0, args.k_pos + kat + r0);
+          if (a.doc_q) part(1, args.k_doc + kat + r0);
+        }
+      }
+      for (int j = (i > ST ? i - ST : 0); j < i; j++)  // no copy is left in flight
+        mbar_wait(&full[j % ST], (uint32_t)((j / ST) & 1), ab, nullptr);
+    }
+  } else if (warp == 1 || warp == 2) {
+    const int w = warp - 1;
+    const uint32_t t0 = tmem + kPair + (uint32_t)w * kPairCols;
+    bool ok = mbar_wait_w(x_ready, 0, ab, status);
+    tc_fence_after();
+    for (int i = w, k = 0; ok && i < n; i += 2, k++) {
+      const int s = i % ST;
+      const uint32_t st = sdesc_lo(smem_u32(smem + (size_t)s * C::STAGE), 16);
+      constexpr uint32_t kImg = C::IMG / 16;
+      if (!(ok = mbar_wait_w(&full[s], (uint32_t)((i / ST) & 1), ab, status))) break;
+      // the products of the pair's last tile have read what S now overwrites
+      if (k > 0 && !(ok = mbar_wait_w(&done[w], (uint32_t)((k - 1) & 1), ab, status))) break;
+      tc_fence_after();
+      issue_rows<TN>(t0 + C::S, tmem + kX0, tmem + kX0 + 32, st, st + kImg);
+      if (M != kFwd) issue_rows<TN>(t0 + C::DP, tmem + kX1, tmem + kX1 + 32, st + 2 * kImg, st + 3 * kImg);
+      mma_commit_w(&s_full[w]);
+      if (!(ok = mbar_wait_w(&p_ready[w], (uint32_t)(k & 1), ab, status))) break;
+      tc_fence_after();
+      const uint32_t c0 = st + C::ROWS * 2 * kImg;
+      if (M == kFwd) issue_cols<TN>(t0 + C::ACC0, t0 + C::S, t0 + C::PLO, c0, c0 + kImg);
+      if (M == kDq) issue_cols<TN>(t0 + C::ACC0, t0 + C::S, t0 + C::DP, c0, c0 + kImg);
+      if (M == kDkv) {
+        issue_cols<TN>(t0 + C::ACC0, t0 + C::DP, t0 + C::DSLO, c0, c0 + kImg);
+        issue_cols<TN>(t0 + C::ACC1, t0 + C::S, t0 + C::PLO, c0 + 2 * kImg, c0 + 3 * kImg);
+      }
+      mma_commit_w(&empty[s]);
+      mma_commit_w(&done[w]);
+    }
+    mma_commit_w(&drain[w]);
+    mbar_wait_w(&drain[w], 0, ab, nullptr);
+  } else if (warp >= 4) {
+    const uint32_t lanes = (uint32_t)(wq * 32) << 16;
+    // own rows' parts into TMEM: warpgroup 0 the first operand of S, warpgroup 1 that of dP
+    if (wg == 0 || M != kFwd) {
+      const float* src = wg == 0 ? own_s.x0 : own_s.x1;
+      float x[32];
+#pragma unroll
+      for (int i = 0; i < 32; i += 4) {
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (own_row < n_own) v = *reinterpret_cast<const float4*>(src + (int64_t)own_row * kD + i);
+        x[i] = v.x; x[i + 1] = v.y; x[i + 2] = v.z; x[i + 3] = v.w;
+      }
+      const uint32_t at = tmem + lanes + (wg == 0 ? kX0 : kX1);
+      store_parts(at, at + 32, x);
+      tmem_wait_st();
+    }
+    tc_fence_before();
+    __syncwarp();
+    if (lane == 0) mbar_arrive(x_ready);
+    Row o;
+    {
+      const int r = min(own_row, n_own - 1), tok = own_s.token(r);
+      o.index = own_s.first + tok;
+      o.doc = own_s.doc ? own_s.doc[tok] : 0;
+      o.prefix = u.prefix;
+      o.pos = a.slopes ? own_s.place(tok) : 0.f;
+      o.slope2 = !own_keys && a.slopes ? a.slopes[u.kvh * (a.H / a.Hkv) + r / a.Gq] * kLog2e : 0.f;
+      o.lse2 = M == kDq ? lse2_of(a.lse[(int64_t)unit * a.rows + r]) : 0.f;
+      o.delta = M == kDq ? a.delta[(int64_t)unit * a.rows + r] : 0.f;
+    }
+    const uint32_t t0 = tmem + lanes + kPair + (uint32_t)wg * kPairCols;
+    const bool plain = a.cap == 0.f && !a.slopes;
+    bool ok = true;
+    float keep = 1.f;  // from the accumulators' base to that of the products not yet added
+    auto flush = [&]() {
+      uint32_t v[32];
+      tmem_ld32(t0 + C::ACC0, v);
+      tmem_wait_ld(v);
+#pragma unroll
+      for (int c = 0; c < 32; c++) {
+        if (M == kFwd) acc0[c] = fmaf(acc0[c], keep, __uint_as_float(v[c]));
+        else acc0[c] += __uint_as_float(v[c]);
+      }
+      if constexpr (M == kDkv) {
+        tmem_ld32(t0 + C::ACC1, v);
+        tmem_wait_ld(v);
+#pragma unroll
+        for (int c = 0; c < 32; c++) acc1[c] += __uint_as_float(v[c]);
+      }
+    };
+    for (int i = wg, k = 0; i < n; i += 2, k++) {
+      if (!(ok = mbar_wait_w(&s_full[wg], (uint32_t)(k & 1), ab, status))) break;
+      tc_fence_after();
+      const Info<M> f(smem + (size_t)(i % ST) * C::STAGE);
+      const int k0 = list[i] * TN;
+      const bool mask = a.doc_q || (M != kDkv && k0 + TN > a.Gk) ||
+                        (a.causal && (M == kDkv ? true : k0 + TN - 1 > own.first && k0 + TN > u.prefix));
+      if constexpr (M == kFwd) {
+        uint32_t r0[32], r1[32];
+        tmem_ld32(t0 + C::S, r0);
+        tmem_ld32(t0 + C::S + 32, r1);
+        tmem_wait_ld2(r0, r1);
+        float s0[32], s1[32];
+#pragma unroll
+        for (int j = 0; j < 32; j++) {
+          s0[j] = __uint_as_float(r0[j]);
+          s1[j] = __uint_as_float(r1[j]);
+        }
+        if (plain && !mask) {
+          forward_scores<true, false>(a, o, f, k0, 0, s0);
+          forward_scores<true, false>(a, o, f, k0, 32, s1);
+        } else if (plain) {
+          forward_scores<true, true>(a, o, f, k0, 0, s0);
+          forward_scores<true, true>(a, o, f, k0, 32, s1);
+        } else {
+          forward_scores<false, true>(a, o, f, k0, 0, s0);
+          forward_scores<false, true>(a, o, f, k0, 32, s1);
+        }
+        float m = top;
+#pragma unroll
+        for (int j = 0; j < 32; j++) m = max3(m, s0[j], s1[j]);
+        const float base = m == -INFINITY ? 0.f : m;
+        if (k > 0) flush();
+        keep = exp2_fast(top - base);
+        top = m;
+        float part = 0.f, part1 = 0.f;
+#pragma unroll
+        for (int j = 0; j < 32; j++) {
+          s0[j] = exp2_fast(s0[j] - base);
+          s1[j] = exp2_fast(s1[j] - base);
+          part += s0[j];
+          part1 += s1[j];
+        }
+        sum = sum * keep + (part + part1);
+        store_parts(t0 + C::S, t0 + C::PLO, s0);
+        store_parts(t0 + C::S + 32, t0 + C::PLO + 32, s1);
+      } else {
+        // 16 columns at a time: the accumulators leave registers for no more
+#pragma unroll
+        for (int h = 0; h < TN; h += 16) {
+          uint32_t r0[16], r1[16];
+          tmem_ld16(t0 + C::S + h, r0);
+          tmem_ld16(t0 + C::DP + h, r1);
+          tmem_wait_ld(r0);
+          tmem_wait_ld(r1);
+          float s[16], d[16];
+#pragma unroll
+          for (int j = 0; j < 16; j++) {
+            s[j] = __uint_as_float(r0[j]);
+            d[j] = __uint_as_float(r1[j]);
+          }
+          if (plain && !mask) backward_scores<M, true, false>(a, o, f, k0, h, s, d);
+          else if (plain) backward_scores<M, true, true>(a, o, f, k0, h, s, d);
+          else backward_scores<M, false, true>(a, o, f, k0, h, s, d);
+          if constexpr (M == kDkv) {
+            store_parts(t0 + C::DP + h, t0 + C::DSLO + h, d);
+            store_parts(t0 + C::S + h, t0 + C::PLO + h, s);
+          } else {
+            store_parts(t0 + C::S + h, t0 + C::DP + h, d);
+          }
+        }
+        if (k > 0) flush();
+      }
+      tmem_wait_st();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&p_ready[wg]);
+    }
+    if (ok && pairs_n[wg] > 0) {
+      if (mbar_wait_w(&done[wg], (uint32_t)((pairs_n[wg] - 1) & 1), ab, status)) {
+        tc_fence_after();
+        flush();
+      }
+    }
+    // Both warpgroups' sums: warpgroup 1's through shared memory, in place of the stages.
+    constexpr int kMerge = M == kDkv ? 68 : 36;  // words of a row
+    named_barrier(1, 256);
+    float* merge = reinterpret_cast<float*>(smem) + (size_t)(wq * 32 + lane) * kMerge;
+    if (wg == 1) {
+#pragma unroll
+      for (int c = 0; c < 32; c += 4) {
+        *reinterpret_cast<float4*>(merge + c) = make_float4(acc0[c], acc0[c + 1], acc0[c + 2], acc0[c + 3]);
+        if constexpr (M == kDkv)
+          *reinterpret_cast<float4*>(merge + 32 + c) = make_float4(acc1[c], acc1[c + 1], acc1[c + 2], acc1[c + 3]);
+      }
+      if (M == kFwd) {
+        merge[32] = top;
+        merge[33] = sum;
+      }
+    }
+    named_barrier(1, 256);
+    if (wg == 0) {
+      float f0 = 1.f, f1 = 1.f;
+      if (M == kFwd) {
+        const float m = fmaxf(top, merge[32]), base = m == -INFINITY ? 0.f : m;
+        f0 = exp2_fast(top - base);
+        f1 = exp2_fast(merge[32] - base);
+        top = m;
+        sum = sum * f0 + merge[33] * f1;
+      }
+      bool bad = false;
+#pragma unroll
+      for (int c = 0; c < 32; c++) {
+        acc0[c] = acc0[c] * f0 + merge[c] * f1;
+        bad |= !(fabsf(acc0[c]) < INFINITY);
+        if constexpr (M == kDkv) {
+          acc1[c] += merge[32 + c];
+          bad |= !(fabsf(acc1[c]) < INFINITY);
+        }
+      }
+      bad = bad && own_row < n_own;
+      const int64_t all = (int64_t)a.units * n_own, at = (int64_t)unit * n_own;
+      float *out0, *out1 = nullptr, *stat = nullptr;
+      if (M == kFwd) {
+        out0 = a.splits > 1 ? a.part + ((int64_t)sp * all + at) * kD : a.out + at * kD;
+        if (a.splits > 1) stat = a.part + (int64_t)a.splits * all * kD + ((int64_t)sp * all + at) * 2;
+      } else if (M == kDq) {
+        out0 = splits > 1 ? a.part + ((int64_t)sp * all + at) * kD : a.dq + at * kD;
+      } else {
+        out0 = splits > 1 ? a.part_kv + ((int64_t)sp * 2 * all + at) * kD : a.dk + at * kD;
+        out1 = splits > 1 ? a.part_kv + (((int64_t)sp * 2 + 1) * all + at) * kD : a.dv + at * kD;
+      }
+      if (own_row < n_own && !bad) {
+        const float w = M == kFwd && !stat ? (sum == 0.f ? 0.f : 1.f / sum) : 1.f;
+#pragma unroll
+        for (int c = 0; c < 32; c += 4) {
+          *reinterpret_cast<float4*>(out0 + (int64_t)own_row * kD + c) =
+              make_float4(acc0[c] * w, acc0[c + 1] * w, acc0[c + 2] * w, acc0[c + 3] * w);
+          if constexpr (M == kDkv)
+            *reinterpret_cast<float4*>(out1 + (int64_t)own_row * kD + c) =
+                make_float4(acc1[c], acc1[c + 1], acc1[c + 2], acc1[c + 3]);
+        }
+        if (M == kFwd) {
+          if (stat) {
+            stat[2 * own_row] = top;
+            stat[2 * own_row + 1] = sum;
+          } else {
+            a.lse[at + own_row] = (top + log2f(sum)) * kLn2;
+          }
+        }
+      }
+      uint32_t rows = __ballot_sync(0xffffffffu, bad);
+      for (; rows; rows &= rows - 1) {
+        const int r = r_blk + wq * 32 + __ffs(rows) - 1, s0 = tile0 * TN, s1 = min(tile1 * TN, n_str);
+        float o0[2], o1[2], m, l;
+        if (M == kFwd) slow_row<kD>(args.a, unit, r, s0, s1, &m, &l, o0);
+        else slow_row_bwd<kD, M == kDkv>(args.a, unit, r, s0, s1, o0, o1);
+        const float w = M == kFwd && !stat ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
+        out0[(int64_t)r * kD + lane] = o0[0] * w;
+        if (M == kDkv) out1[(int64_t)r * kD + lane] = o1[0];
+        if (M == kFwd && lane == 0) {
+          if (stat) {
+            stat[2 * r] = m;
+            stat[2 * r + 1] = l;
+          } else {
+            a.lse[at + r] = (m + log2f(l)) * kLn2;
+          }
+        }
+      }
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == 1) tmem_dealloc(tmem, 512);
+}
+
+__device__ __forceinline__ uint8_t* stages_of(uint8_t* raw) {
+  return reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
+}
+
+// Blocks in the order of their work under a prefix mask: late queries see most keys.
+__global__ void __launch_bounds__(kThreads, 1) k_attn_fwd_tc(const __grid_constant__ AttnTcArgs args) {
+  extern __shared__ __align__(1024) uint8_t raw[];
+  block_of<kFwd>(args, (int)(gridDim.x - 1 - blockIdx.x), blockIdx.y, stages_of(raw));
+}
+// dk and dv first: they have four products a pair, dq three.
+__global__ void __launch_bounds__(kThreads, 1) k_attn_bwd_tc(const __grid_constant__ AttnTcArgs args, int blocks_kv,
+                                                             int blocks_q) {
+  extern __shared__ __align__(1024) uint8_t raw[];
+  const int b = blockIdx.x, nkv = blocks_kv * args.a.splits_kv;
+  if (b < nkv) block_of<kDkv>(args, b / args.a.splits_kv, b % args.a.splits_kv, stages_of(raw));
+  else {
+    const int c = b - nkv;
+    block_of<kDq>(args, blocks_q - 1 - c / args.a.splits, c % args.a.splits, stages_of(raw));
+  }
+}
+
+}  // namespace
+
+cudaError_t attn_tc(const AttnTcArgs& t, bool backward, cudaStream_t st) {
+  const AttnArgs& a = t.a;
+  const int atoms = std::max(t.k_pad, backward ? t.rows_pad : 0) / 32;
+  cudaError_t e = launch(k_attn_prep, dim3((unsigned)(a.units * atoms), backward ? 4 : 2), dim3(256), 0, st, t);
+  if (e != cudaSuccess) return e;
+  const int64_t blocks_q = (int64_t)a.units * ((a.rows + kOwn - 1) / kOwn);
+  const int64_t blocks_kv = (int64_t)a.units * ((a.Gk + kOwn - 1) / kOwn);
+  const int64_t nrows = (int64_t)a.units * a.rows;
+  if (!backward) {
+    constexpr size_t smem = Map<kFwd>::SMEM;
+    e = cudaFuncSetAttribute(k_attn_fwd_tc, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e == cudaSuccess)
+      e = launch(k_attn_fwd_tc, dim3((unsigned)blocks_q, (unsigned)a.splits), dim3(kThreads), smem, st, t);
+    if (e == cudaSuccess && a.splits > 1)
+      e = launch(k_attn_join<kD>, dim3((unsigned)((nrows + 7) / 8)), dim3(256), 0, st, a);
+    return e;
+  }
+  constexpr size_t smem = std::max(Map<kDq>::SMEM, Map<kDkv>::SMEM);
+  e = cudaFuncSetAttribute(k_attn_bwd_tc, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  if (e == cudaSuccess)
+    e = launch(k_attn_bwd_tc, dim3((unsigned)(blocks_kv * a.splits_kv + blocks_q * a.splits)), dim3(kThreads), smem, st,
+               t, (int)blocks_kv, (int)blocks_q);
+  if (e != cudaSuccess || (a.splits == 1 && a.splits_kv == 1)) return e;
+  const int64_t nq = nrows * kD, nk = (int64_t)a.units * a.Gk * kD;
+  const int64_t n = (a.splits > 1 ? nq : 0) + (a.splits_kv > 1 ? 2 * nk : 0);
+  return launch(k_attn_sum, dim3((unsigned)((n / 4 + 255) / 256)), dim3(256), 0, st, a, nq, nk);
+}
+
+}  // namespace fs

@@ -13,7 +13,11 @@ pytestmark = pytest.mark.gpu
 SIZES = [(1, 1, 1, 1, 1, 32), (1, 2, 1, 2, 2, 16), (2, 2, 2, 3, 3, 64), (1, 8, 8, 32, 32, 32), (2, 2, 2, 15, 15, 32),
          (2, 4, 2, 17, 17, 16), (1, 2, 1, 31, 31, 64), (1, 2, 2, 63, 63, 32), (1, 4, 4, 64, 64, 16), (3, 4, 2, 100, 100, 64),
          (1, 3, 3, 65, 65, 32), (1, 2, 1, 129, 129, 32), (1, 8, 2, 130, 130, 32), (1, 1, 1, 257, 257, 64),
-         (1, 2, 2, 300, 300, 16), (2, 8, 2, 1, 700, 32), (1, 4, 1, 5, 1000, 64), (1, 2, 2, 40, 33, 32), (2, 4, 1, 1, 1, 32)]
+         (1, 2, 2, 300, 300, 16), (2, 8, 2, 1, 700, 32), (1, 4, 1, 5, 1000, 64), (1, 2, 2, 40, 33, 32), (2, 4, 1, 1, 1, 32),
+         # tiles of 128 rows (d = 32, 128 rows and keys at least): several heads in a tile, one tile, many, more
+         # queries than keys
+         (1, 4, 1, 40, 300, 32), (2, 2, 2, 256, 256, 32), (1, 2, 2, 600, 129, 32), (1, 1, 1, 128, 1500, 32),
+         (2, 2, 1, 64, 128, 32), (1, 1, 1, 500, 500, 32)]
 PLAIN = [dict(), dict(cap=5.0), dict(bias="index"), dict(bias="place", cap=2.0), dict(docs=2), dict(prefix=0),
          dict(prefix=1, bias="index"), dict(docs=3, prefix=1, cap=3.0, bias="place")]
 
