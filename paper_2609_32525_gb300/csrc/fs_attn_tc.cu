@@ -129,7 +129,7 @@ __global__ void __launch_bounds__(256) k_attn_prep(const __grid_constant__ AttnT
     args.q_tok[at] = doc;
     if (tid == 0) args.q_range[(int64_t)unit * atoms + atom] = make_int2(lo, hi);
   }
-  if (a.causal) args.q_tok[all + at] = first + tok;
+  if (a.causal || docs) args.q_tok[all + at] = first + tok;
 }
 
 // ---- tensor-core pieces -------------------------------------------------------------------------
@@ -205,14 +205,16 @@ __device__ __forceinline__ void store_parts(uint32_t hi_at, uint32_t lo_at, cons
   }
 }
 
-// What a thread knows of its own row.
+// What a thread knows of its own row, and which streamed rows it may see: keys below `limit`
+// (own queries), or queries from `limit` on (own keys).
 struct Row {
-  int index, doc, prefix;
+  int limit, doc;
   float pos, slope2, lse2, delta;
 };
 
+// Of a stage's streamed rows, by column.
 template <Mode M>
-struct Info {  // of a stage's streamed rows
+struct Info {
   const float *lse2, *delta, *slope2, *pos;
   const int *doc, *index;
   __device__ __forceinline__ explicit Info(uint8_t* p) {
@@ -231,45 +233,76 @@ struct Info {  // of a stage's streamed rows
   }
 };
 
-// Whether own row `o` and streamed row j (of the stage; at k0 + j among the keys) see each other.
-template <Mode M>
-__device__ __forceinline__ bool pair_ok(const AttnArgs& a, const Row& o, const Info<M>& f, int k0, int j) {
-  if (M == kDkv) return sees(a, o.prefix, a.causal ? f.index[j] : 0, o.index, a.doc_q ? f.doc[j] : 0, o.doc);
-  return k0 + j < a.Gk && sees(a, o.prefix, o.index, k0 + j, o.doc, a.doc_q ? f.doc[j] : 0);
+// What a tile's scores need, so that each tile runs code without the rest: per pair, each test
+// of a feature at run time cost as much as the feature (a forward with a bias at 1024 tokens
+// took 57 us with the tests inside).
+enum Masks { kSeesAll, kByIndex, kByIndexAndDoc };
+
+// Four neighbouring columns' entries of an info array.
+template <typename T>
+__device__ __forceinline__ void four(T (&v)[4], const T* p) {
+  const float4 f = *reinterpret_cast<const float4*>(p);
+  memcpy(v, &f, sizeof(f));
 }
 
-// Scores of 32 columns in base-2 units, in place.
-template <bool kPlain, bool kMask>
-__device__ __forceinline__ void forward_scores(const AttnArgs& a, const Row& o, const Info<kFwd>& f, int k0, int j0,
-                                               float (&s)[32]) {
-  const float f2 = a.scale * kLog2e;
+// N columns from j0 on of a tile at k0: scores in s become base-2 scores (forward), or weights,
+// and dP in d becomes score gradients.
+template <Mode M, int N, bool kCap, bool kBias, int kMask>
+__device__ __forceinline__ void columns(const AttnArgs& a, const Row& o, const Info<M>& f, int k0, int j0,
+                                        float (&s)[N], float (&d)[N]) {
+  const float f2 = kCap ? a.scale / a.cap : a.scale * kLog2e, cap2 = a.cap * kLog2e;
 #pragma unroll
-  for (int j = 0; j < 32; j++) {
-    if (kPlain) s[j] *= f2;
-    else s[j] = score_of(a, s[j], o.slope2, a.slopes ? fabsf(o.pos - f.pos[j0 + j]) : 0.f).a;
-    if (kMask && !pair_ok<kFwd>(a, o, f, k0, j0 + j)) s[j] = -INFINITY;
+  for (int q = 0; q < N; q += 4) {
+    float lse2[4], delta[4], slope2[4], pos[4];
+    int doc[4], index[4];
+    if (M == kDkv) {
+      four(lse2, f.lse2 + j0 + q);
+      four(delta, f.delta + j0 + q);
+      if (kBias) four(slope2, f.slope2 + j0 + q);
+      if (kMask) four(index, f.index + j0 + q);
+    }
+    if (kBias) four(pos, f.pos + j0 + q);
+    if (kMask == kByIndexAndDoc) four(doc, f.doc + j0 + q);
+#pragma unroll
+    for (int e = 0; e < 4; e++) {
+      const int j = q + e;
+      float x = s[j] * f2, slope = a.scale;
+      if (kCap) {
+        const float t = tanhf(x);
+        x = t * cap2;
+        slope = a.scale - a.scale * (t * t);
+      }
+      if (kBias) x -= (M == kDkv ? slope2[e] : o.slope2) * fabsf(o.pos - pos[e]);
+      bool ok = true;
+      if (kMask) ok = M == kDkv ? index[e] >= o.limit : k0 + j0 + j < o.limit;
+      if (kMask == kByIndexAndDoc) ok = ok && doc[e] == o.doc;
+      if (M == kFwd) {
+        s[j] = ok ? x : -INFINITY;
+      } else {
+        const float p = exp2_fast(x - (M == kDkv ? lse2[e] : o.lse2));
+        const float g = p * slope * (d[j] - (M == kDkv ? delta[e] : o.delta));
+        s[j] = ok ? p : 0.f;
+        d[j] = ok ? g : 0.f;
+      }
+    }
   }
 }
-// Weights and score gradients of 16 columns from scores and dP, in place.
-template <Mode M, bool kPlain, bool kMask>
-__device__ __forceinline__ void backward_scores(const AttnArgs& a, const Row& o, const Info<M>& f, int k0, int j0,
-                                                float (&s)[16], float (&d)[16]) {
-  const float f2 = a.scale * kLog2e;
-#pragma unroll
-  for (int j = 0; j < 16; j++) {
-    const float lse2 = M == kDkv ? f.lse2[j0 + j] : o.lse2, delta = M == kDkv ? f.delta[j0 + j] : o.delta;
-    float p, slope = a.scale;
-    if (kPlain) {
-      p = exp2_fast(fmaf(s[j], f2, -lse2));
-    } else {
-      const float s2 = M == kDkv ? (a.slopes ? f.slope2[j0 + j] : 0.f) : o.slope2;
-      const Score c = score_of(a, s[j], s2, a.slopes ? fabsf(o.pos - f.pos[j0 + j]) : 0.f);
-      p = exp2_fast(c.a - lse2);
-      slope = c.slope;
-    }
-    const bool ok = !kMask || pair_ok<M>(a, o, f, k0, j0 + j);
-    s[j] = ok ? p : 0.f;
-    d[j] = ok ? p * slope * (d[j] - delta) : 0.f;
+template <Mode M, int N, bool kCap, bool kBias>
+__device__ __forceinline__ void columns_by_mask(const AttnArgs& a, const Row& o, const Info<M>& f, int k0, int j0,
+                                                int mask, float (&s)[N], float (&d)[N]) {
+  if (mask == kSeesAll) columns<M, N, kCap, kBias, kSeesAll>(a, o, f, k0, j0, s, d);
+  else if (mask == kByIndex) columns<M, N, kCap, kBias, kByIndex>(a, o, f, k0, j0, s, d);
+  else columns<M, N, kCap, kBias, kByIndexAndDoc>(a, o, f, k0, j0, s, d);
+}
+template <Mode M, int N>
+__device__ __forceinline__ void columns_of(const AttnArgs& a, const Row& o, const Info<M>& f, int k0, int j0, int mask,
+                                           float (&s)[N], float (&d)[N]) {
+  if (a.cap > 0.f) {
+    if (a.slopes) columns_by_mask<M, N, true, true>(a, o, f, k0, j0, mask, s, d);
+    else columns_by_mask<M, N, true, false>(a, o, f, k0, j0, mask, s, d);
+  } else {
+    if (a.slopes) columns_by_mask<M, N, false, true>(a, o, f, k0, j0, mask, s, d);
+    else columns_by_mask<M, N, false, false>(a, o, f, k0, j0, mask, s, d);
   }
 }
 
@@ -377,8 +410,9 @@ __device__ __forceinline__ void block_of(const AttnTcArgs& args, int block, int 
       col0 = args.col_img[M == kFwd ? 1 : M == kDq ? 0 : 2] + at;
       if (M == kDkv) col1 = args.col_img[3] + at;
       const int64_t all = (int64_t)a.units * pad, qat = (int64_t)unit * pad, kat = (int64_t)u.b * pad;
+      const bool index = a.causal || a.doc_q;
       uint32_t bytes = (C::ROWS + C::COLS) * 2 * C::IMG;
-      if (M == kDkv) bytes += TN * 4 * (2 + (a.slopes ? 2 : 0) + (a.doc_q ? 1 : 0) + (a.causal ? 1 : 0));
+      if (M == kDkv) bytes += TN * 4 * (2 + (a.slopes ? 2 : 0) + (a.doc_q ? 1 : 0) + (index ? 1 : 0));
       else bytes += TN * 4 * ((a.slopes ? 1 : 0) + (a.doc_q ? 1 : 0));
       int i = 0;
       for (; i < n; i++) {
@@ -406,7 +440,7 @@ __device__ __forceinline__ void block_of(const AttnTcArgs& args, int block, int 
             part(3, args.q_info + 3 * all + qat + r0);
           }
           if (a.doc_q) part(4, args.q_tok + qat + r0);
-          if (a.causal) part(5, args.q_tok + all + qat + r0);
+          if (index) part(5, args.q_tok + all + qat + r0);
         } else {
           if (a.slopes) part(0, args.k_pos + kat + r0);
           if (a.doc_q) part(1, args.k_doc + kat + r0);
@@ -467,16 +501,19 @@ __device__ __forceinline__ void block_of(const AttnTcArgs& args, int block, int 
     Row o;
     {
       const int r = min(own_row, n_own - 1), tok = own_s.token(r);
-      o.index = own_s.first + tok;
-      o.doc = own_s.doc ? own_s.doc[tok] : 0;
-      o.prefix = u.prefix;
+      const int index = own_s.first + tok;
+      if (own_keys) o.limit = a.causal && index >= u.prefix ? index : INT_MIN;
+      else o.limit = a.causal ? min(a.Gk, max(index + 1, u.prefix)) : a.Gk;
+      // no streamed row has the document of an own row without one
+      o.doc = own_s.doc ? (own_s.doc[tok] >= 0 ? own_s.doc[tok] : INT_MIN) : 0;
       o.pos = a.slopes ? own_s.place(tok) : 0.f;
       o.slope2 = !own_keys && a.slopes ? a.slopes[u.kvh * (a.H / a.Hkv) + r / a.Gq] * kLog2e : 0.f;
       o.lse2 = M == kDq ? lse2_of(a.lse[(int64_t)unit * a.rows + r]) : 0.f;
       o.delta = M == kDq ? a.delta[(int64_t)unit * a.rows + r] : 0.f;
     }
     const uint32_t t0 = tmem + lanes + kPair + (uint32_t)wg * kPairCols;
-    const bool plain = a.cap == 0.f && !a.slopes;
+    // the first key that some own query does not see
+    const int seen_by_all = a.causal ? min(a.Gk, max(own.first + 1, u.prefix)) : a.Gk;
     bool ok = true;
     float keep = 1.f;  // from the accumulators' base to that of the products not yet added
     auto flush = [&]() {
@@ -500,8 +537,15 @@ __device__ __forceinline__ void block_of(const AttnTcArgs& args, int block, int 
       tc_fence_after();
       const Info<M> f(smem + (size_t)(i % ST) * C::STAGE);
       const int k0 = list[i] * TN;
-      const bool mask = a.doc_q || (M != kDkv && k0 + TN > a.Gk) ||
-                        (a.causal && (M == kDkv ? true : k0 + TN - 1 > own.first && k0 + TN > u.prefix));
+      int mask = kSeesAll;
+      if (a.doc_q) {
+        mask = kByIndexAndDoc;
+      } else if (M != kDkv) {
+        if (k0 + TN > seen_by_all) mask = kByIndex;
+      } else if (a.causal && own.last >= u.prefix) {  // some query of the tile may be before some own key
+        const int s1 = min(k0 + TN, n_str), l = u.q.token(s1 - 1), t1 = u.q.token(k0);
+        if (u.q.first + (s1 - k0 > l - t1 + 1 ? 0 : t1) < own.last) mask = kByIndex;
+      }
       if constexpr (M == kFwd) {
         uint32_t r0[32], r1[32];
         tmem_ld32(t0 + C::S, r0);
@@ -513,16 +557,8 @@ __device__ __forceinline__ void block_of(const AttnTcArgs& args, int block, int 
           s0[j] = __uint_as_float(r0[j]);
           s1[j] = __uint_as_float(r1[j]);
         }
-        if (plain && !mask) {
-          forward_scores<true, false>(a, o, f, k0, 0, s0);
-          forward_scores<true, false>(a, o, f, k0, 32, s1);
-        } else if (plain) {
-          forward_scores<true, true>(a, o, f, k0, 0, s0);
-          forward_scores<true, true>(a, o, f, k0, 32, s1);
-        } else {
-          forward_scores<false, true>(a, o, f, k0, 0, s0);
-          forward_scores<false, true>(a, o, f, k0, 32, s1);
-        }
+        columns_of<M, 32>(a, o, f, k0, 0, mask, s0, s0);
+        columns_of<M, 32>(a, o, f, k0, 32, mask, s1, s1);
         float m = top;
 #pragma unroll
         for (int j = 0; j < 32; j++) m = max3(m, s0[j], s1[j]);
@@ -543,7 +579,7 @@ __device__ __forceinline__ void block_of(const AttnTcArgs& args, int block, int 
         store_parts(t0 + C::S + 32, t0 + C::PLO + 32, s1);
       } else {
         // 16 columns at a time: the accumulators leave registers for no more
-#pragma unroll
+#pragma unroll 1
         for (int h = 0; h < TN; h += 16) {
           uint32_t r0[16], r1[16];
           tmem_ld16(t0 + C::S + h, r0);
@@ -556,9 +592,7 @@ __device__ __forceinline__ void block_of(const AttnTcArgs& args, int block, int 
             s[j] = __uint_as_float(r0[j]);
             d[j] = __uint_as_float(r1[j]);
           }
-          if (plain && !mask) backward_scores<M, true, false>(a, o, f, k0, h, s, d);
-          else if (plain) backward_scores<M, true, true>(a, o, f, k0, h, s, d);
-          else backward_scores<M, false, true>(a, o, f, k0, h, s, d);
+          columns_of<M, 16>(a, o, f, k0, h, mask, s, d);
           if constexpr (M == kDkv) {
             store_parts(t0 + C::DP + h, t0 + C::DSLO + h, d);
             store_parts(t0 + C::S + h, t0 + C::PLO + h, s);
