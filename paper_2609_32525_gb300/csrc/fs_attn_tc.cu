@@ -16,12 +16,15 @@
 // towards zero at every step, and one tile is as long as a chain may get (within it the small
 // products come first).
 //
-// Two warpgroups take alternate tiles, each with its own TMEM buffers and its own issuing warp,
-// so that one's products run under the other's exponentials.  First operands in TMEM are what
-// lets products 32 columns wide run at the tensor rate: from shared memory the 128 own rows
-// would be read again for each of them, 4 KB against 1 KB of the tile's.
+// Two pairs of warpgroups take alternate tiles, each pair with its own TMEM buffers and its own
+// issuing warp, so that one's products run under the other's exponentials; the warpgroups of a
+// pair share a tile's columns.  In the forward each of them is a stream of its own, with its
+// maximum, sum and products, so that they need not agree on a maximum.  (With one warpgroup per
+// pair the kernels waited on latency: 21% of the tensor rate, 24% of the issue slots.)  First
+// operands in TMEM are what lets products 32 columns wide run at the tensor rate: from shared
+// memory the 128 own rows would be read again for each of them, 4 KB against 1 KB of the tile's.
 //
-// Warps: 0 loads, 1 and 2 issue, 4 to 11 are the two warpgroups.
+// Warps: 0 loads, 1 and 2 issue, 4 to 19 are the four warpgroups.
 #include "fs_attn.cuh"
 #include "fs_attn_tc.h"
 #include "fs_tc_ptx.cuh"
@@ -33,7 +36,7 @@ namespace {
 
 using namespace tc;
 
-constexpr int kThreads = 384, kOwn = 128, kD = 32;
+constexpr int kThreads = 640, kOwn = 128, kD = 32;
 constexpr int kListMost = kAttnTcTiles;  // tiles of one block's range
 constexpr size_t kMostSmem = 232448;
 
@@ -118,8 +121,8 @@ __global__ void __launch_bounds__(256) k_attn_prep(const __grid_constant__ AttnT
   }
   const int64_t at = (int64_t)unit * pad + mine, all = (int64_t)a.units * pad;
   const int first = a.Gk - a.Gq, h = (unit % a.Hkv) * (a.H / a.Hkv) + (in ? mine / a.Gq : 0);
-  args.q_info[at] = in ? lse2_of(a.lse[(int64_t)unit * n + mine]) : INFINITY;  // weight 0 past the last row
-  args.q_info[all + at] = in ? dot[tid] : 0.f;
+  args.q_info[at] = in ? -lse2_of(a.lse[(int64_t)unit * n + mine]) : -INFINITY;  // weight 0 past the last row
+  args.q_info[all + at] = in ? -dot[tid] : 0.f;
   if (in) a.delta[(int64_t)unit * n + mine] = dot[tid];
   if (a.slopes) {
     args.q_info[2 * all + at] = in ? a.slopes[h] * kLog2e : 0.f;
@@ -188,44 +191,54 @@ struct Map {
 static_assert(Map<kFwd>::SMEM <= kMostSmem && Map<kDq>::SMEM <= kMostSmem && Map<kDkv>::SMEM <= kMostSmem, "");
 constexpr uint32_t kX0 = 0, kX1 = 64, kPair = 128, kPairCols = 192;
 
-// Parts of N values into N columns each.
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t (&r)[8]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(taddr), "r"(r[0]),
+               "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+               : "memory");
+}
+__device__ __forceinline__ uint64_t both(float x) { return pack2(__float_as_uint(x), __float_as_uint(x)); }
+// Parts of N values into N columns each, eight at a time: registers are what the warpgroups lack.
+// (A high part that is cut instead of rounded is an operation less, but leaves a low part that
+// loses twice as much to tf32: dq's error grew from 7e-7 to 1e-6, at no gain in time.)
 template <int N>
-__device__ __forceinline__ void store_parts(uint32_t hi_at, uint32_t lo_at, const float (&p)[N]) {
+__device__ __forceinline__ void store_parts(uint32_t hi_at, uint32_t lo_at, const uint32_t (&p)[N]) {
 #pragma unroll
-  for (int j = 0; j < N; j += 16) {
-    uint32_t h[16], l[16];
+  for (int j = 0; j < N; j += 8) {
+    uint32_t h[8], l[8];
 #pragma unroll
-    for (int i = 0; i < 16; i++) {
-      const Split s = split(p[j + i]);
-      h[i] = s.hi;
-      l[i] = s.lo;
+    for (int i = 0; i < 8; i++) h[i] = tf32_hi(__uint_as_float(p[j + i]));
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) {
+      const uint64_t lo = fma2(pack2(h[i], h[i + 1]), both(-1.f), pack2(p[j + i], p[j + i + 1]));
+      l[i] = (uint32_t)lo;
+      l[i + 1] = (uint32_t)(lo >> 32);
     }
-    tmem_st16(hi_at + j, h);
-    tmem_st16(lo_at + j, l);
+    tmem_st8(hi_at + j, h);
+    tmem_st8(lo_at + j, l);
   }
 }
 
 // What a thread knows of its own row, and which streamed rows it may see: keys below `limit`
-// (own queries), or queries from `limit` on (own keys).
+// (own queries), or queries from `limit` on (own keys).  The statistic and D are negated.
 struct Row {
   int limit, doc;
-  float pos, slope2, lse2, delta;
+  float pos, slope2, nlse2, ndelta;
 };
 
 // Of a stage's streamed rows, by column.
 template <Mode M>
 struct Info {
-  const float *lse2, *delta, *slope2, *pos;
+  const float *nlse2, *ndelta, *slope2, *pos;
   const int *doc, *index;
   __device__ __forceinline__ explicit Info(uint8_t* p) {
     constexpr int TN = Map<M>::TN;
     const float* f = reinterpret_cast<const float*>(p + Map<M>::INFO);
     if (M == kDkv) {
-      lse2 = f; delta = f + TN; slope2 = f + 2 * TN; pos = f + 3 * TN;
+      nlse2 = f; ndelta = f + TN; slope2 = f + 2 * TN; pos = f + 3 * TN;
       doc = reinterpret_cast<const int*>(f + 4 * TN);
       index = reinterpret_cast<const int*>(f + 5 * TN);
     } else {
-      lse2 = delta = slope2 = nullptr;
+      nlse2 = ndelta = slope2 = nullptr;
       index = nullptr;
       pos = f;
       doc = reinterpret_cast<const int*>(f + TN);
@@ -245,74 +258,105 @@ __device__ __forceinline__ void four(T (&v)[4], const T* p) {
   memcpy(v, &f, sizeof(f));
 }
 
-// N columns from j0 on of a tile at k0: scores in s become base-2 scores (forward), or weights,
-// and dP in d becomes score gradients.
+// The factor that takes the forward's scores, as columns() leaves them, to base-2 units.
+template <bool kCap, bool kBias>
+__device__ __forceinline__ float score_unit(const AttnArgs& a) {
+  return kCap || kBias || !(a.scale > 0.f) ? 1.f : a.scale * kLog2e;
+}
+
+// N columns from j0 on of a tile at k0, as the bits of fp32.  Forward: the products in s become
+// scores in score_unit()s.  Backward: s becomes the weights, and dP in d the score gradients
+// without their factor `scale`, which the sums get at the end.
 template <Mode M, int N, bool kCap, bool kBias, int kMask>
 __device__ __forceinline__ void columns(const AttnArgs& a, const Row& o, const Info<M>& f, int k0, int j0,
-                                        float (&s)[N], float (&d)[N]) {
+                                        uint32_t (&s)[N], uint32_t (&d)[N]) {
   const float f2 = kCap ? a.scale / a.cap : a.scale * kLog2e, cap2 = a.cap * kLog2e;
+  const bool unit = M == kFwd && !kCap && !kBias && a.scale > 0.f;
 #pragma unroll
   for (int q = 0; q < N; q += 4) {
-    float lse2[4], delta[4], slope2[4], pos[4];
+    float nlse2[4], ndelta[4], slope2[4], pos[4];
     int doc[4], index[4];
     if (M == kDkv) {
-      four(lse2, f.lse2 + j0 + q);
-      four(delta, f.delta + j0 + q);
+      four(nlse2, f.nlse2 + j0 + q);
+      four(ndelta, f.ndelta + j0 + q);
       if (kBias) four(slope2, f.slope2 + j0 + q);
       if (kMask) four(index, f.index + j0 + q);
     }
     if (kBias) four(pos, f.pos + j0 + q);
     if (kMask == kByIndexAndDoc) four(doc, f.doc + j0 + q);
 #pragma unroll
-    for (int e = 0; e < 4; e++) {
+    for (int e = 0; e < 4; e += 2) {
       const int j = q + e;
-      float x = s[j] * f2, slope = a.scale;
+      uint64_t x = pack2(s[j], s[j + 1]), keep = 0;  // keep: 1 - (c / cap)^2
       if (kCap) {
-        const float t = tanhf(x);
-        x = t * cap2;
-        slope = a.scale - a.scale * (t * t);
+        const uint64_t y = mul2(x, both(f2));
+        const float t0 = tanhf(lo_f(y)), t1 = tanhf(hi_f(y));
+        const uint64_t t = pack2(__float_as_uint(t0), __float_as_uint(t1));
+        x = mul2(t, both(cap2));
+        keep = fma2(mul2(t, both(-1.f)), t, both(1.f));
       }
-      if (kBias) x -= (M == kDkv ? slope2[e] : o.slope2) * fabsf(o.pos - pos[e]);
-      bool ok = true;
-      if (kMask) ok = M == kDkv ? index[e] >= o.limit : k0 + j0 + j < o.limit;
-      if (kMask == kByIndexAndDoc) ok = ok && doc[e] == o.doc;
+      uint64_t shift = 0;  // minus the bias, minus the statistic
+      if (M != kFwd) {
+        shift = M == kDkv ? pack2(__float_as_uint(nlse2[e]), __float_as_uint(nlse2[e + 1])) : both(o.nlse2);
+      }
+      if (kBias) {
+        const float b0 = -(M == kDkv ? slope2[e] : o.slope2) * fabsf(o.pos - pos[e]);
+        const float b1 = -(M == kDkv ? slope2[e + 1] : o.slope2) * fabsf(o.pos - pos[e + 1]);
+        const uint64_t b = pack2(__float_as_uint(b0), __float_as_uint(b1));
+        shift = M == kFwd ? b : add2(shift, b);
+      }
+      if (kCap) {
+        if (M != kFwd || kBias) x = add2(x, shift);
+      } else if (M != kFwd || kBias) {
+        x = fma2(x, both(f2), shift);
+      } else if (!unit) {
+        x = mul2(x, both(f2));
+      }
+      bool ok0 = true, ok1 = true;
+      if (kMask) {
+        ok0 = M == kDkv ? index[e] >= o.limit : k0 + j0 + j < o.limit;
+        ok1 = M == kDkv ? index[e + 1] >= o.limit : k0 + j0 + j + 1 < o.limit;
+      }
+      if (kMask == kByIndexAndDoc) {
+        ok0 = ok0 && doc[e] == o.doc;
+        ok1 = ok1 && doc[e + 1] == o.doc;
+      }
       if (M == kFwd) {
-        s[j] = ok ? x : -INFINITY;
+        s[j] = ok0 ? (uint32_t)x : 0xff800000u;  // -infinity
+        s[j + 1] = ok1 ? (uint32_t)(x >> 32) : 0xff800000u;
       } else {
-        const float p = exp2_fast(x - (M == kDkv ? lse2[e] : o.lse2));
-        const float g = p * slope * (d[j] - (M == kDkv ? delta[e] : o.delta));
-        s[j] = ok ? p : 0.f;
-        d[j] = ok ? g : 0.f;
+        const uint32_t p0 = __float_as_uint(ex2(lo_f(x))), p1 = __float_as_uint(ex2(hi_f(x)));
+        const uint64_t nd = M == kDkv ? pack2(__float_as_uint(ndelta[e]), __float_as_uint(ndelta[e + 1])) : both(o.ndelta);
+        uint64_t w = pack2(p0, p1);
+        if (kCap) w = mul2(w, keep);
+        const uint64_t g = mul2(w, add2(pack2(d[j], d[j + 1]), nd));
+        s[j] = ok0 ? p0 : 0u;
+        s[j + 1] = ok1 ? p1 : 0u;
+        d[j] = ok0 ? (uint32_t)g : 0u;
+        d[j + 1] = ok1 ? (uint32_t)(g >> 32) : 0u;
       }
     }
   }
 }
+// Cap and bias are the kernel's (with all variants in one kernel a backward took a quarter longer,
+// by spilled registers and instruction cache), masks a tile's.
 template <Mode M, int N, bool kCap, bool kBias>
 __device__ __forceinline__ void columns_by_mask(const AttnArgs& a, const Row& o, const Info<M>& f, int k0, int j0,
-                                                int mask, float (&s)[N], float (&d)[N]) {
+                                                int mask, uint32_t (&s)[N], uint32_t (&d)[N]) {
   if (mask == kSeesAll) columns<M, N, kCap, kBias, kSeesAll>(a, o, f, k0, j0, s, d);
   else if (mask == kByIndex) columns<M, N, kCap, kBias, kByIndex>(a, o, f, k0, j0, s, d);
   else columns<M, N, kCap, kBias, kByIndexAndDoc>(a, o, f, k0, j0, s, d);
 }
-template <Mode M, int N>
-__device__ __forceinline__ void columns_of(const AttnArgs& a, const Row& o, const Info<M>& f, int k0, int j0, int mask,
-                                           float (&s)[N], float (&d)[N]) {
-  if (a.cap > 0.f) {
-    if (a.slopes) columns_by_mask<M, N, true, true>(a, o, f, k0, j0, mask, s, d);
-    else columns_by_mask<M, N, true, false>(a, o, f, k0, j0, mask, s, d);
-  } else {
-    if (a.slopes) columns_by_mask<M, N, false, true>(a, o, f, k0, j0, mask, s, d);
-    else columns_by_mask<M, N, false, false>(a, o, f, k0, j0, mask, s, d);
-  }
-}
-
 // ---- a block --------------------------------------------------------------------------------------
 
-template <Mode M>
+template <Mode M, bool kCap, bool kBias>
 __device__ __forceinline__ void block_of(const AttnTcArgs& args, int block, int sp, uint8_t* smem) {
   using C = Map<M>;
   constexpr int TN = C::TN, ST = C::ST;
-  AttnArgs a = args.a;
+  // The call's pointers stay in the constant bank: a copy with the wait's zero added to them would
+  // hold some thirty registers through the loops.  All data is read behind the wait, which is a
+  // barrier to the compiler, and none of it is declared constant.
+  const AttnArgs& a = args.a;
   int* list = reinterpret_cast<int*>(smem + (size_t)ST * C::STAGE);
   uint64_t* bars = reinterpret_cast<uint64_t*>(list + kListMost);
   uint64_t *full = bars, *empty = full + ST, *x_ready = empty + ST, *s_full = x_ready + 1, *p_ready = s_full + 2,
@@ -327,10 +371,10 @@ __device__ __forceinline__ void block_of(const AttnTcArgs& args, int block, int 
       mbar_init(&full[s], 1);
       mbar_init(&empty[s], 1);
     }
-    mbar_init(x_ready, 8);
+    mbar_init(x_ready, 16);
     for (int w = 0; w < 2; w++) {
       mbar_init(&s_full[w], 1);
-      mbar_init(&p_ready[w], 4);
+      mbar_init(&p_ready[w], 8);
       mbar_init(&done[w], 1);
       mbar_init(&drain[w], 1);
     }
@@ -343,7 +387,7 @@ __device__ __forceinline__ void block_of(const AttnTcArgs& args, int block, int 
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
   grid_trigger();
-  grid_wait(a.q, a.k, a.v, a.slopes, a.pos_q, a.pos_k, a.doc_q, a.doc_k, a.prefix, a.lse, a.dout, a.delta);
+  grid_wait();
   uint32_t* status = a.status;
 
   const bool own_keys = M == kDkv;
@@ -390,16 +434,8 @@ __device__ __forceinline__ void block_of(const AttnTcArgs& args, int block, int 
   }
   __syncthreads();
   const int n = *count;
-  const int pairs_n[2] = {(n + 1) / 2, n / 2};  // tiles of each pair
 
-  float acc0[32], acc1[M == kDkv ? 32 : 1];
-  float top = -INFINITY, sum = 0.f;
-#pragma unroll
-  for (int i = 0; i < 32; i++) {
-    acc0[i] = 0.f;
-    if (M == kDkv) acc1[i] = 0.f;
-  }
-  const int wg = (warp - 4) >> 2, wq = warp & 3, own_row = r_blk + wq * 32 + lane;
+  const int wg = (warp - 4) >> 2, pr = wg >> 1, half = wg & 1, wq = warp & 3, own_row = r_blk + wq * 32 + lane;
 
   if (warp == 0) {
     if (lane == 0) {
@@ -453,22 +489,27 @@ __device__ __forceinline__ void block_of(const AttnTcArgs& args, int block, int 
     const int w = warp - 1;
     const uint32_t t0 = tmem + kPair + (uint32_t)w * kPairCols;
     bool ok = mbar_wait_w(x_ready, 0, ab, status);
+    if (ok && w < n) ok = mbar_wait_w(&full[w % ST], 0, ab, status);
     tc_fence_after();
     for (int i = w, k = 0; ok && i < n; i += 2, k++) {
       const int s = i % ST;
       const uint32_t st = sdesc_lo(smem_u32(smem + (size_t)s * C::STAGE), 16);
       constexpr uint32_t kImg = C::IMG / 16;
-      if (!(ok = mbar_wait_w(&full[s], (uint32_t)((i / ST) & 1), ab, status))) break;
       // the products of the pair's last tile have read what S now overwrites
       if (k > 0 && !(ok = mbar_wait_w(&done[w], (uint32_t)((k - 1) & 1), ab, status))) break;
       tc_fence_after();
       issue_rows<TN>(t0 + C::S, tmem + kX0, tmem + kX0 + 32, st, st + kImg);
       if (M != kFwd) issue_rows<TN>(t0 + C::DP, tmem + kX1, tmem + kX1 + 32, st + 2 * kImg, st + 3 * kImg);
       mma_commit_w(&s_full[w]);
+      // the pair's next tile, waited for while the warpgroups work on this one
+      if (i + 2 < n && !(ok = mbar_wait_w(&full[(i + 2) % ST], (uint32_t)(((i + 2) / ST) & 1), ab, status))) break;
       if (!(ok = mbar_wait_w(&p_ready[w], (uint32_t)(k & 1), ab, status))) break;
       tc_fence_after();
       const uint32_t c0 = st + C::ROWS * 2 * kImg;
-      if (M == kFwd) issue_cols<TN>(t0 + C::ACC0, t0 + C::S, t0 + C::PLO, c0, c0 + kImg);
+      if (M == kFwd) {  // 32 keys each
+        issue_cols<32>(t0 + C::ACC0, t0 + C::S, t0 + C::PLO, c0, c0 + kImg);
+        issue_cols<32>(t0 + C::ACC1, t0 + C::S + 32, t0 + C::PLO + 32, c0 + 256, c0 + kImg + 256);
+      }
       if (M == kDq) issue_cols<TN>(t0 + C::ACC0, t0 + C::S, t0 + C::DP, c0, c0 + kImg);
       if (M == kDkv) {
         issue_cols<TN>(t0 + C::ACC0, t0 + C::DP, t0 + C::DSLO, c0, c0 + kImg);
@@ -482,13 +523,13 @@ __device__ __forceinline__ void block_of(const AttnTcArgs& args, int block, int 
   } else if (warp >= 4) {
     const uint32_t lanes = (uint32_t)(wq * 32) << 16;
     // own rows' parts into TMEM: warpgroup 0 the first operand of S, warpgroup 1 that of dP
-    if (wg == 0 || M != kFwd) {
+    if (wg == 0 || (wg == 1 && M != kFwd)) {
       const float* src = wg == 0 ? own_s.x0 : own_s.x1;
-      float x[32];
+      uint32_t x[32];
 #pragma unroll
       for (int i = 0; i < 32; i += 4) {
-        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (own_row < n_own) v = *reinterpret_cast<const float4*>(src + (int64_t)own_row * kD + i);
+        uint4 v = make_uint4(0u, 0u, 0u, 0u);
+        if (own_row < n_own) v = *reinterpret_cast<const uint4*>(src + (int64_t)own_row * kD + i);
         x[i] = v.x; x[i + 1] = v.y; x[i + 2] = v.z; x[i + 3] = v.w;
       }
       const uint32_t at = tmem + lanes + (wg == 0 ? kX0 : kX1);
@@ -508,32 +549,33 @@ __device__ __forceinline__ void block_of(const AttnTcArgs& args, int block, int 
       o.doc = own_s.doc ? (own_s.doc[tok] >= 0 ? own_s.doc[tok] : INT_MIN) : 0;
       o.pos = a.slopes ? own_s.place(tok) : 0.f;
       o.slope2 = !own_keys && a.slopes ? a.slopes[u.kvh * (a.H / a.Hkv) + r / a.Gq] * kLog2e : 0.f;
-      o.lse2 = M == kDq ? lse2_of(a.lse[(int64_t)unit * a.rows + r]) : 0.f;
-      o.delta = M == kDq ? a.delta[(int64_t)unit * a.rows + r] : 0.f;
+      o.nlse2 = M == kDq ? -lse2_of(a.lse[(int64_t)unit * a.rows + r]) : 0.f;
+      o.ndelta = M == kDq ? -a.delta[(int64_t)unit * a.rows + r] : 0.f;
     }
-    const uint32_t t0 = tmem + lanes + kPair + (uint32_t)wg * kPairCols;
+    const uint32_t t0 = tmem + lanes + kPair + (uint32_t)pr * kPairCols;
+    // This thread's share of its row's results: the forward's stream (all channels, half of the
+    // keys), half of dq's channels, or dk (half 0) or dv (half 1).
+    constexpr int NA = M == kDq ? 16 : 32;
+    const uint32_t acc_at = t0 + C::ACC0 + (uint32_t)half * NA;
+    float acc[NA];
+#pragma unroll
+    for (int c = 0; c < NA; c++) acc[c] = 0.f;
+    float top = -INFINITY, sum = 0.f;
+    float keep = 1.f;  // from the accumulators' base to that of the products not yet added
+    auto flush = [&]() {
+      uint32_t v[NA];
+      if constexpr (NA == 32) tmem_ld32(acc_at, v);
+      else tmem_ld16(acc_at, v);
+      tmem_wait_ld(v);
+#pragma unroll
+      for (int c = 0; c < NA; c++)
+        acc[c] = M == kFwd ? fmaf(acc[c], keep, __uint_as_float(v[c])) : acc[c] + __uint_as_float(v[c]);
+    };
     // the first key that some own query does not see
     const int seen_by_all = a.causal ? min(a.Gk, max(own.first + 1, u.prefix)) : a.Gk;
     bool ok = true;
-    float keep = 1.f;  // from the accumulators' base to that of the products not yet added
-    auto flush = [&]() {
-      uint32_t v[32];
-      tmem_ld32(t0 + C::ACC0, v);
-      tmem_wait_ld(v);
-#pragma unroll
-      for (int c = 0; c < 32; c++) {
-        if (M == kFwd) acc0[c] = fmaf(acc0[c], keep, __uint_as_float(v[c]));
-        else acc0[c] += __uint_as_float(v[c]);
-      }
-      if constexpr (M == kDkv) {
-        tmem_ld32(t0 + C::ACC1, v);
-        tmem_wait_ld(v);
-#pragma unroll
-        for (int c = 0; c < 32; c++) acc1[c] += __uint_as_float(v[c]);
-      }
-    };
-    for (int i = wg, k = 0; i < n; i += 2, k++) {
-      if (!(ok = mbar_wait_w(&s_full[wg], (uint32_t)(k & 1), ab, status))) break;
+    for (int i = pr, k = 0; i < n; i += 2, k++) {
+      if (!(ok = mbar_wait_w(&s_full[pr], (uint32_t)(k & 1), ab, status))) break;
       tc_fence_after();
       const Info<M> f(smem + (size_t)(i % ST) * C::STAGE);
       const int k0 = list[i] * TN;
@@ -547,52 +589,55 @@ __device__ __forceinline__ void block_of(const AttnTcArgs& args, int block, int 
         if (u.q.first + (s1 - k0 > l - t1 + 1 ? 0 : t1) < own.last) mask = kByIndex;
       }
       if constexpr (M == kFwd) {
-        uint32_t r0[32], r1[32];
-        tmem_ld32(t0 + C::S, r0);
-        tmem_ld32(t0 + C::S + 32, r1);
-        tmem_wait_ld2(r0, r1);
-        float s0[32], s1[32];
-#pragma unroll
-        for (int j = 0; j < 32; j++) {
-          s0[j] = __uint_as_float(r0[j]);
-          s1[j] = __uint_as_float(r1[j]);
-        }
-        columns_of<M, 32>(a, o, f, k0, 0, mask, s0, s0);
-        columns_of<M, 32>(a, o, f, k0, 32, mask, s1, s1);
+        const int j0 = 32 * half;
+        if (k > 0) flush();  // before the scores take its registers
+        // Twice over the columns, 16 at a time, for the maximum and for the weights: all 32 scores
+        // beside the accumulators would spill, and a spilled accumulator is a load from the
+        // second-level cache (1000 clocks a tile).  Capped or biased scores go back in between.
+        const float unit2 = score_unit<kCap, kBias>(a);
         float m = top;
-#pragma unroll
-        for (int j = 0; j < 32; j++) m = max3(m, s0[j], s1[j]);
-        const float base = m == -INFINITY ? 0.f : m;
-        if (k > 0) flush();
-        keep = exp2_fast(top - base);
-        top = m;
-        float part = 0.f, part1 = 0.f;
-#pragma unroll
-        for (int j = 0; j < 32; j++) {
-          s0[j] = exp2_fast(s0[j] - base);
-          s1[j] = exp2_fast(s1[j] - base);
-          part += s0[j];
-          part1 += s1[j];
-        }
-        sum = sum * keep + (part + part1);
-        store_parts(t0 + C::S, t0 + C::PLO, s0);
-        store_parts(t0 + C::S + 32, t0 + C::PLO + 32, s1);
-      } else {
-        // 16 columns at a time: the accumulators leave registers for no more
 #pragma unroll 1
-        for (int h = 0; h < TN; h += 16) {
-          uint32_t r0[16], r1[16];
-          tmem_ld16(t0 + C::S + h, r0);
-          tmem_ld16(t0 + C::DP + h, r1);
-          tmem_wait_ld(r0);
-          tmem_wait_ld(r1);
-          float s[16], d[16];
+        for (int h = 0; h < 32; h += 16) {
+          uint32_t s[16];
+          tmem_ld16(t0 + C::S + j0 + h, s);
+          tmem_wait_ld(s);
+          columns_by_mask<M, 16, kCap, kBias>(a, o, f, k0, j0 + h, mask, s, s);
+          float x = fmaxf(__uint_as_float(s[0]), __uint_as_float(s[1]));
 #pragma unroll
-          for (int j = 0; j < 16; j++) {
-            s[j] = __uint_as_float(r0[j]);
-            d[j] = __uint_as_float(r1[j]);
+          for (int j = 2; j < 16; j += 2) x = max3(x, __uint_as_float(s[j]), __uint_as_float(s[j + 1]));
+          m = fmaxf(m, x * unit2);
+          if (kCap || kBias) tmem_st16(t0 + C::S + j0 + h, s);
+        }
+        if (kCap || kBias) tmem_wait_st();
+        const float base = m == -INFINITY ? 0.f : m;
+        keep = ex2(top - base);
+        top = m;
+        uint64_t part = 0;
+#pragma unroll 1
+        for (int h = 0; h < 32; h += 16) {
+          uint32_t s[16];
+          tmem_ld16(t0 + C::S + j0 + h, s);
+          tmem_wait_ld(s);
+          if (!(kCap || kBias)) columns_by_mask<M, 16, kCap, kBias>(a, o, f, k0, j0 + h, mask, s, s);
+#pragma unroll
+          for (int j = 0; j < 16; j += 2) {
+            const uint64_t x = fma2(pack2(s[j], s[j + 1]), both(unit2), both(-base));
+            s[j] = __float_as_uint(ex2(lo_f(x)));
+            s[j + 1] = __float_as_uint(ex2(hi_f(x)));
+            part = add2(part, pack2(s[j], s[j + 1]));
           }
-          columns_of<M, 16>(a, o, f, k0, h, mask, s, d);
+          store_parts(t0 + C::S + j0 + h, t0 + C::PLO + j0 + h, s);
+        }
+        sum = sum * keep + (lo_f(part) + hi_f(part));
+      } else {
+#pragma unroll 1
+        for (int h = half * (TN / 2); h < (half + 1) * (TN / 2); h += 16) {
+          uint32_t s[16], d[16];
+          tmem_ld16(t0 + C::S + h, s);
+          tmem_ld16(t0 + C::DP + h, d);
+          tmem_wait_ld(s);
+          tmem_wait_ld(d);
+          columns_by_mask<M, 16, kCap, kBias>(a, o, f, k0, h, mask, s, d);
           if constexpr (M == kDkv) {
             store_parts(t0 + C::DP + h, t0 + C::DSLO + h, d);
             store_parts(t0 + C::S + h, t0 + C::PLO + h, s);
@@ -605,72 +650,72 @@ __device__ __forceinline__ void block_of(const AttnTcArgs& args, int block, int 
       tmem_wait_st();
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(&p_ready[wg]);
+      if (lane == 0) mbar_arrive(&p_ready[pr]);
     }
-    if (ok && pairs_n[wg] > 0) {
-      if (mbar_wait_w(&done[wg], (uint32_t)((pairs_n[wg] - 1) & 1), ab, status)) {
-        tc_fence_after();
-        flush();
-      }
+    const int mine = (n - pr + 1) / 2;  // tiles of this pair
+    if (ok && mine > 0 && mbar_wait_w(&done[pr], (uint32_t)((mine - 1) & 1), ab, status)) {
+      tc_fence_after();
+      flush();
     }
-    // Both warpgroups' sums: warpgroup 1's through shared memory, in place of the stages.
-    constexpr int kMerge = M == kDkv ? 68 : 36;  // words of a row
-    named_barrier(1, 256);
-    float* merge = reinterpret_cast<float*>(smem) + (size_t)(wq * 32 + lane) * kMerge;
-    if (wg == 1) {
+    // The pairs' shares (in the forward all streams' rows) through shared memory, in place of the
+    // stages, which nothing reads any more once every warpgroup is here.
+    constexpr int kRowWords = 36, kFrom = M == kFwd ? 1 : 2;  // warpgroups from kFrom on hand over
+    float* merge = reinterpret_cast<float*>(smem) + (size_t)(wq * 32 + lane) * kRowWords;
+    named_barrier(1, 512);
+    if (wg >= kFrom) {
+      float* to = merge + (size_t)(wg - kFrom) * kOwn * kRowWords;
 #pragma unroll
-      for (int c = 0; c < 32; c += 4) {
-        *reinterpret_cast<float4*>(merge + c) = make_float4(acc0[c], acc0[c + 1], acc0[c + 2], acc0[c + 3]);
-        if constexpr (M == kDkv)
-          *reinterpret_cast<float4*>(merge + 32 + c) = make_float4(acc1[c], acc1[c + 1], acc1[c + 2], acc1[c + 3]);
-      }
+      for (int c = 0; c < NA; c += 4)
+        *reinterpret_cast<float4*>(to + c) = make_float4(acc[c], acc[c + 1], acc[c + 2], acc[c + 3]);
       if (M == kFwd) {
-        merge[32] = top;
-        merge[33] = sum;
+        to[32] = top;
+        to[33] = sum;
       }
     }
-    named_barrier(1, 256);
-    if (wg == 0) {
-      float f0 = 1.f, f1 = 1.f;
-      if (M == kFwd) {
-        const float m = fmaxf(top, merge[32]), base = m == -INFINITY ? 0.f : m;
-        f0 = exp2_fast(top - base);
-        f1 = exp2_fast(merge[32] - base);
+    named_barrier(1, 512);
+    if (wg < kFrom) {
+      if constexpr (M == kFwd) {
+        const float* other = merge;
+        float m = top;
+#pragma unroll
+        for (int g = 0; g < 3; g++) m = fmaxf(m, other[g * kOwn * kRowWords + 32]);
+        const float base = m == -INFINITY ? 0.f : m;
+        const float f0 = exp2_fast(top - base);
+        sum *= f0;
+#pragma unroll
+        for (int c = 0; c < 32; c++) acc[c] *= f0;
+        for (int g = 0; g < 3; g++, other += kOwn * kRowWords) {
+          const float f = exp2_fast(other[32] - base);
+          sum += other[33] * f;
+#pragma unroll
+          for (int c = 0; c < 32; c++) acc[c] += other[c] * f;
+        }
         top = m;
-        sum = sum * f0 + merge[33] * f1;
+      } else {
+        const float* other = merge + (size_t)wg * kOwn * kRowWords;
+#pragma unroll
+        for (int c = 0; c < NA; c++) acc[c] += other[c];
       }
       bool bad = false;
 #pragma unroll
-      for (int c = 0; c < 32; c++) {
-        acc0[c] = acc0[c] * f0 + merge[c] * f1;
-        bad |= !(fabsf(acc0[c]) < INFINITY);
-        if constexpr (M == kDkv) {
-          acc1[c] += merge[32 + c];
-          bad |= !(fabsf(acc1[c]) < INFINITY);
-        }
-      }
+      for (int c = 0; c < NA; c++) bad |= !(fabsf(acc[c]) < INFINITY);
       bad = bad && own_row < n_own;
       const int64_t all = (int64_t)a.units * n_own, at = (int64_t)unit * n_own;
-      float *out0, *out1 = nullptr, *stat = nullptr;
+      float *out, *stat = nullptr;
       if (M == kFwd) {
-        out0 = a.splits > 1 ? a.part + ((int64_t)sp * all + at) * kD : a.out + at * kD;
+        out = a.splits > 1 ? a.part + ((int64_t)sp * all + at) * kD : a.out + at * kD;
         if (a.splits > 1) stat = a.part + (int64_t)a.splits * all * kD + ((int64_t)sp * all + at) * 2;
       } else if (M == kDq) {
-        out0 = splits > 1 ? a.part + ((int64_t)sp * all + at) * kD : a.dq + at * kD;
+        out = (splits > 1 ? a.part + ((int64_t)sp * all + at) * kD : a.dq + at * kD) + 16 * half;
       } else {
-        out0 = splits > 1 ? a.part_kv + ((int64_t)sp * 2 * all + at) * kD : a.dk + at * kD;
-        out1 = splits > 1 ? a.part_kv + (((int64_t)sp * 2 + 1) * all + at) * kD : a.dv + at * kD;
+        out = splits > 1 ? a.part_kv + (((int64_t)sp * 2 + half) * all + at) * kD : (half ? a.dv : a.dk) + at * kD;
       }
       if (own_row < n_own && !bad) {
-        const float w = M == kFwd && !stat ? (sum == 0.f ? 0.f : 1.f / sum) : 1.f;
+        const float w = M == kFwd ? (stat ? 1.f : sum == 0.f ? 0.f : 1.f / sum) : M == kDq || half == 0 ? a.scale : 1.f;
 #pragma unroll
-        for (int c = 0; c < 32; c += 4) {
-          *reinterpret_cast<float4*>(out0 + (int64_t)own_row * kD + c) =
-              make_float4(acc0[c] * w, acc0[c + 1] * w, acc0[c + 2] * w, acc0[c + 3] * w);
-          if constexpr (M == kDkv)
-            *reinterpret_cast<float4*>(out1 + (int64_t)own_row * kD + c) =
-                make_float4(acc1[c], acc1[c + 1], acc1[c + 2], acc1[c + 3]);
-        }
+        for (int c = 0; c < NA; c += 4)
+          *reinterpret_cast<float4*>(out + (int64_t)own_row * kD + c) =
+              make_float4(acc[c] * w, acc[c + 1] * w, acc[c + 2] * w, acc[c + 3] * w);
         if (M == kFwd) {
           if (stat) {
             stat[2 * own_row] = top;
@@ -687,8 +732,8 @@ __device__ __forceinline__ void block_of(const AttnTcArgs& args, int block, int 
         if (M == kFwd) slow_row<kD>(args.a, unit, r, s0, s1, &m, &l, o0);
         else slow_row_bwd<kD, M == kDkv>(args.a, unit, r, s0, s1, o0, o1);
         const float w = M == kFwd && !stat ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
-        out0[(int64_t)r * kD + lane] = o0[0] * w;
-        if (M == kDkv) out1[(int64_t)r * kD + lane] = o1[0];
+        if (M != kDq) out[(int64_t)r * kD + lane] = (M == kDkv && half ? o1[0] : o0[0]) * w;
+        else if ((lane >> 4) == half) out[(int64_t)r * kD + (lane & 15)] = o0[0];
         if (M == kFwd && lane == 0) {
           if (stat) {
             stat[2 * r] = m;
@@ -706,24 +751,25 @@ __device__ __forceinline__ void block_of(const AttnTcArgs& args, int block, int 
   if (warp == 1) tmem_dealloc(tmem, 512);
 }
 
-__device__ __forceinline__ uint8_t* stages_of(uint8_t* raw) {
-  return reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
-}
+// (by an offset: through an integer the pointer would lose its address space)
+__device__ __forceinline__ uint8_t* stages_of(uint8_t* raw) { return raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u); }
 
 // Blocks in the order of their work under a prefix mask: late queries see most keys.
+template <bool kCap, bool kBias>
 __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd_tc(const __grid_constant__ AttnTcArgs args) {
   extern __shared__ __align__(1024) uint8_t raw[];
-  block_of<kFwd>(args, (int)(gridDim.x - 1 - blockIdx.x), blockIdx.y, stages_of(raw));
+  block_of<kFwd, kCap, kBias>(args, (int)(gridDim.x - 1 - blockIdx.x), blockIdx.y, stages_of(raw));
 }
 // dk and dv first: they have four products a pair, dq three.
+template <bool kCap, bool kBias>
 __global__ void __launch_bounds__(kThreads, 1) k_attn_bwd_tc(const __grid_constant__ AttnTcArgs args, int blocks_kv,
                                                              int blocks_q) {
   extern __shared__ __align__(1024) uint8_t raw[];
   const int b = blockIdx.x, nkv = blocks_kv * args.a.splits_kv;
-  if (b < nkv) block_of<kDkv>(args, b / args.a.splits_kv, b % args.a.splits_kv, stages_of(raw));
+  if (b < nkv) block_of<kDkv, kCap, kBias>(args, b / args.a.splits_kv, b % args.a.splits_kv, stages_of(raw));
   else {
     const int c = b - nkv;
-    block_of<kDq>(args, blocks_q - 1 - c / args.a.splits, c % args.a.splits, stages_of(raw));
+    block_of<kDq, kCap, kBias>(args, blocks_q - 1 - c / args.a.splits, c % args.a.splits, stages_of(raw));
   }
 }
 
@@ -737,19 +783,24 @@ cudaError_t attn_tc(const AttnTcArgs& t, bool backward, cudaStream_t st) {
   const int64_t blocks_q = (int64_t)a.units * ((a.rows + kOwn - 1) / kOwn);
   const int64_t blocks_kv = (int64_t)a.units * ((a.Gk + kOwn - 1) / kOwn);
   const int64_t nrows = (int64_t)a.units * a.rows;
+  const bool cap = a.cap > 0.f, bias = a.slopes != nullptr;
   if (!backward) {
     constexpr size_t smem = Map<kFwd>::SMEM;
-    e = cudaFuncSetAttribute(k_attn_fwd_tc, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    const auto kernel = cap ? (bias ? k_attn_fwd_tc<true, true> : k_attn_fwd_tc<true, false>)
+                            : (bias ? k_attn_fwd_tc<false, true> : k_attn_fwd_tc<false, false>);
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e == cudaSuccess)
-      e = launch(k_attn_fwd_tc, dim3((unsigned)blocks_q, (unsigned)a.splits), dim3(kThreads), smem, st, t);
+      e = launch(kernel, dim3((unsigned)blocks_q, (unsigned)a.splits), dim3(kThreads), smem, st, t);
     if (e == cudaSuccess && a.splits > 1)
       e = launch(k_attn_join<kD>, dim3((unsigned)((nrows + 7) / 8)), dim3(256), 0, st, a);
     return e;
   }
   constexpr size_t smem = std::max(Map<kDq>::SMEM, Map<kDkv>::SMEM);
-  e = cudaFuncSetAttribute(k_attn_bwd_tc, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  const auto kernel = cap ? (bias ? k_attn_bwd_tc<true, true> : k_attn_bwd_tc<true, false>)
+                          : (bias ? k_attn_bwd_tc<false, true> : k_attn_bwd_tc<false, false>);
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e == cudaSuccess)
-    e = launch(k_attn_bwd_tc, dim3((unsigned)(blocks_kv * a.splits_kv + blocks_q * a.splits)), dim3(kThreads), smem, st,
+    e = launch(kernel, dim3((unsigned)(blocks_kv * a.splits_kv + blocks_q * a.splits)), dim3(kThreads), smem, st,
                t, (int)blocks_kv, (int)blocks_q);
   if (e != cudaSuccess || (a.splits == 1 && a.splits_kv == 1)) return e;
   const int64_t nq = nrows * kD, nk = (int64_t)a.units * a.Gk * kD;
