@@ -51,15 +51,11 @@ __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint3
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-// lo += ah bl + al bh and hi += ah bh.  The tensor core cuts its accumulator towards zero at
-// every step, which drifts over a long chain: the small terms have a chain of their own, and
-// chains are short (product_cols adds a tile's to fp32 registers).
-__device__ __forceinline__ void mma3(float (&hi)[4], float (&lo)[4], const uint32_t (&ah)[4], const uint32_t (&al)[4],
-                                     Split b0, Split b1) {
-  mma(lo, al, b0.hi, b1.hi);
-  mma(lo, ah, b0.lo, b1.lo);
-  mma(hi, ah, b0.hi, b1.hi);
-}
+// The three products of split operands go to two accumulators, lo += al bh + ah bl and hi += ah bh:
+// the tensor core cuts its accumulator towards zero at every step, which drifts over a long chain,
+// so the small terms have a chain of their own, and chains are short (product_cols adds a tile's to
+// fp32 registers).  A warp issues in order and a product waits some 30 clocks for the one before it
+// in its chain, so several chains take turns.
 
 __device__ __forceinline__ void copy16(void* dst, const void* src, bool ok) {
   const uint32_t d = (uint32_t)__cvta_generic_to_shared(dst);
@@ -186,36 +182,50 @@ struct OwnRows {
   }
 };
 
-// c[n] (columns: tile rows base + 8n + ..) = X Y^T
+// c[n] (columns: tile rows base + 8n + ..) = X Y^T, two or four columns' chains taking turns
 template <int D, int NT>
 __device__ __forceinline__ void product_rows(float (&c)[NT][4], const OwnRows<D>& x,
                                              const float (*y)[row_words<D>()], int base, int g, int t) {
-  constexpr int PER = D < 32 ? D / 4 : 8;
-  float lo[NT][4];
+  constexpr int PER = D < 32 ? D / 4 : 8, GN = NT < 4 ? NT : 4;
 #pragma unroll
-  for (int n = 0; n < NT; n++)
+  for (int n0 = 0; n0 < NT; n0 += GN) {
+    float lo[GN][4];
 #pragma unroll
-    for (int i = 0; i < 4; i++) c[n][i] = lo[n][i] = 0.f;
+    for (int n = 0; n < GN; n++)
 #pragma unroll
-  for (int blk = 0; blk < (D + 31) / 32; blk++) {
-    uint32_t h[PER / 2][4], l[PER / 2][4];
+      for (int i = 0; i < 4; i++) c[n0 + n][i] = lo[n][i] = 0.f;
 #pragma unroll
-    for (int s = 0; s < PER / 2; s++) x.get(blk * (PER / 2) + s, h[s], l[s]);
+    for (int blk = 0; blk < (D + 31) / 32; blk++) {
+      float f[GN][PER];
 #pragma unroll
-    for (int n = 0; n < NT; n++) {
-      float f[PER];
+      for (int n = 0; n < GN; n++)
 #pragma unroll
-      for (int i = 0; i < PER; i += 4)
-        *reinterpret_cast<float4*>(f + i) =
-            *reinterpret_cast<const float4*>(&y[base + 8 * n + g][32 * blk + PER * t + i]);
+        for (int i = 0; i < PER; i += 4)
+          *reinterpret_cast<float4*>(f[n] + i) =
+              *reinterpret_cast<const float4*>(&y[base + 8 * (n0 + n) + g][32 * blk + PER * t + i]);
 #pragma unroll
-      for (int s = 0; s < PER / 2; s++) mma3(c[n], lo[n], h[s], l[s], split(f[2 * s]), split(f[2 * s + 1]));
+      for (int s = 0; s < PER / 2; s++) {
+        uint32_t h[4], l[4];
+        x.get(blk * (PER / 2) + s, h, l);
+        Split b0[GN], b1[GN];
+#pragma unroll
+        for (int n = 0; n < GN; n++) {
+          b0[n] = split(f[n][2 * s]);
+          b1[n] = split(f[n][2 * s + 1]);
+        }
+#pragma unroll
+        for (int n = 0; n < GN; n++) mma(lo[n], l, b0[n].hi, b1[n].hi);
+#pragma unroll
+        for (int n = 0; n < GN; n++) mma(c[n0 + n], h, b0[n].hi, b1[n].hi);
+#pragma unroll
+        for (int n = 0; n < GN; n++) mma(lo[n], h, b0[n].lo, b1[n].lo);
+      }
     }
+#pragma unroll
+    for (int n = 0; n < GN; n++)
+#pragma unroll
+      for (int i = 0; i < 4; i++) c[n0 + n][i] += lo[n][i];
   }
-#pragma unroll
-  for (int n = 0; n < NT; n++)
-#pragma unroll
-    for (int i = 0; i < 4; i++) c[n][i] += lo[n][i];
 }
 
 // acc = keep acc + P Y with P [16 x 8 NT] as product_rows leaves it
@@ -242,16 +252,26 @@ __device__ __forceinline__ void product_cols(float (&acc)[D / 8][4], const float
       }
       const float* y0 = y[base + 8 * n + 2 * t];
       const float* y1 = y[base + 8 * n + 2 * t + 1];
-      float b0[V], b1[V];
+      float f0[V], f1[V];
       if constexpr (V == 4) {
-        *reinterpret_cast<float4*>(b0) = *reinterpret_cast<const float4*>(y0 + 32 * blk + 4 * g);
-        *reinterpret_cast<float4*>(b1) = *reinterpret_cast<const float4*>(y1 + 32 * blk + 4 * g);
+        *reinterpret_cast<float4*>(f0) = *reinterpret_cast<const float4*>(y0 + 32 * blk + 4 * g);
+        *reinterpret_cast<float4*>(f1) = *reinterpret_cast<const float4*>(y1 + 32 * blk + 4 * g);
       } else {
-        *reinterpret_cast<float2*>(b0) = *reinterpret_cast<const float2*>(y0 + 2 * g);
-        *reinterpret_cast<float2*>(b1) = *reinterpret_cast<const float2*>(y1 + 2 * g);
+        *reinterpret_cast<float2*>(f0) = *reinterpret_cast<const float2*>(y0 + 2 * g);
+        *reinterpret_cast<float2*>(f1) = *reinterpret_cast<const float2*>(y1 + 2 * g);
+      }
+      Split b0[V], b1[V];
+#pragma unroll
+      for (int m = 0; m < V; m++) {
+        b0[m] = split(f0[m]);
+        b1[m] = split(f1[m]);
       }
 #pragma unroll
-      for (int m = 0; m < V; m++) mma3(hi[m], lo[m], h, l, split(b0[m]), split(b1[m]));
+      for (int m = 0; m < V; m++) mma(lo[m], l, b0[m].hi, b1[m].hi);
+#pragma unroll
+      for (int m = 0; m < V; m++) mma(hi[m], h, b0[m].hi, b1[m].hi);
+#pragma unroll
+      for (int m = 0; m < V; m++) mma(lo[m], h, b0[m].lo, b1[m].lo);
     }
 #pragma unroll
     for (int m = 0; m < V; m++)
@@ -309,8 +329,8 @@ template <int D>
 __global__ void __launch_bounds__(kMaxWarps * 32) k_attn_fwd(const __grid_constant__ AttnArgs args) {
   constexpr int TR = tile_rows<D>(), NT = TR / 8;
   __shared__ Tile<D> tiles[2];
-  AttnArgs a = args;
-  grid_begin(a.q, a.k, a.v, a.slopes, a.pos_q, a.pos_k, a.doc_q, a.doc_k, a.prefix);
+  const AttnArgs& a = args;  // in the constant bank: no registers through the loops
+  grid_begin();
   if (a.status && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *a.status = kDevOk;
   const int per = 16 * a.warps, blocks = (a.rows + per - 1) / per;
   const int unit = blockIdx.x / blocks, r_blk = (blockIdx.x - unit * blocks) * per, sp = blockIdx.y;
@@ -478,7 +498,7 @@ __global__ void __launch_bounds__(256) k_attn_delta(const AttnArgs args) {
 template <int D, bool kOwnKeys>
 __device__ __forceinline__ void backward_block(const AttnArgs& args, const AttnArgs& a, Tile<D> (&tiles)[2], int block,
                                                int sp) {
-  constexpr int TR = tile_rows<D>(), NT = 4;  // 32 streamed rows at a time
+  constexpr int TR = tile_rows<D>(), NT = D == 64 ? 2 : 4;  // 32 streamed rows at a time (16: registers)
   const int n_own = kOwnKeys ? a.Gk : a.rows, n_str = kOwnKeys ? a.rows : a.Gk;
   const int splits = kOwnKeys ? a.splits_kv : a.splits;
   const int per = 16 * a.warps, blocks = (n_own + per - 1) / per;
@@ -589,8 +609,8 @@ __device__ __forceinline__ void backward_block(const AttnArgs& args, const AttnA
 template <int D>
 __global__ void __launch_bounds__(kMaxWarps * 32) k_attn_bwd(const __grid_constant__ AttnArgs args, int blocks_kv) {
   __shared__ Tile<D> tiles[2];
-  AttnArgs a = args;
-  grid_begin(a.q, a.k, a.v, a.slopes, a.pos_q, a.pos_k, a.doc_q, a.doc_k, a.prefix, a.lse, a.dout, a.delta);
+  const AttnArgs& a = args;
+  grid_begin();
   const int b = blockIdx.x;
   if (b < blocks_kv * a.splits_kv) backward_block<D, true>(args, a, tiles, b / a.splits_kv, b % a.splits_kv);
   else {
@@ -605,7 +625,7 @@ cudaError_t attn_fwd_t(const AttnArgs& a, cudaStream_t st) {
   const dim3 grid((unsigned)(a.units * ((a.rows + per - 1) / per)), (unsigned)a.splits);
   cudaError_t e = launch(k_attn_fwd<D>, grid, dim3(32 * a.warps), 0, st, a);
   if (e == cudaSuccess && a.splits > 1)
-    e = launch(k_attn_join<D>, dim3((unsigned)(((int64_t)a.units * a.rows + 7) / 8)), dim3(256), 0, st, a);
+    e = attn_join<D>(a, st);
   return e;
 }
 
@@ -651,14 +671,14 @@ AttnPlan attn_plan(int64_t units, int64_t rows, int64_t Gk, int d, bool backward
     return p;
   }
   // Blocks take 16 rows a warp, up to 64.  Where they would leave SMs without two warps for
-  // each of the four schedulers, the streamed side is split, into ranges of two tiles at least.
+  // each of the four schedulers, the streamed side is split, down to single tiles.
   const int64_t most = backward ? std::max(rows, Gk) : rows;
   p.warps = most <= 16 ? 1 : most <= 32 ? 2 : 4;
   const int64_t per = 16 * p.warps, tile = d == 64 ? 32 : 64;
   const int64_t want = sms * 8 / p.warps / (backward ? 2 : 1);
   auto split = [&](int64_t own, int64_t streamed) {
     const int64_t blocks = units * ((own + per - 1) / per), tiles = (streamed + tile - 1) / tile;
-    return (int)std::max<int64_t>(1, std::min(want / blocks, tiles / 2));
+    return (int)std::max<int64_t>(1, std::min(want / blocks, tiles));
   };
   p.splits = split(rows, Gk);
   if (backward) p.splits_kv = split(Gk, rows);

@@ -201,33 +201,59 @@ __device__ __noinline__ void slow_row_bwd(const AttnArgs& a, int unit, int own, 
 
 // ---- joins ------------------------------------------------------------------------------------
 
-// Joins the splits' rows: a warp per row.
-template <int D>
-__global__ void __launch_bounds__(256) k_attn_join(const AttnArgs args) {
+// Joins the splits' rows in the order of the splits: a warp per row, or (kBlock: many splits) the
+// four warps of a block, each a quarter of them.
+template <int D, bool kBlock>
+__global__ void __launch_bounds__(128) k_attn_join(const AttnArgs args) {
+  constexpr int W = kBlock ? 4 : 1;
+  __shared__ float part[4][66];
   AttnArgs a = args;
   grid_begin(a.part);
   const int64_t all = (int64_t)a.units * a.rows;
-  const int64_t row = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) >> 5;
-  const int lane = threadIdx.x & 31;
-  if (row >= all) return;
-  const float* stat = a.part + (int64_t)a.splits * all * D;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int64_t row = kBlock ? blockIdx.x : (int64_t)blockIdx.x * 4 + warp;
+  if (row >= all) return;  // whole warps, and whole blocks where they synchronise
+  const float2* stat = reinterpret_cast<const float2*>(a.part + (int64_t)a.splits * all * D) + row;
   float m = -INFINITY;
-  for (int s = 0; s < a.splits; s++) m = fmaxf(m, stat[((int64_t)s * all + row) * 2]);
+  for (int s = lane; s < a.splits; s += 32) m = fmaxf(m, stat[s * all].x);
+#pragma unroll
+  for (int x = 16; x > 0; x >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
   const float base = m == -INFINITY ? 0.f : m;
+  const int per = (a.splits + W - 1) / W, s0 = kBlock ? warp * per : 0, s1 = min(a.splits, s0 + per);
   float l = 0.f, o0 = 0.f, o1 = 0.f;
-  for (int s = 0; s < a.splits; s++) {
-    const float* st = stat + ((int64_t)s * all + row) * 2;
-    const float w = exp2_fast(st[0] - base);
-    const float* o = a.part + ((int64_t)s * all + row) * D;
-    if (w == 0.f && st[0] == -INFINITY) continue;  // nothing visible there
-    l += st[1] * w;
-    if (lane < D) o0 += o[lane] * w;
-    if (lane + 32 < D) o1 += o[lane + 32] * w;
+#pragma unroll 8
+  for (int s = s0; s < s1; s++) {
+    const float2 st = stat[s * all];
+    const float* o = a.part + (s * all + row) * D;
+    const float x0 = lane < D ? o[lane] : 0.f, x1 = lane + 32 < D ? o[lane + 32] : 0.f;
+    const bool any = st.x != -INFINITY;  // else nothing is visible there
+    const float w = any ? exp2_fast(st.x - base) : 0.f;
+    l += any ? st.y * w : 0.f;
+    o0 += any ? x0 * w : 0.f;
+    o1 += any ? x1 * w : 0.f;
+  }
+  if constexpr (kBlock) {
+    part[warp][lane] = o0;
+    part[warp][lane + 32] = o1;
+    if (lane == 0) part[warp][64] = l;
+    __syncthreads();
+    if (warp != 0) return;
+    for (int w = 1; w < 4; w++) {
+      o0 += part[w][lane];
+      o1 += part[w][lane + 32];
+      l += part[w][64];
+    }
   }
   const float f = l == 0.f ? 0.f : 1.f / l;
   if (lane < D) a.out[row * D + lane] = o0 * f;
   if (lane + 32 < D) a.out[row * D + lane + 32] = o1 * f;
   if (lane == 0) a.lse[row] = (m + log2f(l)) * kLn2;
+}
+template <int D>
+cudaError_t attn_join(const AttnArgs& a, cudaStream_t st) {
+  const int64_t all = (int64_t)a.units * a.rows;
+  return a.splits > 8 ? launch(k_attn_join<D, true>, dim3((unsigned)all), dim3(128), 0, st, a)
+                      : launch(k_attn_join<D, false>, dim3((unsigned)((all + 3) / 4)), dim3(128), 0, st, a);
 }
 
 // Sums of the splits' partial gradients, in order, four values a thread: dq's where the keys

@@ -792,7 +792,7 @@ cudaError_t attn_tc(const AttnTcArgs& t, bool backward, cudaStream_t st) {
     if (e == cudaSuccess)
       e = launch(kernel, dim3((unsigned)blocks_q, (unsigned)a.splits), dim3(kThreads), smem, st, t);
     if (e == cudaSuccess && a.splits > 1)
-      e = launch(k_attn_join<kD>, dim3((unsigned)((nrows + 7) / 8)), dim3(256), 0, st, a);
+      e = attn_join<kD>(a, st);
     return e;
   }
   constexpr size_t smem = std::max(Map<kDq>::SMEM, Map<kDkv>::SMEM);

@@ -12,16 +12,17 @@ namespace fs {
 namespace {
 
 // Column sums of part [blocks][2 C] in a fixed order: 32 threads share a column's rows (thread
-// y takes rows y, y + 32, ...), their sums are added in order.
-__global__ void __launch_bounds__(1024) k_norm_reduce(const float* __restrict__ part, int64_t blocks, int C,
-                                                       float* __restrict__ dgamma, float* __restrict__ dbeta,
-                                                       int accumulate) {
-  __shared__ float sm[32][33];
+// y takes rows y, y + 32, ...), their sums are added in order.  Eight columns a block: a call has
+// few columns, and what counts is how many loads are on their way.
+__global__ void __launch_bounds__(256) k_norm_reduce(const float* __restrict__ part, int64_t blocks, int C,
+                                                      float* __restrict__ dgamma, float* __restrict__ dbeta,
+                                                      int accumulate) {
+  __shared__ float sm[32][9];
   grid_begin(part);
-  const int64_t n = 2LL * C, c = (int64_t)blockIdx.x * 32 + threadIdx.x;
+  const int64_t n = 2LL * C, c = (int64_t)blockIdx.x * 8 + threadIdx.x;
   float s = 0.f;
   if (c < n) {
-#pragma unroll 4
+#pragma unroll 8
     for (int64_t b = threadIdx.y; b < blocks; b += 32) s += part[b * n + c];
   }
   sm[threadIdx.y][threadIdx.x] = s;
@@ -128,7 +129,7 @@ fs_status fs_norm_bwd(const fs_rows* s, const void* v, const int8_t* q8, const u
   const int64_t blocks = bwd_blocks(s);
   FS_CUDA(s->dtype == FS_BF16 ? norm_bwd<__nv_bfloat16>(a, blocks, st) : norm_bwd<float>(a, blocks, st));
   if (dgamma)
-    FS_CUDA(launch(k_norm_reduce, dim3((unsigned)((2LL * s->C + 31) / 32)), dim3(32, 32), 0, st, a.part, blocks, s->C,
+    FS_CUDA(launch(k_norm_reduce, dim3((unsigned)((2LL * s->C + 7) / 8)), dim3(8, 32), 0, st, a.part, blocks, s->C,
                    dgamma, dbeta, accumulate));
   return FS_OK;
 }

@@ -24,6 +24,7 @@
 #include "fs_launch.h"
 #include "fs_rows.h"
 
+#include <algorithm>
 #include <cuda_bf16.h>
 
 namespace fs {
@@ -647,22 +648,24 @@ auto with_plan(int C, F f) {
   return with_lanes<T, 1>(C, f);
 }
 
-// ahead: rows that a block's row group takes at a time.
+// Blocks for `rows` rows, `ahead` of them a row group at a time: up to per_sm (of 256 threads) on
+// an SM, but not so many that they have fewer than `least` turns to fill their loads in.
 template <typename V, typename TPR, typename K>
-dim3 grid_of(int64_t rows, int per_sm, int ahead) {
+dim3 grid_of(int64_t rows, int per_sm, int ahead, int least) {
   const int64_t per = (int64_t)(block_threads<TPR::value>() / TPR::value) * ahead;
-  const int64_t most = (int64_t)num_sms() * per_sm * 256 / block_threads<TPR::value>();
-  const int64_t want = (rows + per - 1) / per;
-  return dim3((unsigned)(want < most ? want : (most < 1 ? 1 : most)));
+  const int64_t turns = (rows + per - 1) / per, scale = (int64_t)num_sms() * 256;
+  const int64_t most = std::max<int64_t>(1, scale * per_sm / block_threads<TPR::value>());
+  const int64_t full = std::max<int64_t>(1, scale * 3 / block_threads<TPR::value>());  // a wave
+  return dim3((unsigned)std::min(turns, std::min(most, std::max(full, turns / least))));
 }
-constexpr int kFwdPerSm = 24, kBwdPerSm = 9;  // blocks of 256 threads per SM: several waves, which even out
+constexpr int kFwdPerSm = 24;  // most blocks of 256 threads per SM: several waves, which even out
 
 }  // namespace rows
 
 template <typename T>
 int64_t norm_bwd_blocks(int64_t rows, int C) {
   return rows::with_plan<T>(C, [&](auto v, auto l, auto k) {
-    return (int64_t)rows::grid_of<decltype(v), decltype(l), decltype(k)>(rows, rows::kBwdPerSm, rows::rows_ahead<decltype(k)::value>()).x;
+    return (int64_t)rows::grid_of<decltype(v), decltype(l), decltype(k)>(rows, 9, rows::rows_ahead<decltype(k)::value>(), 16).x;
   });
 }
 
@@ -673,7 +676,7 @@ cudaError_t rows_fwd(const RowsArgs& a, cudaStream_t st) {
     using F = rows::Fwd<T, V::value, L::value, K::value, kNorm>;
     auto kernel = rows::k_rows_fwd<T, V::value, L::value, K::value, kNorm>;
     if (cudaError_t e = rows::allow_smem(kernel, F::SMEM)) return e;
-    return launch(kernel, rows::grid_of<V, L, K>(a.rows, rows::kFwdPerSm, 1), dim3(F::THREADS), F::SMEM, st, a);
+    return launch(kernel, rows::grid_of<V, L, K>(a.rows, rows::kFwdPerSm, 1, 8), dim3(F::THREADS), F::SMEM, st, a);
   });
 }
 template <typename T>
@@ -686,7 +689,7 @@ cudaError_t ckpt_unpack(const RowsArgs& a, cudaStream_t st) {
   return rows::with_plan<T>(a.C, [&](auto v, auto l, auto k) {
     using V = decltype(v); using L = decltype(l); using K = decltype(k);
     return launch(rows::k_ckpt_unpack<T, V::value, L::value, K::value>,
-                  rows::grid_of<V, L, K>(a.rows, rows::kFwdPerSm, 1), dim3(rows::block_threads<L::value>()), 0, st, a);
+                  rows::grid_of<V, L, K>(a.rows, rows::kFwdPerSm, 1, 8), dim3(rows::block_threads<L::value>()), 0, st, a);
   });
 }
 
