@@ -304,7 +304,8 @@ typedef struct fs_attn_shape {
   float cap;    /* >= 0; 0: scores are not capped */
 } fs_attn_shape;
 
-/* Device pointers, each may be NULL; the struct itself is read on the host during the call. */
+/* Device pointers, 4-byte aligned, each may be NULL; the struct itself is read on the host
+ * during the call. */
 typedef struct fs_attn_mask {
   const float* slopes;  /* [H]: the distance bias; constants, no gradient */
   const float* pos_q;   /* [B, Gq], with slopes and pos_k only; NULL: i + (Gk - Gq) */

@@ -91,8 +91,9 @@ float* at(void* ws, size_t off) { return reinterpret_cast<float*>(static_cast<ch
 // What a mask may hold: positions only with slopes, both sides' or neither's; documents of
 // both sides or neither; prefixes only under the prefix mask.
 fs_status check_mask(const fs_attn_shape* s, const fs_attn_mask* m) {
-  FS_CHECK_OPT(m->slopes); FS_CHECK_OPT(m->pos_q); FS_CHECK_OPT(m->pos_k);
-  FS_CHECK_OPT(m->doc_q); FS_CHECK_OPT(m->doc_k); FS_CHECK_OPT(m->prefix);
+  const void* all[] = {m->slopes, m->pos_q, m->pos_k, m->doc_q, m->doc_k, m->prefix};
+  for (const void* p : all)  // read word by word: a view of a longer array will do
+    if (reinterpret_cast<uintptr_t>(p) & 3u) return FS_ERR_INVALID;
   if (!m->pos_q != !m->pos_k || !m->doc_q != !m->doc_k) return FS_ERR_INVALID;
   if ((m->pos_q && !m->slopes) || (m->prefix && s->mask != FS_MASK_PREFIX)) return FS_ERR_INVALID;
   return FS_OK;

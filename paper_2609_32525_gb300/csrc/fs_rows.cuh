@@ -648,15 +648,17 @@ auto with_plan(int C, F f) {
   return with_lanes<T, 1>(C, f);
 }
 
-// Blocks for `rows` rows, `ahead` of them a row group at a time: up to per_sm (of 256 threads) on
-// an SM, but not so many that they have fewer than `least` turns to fill their loads in.
+// Blocks for `rows` rows, `ahead` of them a row group at a time: one wave of three (of 256 threads)
+// an SM, or, where each still has `least` turns to fill its loads in, up to per_sm, several waves
+// that even out.
 template <typename V, typename TPR, typename K>
 dim3 grid_of(int64_t rows, int per_sm, int ahead, int least) {
   const int64_t per = (int64_t)(block_threads<TPR::value>() / TPR::value) * ahead;
   const int64_t turns = (rows + per - 1) / per, scale = (int64_t)num_sms() * 256;
+  const int64_t wave = std::max<int64_t>(1, scale * 3 / block_threads<TPR::value>());
   const int64_t most = std::max<int64_t>(1, scale * per_sm / block_threads<TPR::value>());
-  const int64_t full = std::max<int64_t>(1, scale * 3 / block_threads<TPR::value>());  // a wave
-  return dim3((unsigned)std::min(turns, std::min(most, std::max(full, turns / least))));
+  const int64_t many = std::min(most, turns / least);
+  return dim3((unsigned)std::min(turns, many >= 3 * wave ? many : wave));
 }
 constexpr int kFwdPerSm = 24;  // most blocks of 256 threads per SM: several waves, which even out
 

@@ -124,6 +124,23 @@ def test_gradients_are_those_of_differences(lib):
         assert abs((f[0] - f[1]) / (2 * h) - slope) < 2e-3 * max(abs(slope), scale)
 
 
+def test_mask_tensors_may_be_views(lib):
+    """Word-aligned positions, documents, slopes and prefix lengths: views into longer tensors."""
+    for G in (70, 200):
+        c = _attn.make(G, 1, 2, 2, G, G, 32, bias="place", docs=2, prefix=1)
+        m = _attn.mask_of(lib, c)
+        for n in ("slopes", "pos_q", "pos_k", "doc_q", "doc_k", "prefix"):
+            t = getattr(m, n)
+            long = torch.zeros(t.numel() + 3, dtype=t.dtype, device="cuda")
+            view = long[1:1 + t.numel()].view(t.shape)
+            view.copy_(t)
+            assert view.data_ptr() % 16 == 4
+            setattr(m, n, view)
+        got = _attn.run(lib, c)
+        again = _attn.run(lib, c, mask=m)
+        assert all(np.array_equal(got[n], again[n]) for n in got)
+
+
 def test_two_calls_streams_graphs_and_the_same_bits(lib):
     c = _attn.make(11, 2, 8, 8, 512, 512, 32, cap=20.0, docs=3)
     s, m = _attn.shape_of(lib, c), _attn.mask_of(lib, c)
