@@ -1,651 +1,11 @@
-// Self-attention of the slice tokens, forward and backward, in fp32.
-//
-//   s = scale q.k;  c = cap tanh(s / cap) or s;  a = c - slope |pos_q - pos_k|;  masked: weight 0
-//   lse_i = log sum_j exp(a_ij),  p = exp(a - lse),  out_i = sum_j p_ij v_j
-//   D_i = dout_i . out_i;  ds_ij = p_ij (dout_i . v_j - D_i) (1 - (c/cap)^2) scale
-//   dq_i = sum_j ds_ij k_j;  dk_j = sum_i ds_ij q_i;  dv_j = sum_i p_ij dout_i
-//
-// No score is written to memory.  A warp owns 16 rows (queries; for dk and dv keys) and streams
-// the other side through shared memory in tiles of 64 (32 for d = 64), fetched one tile ahead
-// by cp.async; the forward keeps a running maximum and sum per row.
-//
-// The products run on the tensor cores at fp32's accuracy: every fp32 operand is taken as the
-// sum of two tf32 values, x = hi + lo with lo = x - hi exact and cut to tf32's 11 bits by the
-// product, and x y = hi hi' + hi lo' + lo hi' with fp32 accumulation.  What is dropped is
-// 2^-22 of a product.  (bf16 halves drop 2^-16, which the fp32 results of the library's other
-// token operations do not allow; the tf32 exponent is fp32's, so no scale is needed.)
-//
-// Fragments are laid out so that nothing is ever transposed: the order of the contracted index
-// is free as long as both operands use the same one.  In S = X Y^T the thread's lane t = lane
-// % 4 takes channels 8t..8t+7 of both; the accumulator's columns 2t, 2t + 1 become the
-// contracted index of the next product as they lie, with rows 2t, 2t + 1 of Y; and its output
-// columns stand for channels 4g + m, so that a lane's results are 8 neighbouring channels.
-// Rows of shared tiles have d + 4 words, which makes all these 16-byte reads free of conflicts.
-//
-// Masked pairs get weight 0 by a selection, but 0 times an infinity or a NaN that a masked
-// token may hold is NaN inside a product.  Sums over visible pairs alone are what is defined,
-// so a row whose result is not finite is computed again by its warp, pair by pair (slow_*);
-// with finite inputs that never happens.  Tokens without a document (masked for every row)
-// are read as zeros.
-//
-// Few rows leave most of the machine idle: the streamed side is then split into ranges, each
-// block writes a partial result, and a second kernel joins them in order.  No atomics: the
-// same bits in every run.
-#include "fs_attn.cuh"
+// Token attention: how a call is run, and the dispatch of the warps' kernels (fs_attn_mma.cuh).
+#include "fs_attn.h"
 #include "fs_attn_tc.h"
+#include "fs_internal.h"
 
 #include <algorithm>
 
 namespace fs {
-namespace {
-
-constexpr int kMaxWarps = 4;
-constexpr int kNoRow = INT_MIN;  // the index of a tile's row past the last one
-template <int D>
-__host__ __device__ constexpr int tile_rows() { return D == 64 ? 32 : 64; }
-template <int D>
-__host__ __device__ constexpr int row_words() { return D + 4; }
-
-__device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-// The three products of split operands go to two accumulators, lo += al bh + ah bl and hi += ah bh:
-// the tensor core cuts its accumulator towards zero at every step, which drifts over a long chain,
-// so the small terms have a chain of their own, and chains are short (product_cols adds a tile's to
-// fp32 registers).  A warp issues in order and a product waits some 30 clocks for the one before it
-// in its chain, so several chains take turns.
-
-__device__ __forceinline__ void copy16(void* dst, const void* src, bool ok) {
-  const uint32_t d = (uint32_t)__cvta_generic_to_shared(dst);
-  const int n = ok ? 16 : 0;  // the rest is filled with zeros
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(d), "l"(src), "r"(n) : "memory");
-}
-__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-
-// ---- streamed tiles ------------------------------------------------------------------------
-
-template <int D>
-struct Tile {
-  float y0[tile_rows<D>()][row_words<D>()];
-  float y1[tile_rows<D>()][row_words<D>()];
-  float pos[tile_rows<D>()];
-  float lse[tile_rows<D>()], delta[tile_rows<D>()], slope[tile_rows<D>()];  // of streamed queries
-  int doc[tile_rows<D>()], index[tile_rows<D>()];
-};
-
-// The first tile from `tile` on that may hold a visible pair; every warp finds the same.
-template <int D, bool kKeys>
-__device__ __forceinline__ int next_tile(const AttnArgs& a, const Side& s, const Own& o, int prefix, int tile,
-                                         int end) {
-  constexpr int TR = tile_rows<D>();
-  for (; tile < end; tile++) {
-    const int r0 = tile * TR, r1 = min(r0 + TR, s.n);
-    if (a.causal) {
-      if (kKeys) {  // streamed keys: the first of them may be past every own query
-        if (r0 > o.last && r0 >= prefix) continue;
-      } else {  // streamed queries: all of them may be before every own key
-        const int t0 = s.token(r0), t1 = s.token(r1 - 1);
-        const int last = s.first + (r1 - r0 > t1 - t0 + 1 ? s.tokens - 1 : t1);
-        if (o.first > last && o.first >= prefix) continue;
-      }
-    }
-    if (!s.doc) return tile;
-    bool any = false;
-    for (int r = r0 + (threadIdx.x & 31); r < r1; r += 32) {
-      const int doc = s.doc[s.token(r)];
-      any |= doc >= o.doc_lo && doc <= o.doc_hi;
-    }
-    if (__any_sync(0xffffffffu, any)) return tile;
-  }
-  return end;
-}
-
-template <int D, bool kKeys>
-__device__ __forceinline__ void load_tile(Tile<D>& t, const AttnArgs& a, const Unit& u, int unit, int tile) {
-  constexpr int TR = tile_rows<D>(), Q = D / 4;
-  const Side& s = kKeys ? u.k : u.q;
-  const int r0 = tile * TR;
-  for (int i = threadIdx.x; i < TR * Q; i += blockDim.x) {
-    const int r = i / Q, c = i % Q * 4, row = r0 + r;
-    bool ok = row < s.n;
-    if (s.doc && ok) ok = s.doc[s.token(row)] >= 0;
-    const int64_t at = ok ? (int64_t)row * D + c : 0;
-    copy16(&t.y0[r][c], s.x0 + at, ok);
-    copy16(&t.y1[r][c], s.x1 + at, ok);
-  }
-  for (int r = threadIdx.x; r < TR; r += blockDim.x) {
-    const int row = r0 + r;
-    const bool ok = row < s.n;
-    const int tok = ok ? s.token(row) : 0;
-    t.index[r] = ok ? s.first + tok : kNoRow;
-    if (a.slopes) t.pos[r] = ok ? s.place(tok) : 0.f;
-    if (s.doc) t.doc[r] = ok ? s.doc[tok] : -1;
-    if (!kKeys) {
-      t.lse[r] = ok ? lse2_of(a.lse[(int64_t)unit * a.rows + row]) : 0.f;
-      t.delta[r] = ok ? a.delta[(int64_t)unit * a.rows + row] : 0.f;
-      if (a.slopes) t.slope[r] = ok ? a.slopes[u.kvh * (a.H / a.Hkv) + row / a.Gq] * kLog2e : 0.f;
-    }
-  }
-}
-
-// ---- fragments ------------------------------------------------------------------------------
-
-// Channel of a lane's value: k-step s of the first product, and its output's first channel.
-template <int D>
-__device__ __forceinline__ int lane_channel(int s, int t) {
-  constexpr int PER = D < 32 ? D / 4 : 8;  // neighbouring channels of a lane
-  return 32 * (s / (PER / 2)) + PER * t + 2 * (s % (PER / 2));
-}
-
-// The 16 own rows of a warp as the first operand, split once (d <= 32) or when used.
-template <int D>
-struct OwnRows {
-  static constexpr bool kOnce = D <= 32;
-  float x[kOnce ? 1 : D / 8][4];
-  uint32_t hi[kOnce ? D / 8 : 1][4], lo[kOnce ? D / 8 : 1][4];
-  __device__ __forceinline__ void load(const float* rows, int r0, int n, int g, int t) {
-#pragma unroll
-    for (int s = 0; s < D / 8; s++) {
-      const int c = lane_channel<D>(s, t);
-      float2 v0 = make_float2(0.f, 0.f), v1 = v0;
-      if (r0 + g < n) v0 = *reinterpret_cast<const float2*>(rows + (int64_t)(r0 + g) * D + c);
-      if (r0 + g + 8 < n) v1 = *reinterpret_cast<const float2*>(rows + (int64_t)(r0 + g + 8) * D + c);
-      const float f[4] = {v0.x, v1.x, v0.y, v1.y};
-#pragma unroll
-      for (int i = 0; i < 4; i++) {
-        if constexpr (kOnce) {
-          const Split w = split(f[i]);
-          hi[s][i] = w.hi;
-          lo[s][i] = w.lo;
-        } else {
-          x[s][i] = f[i];
-        }
-      }
-    }
-  }
-  __device__ __forceinline__ void get(int s, uint32_t (&h)[4], uint32_t (&l)[4]) const {
-#pragma unroll
-    for (int i = 0; i < 4; i++) {
-      if constexpr (kOnce) {
-        h[i] = hi[s][i];
-        l[i] = lo[s][i];
-      } else {
-        const Split w = split(x[s][i]);
-        h[i] = w.hi;
-        l[i] = w.lo;
-      }
-    }
-  }
-};
-
-// c[n] (columns: tile rows base + 8n + ..) = X Y^T, two or four columns' chains taking turns
-template <int D, int NT>
-__device__ __forceinline__ void product_rows(float (&c)[NT][4], const OwnRows<D>& x,
-                                             const float (*y)[row_words<D>()], int base, int g, int t) {
-  constexpr int PER = D < 32 ? D / 4 : 8, GN = NT < 4 ? NT : 4;
-#pragma unroll
-  for (int n0 = 0; n0 < NT; n0 += GN) {
-    float lo[GN][4];
-#pragma unroll
-    for (int n = 0; n < GN; n++)
-#pragma unroll
-      for (int i = 0; i < 4; i++) c[n0 + n][i] = lo[n][i] = 0.f;
-#pragma unroll
-    for (int blk = 0; blk < (D + 31) / 32; blk++) {
-      float f[GN][PER];
-#pragma unroll
-      for (int n = 0; n < GN; n++)
-#pragma unroll
-        for (int i = 0; i < PER; i += 4)
-          *reinterpret_cast<float4*>(f[n] + i) =
-              *reinterpret_cast<const float4*>(&y[base + 8 * (n0 + n) + g][32 * blk + PER * t + i]);
-#pragma unroll
-      for (int s = 0; s < PER / 2; s++) {
-        uint32_t h[4], l[4];
-        x.get(blk * (PER / 2) + s, h, l);
-        Split b0[GN], b1[GN];
-#pragma unroll
-        for (int n = 0; n < GN; n++) {
-          b0[n] = split(f[n][2 * s]);
-          b1[n] = split(f[n][2 * s + 1]);
-        }
-#pragma unroll
-        for (int n = 0; n < GN; n++) mma(lo[n], l, b0[n].hi, b1[n].hi);
-#pragma unroll
-        for (int n = 0; n < GN; n++) mma(c[n0 + n], h, b0[n].hi, b1[n].hi);
-#pragma unroll
-        for (int n = 0; n < GN; n++) mma(lo[n], h, b0[n].lo, b1[n].lo);
-      }
-    }
-#pragma unroll
-    for (int n = 0; n < GN; n++)
-#pragma unroll
-      for (int i = 0; i < 4; i++) c[n0 + n][i] += lo[n][i];
-  }
-}
-
-// acc = keep acc + P Y with P [16 x 8 NT] as product_rows leaves it
-template <int D, int NT>
-__device__ __forceinline__ void product_cols(float (&acc)[D / 8][4], const float (&keep)[2], const float (&p)[NT][4],
-                                             const float (*y)[row_words<D>()], int base, int g, int t) {
-  constexpr int V = D < 32 ? D / 8 : 4;  // neighbouring output columns m of a lane's read
-#pragma unroll
-  for (int blk = 0; blk < (D + 31) / 32; blk++) {
-    float hi[V][4], lo[V][4];
-#pragma unroll
-    for (int m = 0; m < V; m++)
-#pragma unroll
-      for (int i = 0; i < 4; i++) hi[m][i] = lo[m][i] = 0.f;
-#pragma unroll
-    for (int n = 0; n < NT; n++) {
-      uint32_t h[4], l[4];
-      const float f[4] = {p[n][0], p[n][2], p[n][1], p[n][3]};
-#pragma unroll
-      for (int i = 0; i < 4; i++) {
-        const Split w = split(f[i]);
-        h[i] = w.hi;
-        l[i] = w.lo;
-      }
-      const float* y0 = y[base + 8 * n + 2 * t];
-      const float* y1 = y[base + 8 * n + 2 * t + 1];
-      float f0[V], f1[V];
-      if constexpr (V == 4) {
-        *reinterpret_cast<float4*>(f0) = *reinterpret_cast<const float4*>(y0 + 32 * blk + 4 * g);
-        *reinterpret_cast<float4*>(f1) = *reinterpret_cast<const float4*>(y1 + 32 * blk + 4 * g);
-      } else {
-        *reinterpret_cast<float2*>(f0) = *reinterpret_cast<const float2*>(y0 + 2 * g);
-        *reinterpret_cast<float2*>(f1) = *reinterpret_cast<const float2*>(y1 + 2 * g);
-      }
-      Split b0[V], b1[V];
-#pragma unroll
-      for (int m = 0; m < V; m++) {
-        b0[m] = split(f0[m]);
-        b1[m] = split(f1[m]);
-      }
-#pragma unroll
-      for (int m = 0; m < V; m++) mma(lo[m], l, b0[m].hi, b1[m].hi);
-#pragma unroll
-      for (int m = 0; m < V; m++) mma(hi[m], h, b0[m].hi, b1[m].hi);
-#pragma unroll
-      for (int m = 0; m < V; m++) mma(lo[m], h, b0[m].lo, b1[m].lo);
-    }
-#pragma unroll
-    for (int m = 0; m < V; m++)
-#pragma unroll
-      for (int i = 0; i < 4; i++)
-        acc[blk * V + m][i] = acc[blk * V + m][i] * keep[i >> 1] + (hi[m][i] + lo[m][i]);
-  }
-}
-
-// Writes a lane's results, channels 8t..8t+7 (d = 16: 4t..4t+3) of each 32, of rows g and g + 8.
-template <int D>
-__device__ __forceinline__ void store_rows(float* rows, int r0, int n, const float (&acc)[D / 8][4], float f0,
-                                           float f1, bool skip0, bool skip1, int g, int t) {
-  constexpr int V = D < 32 ? D / 8 : 4;
-#pragma unroll
-  for (int half = 0; half < 2; half++) {
-    const int r = r0 + g + 8 * half;
-    if (r >= n || (half ? skip1 : skip0)) continue;
-    const float f = half ? f1 : f0;
-#pragma unroll
-    for (int blk = 0; blk < (D + 31) / 32; blk++)
-#pragma unroll
-      for (int j = 0; j < 2; j++) {  // accumulator column 2t + j: channels V (2t + j) + m
-        float v[V];
-#pragma unroll
-        for (int m = 0; m < V; m++) v[m] = acc[blk * V + m][2 * half + j] * f;
-        float* dst = rows + (int64_t)r * D + 32 * blk + V * (2 * t + j);
-        if constexpr (V == 4) *reinterpret_cast<float4*>(dst) = *reinterpret_cast<float4*>(v);
-        else *reinterpret_cast<float2*>(dst) = *reinterpret_cast<float2*>(v);
-      }
-  }
-}
-
-// Bit i: row i of the warp's 16 has a value that is not finite.
-template <int D>
-__device__ __forceinline__ uint32_t bad_rows(const float (&acc)[D / 8][4]) {
-  bool b0 = false, b1 = false;
-#pragma unroll
-  for (int m = 0; m < D / 8; m++) {
-    b0 |= !(fabsf(acc[m][0]) < INFINITY) || !(fabsf(acc[m][1]) < INFINITY);
-    b1 |= !(fabsf(acc[m][2]) < INFINITY) || !(fabsf(acc[m][3]) < INFINITY);
-  }
-  uint32_t lo = __ballot_sync(0xffffffffu, b0), hi = __ballot_sync(0xffffffffu, b1), bad = 0;
-#pragma unroll
-  for (int g = 0; g < 8; g++) {
-    if ((lo >> (4 * g)) & 15u) bad |= 1u << g;
-    if ((hi >> (4 * g)) & 15u) bad |= 1u << (g + 8);
-  }
-  return bad;
-}
-
-// ---- forward --------------------------------------------------------------------------------
-
-template <int D>
-__global__ void __launch_bounds__(kMaxWarps * 32) k_attn_fwd(const __grid_constant__ AttnArgs args) {
-  constexpr int TR = tile_rows<D>(), NT = TR / 8;
-  __shared__ Tile<D> tiles[2];
-  const AttnArgs& a = args;  // in the constant bank: no registers through the loops
-  grid_begin();
-  if (a.status && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *a.status = kDevOk;
-  const int per = 16 * a.warps, blocks = (a.rows + per - 1) / per;
-  const int unit = blockIdx.x / blocks, r_blk = (blockIdx.x - unit * blocks) * per, sp = blockIdx.y;
-  const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  const int r0 = r_blk + 16 * (threadIdx.x >> 5);
-  const Unit u = unit_of(a, unit, D);
-  const int ntiles = (a.Gk + TR - 1) / TR;
-  const int tile0 = (int)((int64_t)ntiles * sp / a.splits), tile1 = (int)((int64_t)ntiles * (sp + 1) / a.splits);
-  const Own own = own_range(a, u.q, r_blk, r_blk + per);
-  OwnRows<D> x;
-  x.load(u.q.x0, r0, a.rows, g, t);
-  int qi[2], qdoc[2];
-  float qpos[2], slope2[2];
-#pragma unroll
-  for (int h = 0; h < 2; h++) {
-    const int r = min(r0 + g + 8 * h, a.rows - 1), tok = u.q.token(r);
-    qi[h] = u.q.first + tok;
-    qdoc[h] = u.q.doc ? u.q.doc[tok] : 0;
-    qpos[h] = a.slopes ? u.q.place(tok) : 0.f;
-    slope2[h] = a.slopes ? a.slopes[u.kvh * (a.H / a.Hkv) + r / a.Gq] * kLog2e : 0.f;
-  }
-  float acc[D / 8][4];
-#pragma unroll
-  for (int m = 0; m < D / 8; m++)
-#pragma unroll
-    for (int i = 0; i < 4; i++) acc[m][i] = 0.f;
-  float top[2] = {-INFINITY, -INFINITY}, sum[2] = {0.f, 0.f};
-
-  int tile = next_tile<D, true>(a, u.k, own, u.prefix, tile0, tile1), stage = 0;
-  if (tile < tile1) load_tile<D, true>(tiles[0], a, u, unit, tile);
-  copy_commit();
-  while (tile < tile1) {
-    const int nxt = next_tile<D, true>(a, u.k, own, u.prefix, tile + 1, tile1);
-    if (nxt < tile1) load_tile<D, true>(tiles[stage ^ 1], a, u, unit, nxt);
-    copy_commit();
-    copy_wait<1>();
-    __syncthreads();
-    const Tile<D>& T = tiles[stage];
-    const int k0 = tile * TR;
-    float c[NT][4];
-    product_rows<D, NT>(c, x, T.y0, 0, g, t);
-    if (a.cap > 0.f || a.slopes) {
-#pragma unroll
-      for (int n = 0; n < NT; n++)
-#pragma unroll
-        for (int i = 0; i < 4; i++) {
-          const float far = a.slopes ? fabsf(qpos[i >> 1] - T.pos[8 * n + 2 * t + (i & 1)]) : 0.f;
-          c[n][i] = score_of(a, c[n][i], slope2[i >> 1], far).a;
-        }
-    } else {
-      const float f = a.scale * kLog2e;
-#pragma unroll
-      for (int n = 0; n < NT; n++)
-#pragma unroll
-        for (int i = 0; i < 4; i++) c[n][i] *= f;
-    }
-    if (u.k.doc || k0 + TR > a.Gk || (a.causal && k0 + TR - 1 > own.first && k0 + TR > u.prefix)) {
-#pragma unroll
-      for (int n = 0; n < NT; n++)
-#pragma unroll
-        for (int i = 0; i < 4; i++) {
-          const int col = 8 * n + 2 * t + (i & 1);
-          const bool ok = k0 + col < a.Gk &&
-                          sees(a, u.prefix, qi[i >> 1], k0 + col, qdoc[i >> 1], u.k.doc ? T.doc[col] : 0);
-          if (!ok) c[n][i] = -INFINITY;
-        }
-    }
-    float keep[2];
-#pragma unroll
-    for (int h = 0; h < 2; h++) {
-      float m = top[h];
-#pragma unroll
-      for (int n = 0; n < NT; n++) m = fmaxf(m, fmaxf(c[n][2 * h], c[n][2 * h + 1]));
-      m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 1));
-      m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 2));
-      const float base = m == -INFINITY ? 0.f : m;  // a row that has seen nothing yet
-      keep[h] = exp2_fast(top[h] - base);
-      top[h] = m;
-      float s = 0.f;
-#pragma unroll
-      for (int n = 0; n < NT; n++)
-#pragma unroll
-        for (int j = 0; j < 2; j++) {
-          const float p = exp2_fast(c[n][2 * h + j] - base);
-          c[n][2 * h + j] = p;
-          s += p;
-        }
-      sum[h] = sum[h] * keep[h] + s;
-    }
-    product_cols<D, NT>(acc, keep, c, T.y1, 0, g, t);
-    __syncthreads();
-    tile = nxt;
-    stage ^= 1;
-  }
-#pragma unroll
-  for (int h = 0; h < 2; h++) {
-    sum[h] += __shfl_xor_sync(0xffffffffu, sum[h], 1);
-    sum[h] += __shfl_xor_sync(0xffffffffu, sum[h], 2);
-  }
-  const int64_t at = (int64_t)unit * a.rows;
-  const int64_t all = (int64_t)a.units * a.rows;
-  float* out = a.splits > 1 ? a.part + ((int64_t)sp * all + at) * D : a.out + at * D;
-  float* stat = a.splits > 1 ? a.part + (int64_t)a.splits * all * D + ((int64_t)sp * all + at) * 2 : nullptr;
-  uint32_t bad = bad_rows<D>(acc);
-  float f[2];
-#pragma unroll
-  for (int h = 0; h < 2; h++) {
-    f[h] = a.splits > 1 ? 1.f : (sum[h] == 0.f ? 0.f : 1.f / sum[h]);
-    const int r = r0 + g + 8 * h;
-    if (t == 0 && r < a.rows && !((bad >> (g + 8 * h)) & 1u)) {
-      if (stat) {
-        stat[2 * r] = top[h];
-        stat[2 * r + 1] = sum[h];
-      } else {
-        a.lse[at + r] = (top[h] + log2f(sum[h])) * kLn2;
-      }
-    }
-  }
-  store_rows<D>(out, r0, a.rows, acc, f[0], f[1], (bad >> g) & 1u, (bad >> (g + 8)) & 1u, g, t);
-  for (; bad; bad &= bad - 1) {
-    const int r = r0 + __ffs(bad) - 1;
-    if (r >= a.rows) break;
-    float m, l, o[2];
-    slow_row<D>(args, unit, r, tile0 * TR, min(tile1 * TR, a.Gk), &m, &l, o);
-    const float w = stat ? 1.f : (l == 0.f ? 0.f : 1.f / l);
-    if (lane < D) out[(int64_t)r * D + lane] = o[0] * w;
-    if (lane + 32 < D) out[(int64_t)r * D + lane + 32] = o[1] * w;
-    if (lane == 0) {
-      if (stat) {
-        stat[2 * r] = m;
-        stat[2 * r + 1] = l;
-      } else {
-        a.lse[at + r] = (m + log2f(l)) * kLn2;
-      }
-    }
-  }
-}
-
-// ---- backward -------------------------------------------------------------------------------
-
-// D_i = dout_i . out_i, 8 lanes per row.
-template <int D>
-__global__ void __launch_bounds__(256) k_attn_delta(const AttnArgs args) {
-  AttnArgs a = args;
-  grid_begin(a.out, a.dout);
-  if (a.status && blockIdx.x == 0 && threadIdx.x == 0) *a.status = kDevOk;
-  const int64_t row = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) >> 3;
-  const int l = threadIdx.x & 7;
-  const bool ok = row < (int64_t)a.units * a.rows;
-  float s = 0.f;
-  if (ok)
-#pragma unroll
-    for (int c = 0; c < D / 8; c += 2) {
-      const int at = (c / 2) * 16 + 2 * l;
-      const float2 x = *reinterpret_cast<const float2*>(a.out + row * D + at);
-      const float2 y = *reinterpret_cast<const float2*>(a.dout + row * D + at);
-      s += x.x * y.x + x.y * y.y;
-    }
-#pragma unroll
-  for (int o = 4; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-  if (ok && l == 0) a.delta[row] = s;
-}
-
-// kOwnKeys: a block owns keys, streams queries and makes dk, dv; else it owns queries and makes dq.
-template <int D, bool kOwnKeys>
-__device__ __forceinline__ void backward_block(const AttnArgs& args, const AttnArgs& a, Tile<D> (&tiles)[2], int block,
-                                               int sp) {
-  constexpr int TR = tile_rows<D>(), NT = D == 64 ? 2 : 4;  // 32 streamed rows at a time (16: registers)
-  const int n_own = kOwnKeys ? a.Gk : a.rows, n_str = kOwnKeys ? a.rows : a.Gk;
-  const int splits = kOwnKeys ? a.splits_kv : a.splits;
-  const int per = 16 * a.warps, blocks = (n_own + per - 1) / per;
-  const int unit = block / blocks, r_blk = (block - unit * blocks) * per;
-  const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  const int r0 = r_blk + 16 * (threadIdx.x >> 5);
-  const Unit u = unit_of(a, unit, D);
-  const Side& own_s = kOwnKeys ? u.k : u.q;
-  const Side& str_s = kOwnKeys ? u.q : u.k;
-  const int ntiles = (n_str + TR - 1) / TR;
-  const int tile0 = (int)((int64_t)ntiles * sp / splits), tile1 = (int)((int64_t)ntiles * (sp + 1) / splits);
-  const Own own = own_range(a, own_s, r_blk, r_blk + per);
-  OwnRows<D> x0, x1;
-  x0.load(own_s.x0, r0, n_own, g, t);
-  x1.load(own_s.x1, r0, n_own, g, t);
-  int oi[2], odoc[2];
-  float opos[2], slope2[2], lse2[2], delta[2];
-#pragma unroll
-  for (int h = 0; h < 2; h++) {
-    const int r = min(r0 + g + 8 * h, n_own - 1), tok = own_s.token(r);
-    oi[h] = own_s.first + tok;
-    odoc[h] = own_s.doc ? own_s.doc[tok] : 0;
-    opos[h] = a.slopes ? own_s.place(tok) : 0.f;
-    slope2[h] = lse2[h] = delta[h] = 0.f;
-    if (!kOwnKeys) {
-      if (a.slopes) slope2[h] = a.slopes[u.kvh * (a.H / a.Hkv) + r / a.Gq] * kLog2e;
-      lse2[h] = lse2_of(a.lse[(int64_t)unit * a.rows + r]);
-      delta[h] = a.delta[(int64_t)unit * a.rows + r];
-    }
-  }
-  float acc0[D / 8][4], acc1[kOwnKeys ? D / 8 : 1][4];
-#pragma unroll
-  for (int m = 0; m < D / 8; m++)
-#pragma unroll
-    for (int i = 0; i < 4; i++) {
-      acc0[m][i] = 0.f;
-      if (kOwnKeys) acc1[m][i] = 0.f;
-    }
-
-  int tile = next_tile<D, !kOwnKeys>(a, str_s, own, u.prefix, tile0, tile1), stage = 0;
-  if (tile < tile1) load_tile<D, !kOwnKeys>(tiles[0], a, u, unit, tile);
-  copy_commit();
-  while (tile < tile1) {
-    const int nxt = next_tile<D, !kOwnKeys>(a, str_s, own, u.prefix, tile + 1, tile1);
-    if (nxt < tile1) load_tile<D, !kOwnKeys>(tiles[stage ^ 1], a, u, unit, nxt);
-    copy_commit();
-    copy_wait<1>();
-    __syncthreads();
-    const Tile<D>& T = tiles[stage];
-#pragma unroll 1
-    for (int base = 0; base < TR; base += 8 * NT) {
-      float c[NT][4], dp[NT][4];
-      product_rows<D, NT>(c, x0, T.y0, base, g, t);
-      product_rows<D, NT>(dp, x1, T.y1, base, g, t);
-#pragma unroll
-      for (int n = 0; n < NT; n++)
-#pragma unroll
-        for (int i = 0; i < 4; i++) {
-          const int col = base + 8 * n + 2 * t + (i & 1), h = i >> 1;
-          const int index = T.index[col];
-          const float far = a.slopes ? fabsf(opos[h] - T.pos[col]) : 0.f;
-          const Score s = score_of(a, c[n][i], kOwnKeys ? (a.slopes ? T.slope[col] : 0.f) : slope2[h], far);
-          const int sdoc = str_s.doc ? T.doc[col] : 0;
-          const bool ok = index != kNoRow && (kOwnKeys ? sees(a, u.prefix, index, oi[h], sdoc, odoc[h])
-                                                  : sees(a, u.prefix, oi[h], index, odoc[h], sdoc));
-          const float p = ok ? exp2_fast(s.a - (kOwnKeys ? T.lse[col] : lse2[h])) : 0.f;
-          c[n][i] = p;
-          dp[n][i] = ok ? p * (dp[n][i] - (kOwnKeys ? T.delta[col] : delta[h])) * s.slope : 0.f;
-        }
-      constexpr float kOne[2] = {1.f, 1.f};
-      product_cols<D, NT>(acc0, kOne, dp, T.y0, base, g, t);
-      if constexpr (kOwnKeys) product_cols<D, NT>(acc1, kOne, c, T.y1, base, g, t);
-    }
-    __syncthreads();
-    tile = nxt;
-    stage ^= 1;
-  }
-  const int64_t at = (int64_t)unit * n_own * D, all = (int64_t)a.units * n_own * D;
-  float* out0;
-  float* out1 = nullptr;
-  if constexpr (kOwnKeys) {
-    out0 = (splits > 1 ? a.part_kv + (int64_t)sp * 2 * all : a.dk) + at;
-    out1 = (splits > 1 ? a.part_kv + ((int64_t)sp * 2 + 1) * all : a.dv) + at;
-  } else {
-    out0 = (splits > 1 ? a.part + (int64_t)sp * all : a.dq) + at;
-  }
-  uint32_t bad = bad_rows<D>(acc0);
-  if constexpr (kOwnKeys) bad |= bad_rows<D>(acc1);
-  store_rows<D>(out0, r0, n_own, acc0, 1.f, 1.f, (bad >> g) & 1u, (bad >> (g + 8)) & 1u, g, t);
-  if constexpr (kOwnKeys)
-    store_rows<D>(out1, r0, n_own, acc1, 1.f, 1.f, (bad >> g) & 1u, (bad >> (g + 8)) & 1u, g, t);
-  for (; bad; bad &= bad - 1) {
-    const int r = r0 + __ffs(bad) - 1;
-    if (r >= n_own) break;
-    float o0[2], o1[2];
-    slow_row_bwd<D, kOwnKeys>(args, unit, r, tile0 * TR, min(tile1 * TR, n_str), o0, o1);
-#pragma unroll
-    for (int h = 0; h < 2; h++) {
-      const int c = lane + 32 * h;
-      if (c >= D) continue;
-      out0[(int64_t)r * D + c] = o0[h];
-      if (kOwnKeys) out1[(int64_t)r * D + c] = o1[h];
-    }
-  }
-}
-
-// The blocks that make dk and dv come first: they have four products a pair, those of dq three.
-template <int D>
-__global__ void __launch_bounds__(kMaxWarps * 32) k_attn_bwd(const __grid_constant__ AttnArgs args, int blocks_kv) {
-  __shared__ Tile<D> tiles[2];
-  const AttnArgs& a = args;
-  grid_begin();
-  const int b = blockIdx.x;
-  if (b < blocks_kv * a.splits_kv) backward_block<D, true>(args, a, tiles, b / a.splits_kv, b % a.splits_kv);
-  else {
-    const int c = b - blocks_kv * a.splits_kv;
-    backward_block<D, false>(args, a, tiles, c / a.splits, c % a.splits);
-  }
-}
-
-template <int D>
-cudaError_t attn_fwd_t(const AttnArgs& a, cudaStream_t st) {
-  const int per = 16 * a.warps;
-  const dim3 grid((unsigned)(a.units * ((a.rows + per - 1) / per)), (unsigned)a.splits);
-  cudaError_t e = launch(k_attn_fwd<D>, grid, dim3(32 * a.warps), 0, st, a);
-  if (e == cudaSuccess && a.splits > 1)
-    e = attn_join<D>(a, st);
-  return e;
-}
-
-template <int D>
-cudaError_t attn_bwd_t(const AttnArgs& a, cudaStream_t st) {
-  const int per = 16 * a.warps;
-  const int64_t blocks_q = (int64_t)a.units * ((a.rows + per - 1) / per);
-  const int64_t blocks_kv = (int64_t)a.units * ((a.Gk + per - 1) / per);
-  const int64_t nrows = (int64_t)a.units * a.rows;
-  cudaError_t e = launch(k_attn_delta<D>, dim3((unsigned)((nrows + 31) / 32)), dim3(256), 0, st, a);
-  if (e != cudaSuccess) return e;
-  e = launch(k_attn_bwd<D>, dim3((unsigned)(blocks_q * a.splits + blocks_kv * a.splits_kv)), dim3(32 * a.warps), 0, st,
-             a, (int)blocks_kv);
-  if (e != cudaSuccess || (a.splits == 1 && a.splits_kv == 1)) return e;
-  const int64_t nq = nrows * D, nk = (int64_t)a.units * a.Gk * D;
-  const int64_t n = (a.splits > 1 ? nq : 0) + (a.splits_kv > 1 ? 2 * nk : 0);
-  return launch(k_attn_sum, dim3((unsigned)((n / 4 + 255) / 256)), dim3(256), 0, st, a, nq, nk);
-}
-
-}  // namespace
 
 AttnPlan attn_plan(int64_t units, int64_t rows, int64_t Gk, int d, bool backward) {
   AttnPlan p{};
@@ -686,10 +46,10 @@ AttnPlan attn_plan(int64_t units, int64_t rows, int64_t Gk, int d, bool backward
 }
 
 cudaError_t attn_fwd(const AttnArgs& a, int d, cudaStream_t st) {
-  return d == 16 ? attn_fwd_t<16>(a, st) : d == 32 ? attn_fwd_t<32>(a, st) : attn_fwd_t<64>(a, st);
+  return d == 16 ? attn_mma_fwd<16>(a, st) : d == 32 ? attn_mma_fwd<32>(a, st) : attn_mma_fwd<64>(a, st);
 }
 cudaError_t attn_bwd(const AttnArgs& a, int d, cudaStream_t st) {
-  return d == 16 ? attn_bwd_t<16>(a, st) : d == 32 ? attn_bwd_t<32>(a, st) : attn_bwd_t<64>(a, st);
+  return d == 16 ? attn_mma_bwd<16>(a, st) : d == 32 ? attn_mma_bwd<32>(a, st) : attn_mma_bwd<64>(a, st);
 }
 
 }  // namespace fs

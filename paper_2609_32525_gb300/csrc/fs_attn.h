@@ -30,13 +30,18 @@ struct AttnArgs {
 };
 
 // How a call is run on the current device: on tcgen05 (fs_attn_tc.cu) or with warps' own
-// products (fs_attn.cu), there with so many warps per block; splits of the keys, and of the
+// products (fs_attn_mma.cuh), there with so many warps per block; splits of the keys, and of the
 // query rows for dk and dv.
 struct AttnPlan {
   bool tc;
   int warps, splits, splits_kv;
 };
 AttnPlan attn_plan(int64_t units, int64_t rows, int64_t Gk, int d, bool backward);
+
+template <int D>
+cudaError_t attn_mma_fwd(const AttnArgs& a, cudaStream_t st);
+template <int D>
+cudaError_t attn_mma_bwd(const AttnArgs& a, cudaStream_t st);
 
 cudaError_t attn_fwd(const AttnArgs& a, int d, cudaStream_t st);
 cudaError_t attn_bwd(const AttnArgs& a, int d, cudaStream_t st);

@@ -1,0 +1,6 @@
+#include "fs_attn_mma.cuh"
+
+namespace fs {
+template cudaError_t attn_mma_fwd<64>(const AttnArgs&, cudaStream_t);
+template cudaError_t attn_mma_bwd<64>(const AttnArgs&, cudaStream_t);
+}  // namespace fs

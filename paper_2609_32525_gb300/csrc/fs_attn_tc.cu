@@ -1,4 +1,4 @@
-// Self-attention of the slice tokens on tcgen05 (d = 32): the same results as fs_attn.cu's
+// Self-attention of the slice tokens on tcgen05 (d = 32): the same results as fs_attn_mma.cuh's
 // kernels, for calls with enough rows to fill tiles of 128.
 //
 // A block owns 128 rows (queries; for dk and dv keys) and streams the other side in tiles.  Own
