@@ -59,7 +59,8 @@
  *
  * Call sequence of one coupling (a training step):
  *   fs_slice_fwd   (x_mid, fx)            -> tokens, wsum, lse
- *   fs_mix         (M, tokens)            -> tokens_mixed   (or fs_mix_channels)
+ *   fs_mix         (M, tokens)            -> tokens_mixed   (or fs_mix_channels, or the
+ *                                            original layer's attention, fs_attn_fwd)
  *   fs_deslice_fwd (x_mid, tokens_mixed, lse) -> out
  *   fs_deslice_bwd (..., dout)            -> d_tokens_mixed, dx_mid, dW, dbias, dtau
  *   fs_mix_bwd     (M, tokens, d_tokens_mixed) -> d_tokens, dM
@@ -189,6 +190,12 @@ fs_status fs_mix_channels(const fs_shape* s, const float* Wc, const float* token
 fs_status fs_mix_channels_bwd(const fs_shape* s, const float* Wc, const float* tokens,
                               const float* d_tokens_mixed, float* d_tokens, float* dWc,
                               fs_stream_t stream);
+
+/* The same with d_tokens added to, for tokens that several maps read (the query, key and value
+ * maps of the token attention); dWc is overwritten. */
+fs_status fs_mix_channels_bwd_add(const fs_shape* s, const float* Wc, const float* tokens,
+                                  const float* d_tokens_mixed, float* d_tokens, float* dWc,
+                                  fs_stream_t stream);
 
 /* Deslice with tied weights (Sec. 2; App. G.1): out[b,n,h,:] = sum_g w z'_g.
  *   lse: statistics from fs_slice_fwd; NULL makes the call compute them first

@@ -5,6 +5,8 @@ from __future__ import annotations
 
 import numpy as np
 
+from . import flashslice_oracle as fso
+
 BLOCK = 32
 
 
@@ -113,3 +115,36 @@ def attention(q, k, v, scale, cap=0.0, slopes=None, pos_q=None, pos_k=None, doc_
                 dq[b, h, i] = ds @ kk
                 dk[b, g, at] += ds[:, None] * q[b, h, i]
     return (out, lse) if dout is None else (out, lse, dq, dk, dv)
+
+
+def attention_coupling(x_mid, fx, W_slice, bias, tau, Wq, Wk, Wv, scale, cap=0.0, gamma_q=None, gamma_k=None,
+                       qk_norm=False, norm_eps=1e-5, eps=1e-5, dout=None, **mask):
+    """slice -> q, k, v maps -> (norms of q and k) -> attention -> deslice; with dout the gradients."""
+    s = fso.slice_fwd(x_mid, fx, W_slice, bias, tau, eps)
+    z = s["tokens"]
+    q, k, v = (fso.mix_channels(W, z) for W in (Wq, Wk, Wv))
+    d = q.shape[-1]
+    qn, kn, stats = q, k, None
+    if qk_norm:
+        (yq, mq, rq), (yk, mk, rk) = (norm(t.reshape(-1, d), g, None, norm_eps) for t, g in ((q, gamma_q), (k, gamma_k)))
+        qn, kn, stats = yq.reshape(q.shape), yk.reshape(k.shape), (mq, rq, mk, rk)
+    tm, lse = attention(qn, kn, v, scale, cap, **mask)
+    res = {"out": fso.deslice_fwd(x_mid, W_slice, bias, tau, tm), "tokens": z, "tokens_mixed": tm}
+    if dout is None:
+        return res
+    dd = fso.deslice_bwd(x_mid, W_slice, bias, tau, tm, dout)
+    _, _, dq, dk, dv = attention(qn, kn, v, scale, cap, dout=dd["d_tokens_mixed"], **mask)
+    if qk_norm:
+        shape = q.shape
+        dq, dgq, _ = norm_bwd(q.reshape(-1, d), gamma_q, stats[0], stats[1], dq.reshape(-1, d))
+        dk, dgk, _ = norm_bwd(k.reshape(-1, d), gamma_k, stats[2], stats[3], dk.reshape(-1, d))
+        dq, dk = dq.reshape(shape), dk.reshape(shape)
+        res.update(dgamma_q=dgq, dgamma_k=dgk)
+    dz = 0.0
+    for name, W, g in (("dWq", Wq, dq), ("dWk", Wk, dk), ("dWv", Wv, dv)):
+        r = fso.mix_channels_bwd(W, z, g)
+        dz = dz + r["d_tokens"]
+        res[name] = r["dWc"]
+    sb = fso.slice_bwd(x_mid, fx, W_slice, bias, tau, z, s["wsum"], dz, eps)
+    res.update({n: dd[n] + sb[n] for n in ("dx_mid", "dW", "dbias", "dtau")}, dfx=sb["dfx"])
+    return res

@@ -347,14 +347,24 @@ fs_status fs_mix_channels(const fs_shape* s, const float* Wc, const float* token
   return cuda_status(simt_mix_channels(to_shape(s), Wc, tokens, tokens_mixed, reinterpret_cast<cudaStream_t>(stream)));
 }
 
-fs_status fs_mix_channels_bwd(const fs_shape* s, const float* Wc, const float* tokens, const float* d_tokens_mixed,
-                              float* d_tokens, float* dWc, fs_stream_t stream) {
+static fs_status mix_channels_bwd(const fs_shape* s, const float* Wc, const float* tokens, const float* d_tokens_mixed,
+                                  float* d_tokens, float* dWc, bool add, fs_stream_t stream) {
   FS_CHECK_SHAPE(s);
   FS_CHECK_PTR(Wc); FS_CHECK_PTR(tokens); FS_CHECK_PTR(d_tokens_mixed); FS_CHECK_PTR(d_tokens); FS_CHECK_PTR(dWc);
   const size_t tb = (size_t)s->B * s->H * s->G * s->d * 4, wb = (size_t)s->H * s->d * s->d * 4;
   if (!disjoint({{Wc, wb}, {tokens, tb}, {d_tokens_mixed, tb}}, {{d_tokens, tb}, {dWc, wb}})) return FS_ERR_INVALID;
-  return cuda_status(simt_mix_channels_bwd(to_shape(s), Wc, tokens, d_tokens_mixed, d_tokens, dWc,
+  return cuda_status(simt_mix_channels_bwd(to_shape(s), Wc, tokens, d_tokens_mixed, d_tokens, dWc, add,
                                            reinterpret_cast<cudaStream_t>(stream)));
+}
+
+fs_status fs_mix_channels_bwd(const fs_shape* s, const float* Wc, const float* tokens, const float* d_tokens_mixed,
+                              float* d_tokens, float* dWc, fs_stream_t stream) {
+  return mix_channels_bwd(s, Wc, tokens, d_tokens_mixed, d_tokens, dWc, false, stream);
+}
+
+fs_status fs_mix_channels_bwd_add(const fs_shape* s, const float* Wc, const float* tokens,
+                                  const float* d_tokens_mixed, float* d_tokens, float* dWc, fs_stream_t stream) {
+  return mix_channels_bwd(s, Wc, tokens, d_tokens_mixed, d_tokens, dWc, true, stream);
 }
 
 fs_status fs_deslice_fwd(const fs_shape* s, const void* x_mid, const float* W_slice, const float* bias,

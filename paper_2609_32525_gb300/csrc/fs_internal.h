@@ -52,10 +52,10 @@ cudaError_t simt_reduce_tokens(const Shape& s, int P, const float* part, int Gs,
 cudaError_t simt_finalize(const Shape& s, float* tokens, const float* wsum, cudaStream_t st);
 cudaError_t simt_mix(const Shape& s, const float* M, const float* z, float* zp, cudaStream_t st);
 // The attention-free core: zp[b,h,g,:] = Wc[h] z[b,h,g,:]; its backward dz = Wc^T dzp,
-// dWc = sum over b and g of dzp z^T.
+// dWc = sum over b and g of dzp z^T; with add, dz is added to.
 cudaError_t simt_mix_channels(const Shape& s, const float* Wc, const float* z, float* zp, cudaStream_t st);
 cudaError_t simt_mix_channels_bwd(const Shape& s, const float* Wc, const float* z, const float* dzp, float* dz,
-                                  float* dWc, cudaStream_t st);
+                                  float* dWc, bool add, cudaStream_t st);
 // simt_mix_bwd in one launch.
 cudaError_t mix_bwd(const Shape& s, const float* M, const float* z, const float* dzp, float* dz, float* dM,
                     cudaStream_t st);

@@ -225,7 +225,8 @@ static_assert(8 * kMixTG * kMixTC <= kMixStages * (kMixKC * kMixTC + kMixTG * (k
 // Per-token channel map (the attention-free core): out[bh][g][c] = sum_k A(c, k)
 // in[bh][g][k], with A = Wc[h] (forward) or Wc[h]^T (its token backward); one
 // thread per output word, the sum over k in a fixed order.
-template <bool kTrans>
+// kAdd: added to what out holds.
+template <bool kTrans, bool kAdd>
 __global__ void k_mix_channels(const float* __restrict__ Wc, const float* __restrict__ in, float* __restrict__ out,
                                int64_t BHG, int H, int G, int D) {
   grid_begin(Wc, in);
@@ -238,7 +239,7 @@ __global__ void k_mix_channels(const float* __restrict__ Wc, const float* __rest
   const float* z = in + t * D;
   float acc = 0.f;
   for (int k = 0; k < D; k++) acc = fmaf(kTrans ? A[(int64_t)k * D + c] : A[(int64_t)c * D + k], z[k], acc);
-  out[idx] = acc;
+  out[idx] = kAdd ? out[idx] + acc : acc;
 }
 
 // dWc[h][c][k] = sum over b and g of dzp[b,h,g,c] z[b,h,g,k] (fixed order: b, then g).
@@ -576,15 +577,16 @@ cudaError_t simt_mix_bwd(const Shape& s, const float* M, const float* z, const f
 
 cudaError_t simt_mix_channels(const Shape& s, const float* Wc, const float* z, float* zp, cudaStream_t st) {
   const int64_t BHG = s.BH() * s.G;
-  return launch(k_mix_channels<false>, dim3((unsigned)((BHG * s.d + 255) / 256)), dim3(256), 0, st, Wc, z, zp, BHG, s.H,
+  return launch(k_mix_channels<false, false>, dim3((unsigned)((BHG * s.d + 255) / 256)), dim3(256), 0, st, Wc, z, zp, BHG, s.H,
                 s.G, s.d);
 }
 
 cudaError_t simt_mix_channels_bwd(const Shape& s, const float* Wc, const float* z, const float* dzp, float* dz,
-                                  float* dWc, cudaStream_t st) {
+                                  float* dWc, bool add, cudaStream_t st) {
   const int64_t BHG = s.BH() * s.G;
-  cudaError_t e = launch(k_mix_channels<true>, dim3((unsigned)((BHG * s.d + 255) / 256)), dim3(256), 0, st, Wc, dzp, dz,
-                         BHG, s.H, s.G, s.d);
+  const auto kernel = add ? k_mix_channels<true, true> : k_mix_channels<true, false>;
+  cudaError_t e = launch(kernel, dim3((unsigned)((BHG * s.d + 255) / 256)), dim3(256), 0, st, Wc, dzp, dz, BHG, s.H,
+                         s.G, s.d);
   if (e != cudaSuccess) return e;
   const int64_t n = (int64_t)s.H * s.d * s.d;
   return launch(k_mix_channels_dW, dim3((unsigned)((n + 127) / 128)), dim3(128), 0, st, z, dzp, dWc, s.B, s.H, s.G,

@@ -35,7 +35,7 @@ FS_OP_SLICE_FWD, FS_OP_DESLICE_FWD, FS_OP_DESLICE_BWD, FS_OP_SLICE_BWD, FS_OP_ST
 EXPORTED = ("fs_workspace_bytes", "fs_slice_fwd", "fs_slice_finalize", "fs_mix", "fs_deslice_fwd",
             "fs_deslice_bwd", "fs_mix_bwd", "fs_slice_bwd", "fs_device_status", "fs_status_string",
             "fs_path_for_shape", "fs_backward_path_for_shape", "fs_forward_launch_count", "fs_backward_launch_count",
-            "fs_slice_fwd_noalloc", "fs_slice_fwd_lse", "fs_mix_channels", "fs_mix_channels_bwd", "fs_stats",
+            "fs_slice_fwd_noalloc", "fs_slice_fwd_lse", "fs_mix_channels", "fs_mix_channels_bwd", "fs_mix_channels_bwd_add", "fs_stats",
             "fs_coupling_bwd", "fs_coupling_bwd_launch_count", "fs_norm_fwd", "fs_norm_bwd",
             "fs_norm_workspace_bytes", "fs_ckpt_pack", "fs_ckpt_unpack", "fs_attn_fwd", "fs_attn_bwd",
             "fs_attn_workspace_bytes")
@@ -81,6 +81,7 @@ _sig = {
     "fs_stats": (_I, [_S, _P, _P, _P, _P, _P, _P, _Z, _P]),
     "fs_mix_channels": (_I, [_S, _P, _P, _P, _P]),
     "fs_mix_channels_bwd": (_I, [_S, _P, _P, _P, _P, _P, _P]),
+    "fs_mix_channels_bwd_add": (_I, [_S, _P, _P, _P, _P, _P, _P]),
     "fs_mix": (_I, [_S, _P, _P, _P, _P]),
     "fs_deslice_fwd": (_I, [_S, _P, _P, _P, _P, _P, _P, _P, _P, _Z, _P]),
     "fs_deslice_bwd": (_I, [_S, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _I, _P, _Z, _P]),
@@ -207,6 +208,12 @@ def fs_mix_channels_bwd(shape, Wc, tokens, d_tokens_mixed, d_tokens, dWc, stream
     _check("fs_mix_channels_bwd", _lib.fs_mix_channels_bwd(ctypes.byref(shape), _ptr(Wc), _ptr(tokens),
                                                            _ptr(d_tokens_mixed), _ptr(d_tokens), _ptr(dWc),
                                                            _stream(stream)))
+
+
+def fs_mix_channels_bwd_add(shape, Wc, tokens, d_tokens_mixed, d_tokens, dWc, stream=None):
+    _check("fs_mix_channels_bwd_add",
+           _lib.fs_mix_channels_bwd_add(ctypes.byref(shape), _ptr(Wc), _ptr(tokens), _ptr(d_tokens_mixed),
+                                        _ptr(d_tokens), _ptr(dWc), _stream(stream)))
 
 
 def fs_slice_finalize(shape, tokens, wsum, stream=None):
@@ -518,6 +525,128 @@ class Coupling:
         worst = FS_OK
         for ws in (self.ws_slice, self.ws_deslice) + (
                 (self.ws_dbwd, self.ws_sbwd, self.ws_cbwd) if hasattr(self, "ws_dbwd") else ()):
+            st = fs_device_status(ws, stream)
+            worst = worst or st
+        return worst
+
+
+class AttentionCoupling:
+    """A coupling with the original layer's token operation, self-attention of a head's G tokens:
+
+      tokens = slice(x_mid, fx);  q, k, v = Wq, Wk, Wv tokens (per head, [H, d, d]);
+      tokens_mixed = attention(q, k, v);  out = deslice(x_mid, tokens_mixed)
+
+    cap, prefix, and the mask of the calls: see make_attn_shape and attn_mask.
+    qk_norm: q and k pass through a layer norm over their d channels, with weights gamma_q, gamma_k
+    [d] (None: 1); it bounds the scores whatever the tokens' size.
+    checkpointed: nothing but the 8-bit checkpoints of x_mid and fx is kept for the backward pass,
+    which restores them into `restored` (a pair of buffers [B, N, H, d], which layers may share:
+    pass another layer's) and computes the tokens again.  Its gradients are those at the restored
+    inputs.  The buffers that the forward fills are scratch then, too."""
+
+    NORM_EPS = 1e-5
+
+    def __init__(self, B, N, H, d, G, dtype=torch.bfloat16, eps=1e-5, backward=False, device="cuda", dot=None,
+                 cap=0.0, prefix=False, qk_norm=False, checkpointed=False, restored=None):
+        if checkpointed and not backward:
+            raise ValueError("a checkpoint is for the backward pass")
+        if dot is None:
+            dot = FS_DOT_BF16X2 if backward else FS_DOT_BF16
+        self.shape = make_shape(B, N, H, d, G, dtype, eps, dot)
+        self.attn = make_attn_shape(B, H, G, d, cap=cap, prefix=prefix)
+        self.token_rows = make_rows(B * H * G, d)
+        self.qk_norm, self.checkpointed = qk_norm, checkpointed
+        f32 = dict(dtype=torch.float32, device=device)
+
+        def tokens():
+            return torch.empty(B, H, G, d, **f32)
+
+        def points():
+            return torch.empty(B, N, H, d, dtype=dtype, device=device)
+
+        self.tokens, self.tokens_mixed = tokens(), tokens()
+        self.wsum, self.attn_lse = torch.empty(B, H, G, **f32), torch.empty(B, H, G, **f32)
+        self.lse = torch.empty(B, H, N, **f32)
+        self.q, self.k, self.v = tokens(), tokens(), tokens()
+        # what the attention reads, and the norms' statistics
+        self.q_in, self.k_in = (tokens(), tokens()) if qk_norm else (self.q, self.k)
+        self.stats = [torch.empty(B * H * G, **f32) for _ in range(4)] if qk_norm else [None] * 4
+        self.out = points()
+        self.ws_slice = workspace(self.shape, FS_OP_SLICE_FWD, device)
+        self.ws_deslice = workspace(self.shape, FS_OP_DESLICE_FWD, device)
+        self.ws_attn = attn_workspace(self.attn, False, device)
+        self.packed = None
+        if checkpointed:
+            self.point_rows = make_rows(B * N, H * d, dtype)
+            self.packed = (checkpoint(self.point_rows, device), checkpoint(self.point_rows, device))
+            self.restored = (points(), points()) if restored is None else restored
+        if backward:
+            self.d_tokens_mixed, self.d_tokens = tokens(), tokens()
+            self.dq, self.dk, self.dv = tokens(), tokens(), tokens()
+            self.dx_mid, self.dfx = points(), points()
+            self.dW = torch.empty(H, d, G, **f32)
+            self.dbias, self.dtau = torch.empty(H, G, **f32), torch.empty(H, **f32)
+            self.dWq, self.dWk, self.dWv = (torch.empty(H, d, d, **f32) for _ in range(3))
+            self.dgamma_q, self.dgamma_k, self.unused = (torch.empty(d, **f32) for _ in range(3))
+            self.ws_dbwd = workspace(self.shape, FS_OP_DESLICE_BWD, device)
+            self.ws_sbwd = workspace(self.shape, FS_OP_SLICE_BWD, device)
+            self.ws_abwd = attn_workspace(self.attn, True, device)
+            self.ws_norm = norm_workspace(self.token_rows, device)
+
+    def _mix(self, x_mid, fx, W_slice, bias, tau, Wq, Wk, Wv, mask, gamma_q, gamma_k, stream):
+        s, r = self.shape, self.token_rows
+        fs_slice_fwd(s, x_mid, fx, W_slice, bias, tau, self.tokens, self.wsum, self.lse, True, self.ws_slice, stream)
+        for W, t in ((Wq, self.q), (Wk, self.k), (Wv, self.v)):
+            fs_mix_channels(s, W, self.tokens, t, stream)
+        if self.qk_norm:
+            mq, rq, mk, rk = self.stats
+            fs_norm_fwd(r, self.q, None, gamma_q, None, self.NORM_EPS, None, self.q_in, mq, rq, stream=stream)
+            fs_norm_fwd(r, self.k, None, gamma_k, None, self.NORM_EPS, None, self.k_in, mk, rk, stream=stream)
+        fs_attn_fwd(self.attn, self.q_in, self.k_in, self.v, mask, self.tokens_mixed, self.attn_lse, self.ws_attn, stream)
+
+    def forward(self, x_mid, fx, W_slice, bias, tau, Wq, Wk, Wv, mask=None, gamma_q=None, gamma_k=None, stream=None):
+        self._mix(x_mid, fx, W_slice, bias, tau, Wq, Wk, Wv, mask, gamma_q, gamma_k, stream)
+        fs_deslice_fwd(self.shape, x_mid, W_slice, bias, tau, self.tokens_mixed, self.lse, self.out, self.ws_deslice,
+                       stream)
+        if self.checkpointed:
+            for x, (q8, e8) in zip((x_mid, fx), self.packed):
+                fs_ckpt_pack(self.point_rows, x, q8, e8, stream)
+        return self.out
+
+    def backward(self, x_mid, fx, W_slice, bias, tau, Wq, Wk, Wv, dout, mask=None, gamma_q=None, gamma_k=None,
+                 stream=None):
+        """x_mid, fx: the forward's, or None from the checkpoint."""
+        s, r = self.shape, self.token_rows
+        if self.checkpointed:
+            if x_mid is not None or fx is not None:
+                raise ValueError("x_mid and fx come from the checkpoint")
+            for x, (q8, e8) in zip(self.restored, self.packed):
+                fs_ckpt_unpack(self.point_rows, q8, e8, x, stream)
+            x_mid, fx = self.restored
+            self._mix(x_mid, fx, W_slice, bias, tau, Wq, Wk, Wv, mask, gamma_q, gamma_k, stream)
+        fs_deslice_bwd(s, x_mid, W_slice, bias, tau, self.tokens_mixed, self.lse, dout, self.d_tokens_mixed,
+                       self.dx_mid, self.dW, self.dbias, self.dtau, False, self.ws_dbwd, stream)
+        fs_attn_bwd(self.attn, self.q_in, self.k_in, self.v, mask, self.tokens_mixed, self.attn_lse,
+                    self.d_tokens_mixed, self.dq, self.dk, self.dv, self.ws_abwd, stream)
+        if self.qk_norm:
+            for t, g, d, dg, mean, rstd in ((self.q, gamma_q, self.dq, self.dgamma_q, *self.stats[:2]),
+                                            (self.k, gamma_k, self.dk, self.dgamma_k, *self.stats[2:])):
+                fs_norm_bwd(r, t, None, None, g, mean, rstd, d, None, d, dg, self.unused, False, self.ws_norm, stream)
+        fs_mix_channels_bwd(s, Wq, self.tokens, self.dq, self.d_tokens, self.dWq, stream)
+        fs_mix_channels_bwd_add(s, Wk, self.tokens, self.dk, self.d_tokens, self.dWk, stream)
+        fs_mix_channels_bwd_add(s, Wv, self.tokens, self.dv, self.d_tokens, self.dWv, stream)
+        fs_slice_bwd(s, x_mid, fx, W_slice, bias, tau, self.tokens, self.wsum, self.lse, self.d_tokens, self.dx_mid,
+                     self.dfx, self.dW, self.dbias, self.dtau, True, self.ws_sbwd, stream)
+        g = {"dx_mid": self.dx_mid, "dfx": self.dfx, "dW": self.dW, "dbias": self.dbias, "dtau": self.dtau,
+             "dWq": self.dWq, "dWk": self.dWk, "dWv": self.dWv}
+        if self.qk_norm:
+            g.update(dgamma_q=self.dgamma_q, dgamma_k=self.dgamma_k)
+        return g
+
+    def device_status(self, stream=None):
+        worst = FS_OK
+        for ws in (self.ws_slice, self.ws_deslice, self.ws_attn) + (
+                (self.ws_dbwd, self.ws_sbwd, self.ws_abwd, self.ws_norm) if hasattr(self, "ws_dbwd") else ()):
             st = fs_device_status(ws, stream)
             worst = worst or st
         return worst
