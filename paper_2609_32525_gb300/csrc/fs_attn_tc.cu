@@ -162,6 +162,13 @@ __device__ __forceinline__ void issue_rows(uint32_t d, uint32_t x_hi, uint32_t x
 #pragma unroll
   for (int k = 0; k < 4; k++) mma_tf32(d, x_hi + 8 * k, y_hi + 2 * k, id, 1);
 }
+// d = X Y_hi^T's large products, d + 32 = the small ones, for 32 streamed rows.
+__device__ __forceinline__ void issue_rows_split(uint32_t d, uint32_t x_hi, uint32_t x_lo, uint32_t y) {
+#pragma unroll
+  for (int k = 0; k < 4; k++) mma_tf32(d, x_hi + 8 * k, y + 2 * k, idesc_tf32(64), k > 0);
+#pragma unroll
+  for (int k = 0; k < 4; k++) mma_tf32(d + 32, x_lo + 8 * k, y + 2 * k, idesc_tf32(32), 1);
+}
 // d = P Y over TN streamed rows: P's parts in TMEM, Y's column image in shared memory.
 template <int TN>
 __device__ __forceinline__ void issue_cols(uint32_t d, uint32_t p_hi, uint32_t p_lo, uint32_t y_hi, uint32_t y_lo) {
@@ -177,7 +184,10 @@ __device__ __forceinline__ void issue_cols(uint32_t d, uint32_t p_hi, uint32_t p
 }
 
 // Columns of a pair's TMEM: S, dP (written over by parts of the weights and score gradients),
-// low parts, accumulators; the own rows' parts before both pairs.
+// low parts, accumulators; the own rows' parts before both pairs.  For dk and dv the products of S
+// and dP are in two chains, x_hi (y_hi, y_lo) with both parts of the tile as one operand of 64
+// rows, and x_lo y_hi: 8 products where one chain takes 12 of the same length (a product 32
+// columns wide takes as long as one of 64).  Their low halves lie where low parts go later.
 template <Mode M>
 struct Map {
   static constexpr int TN = M == kDkv ? 32 : 64;
@@ -185,7 +195,7 @@ struct Map {
   static constexpr uint32_t IMG = TN * 128;                                // bytes of one part
   static constexpr uint32_t INFO = (ROWS + COLS) * 2 * IMG, STAGE = INFO + 1024;
   static constexpr int ST = M == kFwd ? 6 : 4;
-  static constexpr uint32_t S = 0, DP = TN, PLO = 64, DSLO = 96, ACC0 = 128, ACC1 = 160;
+  static constexpr uint32_t S = 0, DP = 64, PLO = M == kDkv ? 32 : 64, DSLO = 96, ACC0 = 128, ACC1 = 160;
   static constexpr size_t SMEM = (size_t)ST * STAGE + 1024 + kListMost * 4 + 512;
 };
 static_assert(Map<kFwd>::SMEM <= kMostSmem && Map<kDq>::SMEM <= kMostSmem && Map<kDkv>::SMEM <= kMostSmem, "");
@@ -498,8 +508,13 @@ __device__ __forceinline__ void block_of(const AttnTcArgs& args, int block, int 
       // the products of the pair's last tile have read what S now overwrites
       if (k > 0 && !(ok = mbar_wait_w(&done[w], (uint32_t)((k - 1) & 1), ab, status))) break;
       tc_fence_after();
-      issue_rows<TN>(t0 + C::S, tmem + kX0, tmem + kX0 + 32, st, st + kImg);
-      if (M != kFwd) issue_rows<TN>(t0 + C::DP, tmem + kX1, tmem + kX1 + 32, st + 2 * kImg, st + 3 * kImg);
+      if (M == kDkv) {
+        issue_rows_split(t0 + C::S, tmem + kX0, tmem + kX0 + 32, st);
+        issue_rows_split(t0 + C::DP, tmem + kX1, tmem + kX1 + 32, st + 2 * kImg);
+      } else {
+        issue_rows<TN>(t0 + C::S, tmem + kX0, tmem + kX0 + 32, st, st + kImg);
+        if (M == kDq) issue_rows<TN>(t0 + C::DP, tmem + kX1, tmem + kX1 + 32, st + 2 * kImg, st + 3 * kImg);
+      }
       mma_commit_w(&s_full[w]);
       // the pair's next tile, waited for while the warpgroups work on this one
       if (i + 2 < n && !(ok = mbar_wait_w(&full[(i + 2) % ST], (uint32_t)(((i + 2) / ST) & 1), ab, status))) break;
@@ -575,6 +590,11 @@ __device__ __forceinline__ void block_of(const AttnTcArgs& args, int block, int 
     const int seen_by_all = a.causal ? min(a.Gk, max(own.first + 1, u.prefix)) : a.Gk;
     bool ok = true;
     for (int i = pr, k = 0; i < n; i += 2, k++) {
+      if (k > 0) {  // the last tile's products, added while this one's scores are formed
+        if (!(ok = mbar_wait_w(&done[pr], (uint32_t)((k - 1) & 1), ab, status))) break;
+        tc_fence_after();
+        flush();
+      }
       if (!(ok = mbar_wait_w(&s_full[pr], (uint32_t)(k & 1), ab, status))) break;
       tc_fence_after();
       const Info<M> f(smem + (size_t)(i % ST) * C::STAGE);
@@ -590,7 +610,6 @@ __device__ __forceinline__ void block_of(const AttnTcArgs& args, int block, int 
       }
       if constexpr (M == kFwd) {
         const int j0 = 32 * half;
-        if (k > 0) flush();  // before the scores take its registers
         // Twice over the columns, 16 at a time, for the maximum and for the weights: all 32 scores
         // beside the accumulators would spill, and a spilled accumulator is a load from the
         // second-level cache (1000 clocks a tile).  Capped or biased scores go back in between.
@@ -635,8 +654,25 @@ __device__ __forceinline__ void block_of(const AttnTcArgs& args, int block, int 
           uint32_t s[16], d[16];
           tmem_ld16(t0 + C::S + h, s);
           tmem_ld16(t0 + C::DP + h, d);
-          tmem_wait_ld(s);
-          tmem_wait_ld(d);
+          if constexpr (M == kDkv) {
+            uint32_t sl[16], dl[16];
+            tmem_ld16(t0 + C::PLO + h, sl);
+            tmem_ld16(t0 + C::DSLO + h, dl);
+            tmem_wait_ld(s);
+            tmem_wait_ld(d);
+            tmem_wait_ld(sl);
+            tmem_wait_ld(dl);
+#pragma unroll
+            for (int j = 0; j < 16; j += 2) {
+              const uint64_t x = add2(pack2(s[j], s[j + 1]), pack2(sl[j], sl[j + 1]));
+              const uint64_t y = add2(pack2(d[j], d[j + 1]), pack2(dl[j], dl[j + 1]));
+              s[j] = (uint32_t)x, s[j + 1] = (uint32_t)(x >> 32);
+              d[j] = (uint32_t)y, d[j + 1] = (uint32_t)(y >> 32);
+            }
+          } else {
+            tmem_wait_ld(s);
+            tmem_wait_ld(d);
+          }
           columns_by_mask<M, 16, kCap, kBias>(a, o, f, k0, h, mask, s, d);
           if constexpr (M == kDkv) {
             store_parts(t0 + C::DP + h, t0 + C::DSLO + h, d);
@@ -645,7 +681,6 @@ __device__ __forceinline__ void block_of(const AttnTcArgs& args, int block, int 
             store_parts(t0 + C::S + h, t0 + C::DP + h, d);
           }
         }
-        if (k > 0) flush();
       }
       tmem_wait_st();
       tc_fence_before();
