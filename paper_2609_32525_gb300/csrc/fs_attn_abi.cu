@@ -19,6 +19,7 @@ bool valid(const fs_attn_shape* s) {
   if (s->mask != FS_MASK_NONE && s->mask != FS_MASK_PREFIX) return false;
   if (s->mask == FS_MASK_PREFIX && s->Gq > s->Gk) return false;
   if (!std::isfinite(s->scale) || !(s->cap >= 0.f) || !std::isfinite(s->cap)) return false;
+  if (s->cap > 0.f && !std::isfinite(s->scale / s->cap)) return false;  // the kernels' factor
   const double most = (double)s->B * s->H * (double)(s->Gq > s->Gk ? s->Gq : s->Gk) * s->d;
   return most < 1099511627776.0;  // 2^40
 }

@@ -123,7 +123,7 @@ __device__ __forceinline__ void load_tile(Tile<D>& t, const AttnArgs& a, const U
     const int tok = ok ? s.token(row) : 0;
     t.index[r] = s.first + tok;
     if (a.slopes) t.pos[r] = ok ? s.place(tok) : 0.f;
-    if (s.doc) t.doc[r] = ok ? s.doc[tok] : -1;
+    if (s.doc) t.doc[r] = ok ? max(s.doc[tok], -1) : -1;  // any negative number: not in use
     if (!kKeys) {
       t.lse[r] = ok ? lse2_of(a.lse[(int64_t)unit * a.rows + row]) : INFINITY;  // weight 0 past the last row
       t.delta[r] = ok ? a.delta[(int64_t)unit * a.rows + row] : 0.f;

@@ -103,7 +103,7 @@ __global__ void __launch_bounds__(256) k_attn_prep(const __grid_constant__ AttnT
   if (tid >= 32 || (job != 0 && job != 3) || (job == 0 && unit % a.Hkv != 0)) return;
   const int mine = atom * 32 + tid, tok = mine % tokens;
   const bool in = mine < n;
-  const int doc = docs && in ? docs[tok] : -1;
+  const int doc = docs && in ? max(docs[tok], -1) : -1;  // any negative number: not in use
   int lo = doc >= 0 ? doc : INT_MAX, hi = doc;
 #pragma unroll
   for (int m = 16; m > 0; m >>= 1) {

@@ -40,6 +40,25 @@ def test_large_scores(lib, d):
         _attn.check(lib, c)
 
 
+@pytest.mark.parametrize("scale", [-0.3, 0.0])
+@pytest.mark.parametrize("cap", [0.0, 3.0])
+def test_negative_and_zero_scale(lib, scale, cap):
+    for G in (50, 140):
+        _attn.check(lib, {**_attn.make(G, 1, 2, 2, G, G, 32, cap=cap), "scale": scale})
+
+
+def test_any_negative_document_is_none(lib):
+    """Unused tokens see nothing, whatever negative numbers they carry."""
+    for G in (60, 150):
+        c = _attn.make(G, 2, 2, 2, G, G, 32, docs=2)
+        rng = np.random.default_rng(G)
+        for n in ("doc_q", "doc_k"):
+            t = c["mask"][n]
+            t[t < 0] = rng.choice([-1, -2, -(2 ** 31)], (t < 0).sum())
+        got = _attn.check(lib, c)
+        assert (got["lse"][np.broadcast_to((c["mask"]["doc_q"] < 0)[:, None], got["lse"].shape)] == -np.inf).all()
+
+
 def test_tiny_and_huge_magnitudes(lib):
     """fp32's exponent range: no scale is assumed."""
     for f in (1e-20, 1e18):
@@ -184,3 +203,17 @@ def test_splits_and_whole_rows_agree_with_the_oracle_at_a_large_size(lib):
         p = np.exp(a - a.max(1, keepdims=True))
         out = (p / p.sum(1, keepdims=True)) @ v
         assert np.linalg.norm(got["out"][0, h, rows] - out) <= 3e-6 * np.linalg.norm(out)
+
+
+def test_one_query_over_a_long_cache(lib):
+    """200,003 keys, split many ways: offsets and joins."""
+    c = _attn.make(13, 2, 2, 1, 1, 200003, 16, bias="index", docs=3, bwd=False)
+    c["mask"]["doc_q"][:] = [[1], [-1]]
+    c["mask"]["slopes"] *= np.float32(1e-4)
+    _attn.check(lib, c)
+
+
+def test_many_units(lib):
+    """More units than SMs, few tokens each."""
+    _attn.check(lib, _attn.make(14, 40, 8, 4, 20, 20, 16, cap=2.0))
+    _attn.check(lib, _attn.make(15, 20, 8, 8, 129, 130, 32))

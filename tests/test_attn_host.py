@@ -44,7 +44,7 @@ def backward(fs, s, m=None, nbytes=1 << 40, **kw):
 
 @pytest.mark.parametrize("bad", [dict(B=0), dict(H=0), dict(Hkv=0), dict(Hkv=3), dict(Gq=0), dict(Gk=0), dict(Gk=-1),
                                  dict(d=0), dict(mask=2), dict(mask=1, Gq=51), dict(scale=float("nan")),
-                                 dict(scale=float("inf")), dict(cap=-1.0), dict(cap=float("nan")), dict(cap=float("inf")),
+                                 dict(scale=float("inf")), dict(cap=-1.0), dict(cap=float("nan")), dict(cap=float("inf")), dict(cap=1e-44, scale=10.0),
                                  dict(B=1 << 40, H=1 << 20)])
 def test_bad_shapes(fs, bad):
     s = shape(fs, **bad)
