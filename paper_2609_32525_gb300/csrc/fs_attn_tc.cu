@@ -201,30 +201,25 @@ struct Map {
 static_assert(Map<kFwd>::SMEM <= kMostSmem && Map<kDq>::SMEM <= kMostSmem && Map<kDkv>::SMEM <= kMostSmem, "");
 constexpr uint32_t kX0 = 0, kX1 = 64, kPair = 128, kPairCols = 192;
 
-__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t (&r)[8]) {
-  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(taddr), "r"(r[0]),
-               "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
-               : "memory");
-}
 __device__ __forceinline__ uint64_t both(float x) { return pack2(__float_as_uint(x), __float_as_uint(x)); }
-// Parts of N values into N columns each, eight at a time: registers are what the warpgroups lack.
-// (A high part that is cut instead of rounded is an operation less, but leaves a low part that
-// loses twice as much to tf32: dq's error grew from 7e-7 to 1e-6, at no gain in time.)
+// Parts of N values into N columns each.  (A high part that is cut instead of rounded is an
+// operation less, but leaves a low part that loses twice as much to tf32: dq's error grew from
+// 7e-7 to 1e-6, at no gain in time.)
 template <int N>
 __device__ __forceinline__ void store_parts(uint32_t hi_at, uint32_t lo_at, const uint32_t (&p)[N]) {
 #pragma unroll
-  for (int j = 0; j < N; j += 8) {
-    uint32_t h[8], l[8];
+  for (int j = 0; j < N; j += 16) {
+    uint32_t h[16], l[16];
 #pragma unroll
-    for (int i = 0; i < 8; i++) h[i] = tf32_hi(__uint_as_float(p[j + i]));
+    for (int i = 0; i < 16; i++) h[i] = tf32_hi(__uint_as_float(p[j + i]));
 #pragma unroll
-    for (int i = 0; i < 8; i += 2) {
+    for (int i = 0; i < 16; i += 2) {
       const uint64_t lo = fma2(pack2(h[i], h[i + 1]), both(-1.f), pack2(p[j + i], p[j + i + 1]));
       l[i] = (uint32_t)lo;
       l[i + 1] = (uint32_t)(lo >> 32);
     }
-    tmem_st8(hi_at + j, h);
-    tmem_st8(lo_at + j, l);
+    tmem_st16(hi_at + j, h);
+    tmem_st16(lo_at + j, l);
   }
 }
 

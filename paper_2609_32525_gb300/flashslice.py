@@ -303,14 +303,20 @@ def _arg(fn, name, t, dtype, numel, dev, optional=False):
     raise ValueError(f"{fn}: {name} is on {t.device}, the call on the current device and its stream")
 
 
+# The handle of a device's current stream, without the object around it where torch has that (a
+# microsecond of a small call's nine).
+_current_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda dev: torch.cuda.current_stream(dev).cuda_stream)
+
+
 def _where(fn, first, stream):
     """The current device, and the raw stream of the call."""
     if not isinstance(first, torch.Tensor) or not first.is_cuda:  # nothing to ask a device for
         return -2, None
     dev = torch.cuda.current_device()
     if stream is None:
-        stream = torch.cuda.current_stream(dev)
-    elif stream.device_index != dev:
+        return dev, _current_raw_stream(dev)
+    if stream.device_index != dev:
         raise ValueError(f"{fn}: the stream is on cuda:{stream.device_index}, the current device is cuda:{dev}")
     return dev, stream.cuda_stream
 
