@@ -11,7 +11,12 @@ AttnPlan attn_plan(int64_t units, int64_t rows, int64_t Gk, int d, bool backward
   AttnPlan p{};
   p.splits_kv = 1;
   const int64_t sms = num_sms();
-  p.tc = d == 32 && rows >= 128 && Gk >= 128;
+  // tcgen05 where a tile of 128 rows is full and there are pairs enough to pay for the images and
+  // for a block's start.  Both sides, d = 32, in us (tcgen05 / warps): forward 8 heads x 256
+  // tokens 11.3 / 9.5, 384: 12.3 / 11.4, 512: 12.5 / 14.9; 32 x 256: 13.4 / 15.0, 32 x 512: 16.0 /
+  // 35.2; 128 x 64: 8.9 / 6.7, 128 x 128: 9.7 / 11.6; 32 x 64 against 4096 keys 38.6 / 35.5.
+  // Backward 8 x 256: 15.9 / 13.3, 384: 17.6 / 18.8, 512: 20.6 / 28.8; 32 x 128: 13.9 / 12.8.
+  p.tc = d == 32 && rows >= 128 && Gk >= 128 && units * rows * Gk >= (backward ? 1100000 : 1500000);
   if (p.tc) {
     // One block of 128 rows per SM at a time: the split whose waves of blocks cost least, a
     // block's time being its tiles and about two more; ranges of two tiles at least, and no

@@ -226,11 +226,12 @@ __global__ void __launch_bounds__(128) k_attn_join(const AttnArgs args) {
     const float2 st = stat[s * all];
     const float* o = a.part + (s * all + row) * D;
     const float x0 = lane < D ? o[lane] : 0.f, x1 = lane + 32 < D ? o[lane + 32] : 0.f;
-    const bool any = st.x != -INFINITY;  // else nothing is visible there
-    const float w = any ? exp2_fast(st.x - base) : 0.f;
-    l += any ? st.y * w : 0.f;
-    o0 += any ? x0 * w : 0.f;
-    o1 += any ? x1 * w : 0.f;
+    // A range in which nothing is visible has sum 0 and zeros; one with a NaN among its scores may
+    // have no maximum either, but its sum is NaN and stays so.
+    const float w = exp2_fast(st.x - base);
+    l += st.y * w;
+    o0 += x0 * w;
+    o1 += x1 * w;
   }
   if constexpr (kBlock) {
     part[warp][lane] = o0;

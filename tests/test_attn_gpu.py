@@ -14,10 +14,12 @@ SIZES = [(1, 1, 1, 1, 1, 32), (1, 2, 1, 2, 2, 16), (2, 2, 2, 3, 3, 64), (1, 8, 8
          (2, 4, 2, 17, 17, 16), (1, 2, 1, 31, 31, 64), (1, 2, 2, 63, 63, 32), (1, 4, 4, 64, 64, 16), (3, 4, 2, 100, 100, 64),
          (1, 3, 3, 65, 65, 32), (1, 2, 1, 129, 129, 32), (1, 8, 2, 130, 130, 32), (1, 1, 1, 257, 257, 64),
          (1, 2, 2, 300, 300, 16), (2, 8, 2, 1, 700, 32), (1, 4, 1, 5, 1000, 64), (1, 2, 2, 40, 33, 32), (2, 4, 1, 1, 1, 32),
-         # tiles of 128 rows (d = 32, 128 rows and keys at least): several heads in a tile, one tile, many, more
-         # queries than keys
-         (1, 4, 1, 40, 300, 32), (2, 2, 2, 256, 256, 32), (1, 2, 2, 600, 129, 32), (1, 1, 1, 128, 1500, 32),
-         (2, 2, 1, 64, 128, 32), (1, 1, 1, 500, 500, 32)]
+         # d = 32, at least 128 rows and keys and 1.5 million pairs: tiles of 128 rows on tcgen05; several heads in a
+         # tile, one tile, many, ragged ones, more queries than keys
+         (1, 16, 4, 100, 1000, 32), (1, 8, 8, 440, 440, 32), (1, 8, 8, 600, 330, 32), (12, 8, 8, 128, 128, 32),
+         (2, 8, 2, 129, 760, 32), (1, 1, 1, 1300, 1301, 32), (1, 16, 1, 33, 3000, 32),
+         # just below: the same shapes by warps
+         (1, 4, 1, 40, 300, 32), (2, 2, 2, 256, 256, 32), (1, 2, 2, 600, 129, 32)]
 PLAIN = [dict(), dict(cap=5.0), dict(bias="index"), dict(bias="place", cap=2.0), dict(docs=2), dict(prefix=0),
          dict(prefix=1, bias="index"), dict(docs=3, prefix=1, cap=3.0, bias="place")]
 
@@ -34,22 +36,23 @@ def test_against_the_oracle(lib, size, what):
 def test_large_scores(lib, d):
     """Scores of some tens, capped and not: the running maximum moves by much from tile to tile."""
     for cap in (0.0, 10.0):
-        c = _attn.make(d, 1, 2, 2, 200, 200, d, cap=cap)
-        c["q"] *= 4
-        c["k"] *= 3
-        _attn.check(lib, c)
+        for H, G in ((2, 200),) + (((4, 640),) if d == 32 else ()):
+            c = _attn.make(d, 1, H, H, G, G, d, cap=cap)
+            c["q"] *= 4
+            c["k"] *= 3
+            _attn.check(lib, c)
 
 
 @pytest.mark.parametrize("scale", [-0.3, 0.0])
 @pytest.mark.parametrize("cap", [0.0, 3.0])
 def test_negative_and_zero_scale(lib, scale, cap):
-    for G in (50, 140):
-        _attn.check(lib, {**_attn.make(G, 1, 2, 2, G, G, 32, cap=cap), "scale": scale})
+    for G in (50, 640):
+        _attn.check(lib, {**_attn.make(G, 1, 4, 4, G, G, 32, cap=cap), "scale": scale})
 
 
 def test_any_negative_document_is_none(lib):
     """Unused tokens see nothing, whatever negative numbers they carry."""
-    for G in (60, 150):
+    for G in (60, 650):
         c = _attn.make(G, 2, 2, 2, G, G, 32, docs=2)
         rng = np.random.default_rng(G)
         for n in ("doc_q", "doc_k"):
@@ -62,14 +65,16 @@ def test_any_negative_document_is_none(lib):
 def test_tiny_and_huge_magnitudes(lib):
     """fp32's exponent range: no scale is assumed."""
     for f in (1e-20, 1e18):
-        c = _attn.make(5, 1, 2, 2, 70, 70, 32)
-        c["v"] *= np.float32(f)
-        c["dout"] *= np.float32(1 / f)
-        _attn.check(lib, c)
+        for G in (70, 900):
+            c = _attn.make(5, 1, 2, 2, G, G, 32)
+            c["v"] *= np.float32(f)
+            c["dout"] *= np.float32(1 / f)
+            _attn.check(lib, c)
 
 
-def test_rows_that_see_nothing(lib):
-    c = _attn.make(6, 2, 4, 2, 90, 90, 32, docs=2)
+@pytest.mark.parametrize("G", [90, 460])
+def test_rows_that_see_nothing(lib, G):
+    c = _attn.make(6, 2, 4, 2, G, G, 32, docs=2)
     c["mask"]["doc_q"][0, :40] = -1
     c["mask"]["doc_k"][1] = -1
     got = _attn.check(lib, c)
@@ -82,8 +87,8 @@ def test_rows_that_see_nothing(lib):
 def test_what_masked_tokens_hold_reaches_no_result(lib, d, bad):
     """Documents: tokens of document 1 and unused ones hold `bad`; document 0's results are those
     of clean tokens."""
-    for prefix in (None, 1):
-        c = _attn.make(7, 2, 4, 2, 150, 150, d, docs=2, cap=4.0, bias="place", prefix=prefix)
+    for prefix, G in ((None, 150), (1, 150)) + (((None, 460), (1, 460)) if d == 32 else ()):
+        c = _attn.make(7, 2, 4, 2, G, G, d, docs=2, cap=4.0, bias="place", prefix=prefix)
         c["mask"]["doc_q"] = c["mask"]["doc_k"].copy()
         other = c["mask"]["doc_k"] != 0
         clean = {n: t.copy() for n, t in c.items() if n in ("q", "k", "v", "dout")}
@@ -100,31 +105,33 @@ def test_what_masked_tokens_hold_reaches_no_result(lib, d, bad):
             assert (got[n][unused] == (-np.inf if n == "lse" else 0)).all(), n
 
 
-def test_what_later_keys_hold_reaches_no_earlier_query(lib):
-    c = _attn.make(8, 1, 2, 2, 150, 150, 32, prefix=0)
+@pytest.mark.parametrize("G", [150, 900])
+def test_what_later_keys_hold_reaches_no_earlier_query(lib, G):
+    c, cut = _attn.make(8, 1, 2, 2, G, G, 32, prefix=0), G - 50
     for n in ("k", "v", "q", "dout"):
-        c[n][:, :, 100:] = np.nan
+        c[n][:, :, cut:] = np.nan
     got = _attn.run(lib, c)
-    ref = _attn.make(8, 1, 2, 2, 150, 150, 32, prefix=0)
+    ref = _attn.make(8, 1, 2, 2, G, G, 32, prefix=0)
     for n in ("k", "v", "q", "dout"):
-        ref[n][:, :, 100:] = 0
+        ref[n][:, :, cut:] = 0
     res = _attn.want(ref)
     for n in ("out", "lse", "dq"):
-        assert np.isfinite(got[n][:, :, :100]).all()
-        assert np.linalg.norm(got[n][:, :, :100] - res[n][:, :, :100]) <= 3e-6 * np.linalg.norm(res[n][:, :, :100])
-        assert np.isnan(got[n][:, :, 100:]).all()
+        assert np.isfinite(got[n][:, :, :cut]).all()
+        assert np.linalg.norm(got[n][:, :, :cut] - res[n][:, :, :cut]) <= 3e-6 * np.linalg.norm(res[n][:, :, :cut])
+        assert np.isnan(got[n][:, :, cut:]).all()
     assert np.isnan(got["dk"]).all()  # every key is seen by the last queries
 
 
-def test_a_visible_nan_or_infinite_score(lib):
-    c = _attn.make(9, 1, 1, 1, 40, 40, 32, bwd=False)
-    c["k"][0, 0, 5, 0] = np.nan
+@pytest.mark.parametrize("H, G", [(1, 40), (4, 640)])
+def test_a_visible_nan_or_infinite_score(lib, H, G):
+    c = _attn.make(9, 1, H, H, G, G, 32, bwd=False)
+    c["k"][0, :, 5, 0] = np.nan
     assert np.isnan(_attn.run(lib, c)["out"]).all()
-    c = _attn.make(9, 1, 1, 1, 40, 40, 32, bwd=False)
-    c["k"][0, 0, :, :] = 0
-    c["k"][0, 0, 5] = -np.inf
+    c = _attn.make(9, 1, H, H, G, G, 32, bwd=False)
+    c["k"][0, :, :, :] = 0
+    c["k"][0, :, 5] = -np.inf
     c["q"][:] = np.abs(c["q"]) + 0.1  # key 5 scores -infinity for every query: weight 0
-    got, clean = _attn.run(lib, c), {**c, "k": np.delete(c["k"], 5, 2), "v": np.delete(c["v"], 5, 2), "Gk": 39}
+    got, clean = _attn.run(lib, c), {**c, "k": np.delete(c["k"], 5, 2), "v": np.delete(c["v"], 5, 2), "Gk": G - 1}
     assert np.abs(got["out"] - _attn.want(clean)["out"]).max() < 1e-6
 
 
@@ -145,7 +152,7 @@ def test_gradients_are_those_of_differences(lib):
 
 def test_mask_tensors_may_be_views(lib):
     """Word-aligned positions, documents, slopes and prefix lengths: views into longer tensors."""
-    for G in (70, 200):
+    for G in (70, 900):
         c = _attn.make(G, 1, 2, 2, G, G, 32, bias="place", docs=2, prefix=1)
         m = _attn.mask_of(lib, c)
         for n in ("slopes", "pos_q", "pos_k", "doc_q", "doc_k", "prefix"):
@@ -216,4 +223,4 @@ def test_one_query_over_a_long_cache(lib):
 def test_many_units(lib):
     """More units than SMs, few tokens each."""
     _attn.check(lib, _attn.make(14, 40, 8, 4, 20, 20, 16, cap=2.0))
-    _attn.check(lib, _attn.make(15, 20, 8, 8, 129, 130, 32))
+    _attn.check(lib, _attn.make(15, 20, 8, 8, 129, 130, 32, bwd=False))
