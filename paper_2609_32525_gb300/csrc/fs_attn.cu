@@ -33,6 +33,7 @@ AttnPlan attn_plan(int64_t units, int64_t rows, int64_t Gk, int d, bool backward
       }
     }
     if (backward) p.splits_kv = p.splits;
+    p.delta = true;
     return p;
   }
   // Blocks take 16 rows a warp, up to 64.  Where they would leave SMs without two warps for
@@ -46,7 +47,15 @@ AttnPlan attn_plan(int64_t units, int64_t rows, int64_t Gk, int d, bool backward
     return (int)std::max<int64_t>(1, std::min(want / blocks, tiles));
   };
   p.splits = split(rows, Gk);
-  if (backward) p.splits_kv = split(Gk, rows);
+  if (backward) {
+    p.splits_kv = split(Gk, rows);
+    // D = dout . out by a kernel of its own where blocks that own keys meet more than two tiles of
+    // queries; else they make it on the way, which saves a launch of three.  Both sides in us
+    // (on the way / own kernel): 8 heads x 64 tokens, d = 32 8.0 / 8.6, 128 x 64 10.7 / 11.9,
+    // 12 x 100, d = 64 13.7 / 14.3; above the rule 4 x 512, d = 64 35.8 / 33.7, 16 x 1024 337 / 324.
+    // A single warp has too few lanes for it: 8 x 16 9.4 / 8.7.
+    p.delta = p.warps == 1 || (rows + tile - 1) / tile > 2 * p.splits_kv;
+  }
   return p;
 }
 

@@ -172,7 +172,9 @@ __device__ void slow_grad(const AttnArgs& a, const Unit& u, int unit, int r, int
   const int64_t row = (int64_t)unit * a.rows + r;
   *p = exp2_fast(s.a - lse2_of(a.lse[row]));
   if (*p == 0.f) return;
-  *ds = *p * (dot_row<D>(u.q.x1 + (int64_t)r * D, u.k.x1 + (int64_t)j * D) - a.delta[row]) * s.slope;
+  const float* g = u.q.x1 + (int64_t)r * D;
+  const float delta = a.delta ? a.delta[row] : dot_row<D>(g, a.out + row * D);
+  *ds = *p * (dot_row<D>(g, u.k.x1 + (int64_t)j * D) - delta) * s.slope;
 }
 // One own row's sums over streamed rows [s0, s1).
 template <int D, bool kOwnKeys>

@@ -18,7 +18,7 @@ struct AttnArgs {
   float *out, *lse;              // forward: written; backward: read
   const float *dout;
   float *dq, *dk, *dv;
-  float *delta;                  // [units, rows]
+  float *delta;                  // [units, rows]; null: made where they are used
   float *part;                   // partial results of the splits
   float *part_kv;
   uint32_t *status;
@@ -34,6 +34,7 @@ struct AttnArgs {
 // query rows for dk and dv.
 struct AttnPlan {
   bool tc;
+  bool delta;  // backward: D by a kernel of its own
   int warps, splits, splits_kv;
 };
 AttnPlan attn_plan(int64_t units, int64_t rows, int64_t Gk, int d, bool backward);

@@ -59,7 +59,7 @@ Layout layout(const fs_attn_shape* s, bool backward) {
     return o;
   };
   if (backward) {
-    l.delta = take(n.units * n.rows);
+    l.delta = take(p.delta ? n.units * n.rows : 0);
     l.part = take(p.splits > 1 ? p.splits * n.nq : 0);
     l.part_kv = take(p.splits_kv > 1 ? p.splits_kv * 2 * n.nk : 0);
   } else {
@@ -125,7 +125,7 @@ AttnArgs args_of(const fs_attn_shape* s, const fs_attn_mask& m, const float* q, 
   a.status = static_cast<uint32_t*>(ws);
   a.part = at(ws, l.part);
   if (backward) {
-    a.delta = at(ws, l.delta);
+    a.delta = p.delta ? at(ws, l.delta) : nullptr;
     a.part_kv = at(ws, l.part_kv);
   }
   return a;

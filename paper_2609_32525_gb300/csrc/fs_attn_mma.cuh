@@ -133,9 +133,37 @@ __device__ __forceinline__ void load_tile(Tile<D>& t, const AttnArgs& a, const U
     if (s.doc) t.doc[r] = ok ? max(s.doc[tok], -1) : -1;  // any negative number: not in use
     if (!kKeys) {
       t.lse[r] = ok ? lse2_of(a.lse[(int64_t)unit * a.rows + row]) : INFINITY;  // weight 0 past the last row
-      t.delta[r] = ok ? a.delta[(int64_t)unit * a.rows + row] : 0.f;
+      if (a.delta) t.delta[r] = ok ? a.delta[(int64_t)unit * a.rows + row] : 0.f;
       if (a.slopes) t.slope[r] = ok ? a.slopes[u.kvh * (a.H / a.Hkv) + row / a.Gq] * kLog2e : 0.f;
     }
+  }
+}
+
+// D_i = dout_i . out_i of a tile's queries where no kernel has made them (few tiles: a launch
+// costs more than the loads), 8 lanes a row.
+template <int D>
+__device__ __forceinline__ void tile_delta(Tile<D>& t, const AttnArgs& a, const Unit& u, int unit, int tile) {
+  constexpr int TR = tile_rows<D>();
+  const int l = threadIdx.x & 7;
+  for (int r = threadIdx.x >> 3; r < TR; r += blockDim.x >> 3) {
+    const int row = tile * TR + r;
+    float s = 0.f;
+    if (tile * TR + (r & ~3) >= a.rows) {  // none of the warp's four rows
+      if (l == 0) t.delta[r] = 0.f;
+      continue;
+    }
+    if (row < a.rows) {
+      const float* x = a.out + ((int64_t)unit * a.rows + row) * D;
+      const float* y = a.dout + ((int64_t)unit * a.rows + row) * D;
+#pragma unroll
+      for (int c = 2 * l; c < D; c += 16) {
+        const float2 v = *reinterpret_cast<const float2*>(x + c), w = *reinterpret_cast<const float2*>(y + c);
+        s += v.x * w.x + v.y * w.y;
+      }
+    }
+#pragma unroll
+    for (int o = 4; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    if (l == 0) t.delta[r] = s;
   }
 }
 
@@ -354,7 +382,7 @@ __device__ __forceinline__ OwnPair own_pair(const AttnArgs& a, const Unit& u, in
     o.lse2[h] = o.delta[h] = 0.f;
     if (!kOwnKeys && backward) {
       o.lse2[h] = lse2_of(a.lse[(int64_t)unit * a.rows + r]);
-      o.delta[h] = a.delta[(int64_t)unit * a.rows + r];
+      o.delta[h] = a.delta ? a.delta[(int64_t)unit * a.rows + r] : 0.f;
     }
   }
   return o;
@@ -562,7 +590,24 @@ __device__ __forceinline__ void backward_block(const AttnArgs& args, const AttnA
   OwnRows<D> x0, x1;
   x0.load(own_s.x0, r0, n_own, g, t);
   x1.load(own_s.x1, r0, n_own, g, t);
-  const OwnPair o = own_pair<kOwnKeys>(a, u, unit, r0, g, true);
+  OwnPair o = own_pair<kOwnKeys>(a, u, unit, r0, g, true);
+  if (!kOwnKeys && !a.delta) {  // a lane has its rows' channels of one k-step of four
+#pragma unroll
+    for (int h = 0; h < 2; h++) {
+      const int64_t at = ((int64_t)unit * a.rows + min(r0 + g + 8 * h, n_own - 1)) * D;
+      float s = 0.f;
+#pragma unroll
+      for (int k = 0; k < D / 8; k++) {
+        const int c = lane_channel<D>(k, t);
+        const float2 v = *reinterpret_cast<const float2*>(a.out + at + c);
+        const float2 w = *reinterpret_cast<const float2*>(a.dout + at + c);
+        s += v.x * w.x + v.y * w.y;
+      }
+      s += __shfl_xor_sync(0xffffffffu, s, 1);
+      s += __shfl_xor_sync(0xffffffffu, s, 2);
+      o.delta[h] = s;
+    }
+  }
   const int seen_by_all = a.causal ? min(a.Gk, max(own.first + 1, u.prefix)) : a.Gk;
   float acc0[D / 8][4], acc1[kOwnKeys ? D / 8 : 1][4];
 #pragma unroll
@@ -576,10 +621,12 @@ __device__ __forceinline__ void backward_block(const AttnArgs& args, const AttnA
   int tile = next_tile<D, !kOwnKeys>(a, str_s, own, u.prefix, tile0, tile1), stage = 0;
   if (tile < tile1) load_tile<D, !kOwnKeys>(tiles[0], a, u, unit, tile);
   copy_commit();
+  if (kOwnKeys && !a.delta && tile < tile1) tile_delta<D>(tiles[0], a, u, unit, tile);
   while (tile < tile1) {
     const int nxt = next_tile<D, !kOwnKeys>(a, str_s, own, u.prefix, tile + 1, tile1);
     if (nxt < tile1) load_tile<D, !kOwnKeys>(tiles[stage ^ 1], a, u, unit, nxt);
     copy_commit();
+    if (kOwnKeys && !a.delta && nxt < tile1) tile_delta<D>(tiles[stage ^ 1], a, u, unit, nxt);
     copy_wait<1>();
     __syncthreads();
     const Tile<D>& T = tiles[stage];
@@ -642,6 +689,7 @@ __global__ void __launch_bounds__(kMaxWarps * 32) k_attn_bwd(const __grid_consta
   __shared__ Tile<D> tiles[2];
   const AttnArgs& a = args;
   grid_begin();
+  if (!a.delta && blockIdx.x == 0 && threadIdx.x == 0) *a.status = kDevOk;
   const int b = blockIdx.x;
   if (b < blocks_kv * a.splits_kv) backward_block<D, true, kCap, kBias>(args, a, tiles, b / a.splits_kv, b % a.splits_kv);
   else {
@@ -666,7 +714,8 @@ cudaError_t bwd_of(const AttnArgs& a, cudaStream_t st) {
   const int64_t blocks_q = (int64_t)a.units * ((a.rows + per - 1) / per);
   const int64_t blocks_kv = (int64_t)a.units * ((a.Gk + per - 1) / per);
   const int64_t nrows = (int64_t)a.units * a.rows;
-  cudaError_t e = launch(k_attn_delta<D>, dim3((unsigned)((nrows + 31) / 32)), dim3(256), 0, st, a);
+  cudaError_t e = cudaSuccess;
+  if (a.delta) e = launch(k_attn_delta<D>, dim3((unsigned)((nrows + 31) / 32)), dim3(256), 0, st, a);
   if (e != cudaSuccess) return e;
   e = launch(k_attn_bwd<D, kCap, kBias>, dim3((unsigned)(blocks_q * a.splits + blocks_kv * a.splits_kv)), dim3(32 * a.warps), 0, st,
              a, (int)blocks_kv);

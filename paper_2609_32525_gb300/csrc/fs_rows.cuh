@@ -468,7 +468,7 @@ __global__ void __launch_bounds__(block_threads<TPR>()) k_ckpt_unpack(const Rows
 
 // kCkpt: v comes from its checkpoint.  Rows on their way stay in registers here, two at a time
 // with three blocks of 256 threads on an SM (1,048,576 rows of 256 bf16 channels: 306 us from
-// rows, 360 us from the checkpoint with dres; four rows and 126 registers took 467 and 520 us).
+// rows, 350 us from the checkpoint with dres; four rows and 126 registers took 467 and 520 us).
 template <typename T, int VE, int TPR, int K, bool kCkpt>
 __global__ void __launch_bounds__(block_threads<TPR>(), bwd_blocks_per_sm<TPR, K * VE>()) k_norm_bwd(const RowsArgs args) {
   constexpr int THREADS = block_threads<TPR>();

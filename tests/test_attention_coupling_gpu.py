@@ -133,3 +133,69 @@ def test_a_layer_of_norm_projections_and_coupling(lib):
         e = error(host(got).reshape(want.shape), want, "f32")
         print(f"PARITY layer {name} {e:.3e}")
         assert e <= tol("f32"), f"{name}: {e:.3e}"
+
+
+@pytest.mark.parametrize("case", [(2, 900, 2, 32, 60, "bf16", 6.0, True, True, 2, False), (1, 1200, 8, 32, 500, "f32", 0.0, True, False, 0, True)],
+                         ids=["warps", "tcgen05"])
+def test_captured_steps_and_two_layers_at_once(lib, case):
+    """A step replayed from a graph on new inputs, and two layers' steps on two streams, have the
+    bits of steps that run alone."""
+    B, N, H, d, G, dtype, cap, _, _, _, prefix = case
+    dt, names = torch.bfloat16 if dtype == "bf16" else torch.float32, ("x_mid", "fx")
+
+    def layer(seed):
+        a, dout, gammas, mask = make(seed, *case)
+        t, g, m, do = dev(a, dtype), {k: to_dev(v, "f32") for k, v in gammas.items()}, device_mask(lib, mask), to_dev(dout, dtype)
+        c = lib.AttentionCoupling(*case[:5], dt, backward=True, cap=cap, prefix=prefix, qk_norm=True, checkpointed=True)
+        w = {k: v for k, v in t.items() if k not in names}
+
+        def step(stream=None):
+            c.forward(**t, mask=m, **g, stream=stream)
+            return c.backward(None, None, **w, dout=do, mask=m, **g, stream=stream)
+
+        def result():
+            assert c.device_status() == lib.FS_OK
+            return {"out": c.out.clone(), **{k: v.clone() for k, v in grads.items()}}
+
+        grads = step()
+        return t, step, result, result()
+
+    first, second = layer(1), layer(2)
+    t, step, result, alone = first
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for n in names:
+        t[n].copy_(second[0][n])
+    graph.replay()
+    replayed = result()
+    step()
+    again = result()
+    assert all(torch.equal(replayed[n], again[n]) for n in again) and not torch.equal(again["out"], alone["out"])
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    for _ in range(4):
+        for (_, go, _, _), s in zip((first, second), streams):
+            go(s)
+    torch.cuda.synchronize()
+    both = result()
+    assert all(torch.equal(both[n], again[n]) for n in again)
+    both = second[2]()
+    assert all(torch.equal(both[n], second[3][n]) for n in both)
+
+
+def test_one_token_per_head(lib):
+    """G = 1: each point's weight and each attention weight is 1; the scores have no gradient."""
+    case = (2, 300, 2, 32, 1, "f32", 0.0, False, False, 0, False)
+    a, dout, _, _ = make(3, *case)
+    t = dev(a, "f32")
+    c = lib.AttentionCoupling(*case[:5], torch.float32, backward=True)
+    out = c.forward(**t)
+    g = c.backward(**t, dout=to_dev(dout, "f32"))
+    ref = orc.attention_coupling(**a, scale=32 ** -0.5, dout=dout)
+    for n, got in (("out", out), ("dfx", g["dfx"]), ("dWv", g["dWv"])):
+        assert error(host(got), ref[n], "f32") <= tol("f32"), n
+    # p (dout . v - dout . out) with out = v: what is left of two equal dot products of 32 terms
+    size = np.abs(host(c.d_tokens_mixed) * host(c.tokens_mixed)).sum(-1).max()
+    assert np.abs(host(c.dq)).max() <= 32 * 2.0 ** -22 * size * 32 ** -0.5 * np.abs(host(c.k)).max()
