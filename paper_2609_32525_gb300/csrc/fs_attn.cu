@@ -12,17 +12,26 @@ AttnPlan attn_plan(int64_t units, int64_t rows, int64_t Gk, int d, bool backward
   p.splits_kv = 1;
   const int64_t sms = num_sms();
   // tcgen05 where a tile of 128 rows is full and there are pairs enough to pay for the images and
-  // for a block's start.  Both sides, d = 32, in us (tcgen05 / warps): forward 8 heads x 256
-  // tokens 11.3 / 9.5, 384: 12.3 / 11.4, 512: 12.5 / 14.9; 32 x 256: 13.4 / 15.0, 32 x 512: 16.0 /
-  // 35.2; 128 x 64: 8.9 / 6.7, 128 x 128: 9.7 / 11.6; 32 x 64 against 4096 keys 38.6 / 35.5.
-  // Backward 8 x 256: 15.9 / 13.3, 384: 17.6 / 18.8, 512: 20.6 / 28.8; 32 x 128: 13.9 / 12.8.
-  p.tc = d == 32 && rows >= 128 && Gk >= 128 && units * rows * Gk >= (backward ? 1100000 : 1500000);
+  // for a block's start; at d = 16, whose warps work least, on more keys a block, too.  Both sides
+  // in us (tcgen05 / warps), heads x tokens:
+  //   forward   d = 16  8 x 384 10.6 / 9.9, 8 x 512 11.9 / 12.4, 8 x 1024 18.3 / 29.2,
+  //                     128 x 256 19.6 / 15.6, 32 x 512 14.8 / 25.9
+  //             d = 32  8 x 256 11.3 / 9.5, 8 x 384 12.3 / 11.4, 8 x 512 12.5 / 14.9,
+  //                     32 x 256 13.4 / 15.0, 32 x 512 16.0 / 35.2, 128 x 128 9.7 / 11.6
+  //             d = 64  4 x 512 16.2 / 13.1, 4 x 768 16.4 / 19.3, 4 x 2048 36 / 94, 64 x 128 13.2 / 13.5
+  //   backward  d = 16  8 x 256 13.7 / 10.4, 8 x 384 14.2 / 16.2, 128 x 128 19.5 / 15.4, 8 x 2048 93 / 173
+  //             d = 32  8 x 256 15.9 / 13.3, 8 x 384 17.6 / 18.8, 8 x 512 20.6 / 28.8, 32 x 128 13.9 / 12.8
+  //             d = 64  4 x 256 19.9 / 15.4, 4 x 384 21.6 / 22.7, 4 x 512 24.6 / 33.7, 4 x 2048 123 / 397,
+  //                     4 x 128 rows against 1024 keys 32 / 23
+  const int64_t keys = d == 16 ? (backward ? 256 : 384) : 128;
+  const int64_t pairs = !backward ? 1500000 : d == 64 ? 700000 : 1100000;
+  p.tc = rows >= 128 && Gk >= keys && units * rows * Gk >= pairs;
   if (p.tc) {
     // One block of 128 rows per SM at a time: the split whose waves of blocks cost least, a
     // block's time being its tiles and about two more; ranges of two tiles at least, and no
     // more tiles than a block lists.
     const int64_t tiles = (std::max(Gk, backward ? rows : 0) + 63) / 64;
-    const int64_t blocks = units * ((rows + 127) / 128 + (backward ? (Gk + 127) / 128 : 0));
+    const int64_t blocks = units * ((rows + 127) / 128 + (backward ? (Gk + 127) / 128 * (d == 64 ? 2 : 1) : 0));
     const int64_t least = (tiles * 2 + kAttnTcTiles - 1) / kAttnTcTiles;
     double best = 1e300;
     for (int64_t n = least; n <= std::max<int64_t>(least, std::min<int64_t>(tiles / 2, 32)); n++) {

@@ -29,7 +29,7 @@ struct AttnArgs {
   float scale, cap;
 };
 
-// How a call is run on the current device: on tcgen05 (fs_attn_tc.cu) or with warps' own
+// How a call is run on the current device: on tcgen05 (fs_attn_tc.cuh) or with warps' own
 // products (fs_attn_mma.cuh), there with so many warps per block; splits of the keys, and of the
 // query rows for dk and dv.
 struct AttnPlan {

@@ -70,7 +70,7 @@ Layout layout(const fs_attn_shape* s, bool backward) {
     l.rows_pad = (n.rows + 63) / 64 * 64;
     // forward: rows of k, columns of v; backward: rows of all four, columns of k, q and dout
     for (int t = 0; t < (backward ? 4 : 2); t++) {
-      const int64_t img = 2 * n.units * (t < 2 ? l.k_pad : l.rows_pad) * 32;
+      const int64_t img = 2 * n.units * (t < 2 ? l.k_pad : l.rows_pad) * (s->d < 32 ? 32 : s->d);
       l.row_img[t] = backward || t == 0 ? take(img) : 0;
       l.col_img[t] = backward == (t != 1) ? take(img) : 0;
     }
@@ -147,7 +147,7 @@ cudaError_t run(const fs_attn_shape* s, const AttnArgs& a, void* ws, const Layou
   t.q_range = reinterpret_cast<int2*>(at(ws, l.q_range));
   t.rows_pad = (int)l.rows_pad;
   t.k_pad = (int)l.k_pad;
-  return attn_tc(t, backward, st);
+  return s->d == 16 ? attn_tc<16>(t, backward, st) : s->d == 32 ? attn_tc<32>(t, backward, st) : attn_tc<64>(t, backward, st);
 }
 
 }  // namespace

@@ -34,9 +34,9 @@
 // same bits in every run.
 //
 // What bounds it: m16n8k8 tf32 runs at 302 TFLOP/s on this chip (a quarter of tcgen05's), so
-// three products of parts at 100; long calls reach half of that (16 x 2074 tokens of 64 channels,
-// backward, 1.3 ms), where the splitting of the streamed fragments and the scores take the issue
-// slots.  Short calls are latency: one query of 4 x 8 heads against 4096 keys takes 12 us in two
+// three products of parts at 100; the longest calls reached half of that, where the splitting of
+// the streamed fragments and the scores take the issue slots (they run on tcgen05 now).  Short
+// calls are latency: one query of 4 x 8 heads against 4096 keys takes 12 us in two
 // launches, 29 before the chains of products took turns and the join loaded at once.
 #pragma once
 

@@ -8,7 +8,7 @@ namespace fs {
 constexpr int kAttnTcTiles = 1024;  // most tiles of a block's range
 
 // What the tensor-core kernels need beside the call: images of k, v, q, dout (null where unused;
-// the low parts lie units * pad * 128 bytes behind), rows padded to whole tiles of 64.
+// the low parts lie behind all units' high ones), rows padded to whole tiles of 64.
 struct AttnTcArgs {
   AttnArgs a;
   uint8_t *row_img[4], *col_img[4];
@@ -21,6 +21,7 @@ struct AttnTcArgs {
   int rows_pad, k_pad;
 };
 
+template <int D>
 cudaError_t attn_tc(const AttnTcArgs& t, bool backward, cudaStream_t st);
 
 }  // namespace fs

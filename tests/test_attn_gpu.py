@@ -14,10 +14,10 @@ SIZES = [(1, 1, 1, 1, 1, 32), (1, 2, 1, 2, 2, 16), (2, 2, 2, 3, 3, 64), (1, 8, 8
          (2, 4, 2, 17, 17, 16), (1, 2, 1, 31, 31, 64), (1, 2, 2, 63, 63, 32), (1, 4, 4, 64, 64, 16), (3, 4, 2, 100, 100, 64),
          (1, 3, 3, 65, 65, 32), (1, 2, 1, 129, 129, 32), (1, 8, 2, 130, 130, 32), (1, 1, 1, 257, 257, 64),
          (1, 2, 2, 300, 300, 16), (2, 8, 2, 1, 700, 32), (1, 4, 1, 5, 1000, 64), (1, 2, 2, 40, 33, 32), (2, 4, 1, 1, 1, 32),
-         # d = 32, at least 128 rows and keys and 1.5 million pairs: tiles of 128 rows on tcgen05; several heads in a
-         # tile, one tile, many, ragged ones, more queries than keys
-         (1, 16, 4, 100, 1000, 32), (1, 8, 8, 440, 440, 32), (1, 8, 8, 600, 330, 32), (12, 8, 8, 128, 128, 32),
-         (2, 8, 2, 129, 760, 32), (1, 1, 1, 1300, 1301, 32), (1, 16, 1, 33, 3000, 32),
+         # at least 128 rows and keys and 1.5 million pairs: tiles of 128 rows on tcgen05; several heads in a tile, one
+         # tile, many, ragged ones, more queries than keys
+         *[(*z, d) for z in ((1, 16, 4, 100, 1000), (1, 8, 8, 440, 440), (1, 8, 8, 600, 330), (12, 8, 8, 128, 128),
+                             (2, 8, 2, 129, 760), (1, 1, 1, 1300, 1301), (1, 16, 1, 33, 3000)) for d in (32, 16, 64)],
          # just below: the same shapes by warps
          (1, 4, 1, 40, 300, 32), (2, 2, 2, 256, 256, 32), (1, 2, 2, 600, 129, 32)]
 PLAIN = [dict(), dict(cap=5.0), dict(bias="index"), dict(bias="place", cap=2.0), dict(docs=2), dict(prefix=0),
@@ -36,7 +36,7 @@ def test_against_the_oracle(lib, size, what):
 def test_large_scores(lib, d):
     """Scores of some tens, capped and not: the running maximum moves by much from tile to tile."""
     for cap in (0.0, 10.0):
-        for H, G in ((2, 200),) + (((4, 640),) if d == 32 else ()):
+        for H, G in ((2, 200), (4, 640)):
             c = _attn.make(d, 1, H, H, G, G, d, cap=cap)
             c["q"] *= 4
             c["k"] *= 3
@@ -72,9 +72,10 @@ def test_tiny_and_huge_magnitudes(lib):
             _attn.check(lib, c)
 
 
+@pytest.mark.parametrize("d", [32, 16, 64])
 @pytest.mark.parametrize("G", [90, 460])
-def test_rows_that_see_nothing(lib, G):
-    c = _attn.make(6, 2, 4, 2, G, G, 32, docs=2)
+def test_rows_that_see_nothing(lib, G, d):
+    c = _attn.make(6, 2, 4, 2, G, G, d, docs=2)
     c["mask"]["doc_q"][0, :40] = -1
     c["mask"]["doc_k"][1] = -1
     got = _attn.check(lib, c)
@@ -87,7 +88,7 @@ def test_rows_that_see_nothing(lib, G):
 def test_what_masked_tokens_hold_reaches_no_result(lib, d, bad):
     """Documents: tokens of document 1 and unused ones hold `bad`; document 0's results are those
     of clean tokens."""
-    for prefix, G in ((None, 150), (1, 150)) + (((None, 460), (1, 460)) if d == 32 else ()):
+    for prefix, G in ((None, 150), (1, 150), (None, 460), (1, 460)):
         c = _attn.make(7, 2, 4, 2, G, G, d, docs=2, cap=4.0, bias="place", prefix=prefix)
         c["mask"]["doc_q"] = c["mask"]["doc_k"].copy()
         other = c["mask"]["doc_k"] != 0
@@ -105,13 +106,14 @@ def test_what_masked_tokens_hold_reaches_no_result(lib, d, bad):
             assert (got[n][unused] == (-np.inf if n == "lse" else 0)).all(), n
 
 
+@pytest.mark.parametrize("d", [32, 16, 64])
 @pytest.mark.parametrize("G", [150, 900])
-def test_what_later_keys_hold_reaches_no_earlier_query(lib, G):
-    c, cut = _attn.make(8, 1, 2, 2, G, G, 32, prefix=0), G - 50
+def test_what_later_keys_hold_reaches_no_earlier_query(lib, G, d):
+    c, cut = _attn.make(8, 1, 2, 2, G, G, d, prefix=0), G - 50
     for n in ("k", "v", "q", "dout"):
         c[n][:, :, cut:] = np.nan
     got = _attn.run(lib, c)
-    ref = _attn.make(8, 1, 2, 2, G, G, 32, prefix=0)
+    ref = _attn.make(8, 1, 2, 2, G, G, d, prefix=0)
     for n in ("k", "v", "q", "dout"):
         ref[n][:, :, cut:] = 0
     res = _attn.want(ref)
@@ -122,12 +124,13 @@ def test_what_later_keys_hold_reaches_no_earlier_query(lib, G):
     assert np.isnan(got["dk"]).all()  # every key is seen by the last queries
 
 
+@pytest.mark.parametrize("d", [32, 16, 64])
 @pytest.mark.parametrize("H, G", [(1, 40), (4, 640)])
-def test_a_visible_nan_or_infinite_score(lib, H, G):
-    c = _attn.make(9, 1, H, H, G, G, 32, bwd=False)
+def test_a_visible_nan_or_infinite_score(lib, H, G, d):
+    c = _attn.make(9, 1, H, H, G, G, d, bwd=False)
     c["k"][0, :, 5, 0] = np.nan
     assert np.isnan(_attn.run(lib, c)["out"]).all()
-    c = _attn.make(9, 1, H, H, G, G, 32, bwd=False)
+    c = _attn.make(9, 1, H, H, G, G, d, bwd=False)
     c["k"][0, :, :, :] = 0
     c["k"][0, :, 5] = -np.inf
     c["q"][:] = np.abs(c["q"]) + 0.1  # key 5 scores -infinity for every query: weight 0
