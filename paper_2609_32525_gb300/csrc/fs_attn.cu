@@ -53,6 +53,10 @@ AttnPlan attn_plan(int64_t units, int64_t rows, int64_t Gk, int d, bool backward
   const int64_t want = sms * 8 / p.warps / (backward ? 2 : 1);
   auto split = [&](int64_t own, int64_t streamed) {
     const int64_t blocks = units * ((own + per - 1) / per), tiles = (streamed + tile - 1) / tile;
+    // The forward takes two tiles in turn: what a join costs is more than the second tile (us, whole
+    // / split, 8 heads x 128 tokens: d = 16 5.9 / 8.4, d = 32 7.1 / 8.3; three tiles 8.5 / 7.4 in a
+    // graph).  The backward's tiles are longer: 8 x 128, d = 32 13.8 / 12.2.
+    if (!backward && tiles <= 2) return 1;
     return (int)std::max<int64_t>(1, std::min(want / blocks, tiles));
   };
   p.splits = split(rows, Gk);

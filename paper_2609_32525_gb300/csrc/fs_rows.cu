@@ -126,8 +126,8 @@ fs_status fs_norm_bwd(const fs_rows* s, const void* v, const int8_t* q8, const u
   a.status = static_cast<uint32_t*>(ws);
   a.part = dgamma ? reinterpret_cast<float*>(static_cast<char*>(ws) + kAlign) : nullptr;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-  const int64_t blocks = bwd_blocks(s);
-  FS_CUDA(s->dtype == FS_BF16 ? norm_bwd<__nv_bfloat16>(a, blocks, st) : norm_bwd<float>(a, blocks, st));
+  int64_t blocks = 0;
+  FS_CUDA(s->dtype == FS_BF16 ? norm_bwd<__nv_bfloat16>(a, &blocks, st) : norm_bwd<float>(a, &blocks, st));
   if (dgamma)
     FS_CUDA(launch(k_norm_reduce, dim3((unsigned)((2LL * s->C + 7) / 8)), dim3(8, 32), 0, st, a.part, blocks, s->C,
                    dgamma, dbeta, accumulate));

@@ -23,6 +23,7 @@
 #include "fs_internal.h"
 #include "fs_launch.h"
 #include "fs_rows.h"
+#include "fs_tc_ptx.cuh"
 
 #include <algorithm>
 #include <cuda_bf16.h>
@@ -81,9 +82,10 @@ __host__ __device__ constexpr int block_threads() { return TPR <= 32 ? 256 : TPR
 // Rows whose loads a thread issues before it uses the first.
 template <int K>
 __host__ __device__ constexpr int rows_ahead() { return K == 1 ? 2 : 1; }
-// Blocks of the backward on an SM: by its registers, for narrow threads.
+// Blocks of the backward on an SM: by its registers (16 channels a lane: 300,000 x 384 bf16 from the
+// checkpoint 389 us with one block, 240 with two, 283 with three).
 template <int TPR, int N>
-__host__ __device__ constexpr int bwd_blocks_per_sm() { return TPR <= 32 && N <= 8 ? 3 : 1; }
+__host__ __device__ constexpr int bwd_blocks_per_sm() { return TPR > 32 ? 1 : N <= 8 ? 3 : 2; }
 
 // The sum over a row's TPR threads, in every one of them, in a fixed order.
 template <int TPR>
@@ -466,20 +468,83 @@ __global__ void __launch_bounds__(block_threads<TPR>()) k_ckpt_unpack(const Rows
   }
 }
 
+// A row's gradient without its factor rstd, in place of dy in g; xh: v.  Past C, dy is 0: nothing is
+// added to the sums there.
+template <int TPR, int N>
+__device__ __forceinline__ void row_grad(Vals<N>& xh, Vals<N>& g, float mean, float rstd, const Vals<N>& gm, float invC,
+                                         float* red, Vals<N>& dg, Vals<N>& db) {
+  constexpr int P = Vals<N>::P;
+  const F2 minus = pair(-mean, -mean), r2 = pair(rstd, rstd);
+  F2 t1 = pair(0.f, 0.f), t2 = t1;
+#pragma unroll
+  for (int i = 0; i < P; i++) {
+    xh.p[i] = (xh.p[i] + minus) * r2;
+    db.p[i] = db.p[i] + g.p[i];
+    dg.p[i] = fma(g.p[i], xh.p[i], dg.p[i]);
+    g.p[i] = g.p[i] * gm.p[i];
+    t1 = t1 + g.p[i];
+    t2 = fma(g.p[i], xh.p[i], t2);
+  }
+  const float s1 = row_sum<TPR>(total(t1), red) * invC;
+  const float s2 = row_sum<TPR>(total(t2), red) * invC;
+  const F2 m1 = pair(-s1, -s1), m2 = pair(-s2, -s2);
+#pragma unroll
+  for (int i = 0; i < P; i++) g.p[i] = fma(xh.p[i], m2, g.p[i] + m1);
+}
+
+// The block's row of partial sums of dgamma (dg) and dbeta (db); acc: W * TPR * N floats.
+template <int TPR, int VE, int N, int THREADS>
+__device__ __forceinline__ void write_partials(const RowsArgs& a, const Vals<N>& dg, const Vals<N>& db, int t, float* acc) {
+  constexpr int W = TPR <= 32 ? THREADS / 32 : 1;  // warps with their own sums of the same channels
+  constexpr int WC = TPR * N, P = Vals<N>::P;      // channels a row group covers
+  const int C = a.C;
+  if (!a.part) return;
+  float* part = a.part + (int64_t)blockIdx.x * 2 * C;
+#pragma unroll
+  for (int which = 0; which < 2; which++) {
+    float sum[2 * P];
+    floats_of(which ? db : dg, sum);
+    if constexpr (TPR < 32) {  // row groups of a warp
+#pragma unroll
+      for (int o = TPR; o < 32; o <<= 1)
+#pragma unroll
+        for (int i = 0; i < N; i++) sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], o);
+    }
+    if constexpr (W > 1) {
+      __syncthreads();
+      if ((threadIdx.x & 31) < TPR) {
+#pragma unroll
+        for (int i = 0; i < N; i++) acc[(threadIdx.x >> 5) * WC + (i / VE * TPR + t) * VE + i % VE] = sum[i];
+      }
+      __syncthreads();
+      for (int c = threadIdx.x; c < C; c += THREADS) {
+        float s = 0.f;
+#pragma unroll
+        for (int w = 0; w < W; w++) s += acc[w * WC + c];
+        part[which * C + c] = s;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; i++) {
+        const int c = (i / VE * TPR + t) * VE + i % VE;
+        if (c < C) part[which * C + c] = sum[i];
+      }
+    }
+  }
+}
+
 // kCkpt: v comes from its checkpoint.  Rows on their way stay in registers here, two at a time
-// with three blocks of 256 threads on an SM (1,048,576 rows of 256 bf16 channels: 306 us from
-// rows, 350 us from the checkpoint with dres; four rows and 126 registers took 467 and 520 us).
+// with three blocks of 256 threads on an SM (1,048,576 rows of 256 bf16 channels: 297 us from
+// rows, 351 us from the checkpoint with dres; four rows and 126 registers took 467 and 520 us).
 template <typename T, int VE, int TPR, int K, bool kCkpt>
 __global__ void __launch_bounds__(block_threads<TPR>(), bwd_blocks_per_sm<TPR, K * VE>()) k_norm_bwd(const RowsArgs args) {
   constexpr int THREADS = block_threads<TPR>();
   constexpr int RPB = THREADS / TPR, RU = rows_ahead<K>();
-  constexpr int W = TPR <= 32 ? THREADS / 32 : 1;  // warps with their own sums of the same channels
-  constexpr int WC = TPR * K * VE;                 // channels a row group covers
   constexpr int N = K * VE, P = Vals<N>::P;
   using R = RawV<T, VE>;
   using Q = RawV<uint8_t, VE>;
   __shared__ float red[32];
-  __shared__ float acc[W > 1 ? W * WC : 1];
+  __shared__ float acc[TPR <= 32 ? THREADS / 32 * TPR * N : 1];
   RowsArgs a = args;
   grid_begin(a.x, a.q8, a.e8, a.gamma, a.mean, a.rstd, a.dy, a.dres);
   if (a.status && blockIdx.x == 0 && threadIdx.x == 0) *a.status = kDevOk;
@@ -534,27 +599,14 @@ __global__ void __launch_bounds__(block_threads<TPR>(), bwd_blocks_per_sm<TPR, K
         xh = vals_of<T, VE, K>(xr[u]);
       }
       Vals<N> g = vals_of<T, VE, K>(yr[u]);
-      const F2 minus = pair(-mean[u], -mean[u]), r2 = pair(rstd[u], rstd[u]);
-      F2 t1 = pair(0.f, 0.f), t2 = t1;
-#pragma unroll
-      for (int i = 0; i < P; i++) {  // past C, dy is 0: nothing is added there
-        xh.p[i] = (xh.p[i] + minus) * r2;
-        db.p[i] = db.p[i] + g.p[i];
-        dg.p[i] = fma(g.p[i], xh.p[i], dg.p[i]);
-        g.p[i] = g.p[i] * gm.p[i];
-        t1 = t1 + g.p[i];
-        t2 = fma(g.p[i], xh.p[i], t2);
-      }
-      const float s1 = row_sum<TPR>(total(t1), red) * invC;
-      const float s2 = row_sum<TPR>(total(t2), red) * invC;
-      const F2 m1 = pair(-s1, -s1), m2 = pair(-s2, -s2);
-#pragma unroll
-      for (int i = 0; i < P; i++) g.p[i] = fma(xh.p[i], m2, g.p[i] + m1);
+      row_grad<TPR, N>(xh, g, mean[u], rstd[u], gm, invC, red, dg, db);
       if (dres) {
         const Vals<N> r = vals_of<T, VE, K>(rr[u]);
+        const F2 r2 = pair(rstd[u], rstd[u]);
 #pragma unroll
         for (int i = 0; i < P; i++) g.p[i] = fma(g.p[i], r2, r.p[i]);
       } else {
+        const F2 r2 = pair(rstd[u], rstd[u]);
 #pragma unroll
         for (int i = 0; i < P; i++) g.p[i] = g.p[i] * r2;
       }
@@ -571,39 +623,177 @@ __global__ void __launch_bounds__(block_threads<TPR>(), bwd_blocks_per_sm<TPR, K
       }
     }
   }
-  if (!a.part) return;
-  float* part = a.part + (int64_t)blockIdx.x * 2 * C;
-#pragma unroll
-  for (int which = 0; which < 2; which++) {
-    float sum[2 * P];
-    floats_of(which ? db : dg, sum);
-    if constexpr (TPR < 32) {  // row groups of a warp
-#pragma unroll
-      for (int o = TPR; o < 32; o <<= 1)
-#pragma unroll
-        for (int i = 0; i < N; i++) sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], o);
+  write_partials<TPR, VE, N, THREADS>(a, dg, db, t, acc);
+}
+
+// The same for rows of one warp each, 16 rows of a block fetched at a time by bulk copies: they
+// are one piece of memory per tensor, whatever C is, which one lane fetches into the block's
+// stages.  No instruction of the other lanes and no register waits for them.  (Pieces of two rows for
+// each warp by itself, 1 KB, took 410 us where these take 333: too many copies.)
+struct Bulk {
+  int stages, bytes, per_sm;  // of a stage; blocks that an SM holds (0: not for these rows)
+};
+constexpr int kBulkRows = 16, kBulkStages = 6;
+
+template <typename T, int VE, int K, bool kCkpt>
+__global__ void __launch_bounds__(256, K * VE <= 8 ? 3 : 2) k_norm_bwd_bulk(const RowsArgs args, const Bulk plan) {
+  constexpr int N = K * VE, P = Vals<N>::P, RU = kBulkRows / 8;
+  using R = RawV<T, VE>;
+  using Q = RawV<uint8_t, VE>;
+  extern __shared__ __align__(128) char stages[];
+  __shared__ uint64_t full[kBulkStages], empty[kBulkStages];
+  __shared__ tc::Abort ab;
+  RowsArgs a = args;
+  const int warp = threadIdx.x >> 5, t = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < plan.stages; s++) {
+      tc::mbar_init(&full[s], 1);
+      tc::mbar_init(&empty[s], 8);
     }
-    if constexpr (W > 1) {
-      __syncthreads();
-      if ((threadIdx.x & 31) < TPR) {
+    ab.flag = 0;
+    tc::fence_mbar_init();
+  }
+  __syncthreads();
+  grid_begin(a.x, a.q8, a.e8, a.gamma, a.mean, a.rstd, a.dy, a.dres);
+  if (blockIdx.x == 0 && threadIdx.x == 0) *a.status = kDevOk;
+  const int C = a.C, nb = (C + kCkptBlock - 1) / kCkptBlock;
+  const int64_t chunks = (a.rows + kBulkRows - 1) / kBulkRows;
+  const uint32_t nd = (uint32_t)(kBulkRows * C * sizeof(T)), nq = (uint32_t)(kBulkRows * C);
+  const uint32_t at_x = a.dres ? 2 * nd : nd, at_e = at_x + nq;  // dy, dres, then v or q8 and e8
+  const char* src_dy = static_cast<const char*>(a.dy);
+  const char* src_dres = static_cast<const char*>(a.dres);
+  const char* src_x = kCkpt ? reinterpret_cast<const char*>(a.q8) : static_cast<const char*>(a.x);
+  auto issue = [&](int64_t chunk, int s) {
+    if ((chunk + 1) * kBulkRows > a.rows) return;  // a last chunk of fewer rows is read by the lanes
+    char* to = stages + (size_t)s * plan.bytes;
+    tc::mbar_expect_tx(&full[s], (uint32_t)plan.bytes);
+    tc::bulk_load(to, src_dy + chunk * nd, nd, &full[s]);
+    if (src_dres) tc::bulk_load(to + nd, src_dres + chunk * nd, nd, &full[s]);
+    tc::bulk_load(to + at_x, src_x + chunk * (kCkpt ? nq : nd), kCkpt ? nq : nd, &full[s]);
+    if (kCkpt) tc::bulk_load(to + at_e, a.e8 + chunk * kBulkRows * nb, (uint32_t)(kBulkRows * nb), &full[s]);
+  };
+  const int64_t first = blockIdx.x, step = gridDim.x;
+  if (threadIdx.x == 0)
+    for (int s = 0; s < plan.stages - 1; s++)
+      if (first + s * step < chunks) issue(first + s * step, s);
+  auto stat = [&](const float* p, int64_t chunk) {  // lane i: of the warp's row i
+    const int64_t row = chunk * kBulkRows + RU * warp + t;
+    return t < RU && row < a.rows ? p[row] : 0.f;
+  };
+  const Vals<N> gm = channels_of<N, VE, 32>(a.gamma, C, t, 1.f);
+  Vals<N> dg, db;
 #pragma unroll
-        for (int i = 0; i < N; i++) acc[(threadIdx.x >> 5) * WC + (i / VE * TPR + t) * VE + i % VE] = sum[i];
+  for (int i = 0; i < P; i++) dg.p[i] = db.p[i] = pair(0.f, 0.f);
+  const float invC = 1.f / (float)C;
+  float mean_next = stat(a.mean, first), rstd_next = stat(a.rstd, first);
+  int s = 0;
+  uint32_t parity = 0;
+#pragma unroll 1
+  for (int64_t chunk = first; chunk < chunks; chunk += step) {
+    const float mean_of = mean_next, rstd_of = rstd_next;
+    mean_next = stat(a.mean, chunk + step);
+    rstd_next = stat(a.rstd, chunk + step);
+    // The stage of the chunk before this one gets the chunk that follows those on their way, once
+    // every warp has read it.
+    const int64_t ahead = chunk + (plan.stages - 1) * step;
+    if (warp == 0 && ahead < chunks) {
+      const int w = s == 0 ? plan.stages - 1 : s - 1;
+      if (chunk > first && !tc::mbar_wait_w(&empty[w], s == 0 ? parity ^ 1u : parity, &ab, a.status)) break;
+      if (t == 0) issue(ahead, w);
+    }
+    const bool whole = (chunk + 1) * kBulkRows <= a.rows;
+    const int64_t row0 = chunk * kBulkRows + RU * warp;
+    char* base = stages + (size_t)s * plan.bytes;
+    char* b_dy = base + RU * warp * C * sizeof(T);  // the warp's rows
+    char* b_dres = b_dy + nd;
+    char* b_x = base + at_x + RU * warp * C * (kCkpt ? 1 : sizeof(T));
+    uint8_t* b_e = reinterpret_cast<uint8_t*>(base + at_e) + RU * warp * nb;
+    if (whole) {
+      if (!tc::mbar_wait_w(&full[s], parity, &ab, a.status)) break;
+    } else {  // each warp its own, in whose place no other reads
+      const int left = (int)max((int64_t)0, min((int64_t)RU, a.rows - row0)) * C;
+#pragma unroll 1
+      for (int i = t; i < left; i += 32) {
+        const int64_t at = row0 * C + i;
+        reinterpret_cast<T*>(b_dy)[i] = static_cast<const T*>(a.dy)[at];
+        if (src_dres) reinterpret_cast<T*>(b_dres)[i] = static_cast<const T*>(a.dres)[at];
+        if (kCkpt) b_x[i] = src_x[at];
+        else reinterpret_cast<T*>(b_x)[i] = static_cast<const T*>(a.x)[at];
       }
-      __syncthreads();
-      for (int c = threadIdx.x; c < C; c += THREADS) {
-        float s = 0.f;
+      if (kCkpt)
+        for (int i = t; i < left / C * nb; i += 32) b_e[i] = a.e8[row0 * nb + i];
+      __syncwarp();
+    }
 #pragma unroll
-        for (int w = 0; w < W; w++) s += acc[w * WC + c];
-        part[which * C + c] = s;
-      }
-    } else {
+    for (int u = 0; u < RU; u++) {
+      const int64_t row = row0 + u;
+      const bool here = row < a.rows;
+      const float mean = __shfl_sync(0xffffffffu, mean_of, u), rstd = __shfl_sync(0xffffffffu, rstd_of, u);
+      R yr[K], rr[K];
+      Vals<N> xh;
+      if constexpr (kCkpt) {
+        float f[N + 1];
+        f[N] = 0.f;
 #pragma unroll
-      for (int i = 0; i < N; i++) {
-        const int c = (i / VE * TPR + t) * VE + i % VE;
-        if (c < C) part[which * C + c] = sum[i];
+        for (int k = 0; k < K; k++) {
+          const int c = (k * 32 + t) * VE;
+          const bool ok = here && c < C;
+          const Q q = ok ? *reinterpret_cast<const Q*>(b_x + u * C + c) : raw_zero<Q>();
+          const uint32_t e = ok ? b_e[u * nb + c / kCkptBlock] : 0u;
+          restore<VE>(q, e, *reinterpret_cast<float(*)[VE]>(f + k * VE));
+        }
+#pragma unroll
+        for (int i = 0; i < P; i++) xh.p[i] = pair(f[2 * i], f[2 * i + 1]);
+      } else {
+        R xr[K];
+#pragma unroll
+        for (int k = 0; k < K; k++) {
+          const int c = (k * 32 + t) * VE;
+          xr[k] = here && c < C ? *reinterpret_cast<const R*>(b_x + (u * C + c) * sizeof(T)) : raw_zero<R>();
+        }
+        xh = vals_of<T, VE, K>(xr);
       }
+#pragma unroll
+      for (int k = 0; k < K; k++) {
+        const int c = (k * 32 + t) * VE;
+        const bool ok = here && c < C;
+        yr[k] = ok ? *reinterpret_cast<const R*>(b_dy + (u * C + c) * sizeof(T)) : raw_zero<R>();
+        if (src_dres) rr[k] = ok ? *reinterpret_cast<const R*>(b_dres + (u * C + c) * sizeof(T)) : raw_zero<R>();
+      }
+      Vals<N> g = vals_of<T, VE, K>(yr);
+      row_grad<32, N>(xh, g, mean, rstd, gm, invC, nullptr, dg, db);
+      const F2 r2 = pair(rstd, rstd);
+      if (src_dres) {
+        const Vals<N> r = vals_of<T, VE, K>(rr);
+#pragma unroll
+        for (int i = 0; i < P; i++) g.p[i] = fma(g.p[i], r2, r.p[i]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < P; i++) g.p[i] = g.p[i] * r2;
+      }
+      if (here) {
+        float f[2 * P];
+        floats_of(g, f);
+#pragma unroll
+        for (int k = 0; k < K; k++) {
+          const int c = (k * 32 + t) * VE;
+          if (c < C)
+            *reinterpret_cast<R*>(static_cast<T*>(a.y) + row * C + c) =
+                from_float<T, VE>(*reinterpret_cast<float(*)[VE]>(f + k * VE));
+        }
+      }
+    }
+    __syncwarp();
+    if (t == 0) tc::mbar_arrive(&empty[s]);
+    if (++s == plan.stages) {
+      s = 0;
+      parity ^= 1u;
     }
   }
+  if (ab.flag)  // no copy is left in flight
+    for (int i = 0; i < plan.stages; i++) tc::mbar_wait_w(&full[i], i < s ? parity ^ 1u : parity, &ab, nullptr);
+  __syncthreads();  // the stages are free for the sums
+  write_partials<32, VE, N, 256>(a, dg, db, t, reinterpret_cast<float*>(stages));
 }
 
 template <typename Kernel>
@@ -639,11 +829,13 @@ auto with_lanes(int C, F f) {
   if constexpr (KM >= 8) if (slots <= 4096) return f(Int<VE>(), Int<512>(), Int<8>());
   return f(Int<VE>(), Int<512>(), Int<KM>());
 }
-// Vectors of 16 bytes where every row starts on one; else pairs of channels, else single ones.
+// Vectors of 16 bytes where every row starts on one; else of four channels, pairs, single ones.
 template <typename T, typename F>
 auto with_plan(int C, F f) {
   constexpr int V16 = 16 / sizeof(T);
   if (C % V16 == 0) return with_lanes<T, V16>(C, f);
+  if constexpr (V16 == 8)
+    if (C % 4 == 0) return with_lanes<T, 4>(C, f);
   if (C % 2 == 0) return with_lanes<T, 2>(C, f);
   return with_lanes<T, 1>(C, f);
 }
@@ -664,10 +856,40 @@ constexpr int kFwdPerSm = 24;  // most blocks of 256 threads per SM: several wav
 
 }  // namespace rows
 
+namespace rows {
+
+// Stages that fit with three blocks on an SM, or with two; and whether bulk copies are the faster
+// way (us, bulk / rows in registers; r: with dres, q: from the checkpoint):
+//   16 channels a lane, of which registers hold few rows: always.  300,000 rows of bf16, C = 512 r
+//     183 / 269, 384 rq 153 / 240, 300 rq 214 / 330
+//   odd C, single loads: always.  300,000 x 101 bf16 77 / 110, fp32 r 91 / 102
+//   8 channels of bf16: with three stages and 32 turns a block.  1,048,576 x 256 274 / 297,
+//     r 349 / 350, rq 333 / 351, q 308 / 302; 20,000 x 256 rq 13.6 / 13.2
+//   else never: fp32 stages are too long.  524,288 x 256 277 / 244, 60,033 x 198 41 / 35
+template <typename T, int VE, int N>
+Bulk bulk_plan(const RowsArgs& a) {
+  const int nb = (a.C + kCkptBlock - 1) / kCkptBlock, nd = kBulkRows * a.C * (int)sizeof(T);
+  const int bytes = nd * (a.dres ? 2 : 1) + (a.q8 ? kBulkRows * (a.C + nb) : nd);
+  for (int per_sm = N <= 8 ? 3 : 2; per_sm >= 2; per_sm--) {
+    const int fit = (232448 / per_sm - 2048) / bytes;
+    if (fit < 2) continue;
+    const bool many = a.rows >= (int64_t)num_sms() * per_sm * kBulkRows * 32;
+    if (N > 8 || VE == 1 || (VE == 8 && fit >= 3 && many)) return {std::min(fit, kBulkStages), bytes, per_sm};
+    break;
+  }
+  return {};
+}
+inline int64_t bulk_blocks(int64_t rows, int per_sm) {
+  return std::min((int64_t)num_sms() * per_sm, (rows + kBulkRows - 1) / kBulkRows);
+}
+
+}  // namespace rows
+
 template <typename T>
 int64_t norm_bwd_blocks(int64_t rows, int C) {
   return rows::with_plan<T>(C, [&](auto v, auto l, auto k) {
-    return (int64_t)rows::grid_of<decltype(v), decltype(l), decltype(k)>(rows, 9, rows::rows_ahead<decltype(k)::value>(), 16).x;
+    const int64_t n = rows::grid_of<decltype(v), decltype(l), decltype(k)>(rows, 9, rows::rows_ahead<decltype(k)::value>(), 16).x;
+    return decltype(l)::value == 32 ? std::max(n, rows::bulk_blocks(rows, 3)) : n;
   });
 }
 
@@ -696,10 +918,24 @@ cudaError_t ckpt_unpack(const RowsArgs& a, cudaStream_t st) {
 }
 
 template <typename T>
-cudaError_t norm_bwd(const RowsArgs& a, int64_t blocks, cudaStream_t st) {
+cudaError_t norm_bwd(const RowsArgs& a, int64_t* blocks, cudaStream_t st) {
   return rows::with_plan<T>(a.C, [&](auto v, auto l, auto k) {
     using V = decltype(v); using L = decltype(l); using K = decltype(k);
-    const dim3 grid((unsigned)blocks), block(rows::block_threads<L::value>());
+    constexpr int N = V::value * K::value;
+    if constexpr (L::value == 32) {
+      const rows::Bulk plan = rows::bulk_plan<T, V::value, N>(a);
+      if (plan.per_sm) {
+        *blocks = rows::bulk_blocks(a.rows, plan.per_sm);
+        const size_t smem = std::max((size_t)plan.stages * plan.bytes, (size_t)8 * 32 * N * sizeof(float));
+        const auto kernel = a.q8 ? rows::k_norm_bwd_bulk<T, V::value, K::value, true>
+                                 : rows::k_norm_bwd_bulk<T, V::value, K::value, false>;
+        if (cudaError_t e = rows::allow_smem(kernel, smem)) return e;
+        return launch(kernel, dim3((unsigned)*blocks), dim3(256), smem, st, a, plan);
+      }
+    }
+    const dim3 grid = rows::grid_of<V, L, K>(a.rows, 9, rows::rows_ahead<K::value>(), 16);
+    const dim3 block(rows::block_threads<L::value>());
+    *blocks = grid.x;
     return a.q8 ? launch(rows::k_norm_bwd<T, V::value, L::value, K::value, true>, grid, block, 0, st, a)
                 : launch(rows::k_norm_bwd<T, V::value, L::value, K::value, false>, grid, block, 0, st, a);
   });

@@ -29,14 +29,14 @@ struct RowsArgs {
 constexpr int kCkptBlock = 32;  // channels that share a scale
 constexpr int kRowsMaxC = 8192;
 
-// Blocks of the backward's main pass: rows of partial sums [blocks][2 C] in the workspace.
+// Most blocks of the backward's main pass: rows of partial sums [blocks][2 C] in the workspace.
 template <typename T>
 int64_t norm_bwd_blocks(int64_t rows, int C);
 
 template <typename T>
 cudaError_t norm_fwd(const RowsArgs& a, cudaStream_t st);
 template <typename T>
-cudaError_t norm_bwd(const RowsArgs& a, int64_t blocks, cudaStream_t st);
+cudaError_t norm_bwd(const RowsArgs& a, int64_t* blocks, cudaStream_t st);  // *blocks: those that it used
 template <typename T>
 cudaError_t ckpt_pack(const RowsArgs& a, cudaStream_t st);
 template <typename T>

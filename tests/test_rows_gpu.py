@@ -16,7 +16,7 @@ pytestmark = pytest.mark.gpu
 U = 2.0 ** -24
 DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
 HALF = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8}
-WIDTHS = [1, 2, 3, 16, 30, 31, 32, 64, 66, 100, 198, 256, 257, 513, 1000, 1023, 1024, 1026, 2048, 2050, 4095, 4100,
+WIDTHS = [1, 2, 3, 4, 16, 30, 31, 32, 64, 66, 100, 196, 198, 256, 257, 300, 384, 512, 513, 1000, 1023, 1024, 1026, 2048, 2050, 4095, 4100,
           5001, 8192]
 
 
@@ -163,6 +163,60 @@ def test_many_rows(lib, dtype, C):
     tol, tg, tb = backward_bounds(vh, None, host(mean), host(rstd), host(dy), wv, dtype, rows / 152 + 64)
     assert (np.abs(host(dv) - wv) <= tol).all()
     assert (np.abs(host(dg) - wg) <= tg).all() and (np.abs(host(db) - wb) <= tb).all()
+
+
+@pytest.mark.parametrize("rows, C, dtype", [(240_011, 256, "bf16"), (233_472, 256, "bf16"), (70_001, 512, "bf16"), (70_001, 384, "bf16"),
+                                            (70_001, 300, "bf16"), (70_001, 101, "bf16"), (70_001, 101, "f32"),
+                                            (70_001, 420, "f32"), (15, 512, "bf16"), (16, 512, "bf16"), (17, 101, "bf16"),
+                                            (30_000, 255, "f32"), (30_000, 511, "bf16")])
+@pytest.mark.parametrize("with_res, with_ckpt", [(False, False), (True, True), (True, False), (False, True)])
+def test_backward_of_rows_in_stages(lib, rows, C, dtype, with_res, with_ckpt):
+    """Rows that come by bulk copies, 16 at a time: whole stages, a last one of fewer rows, several rounds of the
+    stages; out of place, and in place of either gradient.  The formula in 64 bits on the GPU."""
+    g = torch.Generator(device="cuda").manual_seed(rows + C)
+    new = lambda *n: torch.randn(*n, generator=g, device="cuda").to(DTYPES[dtype])  # noqa: E731
+    v, dy, dres, gamma = new(rows, C), new(rows, C), new(rows, C) if with_res else None, new(C).float()
+    r = lib.rows_of(v)
+    mean, rstd = v.float().mean(1), torch.rsqrt(v.float().var(1, unbiased=False) + 1e-5)
+    q8 = e8 = None
+    x = v.double()
+    if with_ckpt:
+        q8, e8 = lib.checkpoint(r)
+        lib.fs_ckpt_pack(r, v, q8, e8)
+        scale = torch.exp2(e8.double() - 127).repeat_interleave(32, 1)[:, :C]
+        x = q8.double() * scale
+    ws = lib.norm_workspace(r)
+
+    def backward(dy, dres, to):
+        dg, db = torch.empty(C, device="cuda"), torch.empty(C, device="cuda")
+        lib.fs_norm_bwd(r, None if with_ckpt else v, q8, e8, gamma, mean, rstd, dy, dres, to, dg, db, False, ws)
+        assert lib.fs_device_status(ws) == lib.FS_OK
+        return to, dg, db
+
+    buf, tail = spare((rows, C), DTYPES[dtype])
+    dv, dg, db = backward(dy, dres, buf)
+    assert untouched(tail)
+    y, m, rs = dy.double(), mean.double()[:, None], rstd.double()[:, None]
+    xh = (x - m) * rs
+    gg = y * gamma.double()
+    a1, a2 = gg.abs().mean(1, keepdim=True), (gg * xh).abs().mean(1, keepdim=True)
+    want = rs * (gg - gg.mean(1, keepdim=True) - xh * (gg * xh).mean(1, keepdim=True))
+    if with_res:
+        want = want + dres.double()
+    # as in backward_bounds
+    tol = rs * (42 * U * a1 + xh.abs() * 48 * U * a2 + 6 * U * (gg.abs() + a1 + xh.abs() * a2))
+    tol = tol + 4 * U * want.abs() + HALF[dtype] * 1.01 * want.abs() + 1e-30
+    if with_res:
+        tol = tol + 2 * U * dres.double().abs()
+    assert bool(((dv.double() - want).abs() <= tol).all())
+    terms = min(rows, rows / 152 + 64) + 64
+    assert bool(((dg.double() - (y * xh).sum(0)).abs() <= (terms + 4) * U * (y * xh).abs().sum(0) + 1e-30).all())
+    assert bool(((db.double() - y.sum(0)).abs() <= terms * U * y.abs().sum(0) + 1e-30).all())
+    a = dy.clone()
+    assert all(torch.equal(p, q) for p, q in zip(backward(a, dres, a), (dv, dg, db)))
+    if with_res:
+        b = dres.clone()
+        assert all(torch.equal(p, q) for p, q in zip(backward(dy, b, b), (dv, dg, db)))
 
 
 @pytest.mark.parametrize("C", [1, 5, 31, 32, 33, 62, 64, 200, 256, 1030, 8192])
