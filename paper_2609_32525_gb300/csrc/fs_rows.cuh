@@ -796,6 +796,177 @@ __global__ void __launch_bounds__(256, K * VE <= 8 ? 3 : 2) k_norm_bwd_bulk(cons
   write_partials<32, VE, N, 256>(a, dg, db, t, reinterpret_cast<float*>(stages));
 }
 
+// One row of the forward of the norm, from its values in raw; load_res(raw) brings those of res.  The
+// same arithmetic as k_rows_fwd's, which keeps its own: sharing this made it slower (1,048,576 x 256
+// bf16 188 -> 203 us).
+template <typename T, int K, typename F>
+__device__ __forceinline__ void forward_row(const RowsArgs& a, int64_t row, bool here, int t, bool whole, float invC,
+                                            const Vals<K>& gm, const Vals<K>& bt, RawV<T, 1> (&raw)[K],
+                                            F load_res) {
+  constexpr int P = Vals<K>::P;
+  using R = RawV<T, 1>;
+  const int C = a.C, nb = (C + kCkptBlock - 1) / kCkptBlock;
+  Vals<K> v = vals_of<T, 1, K>(raw);
+  if (a.res) {
+    load_res(raw);
+    const Vals<K> r = vals_of<T, 1, K>(raw);
+#pragma unroll
+    for (int i = 0; i < P; i++) v.p[i] = v.p[i] + r.p[i];
+    float f[2 * P];
+    floats_of(v, f);
+    // the stream is kept in its own type, and what is kept is what is normalised
+#pragma unroll
+    for (int k = 0; k < K; k++) raw[k] = from_float<T, 1>(*reinterpret_cast<float(*)[1]>(f + k));
+    v = vals_of<T, 1, K>(raw);
+    if (a.sum && here) {
+#pragma unroll
+      for (int k = 0; k < K; k++) {
+        const int c = k * 32 + t;
+        if (c < C) *reinterpret_cast<R*>(static_cast<T*>(a.sum) + row * C + c) = raw[k];
+      }
+    }
+  }
+  if (a.q8) {
+    float f[2 * P];
+    floats_of(v, f);
+#pragma unroll
+    for (int k = 0; k < K; k++) {
+      const int c = k * 32 + t;
+      uint32_t byte;
+      uint8_t q;
+      quantise<1>(f + k, byte, q);
+      if (here && c < C) {
+        reinterpret_cast<uint8_t*>(a.q8)[row * C + c] = q;
+        if (c % kCkptBlock == 0) a.e8[row * nb + c / kCkptBlock] = (uint8_t)byte;
+      }
+    }
+  }
+  F2 s = v.p[0];  // channels past C hold 0
+#pragma unroll
+  for (int i = 1; i < P; i++) s = s + v.p[i];
+  const float mean = row_sum<32>(total(s), nullptr) * invC;
+  const F2 minus = pair(-mean, -mean);
+  float f[2 * P], d2 = 0.f;
+#pragma unroll
+  for (int i = 0; i < P; i++) v.p[i] = v.p[i] + minus;
+  if (whole) {  // every value of the thread lies inside C
+    F2 q = v.p[0] * v.p[0];
+#pragma unroll
+    for (int i = 1; i < P; i++) q = fma(v.p[i], v.p[i], q);
+    d2 = total(q);
+  } else {
+    floats_of(v, f);
+#pragma unroll
+    for (int k = 0; k < K; k++)
+      if (k * 32 + t < C) d2 += f[k] * f[k];
+  }
+  const float rstd = rsqrtf(row_sum<32>(d2, nullptr) * invC + a.eps);
+  const F2 r2 = pair(rstd, rstd);
+#pragma unroll
+  for (int i = 0; i < P; i++) v.p[i] = fma(v.p[i] * r2, gm.p[i], bt.p[i]);
+  floats_of(v, f);
+  if (here) {
+#pragma unroll
+    for (int k = 0; k < K; k++) {
+      const int c = k * 32 + t;
+      if (c < C)
+        *reinterpret_cast<R*>(static_cast<T*>(a.y) + row * C + c) =
+            from_float<T, 1>(*reinterpret_cast<float(*)[1]>(f + k));
+    }
+    if (t == 0) {
+      if (a.mean) a.mean[row] = mean;
+      if (a.rstd) a.rstd[row] = rstd;
+    }
+  }
+}
+
+// The forward for rows of odd C of one warp each, in the same way: single values are below
+// cp.async's size for bf16, and each took a load, a store and a load.  (No status word here: where
+// a wait gives up the lanes read the rows themselves.)
+template <typename T, int K>
+__global__ void __launch_bounds__(256, 3) k_norm_fwd_bulk(const RowsArgs args, const Bulk plan) {
+  constexpr int RU = kBulkRows / 8;
+  using R = RawV<T, 1>;
+  extern __shared__ __align__(128) char stages[];
+  __shared__ uint64_t full[kBulkStages], empty[kBulkStages];
+  __shared__ tc::Abort ab;
+  RowsArgs a = args;
+  const int warp = threadIdx.x >> 5, t = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < plan.stages; s++) {
+      tc::mbar_init(&full[s], 1);
+      tc::mbar_init(&empty[s], 8);
+    }
+    ab.flag = 0;
+    tc::fence_mbar_init();
+  }
+  __syncthreads();
+  grid_begin(a.x, a.res, a.gamma, a.beta);
+  const int C = a.C;
+  const bool res = a.res != nullptr;
+  const int64_t chunks = (a.rows + kBulkRows - 1) / kBulkRows, first = blockIdx.x, step = gridDim.x;
+  const uint32_t nd = (uint32_t)(kBulkRows * C * sizeof(T));
+  auto issue = [&](int64_t chunk, int s) {
+    if ((chunk + 1) * kBulkRows > a.rows) return;  // a last chunk of fewer rows is read by the lanes
+    char* to = stages + (size_t)s * plan.bytes;
+    tc::mbar_expect_tx(&full[s], (uint32_t)plan.bytes);
+    tc::bulk_load(to, static_cast<const char*>(a.x) + chunk * nd, nd, &full[s]);
+    if (res) tc::bulk_load(to + nd, static_cast<const char*>(a.res) + chunk * nd, nd, &full[s]);
+  };
+  if (threadIdx.x == 0)
+    for (int s = 0; s < plan.stages - 1; s++)
+      if (first + s * step < chunks) issue(first + s * step, s);
+  const Vals<K> gm = channels_of<K, 1, 32>(a.gamma, C, t, 1.f);
+  const Vals<K> bt = channels_of<K, 1, 32>(a.beta, C, t, 0.f);
+  const bool inside = K % 2 == 0 && (K - 1) * 32 + t < C;
+  const float invC = 1.f / (float)C;
+  int s = 0;
+  uint32_t parity = 0;
+#pragma unroll 1
+  for (int64_t chunk = first; chunk < chunks; chunk += step) {
+    const int64_t ahead = chunk + (plan.stages - 1) * step;
+    if (warp == 0 && ahead < chunks) {
+      const int w = s == 0 ? plan.stages - 1 : s - 1;
+      const bool free = chunk == first || tc::mbar_wait_w(&empty[w], s == 0 ? parity ^ 1u : parity, &ab, nullptr);
+      if (free && t == 0) issue(ahead, w);
+    }
+    const int64_t row0 = chunk * kBulkRows + RU * warp;
+    T* x = reinterpret_cast<T*>(stages + (size_t)s * plan.bytes) + RU * warp * C;  // the warp's rows
+    T* r = reinterpret_cast<T*>(reinterpret_cast<char*>(x) + nd);
+    if ((chunk + 1) * kBulkRows > a.rows || !tc::mbar_wait_w(&full[s], parity, &ab, nullptr)) {
+      const int left = (int)max((int64_t)0, min((int64_t)RU, a.rows - row0)) * C;
+#pragma unroll 1
+      for (int i = t; i < left; i += 32) {
+        x[i] = static_cast<const T*>(a.x)[row0 * C + i];
+        if (res) r[i] = static_cast<const T*>(a.res)[row0 * C + i];
+      }
+      __syncwarp();
+    }
+#pragma unroll
+    for (int u = 0; u < RU; u++) {
+      const bool here = row0 + u < a.rows;
+      auto load = [&](R (&to)[K], const T* from) {
+#pragma unroll
+        for (int k = 0; k < K; k++) {
+          const int c = k * 32 + t;
+          to[k] = here && c < C ? *reinterpret_cast<const R*>(from + u * C + c) : R(0);
+        }
+      };
+      R raw[K];
+      load(raw, x);
+      forward_row<T, K>(a, row0 + u, here, t, inside, invC, gm, bt, raw, [&](R (&to)[K]) { load(to, r); });
+    }
+    __syncwarp();
+    if (t == 0) tc::mbar_arrive(&empty[s]);
+    if (++s == plan.stages) {
+      s = 0;
+      parity ^= 1u;
+    }
+  }
+  if (ab.flag)  // no copy is left in flight
+    for (int i = 0; i < plan.stages; i++) tc::mbar_wait_w(&full[i], i < s ? parity ^ 1u : parity, &ab, nullptr);
+}
+
 template <typename Kernel>
 cudaError_t allow_smem(Kernel kernel, size_t bytes) {
   if (bytes <= 24576) return cudaSuccess;  // with the static arrays within the default limit
@@ -897,10 +1068,22 @@ template <typename T, bool kNorm>
 cudaError_t rows_fwd(const RowsArgs& a, cudaStream_t st) {
   return rows::with_plan<T>(a.C, [&](auto v, auto l, auto k) {
     using V = decltype(v); using L = decltype(l); using K = decltype(k);
-    using F = rows::Fwd<T, V::value, L::value, K::value, kNorm>;
-    auto kernel = rows::k_rows_fwd<T, V::value, L::value, K::value, kNorm>;
-    if (cudaError_t e = rows::allow_smem(kernel, F::SMEM)) return e;
-    return launch(kernel, rows::grid_of<V, L, K>(a.rows, rows::kFwdPerSm, 1, 8), dim3(F::THREADS), F::SMEM, st, a);
+    // The norm of more than 64 channels, odd C: 300,000 rows of bf16 255 287 -> 88 us, with res and
+    // checkpoint 611 -> 235; 101 92 -> 61 and 193 -> 133; 33 channels 50 / 57, the checkpoint alone 74 / 81
+    // stay with the slots.  At most 256 channels: two stages always fit.
+    if constexpr (kNorm && V::value == 1 && L::value == 32 && K::value >= 4) {
+      const int bytes = rows::kBulkRows * a.C * (int)sizeof(T) * (a.res ? 2 : 1);
+      const rows::Bulk plan{std::min((232448 / 3 - 2048) / bytes, rows::kBulkStages), bytes, 3};
+      auto kernel = rows::k_norm_fwd_bulk<T, K::value>;
+      const size_t smem = (size_t)plan.stages * plan.bytes;
+      if (cudaError_t e = rows::allow_smem(kernel, smem)) return e;
+      return launch(kernel, dim3((unsigned)rows::bulk_blocks(a.rows, plan.per_sm)), dim3(256), smem, st, a, plan);
+    } else {
+      using F = rows::Fwd<T, V::value, L::value, K::value, kNorm>;
+      auto kernel = rows::k_rows_fwd<T, V::value, L::value, K::value, kNorm>;
+      if (cudaError_t e = rows::allow_smem(kernel, F::SMEM)) return e;
+      return launch(kernel, rows::grid_of<V, L, K>(a.rows, rows::kFwdPerSm, 1, 8), dim3(F::THREADS), F::SMEM, st, a);
+    }
   });
 }
 template <typename T>

@@ -342,13 +342,26 @@ class attn_mask:
 
 
 def _attn_mask(fn, s, m, dev):
+    """The struct for the tensors that are there, or None (a small call notices each look at one that is not)."""
     if m is None:
         return None
-    f, i, nq, nk = torch.float32, torch.int32, s.B * s.Gq, s.B * s.Gk
-    return ctypes.byref(fs_attn_mask(
-        _arg(fn, "slopes", m.slopes, f, s.H, dev, True), _arg(fn, "pos_q", m.pos_q, f, nq, dev, True),
-        _arg(fn, "pos_k", m.pos_k, f, nk, dev, True), _arg(fn, "doc_q", m.doc_q, i, nq, dev, True),
-        _arg(fn, "doc_k", m.doc_k, i, nk, dev, True), _arg(fn, "prefix", m.prefix, i, s.B, dev, True)))
+    slopes, pos_q, pos_k, doc_q, doc_k, prefix = m.slopes, m.pos_q, m.pos_k, m.doc_q, m.doc_k, m.prefix
+    if slopes is pos_q is pos_k is doc_q is doc_k is prefix is None:
+        return None
+    c, f, i = fs_attn_mask(), torch.float32, torch.int32
+    if slopes is not None:
+        c.slopes = _arg(fn, "slopes", slopes, f, s.H, dev)
+    if pos_q is not None:
+        c.pos_q = _arg(fn, "pos_q", pos_q, f, s.B * s.Gq, dev)
+    if pos_k is not None:
+        c.pos_k = _arg(fn, "pos_k", pos_k, f, s.B * s.Gk, dev)
+    if doc_q is not None:
+        c.doc_q = _arg(fn, "doc_q", doc_q, i, s.B * s.Gq, dev)
+    if doc_k is not None:
+        c.doc_k = _arg(fn, "doc_k", doc_k, i, s.B * s.Gk, dev)
+    if prefix is not None:
+        c.prefix = _arg(fn, "prefix", prefix, i, s.B, dev)
+    return ctypes.byref(c)
 
 
 def attn_workspace_bytes(shape: fs_attn_shape, backward=False) -> int:

@@ -16,7 +16,7 @@ pytestmark = pytest.mark.gpu
 U = 2.0 ** -24
 DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
 HALF = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8}
-WIDTHS = [1, 2, 3, 4, 16, 30, 31, 32, 64, 66, 100, 196, 198, 256, 257, 300, 384, 512, 513, 1000, 1023, 1024, 1026, 2048, 2050, 4095, 4100,
+WIDTHS = [1, 2, 3, 4, 16, 30, 31, 32, 64, 65, 66, 100, 101, 196, 198, 255, 256, 257, 300, 384, 512, 513, 1000, 1023, 1024, 1026, 2048, 2050, 4095, 4100,
           5001, 8192]
 
 
@@ -163,6 +163,50 @@ def test_many_rows(lib, dtype, C):
     tol, tg, tb = backward_bounds(vh, None, host(mean), host(rstd), host(dy), wv, dtype, rows / 152 + 64)
     assert (np.abs(host(dv) - wv) <= tol).all()
     assert (np.abs(host(dg) - wg) <= tg).all() and (np.abs(host(db) - wb) <= tb).all()
+
+
+@pytest.mark.parametrize("rows", [15, 16, 17, 70_001])
+@pytest.mark.parametrize("C, dtype", [(65, "bf16"), (101, "f32"), (255, "bf16"), (255, "f32")])
+def test_forward_of_odd_rows_in_stages(lib, rows, C, dtype):
+    """Rows that come by bulk copies, 16 at a time: the stream in place of either input, its checkpoint,
+    the norm; the formula in 64 bits on the GPU."""
+    g = torch.Generator(device="cuda").manual_seed(rows + C)
+    new = lambda *n: torch.randn(*n, generator=g, device="cuda").to(DTYPES[dtype])  # noqa: E731
+    x, res, gamma, beta = new(rows, C), new(rows, C), new(C).float(), new(C).float()
+    r = lib.rows_of(x)
+    v = (x.float() + res.float()).to(DTYPES[dtype])
+    want8, want_e = lib.checkpoint(r)
+    lib.fs_ckpt_pack(r, v, want8, want_e)
+
+    def forward(x, res, to):
+        y, t0 = spare((rows, C), DTYPES[dtype])
+        mean, t1 = spare((rows,), torch.float32)
+        rstd, t2 = spare((rows,), torch.float32)
+        q8, t3 = spare((rows, C), torch.int8)
+        e8, t4 = spare(tuple(want_e.shape), torch.uint8)
+        lib.fs_norm_fwd(r, x, res, gamma, beta, 1e-5, to, y, mean, rstd, q8, e8)
+        torch.cuda.synchronize()
+        assert untouched(t0, t1, t2, t3, t4)
+        return to, y, mean, rstd, q8, e8
+
+    got = forward(x, res, torch.empty_like(x))
+    s, y, mean, rstd, q8, e8 = got
+    assert torch.equal(s, v) and torch.equal(q8, want8) and torch.equal(e8, want_e)
+    d = v.double()
+    m = d.mean(1)
+    rs = torch.rsqrt(d.var(1, unbiased=False) + 1e-5)
+    want = (d - m[:, None]) * rs[:, None] * gamma.double() + beta.double()
+    a = d.abs().mean(1)
+    assert bool(((mean - m).abs() <= 41 * U * a).all())
+    assert bool(((rstd - rs).abs() <= 45 * U * rs + rs * rs * 41 * U * a).all())
+    # as in norm_bounds
+    far, g, k = (d - m[:, None]).abs(), gamma.double().abs(), rs[:, None]
+    tol = (g * k * (40 * U * a[:, None] + 40 * U * far) + g * k * k * far * 80 * U * a[:, None]
+           + 4 * U * (want.abs() + beta.double().abs()) + HALF[dtype] * 1.01 * want.abs() + 1e-30)
+    assert bool(((y.double() - want).abs() <= tol).all())
+    for inputs in ((x.clone(), res), (x, res.clone())):
+        to = inputs[0] if inputs[0] is not x else inputs[1]
+        assert all(torch.equal(p, q) for p, q in zip(forward(*inputs, to), got))
 
 
 @pytest.mark.parametrize("rows, C, dtype", [(240_011, 256, "bf16"), (233_472, 256, "bf16"), (70_001, 512, "bf16"), (70_001, 384, "bf16"),
