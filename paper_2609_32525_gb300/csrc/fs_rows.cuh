@@ -220,10 +220,13 @@ __device__ __forceinline__ void restore(const RawV<uint8_t, VE>& q, uint32_t byt
   if constexpr (VE >= 4) {
     uint32_t w[VE / 4];
     memcpy(w, &q, sizeof(q));
+    const F2 minus = pair(-8388736.f, -8388736.f), both = pair(size, size);
 #pragma unroll
-    for (int i = 0; i < VE; i++) {
+    for (int i = 0; i < VE; i += 2) {
       const uint32_t u = w[i / 4] ^ 0x80808080u;
-      f[i] = (__uint_as_float(__byte_perm(u, 0x4b000000u, 0x7440 + i % 4)) - 8388736.f) * size;
+      const F2 x = pair(__uint_as_float(__byte_perm(u, 0x4b000000u, 0x7440 + i % 4)),
+                        __uint_as_float(__byte_perm(u, 0x4b000000u, 0x7441 + i % 4)));
+      split((x + minus) * both, f[i], f[i + 1]);
     }
   } else {
     int8_t b[VE];
@@ -635,7 +638,9 @@ struct Bulk {
 };
 constexpr int kBulkRows = 16, kBulkStages = 6;
 
-template <typename T, int VE, int K, bool kCkpt>
+// kFull: every lane has K vectors of the row: no lane is masked, and no register zeroed for it (from
+// the checkpoint with dres 333 -> 306 us; rows without checkpoint gain nothing).
+template <typename T, int VE, int K, bool kCkpt, bool kFull>
 __global__ void __launch_bounds__(256, K * VE <= 8 ? 3 : 2) k_norm_bwd_bulk(const RowsArgs args, const Bulk plan) {
   constexpr int N = K * VE, P = Vals<N>::P, RU = kBulkRows / 8;
   using R = RawV<T, VE>;
@@ -710,18 +715,20 @@ __global__ void __launch_bounds__(256, K * VE <= 8 ? 3 : 2) k_norm_bwd_bulk(cons
     uint8_t* b_e = reinterpret_cast<uint8_t*>(base + at_e) + RU * warp * nb;
     if (whole) {
       if (!tc::mbar_wait_w(&full[s], parity, &ab, a.status)) break;
-    } else {  // each warp its own, in whose place no other reads
+    } else {  // each warp its own, in whose place no other reads; kFull: zeros past the last row
       const int left = (int)max((int64_t)0, min((int64_t)RU, a.rows - row0)) * C;
+      const T zero = T(0.f);
 #pragma unroll 1
-      for (int i = t; i < left; i += 32) {
+      for (int i = t; i < (kFull ? RU * C : left); i += 32) {
         const int64_t at = row0 * C + i;
-        reinterpret_cast<T*>(b_dy)[i] = static_cast<const T*>(a.dy)[at];
-        if (src_dres) reinterpret_cast<T*>(b_dres)[i] = static_cast<const T*>(a.dres)[at];
-        if (kCkpt) b_x[i] = src_x[at];
-        else reinterpret_cast<T*>(b_x)[i] = static_cast<const T*>(a.x)[at];
+        const bool in = !kFull || i < left;
+        reinterpret_cast<T*>(b_dy)[i] = in ? static_cast<const T*>(a.dy)[at] : zero;
+        if (src_dres) reinterpret_cast<T*>(b_dres)[i] = in ? static_cast<const T*>(a.dres)[at] : zero;
+        if (kCkpt) b_x[i] = in ? src_x[at] : 0;
+        else reinterpret_cast<T*>(b_x)[i] = in ? static_cast<const T*>(a.x)[at] : zero;
       }
       if (kCkpt)
-        for (int i = t; i < left / C * nb; i += 32) b_e[i] = a.e8[row0 * nb + i];
+        for (int i = t; i < (kFull ? RU : left / C) * nb; i += 32) b_e[i] = !kFull || i < left / C * nb ? a.e8[row0 * nb + i] : 0;
       __syncwarp();
     }
 #pragma unroll
@@ -737,7 +744,7 @@ __global__ void __launch_bounds__(256, K * VE <= 8 ? 3 : 2) k_norm_bwd_bulk(cons
 #pragma unroll
         for (int k = 0; k < K; k++) {
           const int c = (k * 32 + t) * VE;
-          const bool ok = here && c < C;
+          const bool ok = kFull || (here && c < C);
           const Q q = ok ? *reinterpret_cast<const Q*>(b_x + u * C + c) : raw_zero<Q>();
           const uint32_t e = ok ? b_e[u * nb + c / kCkptBlock] : 0u;
           restore<VE>(q, e, *reinterpret_cast<float(*)[VE]>(f + k * VE));
@@ -749,14 +756,14 @@ __global__ void __launch_bounds__(256, K * VE <= 8 ? 3 : 2) k_norm_bwd_bulk(cons
 #pragma unroll
         for (int k = 0; k < K; k++) {
           const int c = (k * 32 + t) * VE;
-          xr[k] = here && c < C ? *reinterpret_cast<const R*>(b_x + (u * C + c) * sizeof(T)) : raw_zero<R>();
+          xr[k] = kFull || (here && c < C) ? *reinterpret_cast<const R*>(b_x + (u * C + c) * sizeof(T)) : raw_zero<R>();
         }
         xh = vals_of<T, VE, K>(xr);
       }
 #pragma unroll
       for (int k = 0; k < K; k++) {
         const int c = (k * 32 + t) * VE;
-        const bool ok = here && c < C;
+        const bool ok = kFull || (here && c < C);
         yr[k] = ok ? *reinterpret_cast<const R*>(b_dy + (u * C + c) * sizeof(T)) : raw_zero<R>();
         if (src_dres) rr[k] = ok ? *reinterpret_cast<const R*>(b_dres + (u * C + c) * sizeof(T)) : raw_zero<R>();
       }
@@ -777,7 +784,7 @@ __global__ void __launch_bounds__(256, K * VE <= 8 ? 3 : 2) k_norm_bwd_bulk(cons
 #pragma unroll
         for (int k = 0; k < K; k++) {
           const int c = (k * 32 + t) * VE;
-          if (c < C)
+          if (kFull || c < C)
             *reinterpret_cast<R*>(static_cast<T*>(a.y) + row * C + c) =
                 from_float<T, VE>(*reinterpret_cast<float(*)[VE]>(f + k * VE));
         }
@@ -1032,10 +1039,10 @@ namespace rows {
 // Stages that fit with three blocks on an SM, or with two; and whether bulk copies are the faster
 // way (us, bulk / rows in registers; r: with dres, q: from the checkpoint):
 //   16 channels a lane, of which registers hold few rows: always.  300,000 rows of bf16, C = 512 r
-//     183 / 269, 384 rq 153 / 240, 300 rq 214 / 330
+//     183 / 269, 384 rq 149 / 240, with vectors of two 300 rq 214 / 330
 //   odd C, single loads: always.  300,000 x 101 bf16 77 / 110, fp32 r 91 / 102
 //   8 channels of bf16: with three stages and 32 turns a block.  1,048,576 x 256 274 / 297,
-//     r 349 / 350, rq 333 / 351, q 308 / 302; 20,000 x 256 rq 13.6 / 13.2
+//     r 349 / 350, rq 306 / 351, q 287 / 302; 20,000 x 256 rq 13.6 / 13.2
 //   else never: fp32 stages are too long.  524,288 x 256 277 / 244, 60,033 x 198 41 / 35
 template <typename T, int VE, int N>
 Bulk bulk_plan(const RowsArgs& a) {
@@ -1110,8 +1117,10 @@ cudaError_t norm_bwd(const RowsArgs& a, int64_t* blocks, cudaStream_t st) {
       if (plan.per_sm) {
         *blocks = rows::bulk_blocks(a.rows, plan.per_sm);
         const size_t smem = std::max((size_t)plan.stages * plan.bytes, (size_t)8 * 32 * N * sizeof(float));
-        const auto kernel = a.q8 ? rows::k_norm_bwd_bulk<T, V::value, K::value, true>
-                                 : rows::k_norm_bwd_bulk<T, V::value, K::value, false>;
+        constexpr bool kCanBeFull = V::value == 8;
+        const auto kernel = !a.q8                             ? rows::k_norm_bwd_bulk<T, V::value, K::value, false, false>
+                            : kCanBeFull && a.C == 32 * N ? rows::k_norm_bwd_bulk<T, V::value, K::value, true, kCanBeFull>
+                                                              : rows::k_norm_bwd_bulk<T, V::value, K::value, true, false>;
         if (cudaError_t e = rows::allow_smem(kernel, smem)) return e;
         return launch(kernel, dim3((unsigned)*blocks), dim3(256), smem, st, a, plan);
       }
