@@ -891,7 +891,7 @@ cudaError_t attn_tc(const AttnTcArgs& t, bool backward, cudaStream_t st) {
     constexpr size_t smem = Map<kFwd, D>::SMEM;
     const auto kernel = cap ? (bias ? k_attn_fwd_tc<D, true, true> : k_attn_fwd_tc<D, true, false>)
                             : (bias ? k_attn_fwd_tc<D, false, true> : k_attn_fwd_tc<D, false, false>);
-    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    e = allow_smem<smem>(kernel);
     if (e == cudaSuccess)
       e = launch(kernel, dim3((unsigned)blocks_q, (unsigned)a.splits), dim3(kThreads), smem, st, t);
     if (e == cudaSuccess && a.splits > 1)
@@ -901,7 +901,7 @@ cudaError_t attn_tc(const AttnTcArgs& t, bool backward, cudaStream_t st) {
   constexpr size_t smem = bwd_smem<D>();
   const auto kernel = cap ? (bias ? k_attn_bwd_tc<D, true, true> : k_attn_bwd_tc<D, true, false>)
                           : (bias ? k_attn_bwd_tc<D, false, true> : k_attn_bwd_tc<D, false, false>);
-  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  e = allow_smem<smem>(kernel);
   const int64_t kinds = D == 64 ? 2 : 1;  // dk and dv apart
   if (e == cudaSuccess)
     e = launch(kernel, dim3((unsigned)(kinds * blocks_kv * a.splits_kv + blocks_q * a.splits)), dim3(kThreads), smem, st,

@@ -38,6 +38,14 @@ __device__ __forceinline__ int64_t grid_begin(P&... p) {
   return grid_wait(p...);
 }
 
+// Lets a kernel be launched with up to kBytes of dynamic shared memory.  The limit belongs to the
+// function, not to a launch: a call that set it to its own need would lower it between another
+// host thread's setting and its launch.  So it is one constant per kernel.
+template <size_t kBytes, typename Kernel>
+cudaError_t allow_smem(Kernel kernel) {
+  return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kBytes);
+}
+
 template <typename... P, typename... A>
 cudaError_t launch(void (*kernel)(P...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, A&&... args) {
   cudaLaunchAttribute attr;

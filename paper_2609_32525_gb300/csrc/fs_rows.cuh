@@ -637,6 +637,8 @@ struct Bulk {
   int stages, bytes, per_sm;  // of a stage; blocks that an SM holds (0: not for these rows)
 };
 constexpr int kBulkRows = 16, kBulkStages = 6;
+// Dynamic shared memory of a block where per_sm of them share an SM; the rest is for static arrays.
+constexpr int bulk_room(int per_sm) { return 232448 / per_sm - 2048; }
 
 // kFull: every lane has K vectors of the row: no lane is masked, and no register zeroed for it (from
 // the checkpoint with dres 333 -> 306 us; rows without checkpoint gain nothing).
@@ -974,12 +976,6 @@ __global__ void __launch_bounds__(256, 3) k_norm_fwd_bulk(const RowsArgs args, c
     for (int i = 0; i < plan.stages; i++) tc::mbar_wait_w(&full[i], i < s ? parity ^ 1u : parity, &ab, nullptr);
 }
 
-template <typename Kernel>
-cudaError_t allow_smem(Kernel kernel, size_t bytes) {
-  if (bytes <= 24576) return cudaSuccess;  // with the static arrays within the default limit
-  return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
-}
-
 // ---- choice of the plan ----------------------------------------------------------------------
 
 // Calls f(VE, TPR, K) as integral constants.  A row goes to the fewest threads that hold it in
@@ -1049,7 +1045,7 @@ Bulk bulk_plan(const RowsArgs& a) {
   const int nb = (a.C + kCkptBlock - 1) / kCkptBlock, nd = kBulkRows * a.C * (int)sizeof(T);
   const int bytes = nd * (a.dres ? 2 : 1) + (a.q8 ? kBulkRows * (a.C + nb) : nd);
   for (int per_sm = N <= 8 ? 3 : 2; per_sm >= 2; per_sm--) {
-    const int fit = (232448 / per_sm - 2048) / bytes;
+    const int fit = bulk_room(per_sm) / bytes;
     if (fit < 2) continue;
     const bool many = a.rows >= (int64_t)num_sms() * per_sm * kBulkRows * 32;
     if (N > 8 || VE == 1 || (VE == 8 && fit >= 3 && many)) return {std::min(fit, kBulkStages), bytes, per_sm};
@@ -1080,15 +1076,16 @@ cudaError_t rows_fwd(const RowsArgs& a, cudaStream_t st) {
     // stay with the slots.  At most 256 channels: two stages always fit.
     if constexpr (kNorm && V::value == 1 && L::value == 32 && K::value >= 4) {
       const int bytes = rows::kBulkRows * a.C * (int)sizeof(T) * (a.res ? 2 : 1);
-      const rows::Bulk plan{std::min((232448 / 3 - 2048) / bytes, rows::kBulkStages), bytes, 3};
+      const rows::Bulk plan{std::min(rows::bulk_room(3) / bytes, rows::kBulkStages), bytes, 3};
       auto kernel = rows::k_norm_fwd_bulk<T, K::value>;
       const size_t smem = (size_t)plan.stages * plan.bytes;
-      if (cudaError_t e = rows::allow_smem(kernel, smem)) return e;
+      if (cudaError_t e = allow_smem<rows::bulk_room(3)>(kernel)) return e;
       return launch(kernel, dim3((unsigned)rows::bulk_blocks(a.rows, plan.per_sm)), dim3(256), smem, st, a, plan);
     } else {
       using F = rows::Fwd<T, V::value, L::value, K::value, kNorm>;
       auto kernel = rows::k_rows_fwd<T, V::value, L::value, K::value, kNorm>;
-      if (cudaError_t e = rows::allow_smem(kernel, F::SMEM)) return e;
+      if constexpr (F::SMEM > 24576)  // with the static arrays past the default limit
+        if (cudaError_t e = allow_smem<F::SMEM>(kernel)) return e;
       return launch(kernel, rows::grid_of<V, L, K>(a.rows, rows::kFwdPerSm, 1, 8), dim3(F::THREADS), F::SMEM, st, a);
     }
   });
@@ -1121,7 +1118,7 @@ cudaError_t norm_bwd(const RowsArgs& a, int64_t* blocks, cudaStream_t st) {
         const auto kernel = !a.q8                             ? rows::k_norm_bwd_bulk<T, V::value, K::value, false, false>
                             : kCanBeFull && a.C == 32 * N ? rows::k_norm_bwd_bulk<T, V::value, K::value, true, kCanBeFull>
                                                               : rows::k_norm_bwd_bulk<T, V::value, K::value, true, false>;
-        if (cudaError_t e = rows::allow_smem(kernel, smem)) return e;
+        if (cudaError_t e = allow_smem<rows::bulk_room(2)>(kernel)) return e;  // no plan has fewer blocks an SM
         return launch(kernel, dim3((unsigned)*blocks), dim3(256), smem, st, a, plan);
       }
     }

@@ -973,10 +973,6 @@ __global__ void __launch_bounds__(Tile<D, TG>::kThreads, resident<D, TG>(2))
 }
 
 // ---- launches --------------------------------------------------------------------------------------
-template <typename K>
-cudaError_t allow_smem(K kernel, size_t bytes) {
-  return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
-}
 inline bool many_waves(const Shape& s) { return simt_point_blocks(s) * s.BH() > 3 * num_sms(); }
 inline dim3 point_grid(const Shape& s) { return dim3((unsigned)((s.N + TP - 1) / TP), (unsigned)s.BH()); }
 template <int TG>
@@ -1014,7 +1010,7 @@ cudaError_t SimtTiles<T>::stats(const Shape& s, const T* x, const float* W, cons
     constexpr int D = decltype(d)::value, TG = decltype(tg)::value;
     constexpr size_t sm = tile_bytes<D, TG>(1, 1, 0);
     const auto k = many_waves(s) ? k_tile_stats<D, TG, T, resident_many<D, TG>(3)> : k_tile_stats<D, TG, T, resident<D, TG>(3)>;
-    if (cudaError_t e = allow_smem(k, sm)) return e;
+    if (cudaError_t e = allow_smem<sm>(k)) return e;
     return launch(k, point_grid(s), dim3(Tile<D, TG>::kThreads), sm, st, x, W, bias, tau, lse, s.N, s.H, s.G, reset,
                   status);
   });
@@ -1028,7 +1024,7 @@ cudaError_t SimtTiles<T>::slice(const Shape& s, int P, const T* x, const T* f, c
     constexpr int D = decltype(d)::value, TG = decltype(tg)::value;
     constexpr size_t sm = tile_bytes<D, TG>(2, 1, 1);
     const auto k = k_tile_slice<D, TG, T>;
-    if (cudaError_t e = allow_smem(k, sm)) return e;
+    if (cudaError_t e = allow_smem<sm>(k)) return e;
     return launch(k, slot_grid<TG>(s, P), dim3(Tile<D, TG>::kThreads), sm, st, x, f, W, bias, tau, lse, part, s.N, s.H,
                   s.G, P, reset, status);
   });
@@ -1043,7 +1039,7 @@ cudaError_t SimtTiles<T>::deslice(const Shape& s, const T* x, const float* W, co
     constexpr size_t sm = tile_bytes<D, TG>(1, 2, 1);
     const auto k =
         many_waves(s) ? k_tile_deslice<D, TG, T, resident_many<D, TG>(2)> : k_tile_deslice<D, TG, T, resident<D, TG>(2)>;
-    if (cudaError_t e = allow_smem(k, sm)) return e;
+    if (cudaError_t e = allow_smem<sm>(k)) return e;
     return launch(k, point_grid(s), dim3(Tile<D, TG>::kThreads), sm, st, x, W, bias, tau, zp, lse, out, s.N, s.H, s.G,
                   reset, status);
   });
@@ -1060,12 +1056,12 @@ cudaError_t SimtTiles<T>::backward(const Shape& s, int mode, int P, const T* x, 
       constexpr int MODE = decltype(m)::value, V = MODE == 2 ? 3 : 2;
       constexpr size_t sm = tile_bytes<D, TG>(V, V, 1);
       const auto kp = k_tile_bwd_point<D, TG, T, MODE>;
-      if (cudaError_t e = allow_smem(kp, sm)) return e;
+      if (cudaError_t e = allow_smem<sm>(kp)) return e;
       if (cudaError_t e = launch(kp, point_grid(s), dim3(NT), sm, st, x, dO, fx, W, bias, tau, zp, dUS, lse, dx, dfx,
                                  delta, dt_part, accumulate, s.N, s.H, s.G, reset, status))
         return e;
       const auto ks = k_tile_bwd_slot<D, TG, T, MODE>;
-      if (cudaError_t e = allow_smem(ks, sm)) return e;
+      if (cudaError_t e = allow_smem<sm>(ks)) return e;
       return launch(ks, slot_grid<TG>(s, P), dim3(NT), sm, st, x, dO, fx, W, bias, tau, zp, dUS, lse, delta, part, s.N,
                     s.H, s.G, P);
     };

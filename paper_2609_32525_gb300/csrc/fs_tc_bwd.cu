@@ -1069,7 +1069,7 @@ struct BwdCall {
     if (!make_maps(x, v, f3, &xmap, &vmap, &pmap, &dmap, &fmap)) return cudaErrorInvalidValue;
     const size_t sm = smem_bwd_slot(MODE);
     const auto kernel = k_bwd_slot_tc<MODE, true>;
-    if (cudaError_t e = set_smem(kernel, sm)) return e;
+    if (cudaError_t e = allow_smem<kMaxSmem>(kernel)) return e;
     const int P = bwd_slot_splits(s, MODE);
     return launch(kernel, dim3((unsigned)bwd_slot_blocks(s), (unsigned)P, (unsigned)s.BH()), dim3(kThreads), sm, st,
                   xmap, vmap, pmap, dmap, fmap, ws + L.wimg, ws + L.timg, ws + L.timg2, f(L.part), f(L.dtp), s.N,
@@ -1091,7 +1091,7 @@ struct BwdCall {
     const size_t sm = smem_bwd_dx(r.size, hilo, kComb);
     if (sm > kMaxSmem) return cudaErrorInvalidValue;
     const auto kernel = k_bwd_dx_tc<true, kComb>;
-    if (cudaError_t e = set_smem(kernel, sm)) return e;
+    if (cudaError_t e = allow_smem<kMaxSmem>(kernel)) return e;
     const int P = point_splits(s, (int)s.BH(), r.size / 64);
     for (int k = 0; k < r.n; k++) {
       const int g0 = k * r.size;

@@ -541,10 +541,6 @@ int point_splits(const Shape& s, int units, int blocks) {
 }
 
 constexpr size_t kMaxSmem = 232448;  // opt-in shared memory per block on sm_103
-template <typename K>
-cudaError_t set_smem(K kernel, size_t bytes) {
-  return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
-}
 
 // A call's preparation: jobs are added in any order, run() launches them as one kernel.
 struct Prepare {

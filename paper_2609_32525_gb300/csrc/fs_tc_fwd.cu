@@ -1117,7 +1117,7 @@ cudaError_t run_stats(const Shape& s, const void* x, const void* xr, const uint8
   while (nst > 1 && smem_stats(s.G, split, x3, nst) > kMaxSmem) nst--;
   const size_t sm = smem_stats(s.G, split, x3, nst);
   const auto kernel = x3 ? k_stats<true, true> : (split ? k_stats<true, false> : k_stats<false, false>);
-  cudaError_t e = set_smem(kernel, sm);
+  cudaError_t e = allow_smem<kMaxSmem>(kernel);
   if (e != cudaSuccess) return e;
   return launch(kernel, dim3((unsigned)P, (unsigned)s.BH()), dim3(kStatsThreads), sm, st, xmap, xrmap, wimg, lse,
                 static_cast<uint4*>(px), s.N, padded_n(s), s.H, s.G, P, nst, std::min(nst, kStatsWGs), status);
@@ -1238,7 +1238,7 @@ cudaError_t run_slice(const Shape& s, int G, const void* x, const void* f, const
   dim3 grid((unsigned)R, (unsigned)P, (unsigned)s.BH());
   const size_t sm = smem_slice(x3);
   const auto kernel = x3 ? k_slice<true, true> : (s.dot == FS_DOT_BF16X2 ? k_slice<true, false> : k_slice<false, false>);
-  if ((e = set_smem(kernel, sm)) != cudaSuccess) return e;
+  if ((e = allow_smem<kMaxSmem>(kernel)) != cudaSuccess) return e;
   if ((e = launch(kernel, grid, dim3(kThreads), sm, st, xmap, fmap, pmap, xrmap, frmap, wimg, part, s.N, padded_n(s),
                   s.H, s.G, P, status)) != cudaSuccess) return e;
   Shape so = s;
@@ -1276,7 +1276,7 @@ cudaError_t tc_deslice_fwd(const Shape& s0, const void* x, const float* W, const
   const size_t sm = smem_deslice(xr.size, hilo, 0, ps, x3);
   if (sm > kMaxSmem) return cudaErrorInvalidValue;
   const auto kernel = x3 ? k_deslice<0, true, true> : k_deslice<0, false>;
-  if ((e = set_smem(kernel, sm)) != cudaSuccess) return e;
+  if ((e = allow_smem<kMaxSmem>(kernel)) != cudaSuccess) return e;
   for (int k = 0; k < xr.n; k++) {
     const int g0 = k * xr.size;
     if ((e = launch(kernel, dim3((unsigned)P, (unsigned)s.BH()), dim3(kDesl3Threads), sm, st, xmap,
@@ -1308,7 +1308,7 @@ cudaError_t tc_rows_bwd(const Shape& s, int Gi, int g0, int mode, const void* x,
   const int P = point_splits(s, (int)s.BH(), s.G / 64);
   dim3 grid((unsigned)P, (unsigned)s.BH());
   const auto kernel = mode == 1 ? k_deslice<1, true> : mode == 2 ? k_deslice<2, true> : k_deslice<3, true>;
-  cudaError_t e = set_smem(kernel, sm);
+  cudaError_t e = allow_smem<kMaxSmem>(kernel);
   if (e != cudaSuccess) return e;
   return launch(kernel, grid, dim3(mode == 2 ? kThreads : kDesl3Threads), sm, st, xmap, pmap, xmap,
                 wimg, zimg, zimg2, static_cast<__nv_bfloat16*>(dfx), static_cast<const __nv_bfloat16*>(v),
