@@ -809,9 +809,8 @@ __global__ void __launch_bounds__(256, K * VE <= 8 ? 3 : 2) k_norm_bwd_bulk(cons
 // same arithmetic as k_rows_fwd's, which keeps its own: sharing this made it slower (1,048,576 x 256
 // bf16 188 -> 203 us).
 template <typename T, int K, typename F>
-__device__ __forceinline__ void forward_row(const RowsArgs& a, int64_t row, bool here, int t, bool whole, float invC,
-                                            const Vals<K>& gm, const Vals<K>& bt, RawV<T, 1> (&raw)[K],
-                                            F load_res) {
+__device__ __forceinline__ void forward_row(const RowsArgs& a, int64_t row, int t, bool whole, float invC, const Vals<K>& gm,
+                                            const Vals<K>& bt, RawV<T, 1> (&raw)[K], F load_res) {
   constexpr int P = Vals<K>::P;
   using R = RawV<T, 1>;
   const int C = a.C, nb = (C + kCkptBlock - 1) / kCkptBlock;
@@ -827,7 +826,7 @@ __device__ __forceinline__ void forward_row(const RowsArgs& a, int64_t row, bool
 #pragma unroll
     for (int k = 0; k < K; k++) raw[k] = from_float<T, 1>(*reinterpret_cast<float(*)[1]>(f + k));
     v = vals_of<T, 1, K>(raw);
-    if (a.sum && here) {
+    if (a.sum) {
 #pragma unroll
       for (int k = 0; k < K; k++) {
         const int c = k * 32 + t;
@@ -844,7 +843,7 @@ __device__ __forceinline__ void forward_row(const RowsArgs& a, int64_t row, bool
       uint32_t byte;
       uint8_t q;
       quantise<1>(f + k, byte, q);
-      if (here && c < C) {
+      if (c < C) {
         reinterpret_cast<uint8_t*>(a.q8)[row * C + c] = q;
         if (c % kCkptBlock == 0) a.e8[row * nb + c / kCkptBlock] = (uint8_t)byte;
       }
@@ -874,24 +873,26 @@ __device__ __forceinline__ void forward_row(const RowsArgs& a, int64_t row, bool
 #pragma unroll
   for (int i = 0; i < P; i++) v.p[i] = fma(v.p[i] * r2, gm.p[i], bt.p[i]);
   floats_of(v, f);
-  if (here) {
 #pragma unroll
-    for (int k = 0; k < K; k++) {
-      const int c = k * 32 + t;
-      if (c < C)
-        *reinterpret_cast<R*>(static_cast<T*>(a.y) + row * C + c) =
-            from_float<T, 1>(*reinterpret_cast<float(*)[1]>(f + k));
-    }
-    if (t == 0) {
-      if (a.mean) a.mean[row] = mean;
-      if (a.rstd) a.rstd[row] = rstd;
-    }
+  for (int k = 0; k < K; k++) {
+    const int c = k * 32 + t;
+    if (c < C)
+      *reinterpret_cast<R*>(static_cast<T*>(a.y) + row * C + c) =
+          from_float<T, 1>(*reinterpret_cast<float(*)[1]>(f + k));
+  }
+  if (t == 0) {
+    if (a.mean) a.mean[row] = mean;
+    if (a.rstd) a.rstd[row] = rstd;
   }
 }
 
 // The forward for rows of odd C of one warp each, in the same way: single values are below
-// cp.async's size for bf16, and each took a load, a store and a load.  (No status word here: where
-// a wait gives up the lanes read the rows themselves.)
+// cp.async's size for bf16, and each took a load, a store and a load.
+//
+// No status word here: a warp whose wait gives up (`staged` ends) reads its rows from global memory
+// from then on, and so does the last chunk of fewer rows.  Such a warp waits at no barrier of the
+// stages again, since a wait for the use after one that it has not seen complete would pass at
+// once; and it frees no stage again, so that none is filled anew while a copy may be on its way to it.
 template <typename T, int K>
 __global__ void __launch_bounds__(256, 3) k_norm_fwd_bulk(const RowsArgs args, const Bulk plan) {
   constexpr int RU = kBulkRows / 8;
@@ -915,8 +916,10 @@ __global__ void __launch_bounds__(256, 3) k_norm_fwd_bulk(const RowsArgs args, c
   const bool res = a.res != nullptr;
   const int64_t chunks = (a.rows + kBulkRows - 1) / kBulkRows, first = blockIdx.x, step = gridDim.x;
   const uint32_t nd = (uint32_t)(kBulkRows * C * sizeof(T));
+  int issued = 0;  // by thread 0: chunk number i of the block goes to stage i % plan.stages
   auto issue = [&](int64_t chunk, int s) {
     if ((chunk + 1) * kBulkRows > a.rows) return;  // a last chunk of fewer rows is read by the lanes
+    issued++;
     char* to = stages + (size_t)s * plan.bytes;
     tc::mbar_expect_tx(&full[s], (uint32_t)plan.bytes);
     tc::bulk_load(to, static_cast<const char*>(a.x) + chunk * nd, nd, &full[s]);
@@ -931,49 +934,59 @@ __global__ void __launch_bounds__(256, 3) k_norm_fwd_bulk(const RowsArgs args, c
   const float invC = 1.f / (float)C;
   int s = 0;
   uint32_t parity = 0;
+  bool staged = true;
 #pragma unroll 1
   for (int64_t chunk = first; chunk < chunks; chunk += step) {
     const int64_t ahead = chunk + (plan.stages - 1) * step;
-    if (warp == 0 && ahead < chunks) {
+    if (warp == 0 && staged && ahead < chunks) {
       const int w = s == 0 ? plan.stages - 1 : s - 1;
-      const bool free = chunk == first || tc::mbar_wait_w(&empty[w], s == 0 ? parity ^ 1u : parity, &ab, nullptr);
-      if (free && t == 0) issue(ahead, w);
+      staged = chunk == first || tc::mbar_wait_w(&empty[w], s == 0 ? parity ^ 1u : parity, &ab, nullptr);
+      if (staged && t == 0) issue(ahead, w);
     }
     const int64_t row0 = chunk * kBulkRows + RU * warp;
-    T* x = reinterpret_cast<T*>(stages + (size_t)s * plan.bytes) + RU * warp * C;  // the warp's rows
-    T* r = reinterpret_cast<T*>(reinterpret_cast<char*>(x) + nd);
-    if ((chunk + 1) * kBulkRows > a.rows || !tc::mbar_wait_w(&full[s], parity, &ab, nullptr)) {
-      const int left = (int)max((int64_t)0, min((int64_t)RU, a.rows - row0)) * C;
-#pragma unroll 1
-      for (int i = t; i < left; i += 32) {
-        x[i] = static_cast<const T*>(a.x)[row0 * C + i];
-        if (res) r[i] = static_cast<const T*>(a.res)[row0 * C + i];
+    const T* x = reinterpret_cast<const T*>(stages + (size_t)s * plan.bytes) + RU * warp * C;  // the warp's rows
+    const T* r = reinterpret_cast<const T*>(reinterpret_cast<const char*>(x) + nd);
+    const bool whole = (chunk + 1) * kBulkRows <= a.rows;
+    if (whole && staged) staged = tc::mbar_wait_w(&full[s], parity, &ab, nullptr);
+    if (whole && staged) {
+#pragma unroll
+      for (int u = 0; u < RU; u++) {
+        auto load = [&](R (&to)[K], const T* from) {
+#pragma unroll
+          for (int k = 0; k < K; k++) {
+            const int c = k * 32 + t;
+            to[k] = c < C ? *reinterpret_cast<const R*>(from + u * C + c) : R(0);
+          }
+        };
+        R raw[K];
+        load(raw, x);
+        forward_row<T, K>(a, row0 + u, t, inside, invC, gm, bt, raw, [&](R (&to)[K]) { load(to, r); });
       }
-      __syncwarp();
-    }
+    } else {
+#pragma unroll 1
+      for (int64_t row = row0; row < min(row0 + RU, a.rows); row++) {
+        auto load = [&](R (&to)[K], const void* from) {
 #pragma unroll
-    for (int u = 0; u < RU; u++) {
-      const bool here = row0 + u < a.rows;
-      auto load = [&](R (&to)[K], const T* from) {
-#pragma unroll
-        for (int k = 0; k < K; k++) {
-          const int c = k * 32 + t;
-          to[k] = here && c < C ? *reinterpret_cast<const R*>(from + u * C + c) : R(0);
-        }
-      };
-      R raw[K];
-      load(raw, x);
-      forward_row<T, K>(a, row0 + u, here, t, inside, invC, gm, bt, raw, [&](R (&to)[K]) { load(to, r); });
+          for (int k = 0; k < K; k++) {
+            const int c = k * 32 + t;
+            to[k] = c < C ? *reinterpret_cast<const R*>(static_cast<const T*>(from) + row * C + c) : R(0);
+          }
+        };
+        R raw[K];
+        load(raw, a.x);
+        forward_row<T, K>(a, row, t, inside, invC, gm, bt, raw, [&](R (&to)[K]) { load(to, a.res); });
+      }
     }
     __syncwarp();
-    if (t == 0) tc::mbar_arrive(&empty[s]);
+    if (t == 0 && staged) tc::mbar_arrive(&empty[s]);
     if (++s == plan.stages) {
       s = 0;
       parity ^= 1u;
     }
   }
-  if (ab.flag)  // no copy is left in flight
-    for (int i = 0; i < plan.stages; i++) tc::mbar_wait_w(&full[i], i < s ? parity ^ 1u : parity, &ab, nullptr);
+  if (threadIdx.x == 0 && !staged)  // the block keeps its stages until the copies have landed
+    for (int i = max(0, issued - plan.stages); i < issued; i++)
+      tc::mbar_drain(&full[i % plan.stages], (uint32_t)(i / plan.stages) & 1u);
 }
 
 // ---- choice of the plan ----------------------------------------------------------------------
@@ -1071,8 +1084,8 @@ template <typename T, bool kNorm>
 cudaError_t rows_fwd(const RowsArgs& a, cudaStream_t st) {
   return rows::with_plan<T>(a.C, [&](auto v, auto l, auto k) {
     using V = decltype(v); using L = decltype(l); using K = decltype(k);
-    // The norm of more than 64 channels, odd C: 300,000 rows of bf16 255 287 -> 88 us, with res and
-    // checkpoint 611 -> 235; 101 92 -> 61 and 193 -> 133; 33 channels 50 / 57, the checkpoint alone 74 / 81
+    // The norm of more than 64 channels, odd C: 300,000 rows of bf16 255 287 -> 86 us, with res and
+    // checkpoint 611 -> 225; 101 92 -> 62 and 193 -> 131; 33 channels 50 / 57, the checkpoint alone 74 / 81
     // stay with the slots.  At most 256 channels: two stages always fit.
     if constexpr (kNorm && V::value == 1 && L::value == 32 && K::value >= 4) {
       const int bytes = rows::kBulkRows * a.C * (int)sizeof(T) * (a.res ? 2 : 1);

@@ -88,6 +88,15 @@ __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, Abort*
   }
 }
 
+// Waits for a phase that copies or products on their way complete, before their shared memory or
+// TMEM is given back: whatever the abort flag says, and not past the same limit.
+__device__ __forceinline__ void mbar_drain(uint64_t* bar, uint32_t parity, uint64_t limit_ns = 2000000000ull) {
+  if (mbar_try_wait(bar, parity)) return;
+  const uint64_t t0 = globaltimer();
+  for (uint32_t polls = 0; !mbar_try_wait_sleep(bar, parity, 20000u); polls++)
+    if (polls > kMinPolls && globaltimer() - t0 > limit_ns) return;
+}
+
 // ---- async proxy fences ---------------------------------------------------------------
 __device__ __forceinline__ void fence_proxy_async_smem() {
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
