@@ -530,7 +530,7 @@ __device__ __forceinline__ void block_of(const AttnTcArgs& args, int block, int 
         }
       }
       for (int j = (i > ST ? i - ST : 0); j < i; j++)  // no copy is left in flight
-        mbar_wait(&full[j % ST], (uint32_t)((j / ST) & 1), ab, nullptr);
+        mbar_drain(&full[j % ST], (uint32_t)((j / ST) & 1));
     }
   } else if (warp == 1 || warp == 2) {
     const int w = warp - 1;
@@ -572,7 +572,7 @@ __device__ __forceinline__ void block_of(const AttnTcArgs& args, int block, int 
       mma_commit_w(&done[w]);
     }
     mma_commit_w(&drain[w]);
-    mbar_wait_w(&drain[w], 0, ab, nullptr);
+    mbar_drain_w(&drain[w], 0);
   } else if (warp >= 4) {
     const uint32_t lanes = (uint32_t)(wq * 32) << 16;
     // own rows' parts into TMEM: warpgroup 0 the first operand of S, warpgroup 1 that of dP

@@ -650,6 +650,7 @@ __global__ void __launch_bounds__(256, K * VE <= 8 ? 3 : 2) k_norm_bwd_bulk(cons
   extern __shared__ __align__(128) char stages[];
   __shared__ uint64_t full[kBulkStages], empty[kBulkStages];
   __shared__ tc::Abort ab;
+  __shared__ int issued;  // by thread 0: chunk number i of the block goes to stage i % plan.stages
   RowsArgs a = args;
   const int warp = threadIdx.x >> 5, t = threadIdx.x & 31;
   if (threadIdx.x == 0) {
@@ -658,6 +659,7 @@ __global__ void __launch_bounds__(256, K * VE <= 8 ? 3 : 2) k_norm_bwd_bulk(cons
       tc::mbar_init(&empty[s], 8);
     }
     ab.flag = 0;
+    issued = 0;
     tc::fence_mbar_init();
   }
   __syncthreads();
@@ -672,6 +674,7 @@ __global__ void __launch_bounds__(256, K * VE <= 8 ? 3 : 2) k_norm_bwd_bulk(cons
   const char* src_x = kCkpt ? reinterpret_cast<const char*>(a.q8) : static_cast<const char*>(a.x);
   auto issue = [&](int64_t chunk, int s) {
     if ((chunk + 1) * kBulkRows > a.rows) return;  // a last chunk of fewer rows is read by the lanes
+    issued++;
     char* to = stages + (size_t)s * plan.bytes;
     tc::mbar_expect_tx(&full[s], (uint32_t)plan.bytes);
     tc::bulk_load(to, src_dy + chunk * nd, nd, &full[s]);
@@ -799,8 +802,11 @@ __global__ void __launch_bounds__(256, K * VE <= 8 ? 3 : 2) k_norm_bwd_bulk(cons
       parity ^= 1u;
     }
   }
-  if (ab.flag)  // no copy is left in flight
-    for (int i = 0; i < plan.stages; i++) tc::mbar_wait_w(&full[i], i < s ? parity ^ 1u : parity, &ab, nullptr);
+  // The block keeps its stages until the copies have landed.  (From stage s on: in the order of the
+  // numbers the compiler spills 44 bytes more with single loads, 300,000 x 255 bf16 235 -> 241 us.)
+  if (threadIdx.x == 0 && ab.flag)
+    for (int k = 0, i = s; k < plan.stages; k++, i = i + 1 == plan.stages ? 0 : i + 1)
+      if (i < issued) tc::mbar_drain(&full[i], (uint32_t)((issued - 1 - i) / plan.stages) & 1u);
   __syncthreads();  // the stages are free for the sums
   write_partials<32, VE, N, 256>(a, dg, db, t, reinterpret_cast<float*>(stages));
 }

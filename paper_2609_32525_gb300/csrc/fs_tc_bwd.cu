@@ -387,8 +387,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (MODE == 3) tma_load_3d(st + kBStage, &fmap, h * kD, n0, (int)b, &x_full[s]);
       }
       for (int j = (i > kNSt ? i - kNSt : 0); j < i; j++)
-        mbar_wait(&x_full[j % kNSt], (uint32_t)((j / kNSt) & 1), ab, nullptr, kWaitNs);
-      mbar_wait(w_full, 0, ab, nullptr, kWaitNs);
+        mbar_drain(&x_full[j % kNSt], (uint32_t)((j / kNSt) & 1));
+      mbar_drain(w_full, 0);
     }
   } else if (warp == 1 || (warp == 2 && MODE != 0)) {
     // ------------------------------ logits (warp 1) and dw (warp 2) issuers ------------------------------
@@ -444,7 +444,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       mma_commit_w(&st_empty[stg.i]);
     }
     mma_commit_w(&drain[warp - 1]);
-    mbar_wait_w(&drain[warp - 1], 0, ab, nullptr, kWaitNs);
+    mbar_drain_w(&drain[warp - 1], 0);
   } else if (warp == 3) {
     // ------------------------------ product issuer ------------------------------
     // Units u (half u & 1 of every tile) into accumulator u & 1.
@@ -488,7 +488,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     if (ok) mma_commit_w(acc_full);
     mma_commit_w(&drain[2]);
-    mbar_wait_w(&drain[2], 0, ab, nullptr, kWaitNs);
+    mbar_drain_w(&drain[2], 0);
   } else if (warp >= kSoftmaxWarp0) {
     // ------------------------------ softmax warpgroups ------------------------------
     const int wg = (warp - kSoftmaxWarp0) >> 2;
@@ -755,8 +755,8 @@ __global__ void __launch_bounds__(kDxThreads, 1)
         if (kComb) tma_load_3d(st + kBStage, &fmap, h * kD, n0, (int)b, &x_full[s]);
       }
       for (int j = (i > kDxStages ? i - kDxStages : 0); j < i; j++)
-        mbar_wait(&x_full[j % kDxStages], (uint32_t)((j / kDxStages) & 1), ab, nullptr, kWaitNs);
-      mbar_wait(wz_full, 0, ab, nullptr, kWaitNs);
+        mbar_drain(&x_full[j % kDxStages], (uint32_t)((j / kDxStages) & 1));
+      mbar_drain(wz_full, 0);
     }
   } else if (warp == 1 || warp == 2) {
     // ------------------------------ logits (warp 1) and dw (warp 2) issuers ------------------------------
@@ -797,7 +797,7 @@ __global__ void __launch_bounds__(kDxThreads, 1)
         mma_commit_w(&x_empty[stg.i]);
       }
       mma_commit_w(&drain[warp - 1]);
-      mbar_wait_w(&drain[warp - 1], 0, ab, nullptr, kWaitNs);
+      mbar_drain_w(&drain[warp - 1], 0);
     }
   } else if (warp == 3) {
     // ------------------------------ product issuer ------------------------------
@@ -831,7 +831,7 @@ __global__ void __launch_bounds__(kDxThreads, 1)
         mma_commit_w(&o_full[i % kDxOFull]);
       }
       mma_commit_w(&drain[2]);
-      mbar_wait_w(&drain[2], 0, ab, nullptr, kWaitNs);
+      mbar_drain_w(&drain[2], 0);
     }
   } else {
     const int wg = (warp - kSoftmaxWarp0) >> 2;

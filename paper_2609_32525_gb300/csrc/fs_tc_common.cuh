@@ -30,7 +30,6 @@ constexpr uint32_t kXBytes = kTile * 64;   // 128 points x 32 bf16
 constexpr uint32_t kExBytes = kTile * 32;  // 128 rows x 16 bf16
 constexpr uint32_t kFBlock = kTile * 32;   // 128 points x 16 channels
 constexpr uint32_t kPxBytes = kTile * 16;  // 128 point-extra rows of 8 bf16 (k = 0..7)
-constexpr uint64_t kWaitNs = 2000000000ull;
 
 // ---- operand images written by the prep kernels -------------------------------------------
 // W image for head h (kWRow = 160 bytes per slot): G rows (slots) x 64 B of

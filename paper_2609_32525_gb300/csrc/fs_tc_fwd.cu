@@ -239,8 +239,8 @@ __global__ void __launch_bounds__(desl_wg3<MODE>() ? kDesl3Threads : kThreads, 1
       }
       // Drain: the newest load of each stage has landed before the CTA exits.
       for (int j = (i > ns ? i - ns : 0); j < i; j++)
-        mbar_wait(&x_full[j % ns], (uint32_t)((j / ns) & 1), ab, nullptr, kWaitNs);
-      mbar_wait(wz_full, 0, ab, nullptr, kWaitNs);
+        mbar_drain(&x_full[j % ns], (uint32_t)((j / ns) & 1));
+      mbar_drain(wz_full, 0);
     }
   } else if (warp == 1) {
     // ------------------------------ logits issuer ------------------------------
@@ -271,7 +271,7 @@ __global__ void __launch_bounds__(desl_wg3<MODE>() ? kDesl3Threads : kThreads, 1
         mma_commit_w(&x_empty[st.i]);
       }
       mma_commit_w(&drain[0]);
-      mbar_wait_w(&drain[0], 0, ab, nullptr, kWaitNs);
+      mbar_drain_w(&drain[0], 0);
     }
   } else if (MODE == 3 && warp == 3) {
     // ------------------------------ P x [Z' | T2] issuer ------------------------------
@@ -304,7 +304,7 @@ __global__ void __launch_bounds__(desl_wg3<MODE>() ? kDesl3Threads : kThreads, 1
         mma_commit_w(&o_full[i % kOFull]);
       }
       mma_commit_w(&drain[1]);
-      mbar_wait_w(&drain[1], 0, ab, nullptr, kWaitNs);
+      mbar_drain_w(&drain[1], 0);
     }
   } else if (MODE != 3 && (warp == 2 || warp == 3)) {
     // ------------------------------ P x Z' issuers ------------------------------
@@ -339,7 +339,7 @@ __global__ void __launch_bounds__(desl_wg3<MODE>() ? kDesl3Threads : kThreads, 1
         mma_commit_w(&o_full[i % kOFull]);
       }
       mma_commit_w(&drain[1 + j]);
-      mbar_wait_w(&drain[1 + j], 0, ab, nullptr, kWaitNs);
+      mbar_drain_w(&drain[1 + j], 0);
     }
   } else if (warp >= kSoftmaxWarp0) {
     // ------------------------------ softmax warpgroups ------------------------------
@@ -633,8 +633,8 @@ __global__ void __launch_bounds__(kStatsThreads, 1)
         if (++s == nst) s = 0, pass ^= 1u;
       }
       for (int j = (i > nst ? i - nst : 0); j < i; j++)
-        mbar_wait(&x_full[j % nst], (uint32_t)((j / nst) & 1), ab, nullptr, kWaitNs);
-      mbar_wait(w_full, 0, ab, nullptr, kWaitNs);
+        mbar_drain(&x_full[j % nst], (uint32_t)((j / nst) & 1));
+      mbar_drain(w_full, 0);
     }
   } else if (warp == 1) {
     if (wk.ntiles > 0) {
@@ -667,7 +667,7 @@ __global__ void __launch_bounds__(kStatsThreads, 1)
         if (s0 >= nst) s0 -= nst, pass0 ^= 1u;
       }
       mma_commit_w(drain);
-      mbar_wait_w(drain, 0, ab, nullptr, kWaitNs);
+      mbar_drain_w(drain, 0);
     }
   } else if (warp >= kSoftmaxWarp0) {
     const int wg = (warp - kSoftmaxWarp0) >> 2;
@@ -895,8 +895,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
       }
       for (int j = (i > kSBuft ? i - kSBuft : 0); j < i; j++)
-        mbar_wait(&x_full[j % kSBuft], (uint32_t)((j / kSBuft) & 1), ab, nullptr, kWaitNs);
-      mbar_wait(w_full, 0, ab, nullptr, kWaitNs);
+        mbar_drain(&x_full[j % kSBuft], (uint32_t)((j / kSBuft) & 1));
+      mbar_drain(w_full, 0);
     }
   } else if (warp == 1) {
     // ------------------------------ logits issuer (transposed) ------------------------------
@@ -928,7 +928,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         mma_commit_w(&st_empty[st.i]);
       }
       mma_commit_w(&drain[0]);
-      mbar_wait_w(&drain[0], 0, ab, nullptr, kWaitNs);
+      mbar_drain_w(&drain[0], 0);
     }
   } else if (warp == 2 || warp == 3) {
     // ------------------------------ product issuers ------------------------------
@@ -969,7 +969,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       if (ok) mma_commit_w(acc_full);
       mma_commit_w(&drain[1 + j]);
-      mbar_wait_w(&drain[1 + j], 0, ab, nullptr, kWaitNs);
+      mbar_drain_w(&drain[1 + j], 0);
     }
   } else if (warp >= kSoftmaxWarp0) {
     const int wg = (warp - kSoftmaxWarp0) >> 2;

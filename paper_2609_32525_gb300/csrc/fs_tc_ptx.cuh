@@ -73,8 +73,9 @@ struct Abort {
 // The wall time also runs while a kernel is preempted (a profiler that replays the kernel
 // launched after it, for seconds), so a wait has to have polled kMinPolls times as well.
 constexpr uint32_t kMinPolls = 2000;
+constexpr uint64_t kWaitNs = 2000000000ull;
 __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, Abort* ab, uint32_t* status,
-                                          uint64_t limit_ns = 2000000000ull) {
+                                          uint64_t limit_ns = kWaitNs) {
   if (mbar_try_wait(bar, parity)) return true;
   const uint64_t t0 = globaltimer();
   for (uint32_t polls = 0;; polls++) {
@@ -90,11 +91,11 @@ __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, Abort*
 
 // Waits for a phase that copies or products on their way complete, before their shared memory or
 // TMEM is given back: whatever the abort flag says, and not past the same limit.
-__device__ __forceinline__ void mbar_drain(uint64_t* bar, uint32_t parity, uint64_t limit_ns = 2000000000ull) {
+__device__ __forceinline__ void mbar_drain(uint64_t* bar, uint32_t parity) {
   if (mbar_try_wait(bar, parity)) return;
   const uint64_t t0 = globaltimer();
   for (uint32_t polls = 0; !mbar_try_wait_sleep(bar, parity, 20000u); polls++)
-    if (polls > kMinPolls && globaltimer() - t0 > limit_ns) return;
+    if (polls > kMinPolls && globaltimer() - t0 > kWaitNs) return;
 }
 
 // ---- async proxy fences ---------------------------------------------------------------
@@ -279,8 +280,13 @@ __device__ __forceinline__ void mma_commit_w(uint64_t* bar) {
 // Bounded wait by a whole warp; the outcome is made warp-uniform so that the warp
 // stays converged (a lane that gave up makes the whole warp give up).
 __device__ __forceinline__ bool mbar_wait_w(uint64_t* bar, uint32_t parity, Abort* ab, uint32_t* status,
-                                            uint64_t limit_ns = 2000000000ull) {
+                                            uint64_t limit_ns = kWaitNs) {
   return __all_sync(0xffffffffu, mbar_wait(bar, parity, ab, status, limit_ns));
+}
+
+__device__ __forceinline__ void mbar_drain_w(uint64_t* bar, uint32_t parity) {
+  mbar_drain(bar, parity);
+  __syncwarp();
 }
 
 // Shared-memory matrix descriptor (tcgen05 format) as its two words.
