@@ -29,19 +29,26 @@ AttnPlan attn_plan(int64_t units, int64_t rows, int64_t Gk, int d, bool backward
   if (p.tc) {
     // One block of 128 rows per SM at a time: the split whose waves of blocks cost least, a
     // block's time being its tiles and about two more; ranges of two tiles at least, and no
-    // more tiles than a block lists.
-    const int64_t tiles = (std::max(Gk, backward ? rows : 0) + 63) / 64;
-    const int64_t blocks = units * ((rows + 127) / 128 + (backward ? (Gk + 127) / 128 * (d == 64 ? 2 : 1) : 0));
+    // more tiles than a block lists.  n splits the longer side; the other one is split into ranges
+    // of the same length, so that few keys against the rows of many heads stay whole.  (One count
+    // for both left most dq blocks without a tile, each with a share of dq to write and to add: us,
+    // one count / two, backward at d = 32 of 8 heads that share their keys, 1024 queries x 256 keys
+    // 122 / 25, 2048 x 2048 520 / 110, 8192 x 128 888 / 89.)
+    const int64_t kt = (Gk + 63) / 64, rt = (rows + 63) / 64, tiles = backward ? std::max(kt, rt) : kt;
+    const int64_t blocks_q = units * ((rows + 127) / 128);
+    const int64_t blocks_kv = backward ? units * ((Gk + 127) / 128) * (d == 64 ? 2 : 1) : 0;
     const int64_t least = (tiles * 2 + kAttnTcTiles - 1) / kAttnTcTiles;
     double best = 1e300;
     for (int64_t n = least; n <= std::max<int64_t>(least, std::min<int64_t>(tiles / 2, 32)); n++) {
-      const double t = (double)((blocks * n + sms - 1) / sms) * ((double)((tiles + n - 1) / n) + 2.0);
+      const int64_t of_keys = (n * kt + tiles - 1) / tiles, of_rows = (n * rt + tiles - 1) / tiles;
+      const int64_t blocks = blocks_q * of_keys + blocks_kv * of_rows;
+      const double t = (double)((blocks + sms - 1) / sms) * ((double)((tiles + n - 1) / n) + 2.0);
       if (t < 0.97 * best) {
         best = t;
-        p.splits = (int)n;
+        p.splits = (int)of_keys;
+        if (backward) p.splits_kv = (int)of_rows;
       }
     }
-    if (backward) p.splits_kv = p.splits;
     p.delta = true;
     return p;
   }
