@@ -337,6 +337,11 @@ fs_status fs_attn_bwd(const fs_attn_shape* s, const float* q, const float* k, co
 /* Bytes of scratch on the current device; 0 for an invalid or unsupported shape. */
 size_t fs_attn_workspace_bytes(const fs_attn_shape* s, int backward);
 
+/* Kernel path of fs_attn_fwd, or of fs_attn_bwd (backward != 0), for this shape: 0 = warps of 16
+ * rows, 1 = tcgen05 tiles of 128 rows; -1 for an invalid or unsupported shape.  For tests and
+ * benchmarks. */
+int fs_attn_path_for_shape(const fs_attn_shape* s, int backward);
+
 /* ---- Layer norm and 8-bit checkpoints of point features ----------------------------------
  *
  * The original layer normalises the residual stream before the coupling's projections

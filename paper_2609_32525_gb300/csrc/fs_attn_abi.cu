@@ -168,6 +168,11 @@ size_t fs_attn_workspace_bytes(const fs_attn_shape* s, int backward) {
   return layout(s, backward != 0).total;
 }
 
+int fs_attn_path_for_shape(const fs_attn_shape* s, int backward) {
+  if (!valid(s) || !supported(s)) return -1;
+  return layout(s, backward != 0).plan.tc ? 1 : 0;
+}
+
 fs_status fs_attn_fwd(const fs_attn_shape* s, const float* q, const float* k, const float* v,
                       const fs_attn_mask* mask, float* out, float* lse, void* ws, size_t ws_bytes,
                       fs_stream_t stream) {

@@ -38,7 +38,7 @@ EXPORTED = ("fs_workspace_bytes", "fs_slice_fwd", "fs_slice_finalize", "fs_mix",
             "fs_slice_fwd_noalloc", "fs_slice_fwd_lse", "fs_mix_channels", "fs_mix_channels_bwd", "fs_mix_channels_bwd_add", "fs_stats",
             "fs_coupling_bwd", "fs_coupling_bwd_launch_count", "fs_norm_fwd", "fs_norm_bwd",
             "fs_norm_workspace_bytes", "fs_ckpt_pack", "fs_ckpt_unpack", "fs_attn_fwd", "fs_attn_bwd",
-            "fs_attn_workspace_bytes")
+            "fs_attn_workspace_bytes", "fs_attn_path_for_shape")
 
 
 class fs_shape(ctypes.Structure):
@@ -98,6 +98,7 @@ _sig = {
     "fs_attn_fwd": (_I, [_A, _P, _P, _P, _M, _P, _P, _P, _Z, _P]),
     "fs_attn_bwd": (_I, [_A, _P, _P, _P, _M, _P, _P, _P, _P, _P, _P, _P, _Z, _P]),
     "fs_attn_workspace_bytes": (_Z, [_A, _I]),
+    "fs_attn_path_for_shape": (_I, [_A, _I]),
     "fs_norm_fwd": (_I, [_R] + [_P] * 4 + [_F] + [_P] * 7),
     "fs_norm_bwd": (_I, [_R] + [_P] * 11 + [_I, _P, _Z, _P]),
     "fs_norm_workspace_bytes": (_Z, [_R]),
@@ -366,6 +367,11 @@ def _attn_mask(fn, s, m, dev):
 
 def attn_workspace_bytes(shape: fs_attn_shape, backward=False) -> int:
     return int(_lib.fs_attn_workspace_bytes(ctypes.byref(shape), int(bool(backward))))
+
+
+def attn_path_for_shape(shape: fs_attn_shape, backward=False) -> int:
+    """0: warps; 1: tcgen05."""
+    return int(_lib.fs_attn_path_for_shape(ctypes.byref(shape), int(bool(backward))))
 
 
 def attn_workspace(shape: fs_attn_shape, backward=False, device="cuda") -> torch.Tensor:
