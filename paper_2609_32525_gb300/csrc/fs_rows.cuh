@@ -1047,10 +1047,6 @@ dim3 grid_of(int64_t rows, int per_sm, int ahead, int least) {
 }
 constexpr int kFwdPerSm = 24;  // most blocks of 256 threads per SM: several waves, which even out
 
-}  // namespace rows
-
-namespace rows {
-
 // Stages that fit with three blocks on an SM, or with two; and whether bulk copies are the faster
 // way (us, bulk / rows in registers; r: with dres, q: from the checkpoint):
 //   16 channels a lane, of which registers hold few rows: always.  300,000 rows of bf16, C = 512 r
@@ -1059,6 +1055,15 @@ namespace rows {
 //   8 channels of bf16: with three stages and 32 turns a block.  1,048,576 x 256 274 / 297,
 //     r 349 / 350, rq 306 / 351, q 287 / 302; 20,000 x 256 rq 13.6 / 13.2
 //   else never: fp32 stages are too long.  524,288 x 256 277 / 244, 60,033 x 198 41 / 35
+// Only the kernels that some call reaches are compiled: bulk copies where they may be the faster
+// way, rows in registers where they are not always.
+template <typename T, int VE, int N>
+constexpr bool bulk_always() {
+  if (N <= 8 && VE != 1) return false;
+  return bulk_room(2) / (kBulkRows * 32 * N * (int)sizeof(T) * 3) >= 2;  // two stages of the widest rows, dy, dres and v
+}
+template <typename T, int VE, int N>
+constexpr bool bulk_ever() { return N > 8 || VE == 1 || VE == 8; }
 template <typename T, int VE, int N>
 Bulk bulk_plan(const RowsArgs& a) {
   const int nb = (a.C + kCkptBlock - 1) / kCkptBlock, nd = kBulkRows * a.C * (int)sizeof(T);
@@ -1067,7 +1072,7 @@ Bulk bulk_plan(const RowsArgs& a) {
     const int fit = bulk_room(per_sm) / bytes;
     if (fit < 2) continue;
     const bool many = a.rows >= (int64_t)num_sms() * per_sm * kBulkRows * 32;
-    if (N > 8 || VE == 1 || (VE == 8 && fit >= 3 && many)) return {std::min(fit, kBulkStages), bytes, per_sm};
+    if (N > 8 || VE == 1 || (fit >= 3 && many)) return {std::min(fit, kBulkStages), bytes, per_sm};
     break;
   }
   return {};
@@ -1128,7 +1133,7 @@ cudaError_t norm_bwd(const RowsArgs& a, int64_t* blocks, cudaStream_t st) {
   return rows::with_plan<T>(a.C, [&](auto v, auto l, auto k) {
     using V = decltype(v); using L = decltype(l); using K = decltype(k);
     constexpr int N = V::value * K::value;
-    if constexpr (L::value == 32) {
+    if constexpr (L::value == 32 && rows::bulk_ever<T, V::value, N>()) {
       const rows::Bulk plan = rows::bulk_plan<T, V::value, N>(a);
       if (plan.per_sm) {
         *blocks = rows::bulk_blocks(a.rows, plan.per_sm);
@@ -1141,11 +1146,15 @@ cudaError_t norm_bwd(const RowsArgs& a, int64_t* blocks, cudaStream_t st) {
         return launch(kernel, dim3((unsigned)*blocks), dim3(256), smem, st, a, plan);
       }
     }
-    const dim3 grid = rows::grid_of<V, L, K>(a.rows, 9, rows::rows_ahead<K::value>(), 16);
-    const dim3 block(rows::block_threads<L::value>());
-    *blocks = grid.x;
-    return a.q8 ? launch(rows::k_norm_bwd<T, V::value, L::value, K::value, true>, grid, block, 0, st, a)
-                : launch(rows::k_norm_bwd<T, V::value, L::value, K::value, false>, grid, block, 0, st, a);
+    if constexpr (L::value == 32 && rows::bulk_always<T, V::value, N>()) {
+      return cudaErrorInvalidValue;  // the plan above was not empty
+    } else {
+      const dim3 grid = rows::grid_of<V, L, K>(a.rows, 9, rows::rows_ahead<K::value>(), 16);
+      const dim3 block(rows::block_threads<L::value>());
+      *blocks = grid.x;
+      return a.q8 ? launch(rows::k_norm_bwd<T, V::value, L::value, K::value, true>, grid, block, 0, st, a)
+                  : launch(rows::k_norm_bwd<T, V::value, L::value, K::value, false>, grid, block, 0, st, a);
+    }
   });
 }
 
