@@ -352,9 +352,10 @@ int fs_attn_path_for_shape(const fs_attn_shape* s, int backward);
  *
  * An 8-bit checkpoint of x [rows, C] is q8 [rows, C] (int8) with e8 [rows, ceil(C / 32)]
  * (uint8): each block of 32 channels of a row (the last one may be shorter) is kept as
- * x ~ q 2^s with e8 = s + 127, where s >= -126 is the smallest that brings the block's
- * largest magnitude to at most 127; q is rounded to nearest, ties to even, so each value is
- * off by at most half a step, 2^(s-1) <= 2^-6.99 of the block's largest magnitude (or 2^-127).
+ * x ~ q 2^s with e8 = s + 127; q is x 2^-s rounded to nearest, ties to even, and s is the
+ * smallest >= -126 at which the ROUNDED largest magnitude of the block is at most 127 (so up to
+ * just below 127.5 steps).  Each value is off by at most half a step, 2^(s-1), which is at most
+ * 1/127.5 = 2^-6.994 of the block's largest magnitude (where s is -126: 2^-127).
  * A block that holds NaN or infinity has e8 = 255 and restores to NaN.  The values are exact
  * in both dtypes.
  *

@@ -46,7 +46,7 @@ def pack(x):
             if not np.isfinite(f).all():
                 e[r, b] = 255
                 continue
-            s = -126  # the smallest exponent that brings every magnitude to at most 127
+            s = -126  # the smallest exponent at which every rounded magnitude is at most 127
             if np.abs(f).max() > 0:
                 s = max(s, int(np.frexp(np.abs(f).max())[1]) - 8)
             while np.abs(np.rint(np.ldexp(f, -s))).max() > 127:

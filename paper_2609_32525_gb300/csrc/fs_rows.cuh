@@ -4,10 +4,11 @@
 //              rstd = 1 / sqrt(var + eps)
 //   backward   xh = (v - mean) rstd, g = dy gamma:
 //              dv = rstd (g - avg(g) - xh avg(g xh)) + dres;  dgamma = sum dy xh, dbeta = sum dy
-//   checkpoint blocks of 32 channels: v ~ q 2^s, q whole in [-127, 127], s the smallest that
-//              brings the block's largest magnitude to 127; the byte s + 127 is kept, 255 for a
-//              block with NaN or infinity.  2^s scales exactly, so that the only rounding is
-//              q's (half a step, at most 2^-7 of the block's largest magnitude).
+//   checkpoint blocks of 32 channels: v ~ q 2^s, q = v 2^-s rounded, s the smallest >= -126 at
+//              which the block's largest magnitude rounds to at most 127; the byte s + 127 is
+//              kept, 255 for a block with NaN or infinity.  2^s scales exactly, so that the only
+//              rounding is q's: half a step, at most 1/127.5 = 2^-6.994 of the block's largest
+//              magnitude (which is 63.75 steps at least: 127.5 of the next smaller ones round up).
 //
 // Every pass reads each input once and writes each output once: a row lies in the registers of
 // its threads between its sums and its outputs, so memory bandwidth bounds all of them.  Sums
