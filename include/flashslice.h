@@ -307,8 +307,9 @@ typedef struct fs_attn_shape {
   int32_t Gk;   /* keys per head */
   int32_t d;    /* head width, 16, 32 or 64 */
   int32_t mask; /* fs_mask */
-  float scale;  /* finite */
-  float cap;    /* >= 0; 0: scores are not capped */
+  float scale;  /* finite, as is scale log2(e) */
+  float cap;    /* >= 0; 0: scores are not capped.  scale / cap is finite, and so is cap log2(e)
+                 * unless |scale / cap| < 2^-126, where a cap has no effect and is not applied */
 } fs_attn_shape;
 
 /* Device pointers, 4-byte aligned, each may be NULL; the struct itself is read on the host

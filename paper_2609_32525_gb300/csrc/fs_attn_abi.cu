@@ -5,6 +5,7 @@
 #include "fs_check.h"
 #include "fs_internal.h"
 
+#include <cfloat>
 #include <cmath>
 
 namespace fs {
@@ -13,13 +14,21 @@ namespace {
 constexpr size_t kAlign = 256;
 constexpr int64_t kMostTokens = 1 << 20;
 
+// The cap as the kernels apply it, cap tanh(q.k scale / cap): not at all where scale / cap is below
+// fp32's normal range, whose few bits would round every score.  There tanh(x) is x (to 2^-25 of it
+// for products up to 2^114), and c is s.
+float applied_cap(const fs_attn_shape* s) {
+  return s->cap > 0.f && std::fabs(s->scale / s->cap) < FLT_MIN ? 0.f : s->cap;
+}
 bool valid(const fs_attn_shape* s) {
   if (!s || s->B < 1 || s->H < 1 || s->Hkv < 1 || s->Gq < 1 || s->Gk < 1 || s->d < 1) return false;
   if (s->H % s->Hkv != 0) return false;
   if (s->mask != FS_MASK_NONE && s->mask != FS_MASK_PREFIX) return false;
   if (s->mask == FS_MASK_PREFIX && s->Gq > s->Gk) return false;
   if (!std::isfinite(s->scale) || !(s->cap >= 0.f) || !std::isfinite(s->cap)) return false;
-  if (s->cap > 0.f && !std::isfinite(s->scale / s->cap)) return false;  // the kernels' factor
+  // the kernels' factors
+  const float cap = applied_cap(s);
+  if (!std::isfinite(cap > 0.f ? s->scale / cap : s->scale * kLog2e) || !std::isfinite(cap * kLog2e)) return false;
   const double most = (double)s->B * s->H * (double)(s->Gq > s->Gk ? s->Gq : s->Gk) * s->d;
   return most < 1099511627776.0;  // 2^40
 }
@@ -121,7 +130,7 @@ AttnArgs args_of(const fs_attn_shape* s, const fs_attn_mask& m, const float* q, 
   a.rows = (int)n.rows; a.units = (int)n.units;
   a.causal = s->mask == FS_MASK_PREFIX;
   a.warps = p.warps; a.splits = p.splits; a.splits_kv = p.splits_kv;
-  a.scale = s->scale; a.cap = s->cap;
+  a.scale = s->scale; a.cap = applied_cap(s);
   a.status = static_cast<uint32_t*>(ws);
   a.part = at(ws, l.part);
   if (backward) {
