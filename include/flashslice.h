@@ -293,7 +293,9 @@ fs_status fs_coupling_bwd(const fs_shape* s, const void* x_mid, const void* fx,
  *
  * Everything is fp32: [B, H, Gq, d] for q, out, dout, dq; [B, Hkv, Gk, d] for k, v, dk, dv;
  * lse [B, H, Gq].  The products run on the tensor cores with every operand split into two
- * tf32 parts (2^-22 relative), accumulation is fp32.  Hkv divides H; heads that share a key
+ * tf32 parts (2^-22 relative, where an fp32 product rounds by 2^-24), the exponential is the
+ * hardware's 2^x (2^-22 relative), accumulation is fp32.  A pair whose weight
+ * underflows to 0 adds nothing, whatever its tokens hold.  Hkv divides H; heads that share a key
  * head have their dk and dv summed.  Supported: d in {16, 32, 64}; Gk and (H / Hkv) Gq up to
  * 2^20; B*H <= 65535; B*H*max(Gq, Gk)*d < 2^40.  No output may share a byte with an input or
  * another output (FS_ERR_INVALID). */

@@ -23,6 +23,8 @@ __device__ __forceinline__ Split split(float x) {
   return {h, __float_as_uint(x - __uint_as_float(h))};
 }
 
+// The hardware's 2^x, 2^-22 relative: as much as the rounding of x costs from |x| = 6 on.  Below
+// 2^-126 it is 0.
 __device__ __forceinline__ float exp2_fast(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
