@@ -1048,14 +1048,6 @@ dim3 grid_of(int64_t rows, int per_sm, int ahead, int least) {
 }
 constexpr int kFwdPerSm = 24;  // most blocks of 256 threads per SM: several waves, which even out
 
-// Stages that fit with three blocks on an SM, or with two; and whether bulk copies are the faster
-// way (us, bulk / rows in registers; r: with dres, q: from the checkpoint):
-//   16 channels a lane, of which registers hold few rows: always.  300,000 rows of bf16, C = 512 r
-//     183 / 269, 384 rq 149 / 240, with vectors of two 300 rq 214 / 330
-//   odd C, single loads: always.  300,000 x 101 bf16 77 / 110, fp32 r 91 / 102
-//   8 channels of bf16: with three stages and 32 turns a block.  1,048,576 x 256 274 / 297,
-//     r 349 / 350, rq 306 / 351, q 287 / 302; 20,000 x 256 rq 13.6 / 13.2
-//   else never: fp32 stages are too long.  524,288 x 256 277 / 244, 60,033 x 198 41 / 35
 // Only the kernels that some call reaches are compiled: bulk copies where they may be the faster
 // way, rows in registers where they are not always.
 template <typename T, int VE, int N>
@@ -1065,6 +1057,15 @@ constexpr bool bulk_always() {
 }
 template <typename T, int VE, int N>
 constexpr bool bulk_ever() { return N > 8 || VE == 1 || VE == 8; }
+
+// Stages that fit with three blocks on an SM, or with two; and whether bulk copies are the faster
+// way (us, bulk / rows in registers; r: with dres, q: from the checkpoint):
+//   16 channels a lane, of which registers hold few rows: always.  300,000 rows of bf16, C = 512 r
+//     183 / 269, 384 rq 149 / 240, with vectors of two 300 rq 214 / 330
+//   odd C, single loads: always.  300,000 x 101 bf16 77 / 110, fp32 r 91 / 102
+//   8 channels of bf16: with three stages and 32 turns a block.  1,048,576 x 256 274 / 297,
+//     r 349 / 350, rq 306 / 351, q 287 / 302; 20,000 x 256 rq 13.6 / 13.2
+//   else never: fp32 stages are too long.  524,288 x 256 277 / 244, 60,033 x 198 41 / 35
 template <typename T, int VE, int N>
 Bulk bulk_plan(const RowsArgs& a) {
   const int nb = (a.C + kCkptBlock - 1) / kCkptBlock, nd = kBulkRows * a.C * (int)sizeof(T);
