@@ -405,6 +405,78 @@ fs_status fs_ckpt_pack(const fs_rows* s, const void* x, int8_t* q8, uint8_t* e8,
 fs_status fs_ckpt_unpack(const fs_rows* s, const int8_t* q8, const uint8_t* e8, void* x,
                          fs_stream_t stream);
 
+/* ---- Linear maps of rows, and dropout -----------------------------------------------------
+ *
+ * Around the coupling, the original layer (Sec. 2 "The Transolver layer") projects the normalised
+ * stream to x_mid and fx, projects the coupling's output back and adds it to the stream, and ends
+ * with a two-layer MLP, dropout behind each.  One call does a product with all that follows it:
+ *   u = x W^T + bias,   y = res + drop(act(u))
+ *   x [rows, Cin], res, y [rows, Cout] in the dtype; W [Cout, Cin] in the dtype; bias [Cout] fp32.
+ *   pre: NULL, or receives u (rounded to the dtype), which the backward of an activation needs.
+ *   bias, res: NULL for none.  res may be y itself (the stream in place).
+ * Activations: NONE; RELU; GELU u Phi(u), Phi the normal distribution's function; SILU u / (1 + e^-u).
+ *
+ * Dropout: drop(a) = a / (1 - p) where the value is kept, 0 where it is not (what it holds, NaN and
+ * infinities included, is not looked at).  p in [0, 1); 0: none, rng may be NULL.  The mask is
+ * never stored: channel c of row r is kept if word c % 4 of Philox 4x32-10 (Salmon et al., 2011),
+ * with the key rng[0] and the 128-bit counter (r ceil(C / 4) + c / 4) + 2^64 rng[1], is at least
+ * floor(p 2^32); C: the row's channels.  rng: two 64-bit words {seed, offset} in DEVICE memory, so
+ * that a captured graph draws anew when the caller advances the offset.  A call whose backward
+ * shall see its mask gets the same two words there; calls that shall not share a mask (another
+ * layer, another step) get different offsets.
+ *
+ * Sums are fp32.  FS_BF16: products of bf16 values, exact; GELU and SILU to 2^-12 of themselves
+ * (for u > -5; below, where |gelu| < 2e-6, to 2e-7), y, pre and dx rounded to bf16.  FS_F32: fp32
+ * throughout, sums of products to a few 2^-24 of their terms' magnitudes.  An infinity or NaN in
+ * x, W or g makes results that it enters non-finite, and no others.
+ *
+ * Supported: rows >= 1; Cin, Cout in [1, 8192]; rows*max(Cin, Cout) < 2^40.  No output may share a
+ * byte with an input or another output, except where a call says so (FS_ERR_INVALID). */
+typedef enum fs_act { FS_ACT_NONE = 0, FS_ACT_RELU = 1, FS_ACT_GELU = 2, FS_ACT_SILU = 3 } fs_act;
+
+typedef struct fs_linear {
+  int64_t rows;  /* >= 1 */
+  int32_t Cin;   /* channels of x, 1..8192 */
+  int32_t Cout;  /* channels of y, 1..8192 */
+  int32_t dtype; /* fs_dtype of x, W, y */
+} fs_linear;
+
+/* ws: fs_linear_workspace_bytes(s, 0). */
+fs_status fs_linear_fwd(const fs_linear* s, const void* x, const void* W, const float* bias, int act, float p,
+                        const uint64_t* rng, const void* res, void* y, void* pre, void* ws, size_t ws_bytes,
+                        fs_stream_t stream);
+
+/* Gradients given g [rows, Cout], the gradient of u:
+ *   dx = drop'(g W) act'(pre) + dres,   dW = g^T x,   dbias = sum_rows g
+ *   act, p, rng, pre [rows, Cin]: those of the call that made x (y there), so that dx is the
+ *   gradient of ITS u, ready for its own backward; FS_ACT_NONE, 0, NULL, NULL where x came from
+ *   elsewhere.  drop' keeps what that call's dropout kept, times 1 / (1 - p).
+ *   dres: NULL, or a gradient that reaches x along another way; may be dx itself.
+ *   A layer's own residual takes the gradient of y as it is; where the call that made y had an
+ *   activation or dropout, fs_dropout_bwd makes g from the gradient of y.
+ *   dx: NULL to leave it out (W is then not read).  dW, dbias (fp32): NULL to leave them out
+ *   (dbias only with dW), else written (accumulate == 0) or added to (accumulate != 0).
+ * ws: fs_linear_workspace_bytes(s, 1). */
+fs_status fs_linear_bwd(const fs_linear* s, const void* x, const void* W, const void* g, int act, float p,
+                        const uint64_t* rng, const void* pre, const void* dres, void* dx, float* dW, float* dbias,
+                        int accumulate, void* ws, size_t ws_bytes, fs_stream_t stream);
+
+/* Bytes of scratch on the current device; 0 for an invalid or unsupported shape. */
+size_t fs_linear_workspace_bytes(const fs_linear* s, int backward);
+
+/* Kernel path of fs_linear_fwd, or of fs_linear_bwd's dx (backward != 0), for this shape: 0 = fp32
+ * multiply-adds, 1 = tcgen05; -1 for an invalid or unsupported shape.  For tests and benchmarks. */
+int fs_linear_path_for_shape(const fs_linear* s, int backward);
+
+/* Dropout alone: y = res + drop(act(x)) over rows of C channels.  res: NULL for none; y may be x or
+ * res. */
+fs_status fs_dropout_fwd(const fs_rows* s, const void* x, int act, float p, const uint64_t* rng, const void* res, void* y,
+                         fs_stream_t stream);
+/* Its backward: dx = drop'(dy) act'(pre), pre what the activation saw (not read, and may be NULL, for
+ * FS_ACT_NONE).  dx may be dy or pre. */
+fs_status fs_dropout_bwd(const fs_rows* s, const void* dy, int act, float p, const uint64_t* rng, const void* pre,
+                         void* dx, fs_stream_t stream);
+
 /* Fixed-scratch variant of fs_slice_fwd.  The paper has no counterpart.
  *
  * For callers that cannot give the library device memory at the call site: a

@@ -148,3 +148,72 @@ def attention_coupling(x_mid, fx, W_slice, bias, tau, Wq, Wk, Wv, scale, cap=0.0
     sb = fso.slice_bwd(x_mid, fx, W_slice, bias, tau, z, s["wsum"], dz, eps)
     res.update({n: dd[n] + sb[n] for n in ("dx_mid", "dW", "dbias", "dtau")}, dfx=sb["dfx"])
     return res
+
+
+def activation(name, u):
+    """act(u) and act'(u)."""
+    from scipy.special import erfc, expit
+
+    u = np.asarray(u, np.float64)
+    if name == "relu":
+        return np.where(u < 0, 0.0, u), np.where(np.isnan(u), u, u > 0)
+    if name == "gelu":
+        with np.errstate(all="ignore"):
+            cdf = 0.5 * erfc(-u / np.sqrt(2.0))
+            a = np.where(u == -np.inf, 0.0, u * cdf)
+            return a, cdf + np.where(np.isinf(u), 0.0, u * np.exp(-0.5 * u * u)) / np.sqrt(2.0 * np.pi)
+    if name == "silu":
+        s = expit(u)
+        with np.errstate(all="ignore"):
+            return np.where(u == -np.inf, 0.0, u * s), s * (1.0 + np.where(np.isinf(u), 0.0, u * expit(-u)))
+    return u, np.ones_like(u)
+
+
+def philox(counter, key):
+    """Philox 4x32-10 (Salmon, Moraes, Dror, Shaw, 2011) of counters [..., 4] of 32-bit words under
+    the key (k0, k1)."""
+    c = [np.asarray(counter, np.uint64)[..., i] for i in range(4)]
+    low, (k0, k1) = np.uint64(0xFFFFFFFF), (int(k) for k in key)
+    for _ in range(10):
+        p, q = c[0] * np.uint64(0xD2511F53), c[2] * np.uint64(0xCD9E8D57)
+        c = [(q >> np.uint64(32)) ^ c[1] ^ np.uint64(k0), q & low, (p >> np.uint64(32)) ^ c[3] ^ np.uint64(k1), p & low]
+        k0, k1 = (k0 + 0x9E3779B9) & 0xFFFFFFFF, (k1 + 0xBB67AE85) & 0xFFFFFFFF
+    return np.stack(c, -1).astype(np.uint32)
+
+
+def kept(R, C, p, seed, offset):
+    """[R, C] truth values: what a dropout of rate p (an fp32 value) keeps."""
+    quads = -(-C // 4)
+    n = np.arange(R * quads, dtype=np.uint64)
+    at = np.empty((R * quads, 4), np.uint64)
+    at[:, 0], at[:, 1] = n & np.uint64(0xFFFFFFFF), n >> np.uint64(32)
+    at[:, 2], at[:, 3] = offset & 0xFFFFFFFF, offset >> 32
+    w = philox(at, (seed & 0xFFFFFFFF, seed >> 32)).reshape(R, 4 * quads)[:, :C]
+    return w >= int(float(np.float32(p)) * 2.0 ** 32)
+
+
+def dropout(a, p, seed=0, offset=0):
+    if not p:
+        return np.asarray(a, np.float64)
+    return np.where(kept(*np.shape(a), p, seed, offset), np.asarray(a, np.float64) / (1.0 - float(np.float32(p))), 0.0)
+
+
+def linear(x, W, bias=None, act="none", p=0.0, seed=0, offset=0, res=None):
+    """y = res + drop(act(u)), and u = x W^T + bias."""
+    u = np.asarray(x, np.float64) @ np.asarray(W, np.float64).T
+    if bias is not None:
+        u = u + np.asarray(bias, np.float64)
+    y = dropout(activation(act, u)[0], p, seed, offset)
+    return (y if res is None else y + np.asarray(res, np.float64)), u
+
+
+def linear_bwd(x, W, g, act="none", p=0.0, seed=0, offset=0, pre=None, dres=None):
+    """dx, dW, dbias for g, the gradient of u; act, p, seed, offset, pre: of the call that made x."""
+    g = np.asarray(g, np.float64)
+    d = g @ np.asarray(W, np.float64)
+    if act != "none":
+        d = d * activation(act, pre)[1]
+    d = dropout(d, p, seed, offset)
+    if dres is not None:
+        d = d + np.asarray(dres, np.float64)
+    return d, g.T @ np.asarray(x, np.float64), g.sum(0)

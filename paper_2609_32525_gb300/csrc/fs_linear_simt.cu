@@ -1,0 +1,201 @@
+// Linear maps in fp32 multiply-adds, for sizes that fill no tensor-core tiles and for rows that TMA
+// cannot address, and the fixed-order join of products whose sums were split.
+//
+// A block owns 64 x 64 values of D and runs over the sum in steps of 16, which it stages in shared
+// memory two deep; a thread owns 4 x 4 values, so that four neighbouring channels, which share a
+// dropout counter, are in one thread.  Sums are added up over 128 terms at a time and these added
+// in turn: a chain of 8192 terms then rounds like one of 128 and one of 64.
+#include "fs_launch.h"
+#include "fs_linear_end.cuh"
+
+#include <algorithm>
+
+namespace fs {
+namespace {
+
+constexpr int kT = 64, kK = 16, kPitch = kT + 4;
+
+struct SimtArgs {
+  const void *a, *b;
+  int64_t M, K, per;
+  int N, splits, ld;
+  float *part, *part_sums;
+  uint32_t* status;  // to clear, or null
+  LinearEnd e;
+};
+
+template <typename T, int OP>
+__global__ void __launch_bounds__(256) k_linear_simt(SimtArgs a) {
+  __shared__ __align__(16) float As[2][kK][kPitch], Bs[2][kK][kPitch];
+  const int64_t zero = grid_begin();
+  const T* A = static_cast<const T*>(a.a) + zero;
+  const T* B = static_cast<const T*>(a.b) + zero;
+  const int t = threadIdx.x, tx = t & 15, ty = t >> 4;
+  if (a.status && t == 0 && (blockIdx.x | blockIdx.y | blockIdx.z) == 0) *a.status = 0;
+  const int64_t m0 = (int64_t)blockIdx.x * kT;
+  const int n0 = blockIdx.y * kT;
+  const int64_t k0 = (int64_t)blockIdx.z * a.per, k1 = k0 + a.per < a.K ? k0 + a.per : a.K;
+  // A: x and g have their channels (k) next to each other, g transposed its m; B: W has its k next
+  // to each other in the forward product, its n in dx, and x transposed its n.
+  constexpr bool kAk = OP != kLinDw, kBk = OP == kLinFwd;
+  const int64_t lda = kAk ? a.K : a.M, ldb = kBk ? a.K : a.N;
+  float ra[4], rb[4];
+  auto fetch = [&](int64_t k) {
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+      const int kk = kAk ? t & 15 : (t >> 6) + 4 * i, m = kAk ? (t >> 4) + 16 * i : t & 63;
+      const bool in = k + kk < k1 && m0 + m < a.M;
+      ra[i] = in ? (float)(kAk ? A[(m0 + m) * lda + k + kk] : A[(k + kk) * lda + m0 + m]) : 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+      const int kk = kBk ? t & 15 : (t >> 6) + 4 * i, n = kBk ? (t >> 4) + 16 * i : t & 63;
+      const bool in = k + kk < k1 && n0 + n < a.N;
+      rb[i] = in ? (float)(kBk ? B[(int64_t)(n0 + n) * ldb + k + kk] : B[(k + kk) * ldb + n0 + n]) : 0.f;
+    }
+  };
+  auto put = [&](int s) {
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+      As[s][kAk ? t & 15 : (t >> 6) + 4 * i][kAk ? (t >> 4) + 16 * i : t & 63] = ra[i];
+      Bs[s][kBk ? t & 15 : (t >> 6) + 4 * i][kBk ? (t >> 4) + 16 * i : t & 63] = rb[i];
+    }
+  };
+  float acc[4][4] = {}, sub[4][4] = {}, sum[4] = {}, sub_sum[4] = {};
+  fetch(k0);
+  put(0);
+  int s = 0, step = 0;
+  for (int64_t k = k0; k < k1; k += kK) {
+    __syncthreads();
+    if (k + kK < k1) fetch(k + kK);
+#pragma unroll
+    for (int kk = 0; kk < kK; kk++) {
+      const float4 x = *reinterpret_cast<const float4*>(&As[s][kk][ty * 4]);
+      const float4 y = *reinterpret_cast<const float4*>(&Bs[s][kk][tx * 4]);
+      const float xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+      for (int i = 0; i < 4; i++) {
+#pragma unroll
+        for (int j = 0; j < 4; j++) sub[i][j] = fmaf(xs[i], ys[j], sub[i][j]);
+        if (OP == kLinDw) sub_sum[i] += xs[i];
+      }
+    }
+    s ^= 1;
+    if (k + kK < k1) put(s);
+    if ((++step & 7) == 0 || k + kK >= k1) {
+#pragma unroll
+      for (int i = 0; i < 4; i++) {
+#pragma unroll
+        for (int j = 0; j < 4; j++) acc[i][j] += sub[i][j], sub[i][j] = 0.f;
+        sum[i] += sub_sum[i], sub_sum[i] = 0.f;
+      }
+    }
+  }
+  const int col = n0 + tx * 4;
+  const act::DropKey key = lin::drop_key(a.e);
+#pragma unroll
+  for (int i = 0; i < 4; i++) {
+    const int64_t m = m0 + ty * 4 + i;
+    if (m >= a.M) break;
+    if (OP == kLinDw && a.e.sums && blockIdx.y == 0 && tx == 0) {
+      if (a.splits > 1) a.part_sums[(int64_t)blockIdx.z * a.M + m] = sum[i];
+      else lin::end_sum(a.e, m, sum[i]);
+    }
+    if (col >= a.N) continue;
+    if (a.splits > 1)
+      *reinterpret_cast<float4*>(a.part + ((int64_t)blockIdx.z * a.M + m) * a.ld + col) =
+          make_float4(acc[i][0], acc[i][1], acc[i][2], acc[i][3]);
+    else
+      lin::end4<T, OP>(a.e, key, m, col, a.N, acc[i]);
+  }
+}
+
+// 32 quads of columns a block; eight threads share a quad's parts (thread y takes parts y, y + 8, ...),
+// and their sums are added in order.  What counts is how many loads are on their way.
+template <typename T, int OP>
+__global__ void __launch_bounds__(256) k_linear_join(int64_t M, int N, int ld, int splits, const float* __restrict__ part,
+                                                      const float* __restrict__ part_sums, LinearEnd e) {
+  __shared__ float4 sm[8][33];
+  grid_begin(part, part_sums);
+  const int64_t quads = M * (ld >> 2), i = (int64_t)blockIdx.x * 32 + threadIdx.x;
+  const bool tail = i >= quads;  // dbias
+  const int64_t m4 = (i - quads) * 4;
+  float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (!tail) {
+#pragma unroll 4
+    for (int p = threadIdx.y; p < splits; p += 8) {
+      const float4 v = reinterpret_cast<const float4*>(part)[(int64_t)p * quads + i];
+      s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
+    }
+  } else if (OP == kLinDw && e.sums && m4 < M) {
+    float v[4];
+    for (int p = threadIdx.y; p < splits; p += 8) {
+      act::load4(part_sums + (int64_t)p * M + m4, (int)(M - m4 < 4 ? M - m4 : 4), (M & 3) == 0, v);
+      s.x += v[0], s.y += v[1], s.z += v[2], s.w += v[3];
+    }
+  }
+  sm[threadIdx.y][threadIdx.x] = s;
+  __syncthreads();
+  if (threadIdx.y != 0) return;
+#pragma unroll
+  for (int y = 1; y < 8; y++) {
+    const float4 v = sm[y][threadIdx.x];
+    s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
+  }
+  float v[4] = {s.x, s.y, s.z, s.w};
+  if (tail) {
+    if (OP == kLinDw && e.sums)
+#pragma unroll
+      for (int j = 0; j < 4; j++)
+        if (m4 + j < M) lin::end_sum(e, m4 + j, v[j]);
+    return;
+  }
+  const int64_t row = i / (ld >> 2);
+  lin::end4<T, OP>(e, lin::drop_key(e), row, (int)(i - row * (ld >> 2)) * 4, N, v);
+}
+
+template <typename T, int OP>
+cudaError_t run_simt(const LinearProblem& p, const LinearPlan& plan, const LinearEnd& e, void* scratch, cudaStream_t st) {
+  SimtArgs a{};
+  a.a = p.a; a.b = p.b; a.M = p.M; a.N = p.N; a.K = p.K; a.per = plan.per; a.splits = plan.splits;
+  a.ld = (p.N + 3) & ~3;
+  a.part = static_cast<float*>(scratch);
+  a.part_sums = a.part + (int64_t)plan.splits * p.M * a.ld;
+  a.status = p.reset ? p.status : nullptr;
+  a.e = e;
+  const dim3 grid((unsigned)((p.M + kT - 1) / kT), (unsigned)((p.N + kT - 1) / kT), (unsigned)plan.splits);
+  cudaError_t err = launch(k_linear_simt<T, OP>, grid, dim3(256), 0, st, a);
+  if (err == cudaSuccess && plan.splits > 1) err = linear_join(p, plan.splits, a.part, a.part_sums, e, st);
+  return err;
+}
+
+template <typename T, int OP>
+cudaError_t run_join(const LinearProblem& p, int splits, const float* part, const float* sums, const LinearEnd& e,
+                     cudaStream_t st) {
+  const int ld = (p.N + 3) & ~3;
+  const int64_t jobs = p.M * (ld >> 2) + (OP == kLinDw && e.sums ? (p.M + 3) / 4 : 0);
+  return launch(k_linear_join<T, OP>, dim3((unsigned)((jobs + 31) / 32)), dim3(32, 8), 0, st, p.M, p.N, ld, splits, part,
+                sums, e);
+}
+
+}  // namespace
+
+cudaError_t linear_simt(const LinearProblem& p, const LinearPlan& plan, const LinearEnd& e, void* scratch,
+                        cudaStream_t st) {
+  using B = __nv_bfloat16;
+  const bool b = p.dtype == FS_BF16;
+  if (p.op == kLinFwd) return b ? run_simt<B, kLinFwd>(p, plan, e, scratch, st) : run_simt<float, kLinFwd>(p, plan, e, scratch, st);
+  if (p.op == kLinDx) return b ? run_simt<B, kLinDx>(p, plan, e, scratch, st) : run_simt<float, kLinDx>(p, plan, e, scratch, st);
+  return b ? run_simt<B, kLinDw>(p, plan, e, scratch, st) : run_simt<float, kLinDw>(p, plan, e, scratch, st);
+}
+
+cudaError_t linear_join(const LinearProblem& p, int splits, const float* part, const float* sums, const LinearEnd& e,
+                        cudaStream_t st) {
+  using B = __nv_bfloat16;
+  const bool b = p.dtype == FS_BF16;
+  if (p.op == kLinFwd) return b ? run_join<B, kLinFwd>(p, splits, part, sums, e, st) : run_join<float, kLinFwd>(p, splits, part, sums, e, st);
+  if (p.op == kLinDx) return b ? run_join<B, kLinDx>(p, splits, part, sums, e, st) : run_join<float, kLinDx>(p, splits, part, sums, e, st);
+  return run_join<float, kLinDw>(p, splits, part, sums, e, st);  // D is fp32
+}
+
+}  // namespace fs

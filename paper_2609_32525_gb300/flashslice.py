@@ -30,6 +30,7 @@ FS_NOALLOC_SCRATCH_BYTES = 16 << 20
 FS_F32, FS_BF16 = 0, 1
 FS_DOT_BF16, FS_DOT_BF16X2 = 0, 1
 FS_MASK_NONE, FS_MASK_PREFIX = 0, 1
+FS_ACT_NONE, FS_ACT_RELU, FS_ACT_GELU, FS_ACT_SILU = range(4)
 FS_OP_SLICE_FWD, FS_OP_DESLICE_FWD, FS_OP_DESLICE_BWD, FS_OP_SLICE_BWD, FS_OP_STATS, FS_OP_COUPLING_BWD = range(6)
 
 EXPORTED = ("fs_workspace_bytes", "fs_slice_fwd", "fs_slice_finalize", "fs_mix", "fs_deslice_fwd",
@@ -38,7 +39,8 @@ EXPORTED = ("fs_workspace_bytes", "fs_slice_fwd", "fs_slice_finalize", "fs_mix",
             "fs_slice_fwd_noalloc", "fs_slice_fwd_lse", "fs_mix_channels", "fs_mix_channels_bwd", "fs_mix_channels_bwd_add", "fs_stats",
             "fs_coupling_bwd", "fs_coupling_bwd_launch_count", "fs_norm_fwd", "fs_norm_bwd",
             "fs_norm_workspace_bytes", "fs_ckpt_pack", "fs_ckpt_unpack", "fs_attn_fwd", "fs_attn_bwd",
-            "fs_attn_workspace_bytes", "fs_attn_path_for_shape")
+            "fs_attn_workspace_bytes", "fs_attn_path_for_shape", "fs_linear_fwd", "fs_linear_bwd",
+            "fs_linear_workspace_bytes", "fs_linear_path_for_shape", "fs_dropout_fwd", "fs_dropout_bwd")
 
 
 class fs_shape(ctypes.Structure):
@@ -48,6 +50,10 @@ class fs_shape(ctypes.Structure):
 
 class fs_rows(ctypes.Structure):
     _fields_ = [("rows", ctypes.c_int64), ("C", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+
+class fs_linear(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("Cin", ctypes.c_int32), ("Cout", ctypes.c_int32), ("dtype", ctypes.c_int32)]
 
 
 class fs_attn_shape(ctypes.Structure):
@@ -73,6 +79,7 @@ _F = ctypes.c_float
 _R = ctypes.POINTER(fs_rows)
 _A = ctypes.POINTER(fs_attn_shape)
 _M = ctypes.POINTER(fs_attn_mask)
+_L = ctypes.POINTER(fs_linear)
 _sig = {
     "fs_workspace_bytes": (_Z, [_S, _I]),
     "fs_slice_fwd": (_I, [_S, _P, _P, _P, _P, _P, _P, _P, _P, _I, _P, _Z, _P]),
@@ -104,6 +111,12 @@ _sig = {
     "fs_norm_workspace_bytes": (_Z, [_R]),
     "fs_ckpt_pack": (_I, [_R, _P, _P, _P, _P]),
     "fs_ckpt_unpack": (_I, [_R, _P, _P, _P, _P]),
+    "fs_linear_fwd": (_I, [_L, _P, _P, _P, _I, _F, _P, _P, _P, _P, _P, _Z, _P]),
+    "fs_linear_bwd": (_I, [_L, _P, _P, _P, _I, _F] + [_P] * 6 + [_I, _P, _Z, _P]),
+    "fs_linear_workspace_bytes": (_Z, [_L, _I]),
+    "fs_linear_path_for_shape": (_I, [_L, _I]),
+    "fs_dropout_fwd": (_I, [_R, _P, _I, _F, _P, _P, _P, _P]),
+    "fs_dropout_bwd": (_I, [_R, _P, _I, _F, _P, _P, _P, _P]),
     "fs_slice_fwd_noalloc": (_I, [_S, _P, _P, _P, _P, _P, _P, _P, _P, _I, ctypes.POINTER(_P), _P]),
 }
 for _name, (_res, _args) in _sig.items():
@@ -485,6 +498,84 @@ def fs_ckpt_unpack(rows, q8, e8, x, stream=None):
     dev, st = _where(fn, x, stream)
     _check(fn, _lib.fs_ckpt_unpack(rows, _arg(fn, "q8", q8, torch.int8, n, dev),
                                    _arg(fn, "e8", e8, torch.uint8, nb, dev), _arg(fn, "x", x, dt, n, dev), st))
+
+
+# ---- linear maps and dropout ---------------------------------------------------------------
+
+
+def make_linear(rows, Cin, Cout, dtype=FS_F32) -> fs_linear:
+    """rows rows of Cin channels to rows of Cout, in dtype (a torch.dtype or FS_F32 / FS_BF16)."""
+    r = make_rows(rows, Cin, dtype)
+    return fs_linear(r.rows, r.C, int(Cout), r.dtype)
+
+
+def linear_workspace_bytes(s: fs_linear, backward=False) -> int:
+    return int(_lib.fs_linear_workspace_bytes(ctypes.byref(s), int(bool(backward))))
+
+
+def linear_path_for_shape(s: fs_linear, backward=False) -> int:
+    """0: fp32 multiply-adds; 1: tcgen05."""
+    return int(_lib.fs_linear_path_for_shape(ctypes.byref(s), int(bool(backward))))
+
+
+def linear_workspace(s: fs_linear, backward=False, device="cuda") -> torch.Tensor:
+    """Scratch of fs_linear_fwd, or of fs_linear_bwd."""
+    ws = torch.empty(max(16, linear_workspace_bytes(s, backward)), dtype=torch.uint8, device=device)
+    ws[:16].zero_()
+    return ws
+
+
+def dropout_rng(seed, offset=0, device="cuda") -> torch.Tensor:
+    """The two words {seed, offset} of a dropout (taken modulo 2^64), which `rng` arguments want."""
+    return torch.tensor([((int(w) + (1 << 63)) % (1 << 64)) - (1 << 63) for w in (seed, offset)], dtype=torch.int64,
+                        device=device)
+
+
+def fs_linear_fwd(s, x, W, bias, act, p, rng, res, y, pre, ws, stream=None):
+    """act: FS_ACT_*; rng: see dropout_rng, None without dropout; bias, res, pre may be None."""
+    fn, ci, co, r = "fs_linear_fwd", s.Cin, s.Cout, s.rows
+    dt, ny = torch.bfloat16 if s.dtype == FS_BF16 else torch.float32, r * co
+    dev, st = _where(fn, x, stream)
+    nw = 0 if ws is None else ws.numel()
+    _check(fn, _lib.fs_linear_fwd(
+        s, _arg(fn, "x", x, dt, r * ci, dev), _arg(fn, "W", W, dt, co * ci, dev),
+        _arg(fn, "bias", bias, torch.float32, co, dev, True), act, p, _arg(fn, "rng", rng, torch.int64, 2, dev, True),
+        _arg(fn, "res", res, dt, ny, dev, True), _arg(fn, "y", y, dt, ny, dev), _arg(fn, "pre", pre, dt, ny, dev, True),
+        _arg(fn, "ws", ws, torch.uint8, nw, dev), nw, st))
+
+
+def fs_linear_bwd(s, x, W, g, act, p, rng, pre, dres, dx, dW, dbias, accumulate, ws, stream=None):
+    """act, p, rng, pre: of the call that made x; x, W, pre, dres, dx, dW, dbias may be None (see the header)."""
+    fn, ci, co, r, f = "fs_linear_bwd", s.Cin, s.Cout, s.rows, torch.float32
+    dt, nx = torch.bfloat16 if s.dtype == FS_BF16 else torch.float32, r * ci
+    dev, st = _where(fn, g, stream)
+    nw = 0 if ws is None else ws.numel()
+    _check(fn, _lib.fs_linear_bwd(
+        s, _arg(fn, "x", x, dt, nx, dev, True), _arg(fn, "W", W, dt, co * ci, dev, True),
+        _arg(fn, "g", g, dt, r * co, dev), act, p, _arg(fn, "rng", rng, torch.int64, 2, dev, True),
+        _arg(fn, "pre", pre, dt, nx, dev, True), _arg(fn, "dres", dres, dt, nx, dev, True),
+        _arg(fn, "dx", dx, dt, nx, dev, True), _arg(fn, "dW", dW, f, co * ci, dev, True),
+        _arg(fn, "dbias", dbias, f, co, dev, True), int(bool(accumulate)), _arg(fn, "ws", ws, torch.uint8, nw, dev), nw,
+        st))
+
+
+def fs_dropout_fwd(rows, x, act, p, rng, res, y, stream=None):
+    """act: FS_ACT_*; rng: see dropout_rng, None for p = 0; res may be None."""
+    fn = "fs_dropout_fwd"
+    dt, n, _ = _row_sizes(rows)
+    dev, st = _where(fn, x, stream)
+    _check(fn, _lib.fs_dropout_fwd(
+        rows, _arg(fn, "x", x, dt, n, dev), act, p, _arg(fn, "rng", rng, torch.int64, 2, dev, True),
+        _arg(fn, "res", res, dt, n, dev, True), _arg(fn, "y", y, dt, n, dev), st))
+
+
+def fs_dropout_bwd(rows, dy, act, p, rng, pre, dx, stream=None):
+    fn = "fs_dropout_bwd"
+    dt, n, _ = _row_sizes(rows)
+    dev, st = _where(fn, dy, stream)
+    _check(fn, _lib.fs_dropout_bwd(
+        rows, _arg(fn, "dy", dy, dt, n, dev), act, p, _arg(fn, "rng", rng, torch.int64, 2, dev, True),
+        _arg(fn, "pre", pre, dt, n, dev, True), _arg(fn, "dx", dx, dt, n, dev), st))
 
 
 # ---- convenience: one coupling, buffers allocated through torch ----------------------------
