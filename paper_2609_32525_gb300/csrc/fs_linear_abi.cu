@@ -51,22 +51,87 @@ LinearProblem problem(const fs_linear* s, int op, const void* a, const void* b, 
 }
 LinearPlan plan_of(const fs_linear* s, int op) {
   const LinearProblem p = problem(s, op, nullptr, nullptr);
-  return linear_plan(op, p.dtype, p.M, p.N, p.K, true);
+  return linear_plan(op, p.dtype, p.M, p.N, p.K);
 }
-cudaError_t run(const LinearProblem& p, const LinearPlan& plan, const LinearEnd& e, char* scratch, cudaStream_t st) {
-  return linear_simt(p, plan, e, scratch, st);
+cudaError_t run(LinearProblem p, const LinearPlan& plan, const LinearEnd& e, char* scratch, cudaStream_t st) {
+  return plan.path ? linear_tc(p, plan, e, scratch, st) : linear_simt(p, plan, e, scratch, st);
+}
+
+// A call's scratch: the status word, the operands that tensor cores cannot take as they are, and the parts
+// of split sums.
+struct Scratch {
+  size_t need = kAlign;
+  LinearPack packs[3];
+  int n = 0;
+  int dtype;
+  explicit Scratch(int dtype_) : dtype(dtype_) {}
+  // Where a product finds operand p: itself, or (from at()) its packed form.
+  void pack(bool tc, const void* p, int64_t rows, int C) {
+    if (!tc || !linear_packed(dtype, C)) return;
+    packs[n++] = {p, reinterpret_cast<void*>(need), rows, C};
+    need += align_up(linear_pack_bytes(dtype, rows, C), kAlign);
+  }
+  size_t add(size_t bytes) {
+    need += bytes;
+    return need - bytes;
+  }
+  cudaError_t launch(void* ws, cudaStream_t st) {
+    for (int i = 0; i < n; i++) packs[i].dst = static_cast<char*>(ws) + reinterpret_cast<size_t>(packs[i].dst);
+    return n ? linear_pack(packs, n, dtype, static_cast<uint32_t*>(ws), st) : cudaSuccess;
+  }
+  const void* at(bool tc, const void* p, int64_t rows, int C) const {
+    for (int i = 0; tc && i < n; i++)
+      if (packs[i].src == p && packs[i].rows == rows && packs[i].C == C) return packs[i].dst;
+    return p;
+  }
+};
+struct Plans {
+  LinearPlan fwd, dx, dw;
+  Scratch scratch;
+  size_t at_fwd = 0, at_dx = 0, at_dw = 0;
+};
+// (The pointers of a size query are stand-ins.)
+Plans plan_fwd(const fs_linear* s, const void* x, const void* W) {
+  Plans p{plan_of(s, kLinFwd), {}, {}, Scratch(s->dtype)};
+  p.scratch.pack(p.fwd.path, x, s->rows, s->Cin);
+  p.scratch.pack(p.fwd.path, W, s->Cout, s->Cin);
+  p.at_fwd = p.scratch.add(p.fwd.total);
+  return p;
+}
+// dx, dw: wanted.  What a call does not want it does not pack, but its workspace has room for it.
+Plans plan_bwd(const fs_linear* s, bool dx, bool dw, const void* x, const void* W, const void* g) {
+  Plans p{{}, plan_of(s, kLinDx), plan_of(s, kLinDw), Scratch(s->dtype)};
+  const bool tx = dx && p.dx.path, tw = dw && p.dw.path;
+  p.scratch.pack(tx || tw, g, s->rows, s->Cout);
+  p.scratch.pack(tx, W, s->Cout, s->Cin);
+  p.scratch.pack(tw, x, s->rows, s->Cin);
+  p.at_dx = p.scratch.add(p.dx.total);
+  p.at_dw = p.scratch.add(p.dw.total);
+  return p;
 }
 // [p, n] or nothing where p is one of the buffers that a call may update in place.
 Span unless(const void* p, size_t n, const void* same) { return {p == same ? nullptr : p, n}; }
 
 }  // namespace
 
-LinearPlan linear_plan(int op, int dtype, int64_t M, int N, int64_t K, bool aligned) {
+LinearPlan linear_plan(int op, int dtype, int64_t M, int N, int64_t K) {
   LinearPlan p{};
-  const int64_t tiles = ((M + 63) / 64) * ((N + 63) / 64);
-  // Sums are split until the blocks fill the device twice, into parts of at least 64 terms.
-  int64_t splits = std::max<int64_t>(1, std::min<int64_t>(2LL * num_sms() / tiles, (K + 63) / 64));
-  p.per = ((K + splits - 1) / splits + 15) / 16 * 16;
+  const double work = (double)M * N * (double)K;
+  p.path = work >= 4194304.0 && M >= 64 && N >= 16 && K >= 16 && std::max(M, K) < (1LL << 31) - 512;
+  int64_t splits;
+  if (p.path) {
+    // Pairs of CTAs take tiles; where there are fewer than half as many tiles, sums are split into parts of
+    // at least 512 terms.
+    const int bn = linear_tile_n(N, op != kLinFwd, dtype == FS_F32);
+    const int64_t tiles = ((M + 255) / 256) * ((N + bn - 1) / bn), pairs = num_sms() / 2;
+    splits = std::max<int64_t>(1, std::min<int64_t>(pairs / tiles, K / 512));
+    p.per = ((K + splits - 1) / splits + 63) / 64 * 64;
+  } else {
+    // Sums are split until the blocks fill the device twice, into parts of at least 64 terms.
+    const int64_t tiles = ((M + 63) / 64) * ((N + 63) / 64);
+    splits = std::max<int64_t>(1, std::min<int64_t>(2LL * num_sms() / tiles, (K + 63) / 64));
+    p.per = ((K + splits - 1) / splits + 15) / 16 * 16;
+  }
   p.splits = (int)((K + p.per - 1) / p.per);
   if (p.splits > 1)
     p.part = ((size_t)p.splits * M * (((size_t)N + 3) & ~(size_t)3) + (op == kLinDw ? (size_t)p.splits * M : 0)) * 4;
@@ -93,8 +158,8 @@ extern "C" {
 
 size_t fs_linear_workspace_bytes(const fs_linear* s, int backward) {
   if (!valid(s) || !supported(s)) return 0;
-  if (!backward) return kAlign + plan_of(s, kLinFwd).total;
-  return kAlign + plan_of(s, kLinDx).total + plan_of(s, kLinDw).total;
+  return backward ? plan_bwd(s, true, true, nullptr, nullptr, nullptr).scratch.need
+                  : plan_fwd(s, nullptr, nullptr).scratch.need;
 }
 
 int fs_linear_path_for_shape(const fs_linear* s, int backward) {
@@ -109,8 +174,8 @@ fs_status fs_linear_fwd(const fs_linear* s, const void* x, const void* W, const 
   if (!valid_drop(act, p, rng)) return FS_ERR_INVALID;
   FS_CHECK_PTR(x); FS_CHECK_PTR(W); FS_CHECK_PTR(y); FS_CHECK_PTR(ws);
   FS_CHECK_OPT(bias); FS_CHECK_OPT(rng); FS_CHECK_OPT(res); FS_CHECK_OPT(pre);
-  const LinearPlan plan = plan_of(s, kLinFwd);
-  const size_t need = kAlign + plan.total;
+  Plans plan = plan_fwd(s, x, W);
+  const size_t need = plan.scratch.need;
   if (ws_bytes < need) return FS_ERR_INVALID;
   const Sizes z = sizes(s);
   if (!disjoint({{x, z.x}, {W, z.w}, {bias, z.bias}, {rng, 16}, unless(res, z.y, y)}, {{y, z.y}, {pre, z.y}, {ws, need}}) ||
@@ -119,8 +184,11 @@ fs_status fs_linear_fwd(const fs_linear* s, const void* x, const void* W, const 
   LinearEnd e{};
   e.bias = bias; e.act = act; e.rng = p > 0.f ? rng : nullptr; e.threshold = threshold_of(p); e.scale = scale_of(p);
   e.res = res; e.y = y; e.pre_out = pre;
-  return cuda_status(run(problem(s, kLinFwd, x, W, ws), plan, e, static_cast<char*>(ws) + kAlign,
-                         reinterpret_cast<cudaStream_t>(stream)));
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  const bool tc = plan.fwd.path;
+  FS_CUDA(plan.scratch.launch(ws, st));
+  return cuda_status(run(problem(s, kLinFwd, plan.scratch.at(tc, x, s->rows, s->Cin), plan.scratch.at(tc, W, s->Cout, s->Cin), ws, plan.scratch.n == 0),
+                         plan.fwd, e, static_cast<char*>(ws) + plan.at_fwd, st));
 }
 
 fs_status fs_linear_bwd(const fs_linear* s, const void* x, const void* W, const void* g, int act, float p,
@@ -134,8 +202,7 @@ fs_status fs_linear_bwd(const fs_linear* s, const void* x, const void* W, const 
   // dx needs W, and pre behind an activation; dW needs x; dbias comes with dW; one of the two is wanted
   if ((!dx && !dW) || (dx && !W) || (dx && act != FS_ACT_NONE && !pre) || (dW && !x) || (dbias && !dW) || (dres && !dx))
     return FS_ERR_INVALID;
-  const LinearPlan plan_x = plan_of(s, kLinDx), plan_w = plan_of(s, kLinDw);
-  const size_t need = kAlign + plan_x.total + plan_w.total;
+  const size_t need = fs_linear_workspace_bytes(s, 1);
   if (ws_bytes < need) return FS_ERR_INVALID;
   const Sizes z = sizes(s);
   if (!disjoint({{x, z.x}, {W, z.w}, {g, z.y}, {rng, 16}, {pre, z.x}, unless(dres, z.x, dx)},
@@ -143,17 +210,23 @@ fs_status fs_linear_bwd(const fs_linear* s, const void* x, const void* W, const 
       !disjoint({{dres, z.x}}, {{dW, z.dw}, {dbias, z.bias}, {ws, need}}))
     return FS_ERR_INVALID;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-  char* scratch = static_cast<char*>(ws) + kAlign;
+  Plans plan = plan_bwd(s, dx != nullptr, dW != nullptr, x, W, g);
+  char* w = static_cast<char*>(ws);
+  FS_CUDA(plan.scratch.launch(ws, st));
+  bool reset = plan.scratch.n == 0;
   if (dx) {
     LinearEnd e{};
     e.act = act; e.rng = p > 0.f ? rng : nullptr; e.threshold = threshold_of(p); e.scale = scale_of(p);
     e.pre_in = pre; e.res = dres; e.y = dx;
-    FS_CUDA(run(problem(s, kLinDx, g, W, ws), plan_x, e, scratch, st));
+    const bool tc = plan.dx.path;
+    FS_CUDA(run(problem(s, kLinDx, plan.scratch.at(tc, g, s->rows, s->Cout), plan.scratch.at(tc, W, s->Cout, s->Cin), ws, reset), plan.dx, e, w + plan.at_dx, st));
+    reset = false;
   }
   if (dW) {
     LinearEnd e{};
     e.y = dW; e.sums = dbias; e.accumulate = accumulate;
-    FS_CUDA(run(problem(s, kLinDw, g, x, ws, !dx), plan_w, e, scratch + plan_x.total, st));
+    const bool tc = plan.dw.path;
+    FS_CUDA(run(problem(s, kLinDw, plan.scratch.at(tc, g, s->rows, s->Cout), plan.scratch.at(tc, x, s->rows, s->Cin), ws, reset), plan.dw, e, w + plan.at_dw, st));
   }
   return FS_OK;
 }
