@@ -4,8 +4,7 @@
 // Dropout: the mask is a function of (seed, offset, row, channel) and is computed wherever it is
 // needed, so that the forward and the backward agree without storing it.  Four channels share one
 // counter of Philox 4x32-10 (Salmon, Moraes, Dror, Shaw, "Parallel random numbers: as easy as
-// 1, 2, 3", 2011): two 32 x 32 -> 64 bit products and two three-way xors a round, 40 instructions
-// for four values, which stay under the memory time of a row that is read and written.
+// 1, 2, 3", 2011): two 32 x 32 -> 64 bit products and two three-way xors a round.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -20,20 +19,14 @@ struct Words {
   uint32_t w[4];
 };
 
-__device__ __forceinline__ Words philox(uint64_t counter, uint64_t offset, uint64_t seed) {
-  uint32_t c0 = (uint32_t)counter, c1 = (uint32_t)(counter >> 32), c2 = (uint32_t)offset, c3 = (uint32_t)(offset >> 32);
-  uint32_t k0 = (uint32_t)seed, k1 = (uint32_t)(seed >> 32);
-#pragma unroll
-  for (int r = 0; r < 10; r++) {
-    const uint64_t p = (uint64_t)0xD2511F53u * c0, q = (uint64_t)0xCD9E8D57u * c2;
-    c0 = (uint32_t)(q >> 32) ^ c1 ^ k0;
-    c1 = (uint32_t)q;
-    c2 = (uint32_t)(p >> 32) ^ c3 ^ k1;
-    c3 = (uint32_t)p;
-    k0 += 0x9E3779B9u;
-    k1 += 0xBB67AE85u;
-  }
-  return {{c0, c1, c2, c3}};
+constexpr uint32_t kM0 = 0xD2511F53u, kM1 = 0xCD9E8D57u, kW0 = 0x9E3779B9u, kW1 = 0xBB67AE85u;
+
+__device__ __forceinline__ void philox_round(uint32_t (&c)[4], uint32_t k0, uint32_t k1) {
+  const uint64_t p = (uint64_t)kM0 * c[0], q = (uint64_t)kM1 * c[2];
+  c[0] = (uint32_t)(q >> 32) ^ c[1] ^ k0;
+  c[1] = (uint32_t)q;
+  c[2] = (uint32_t)(p >> 32) ^ c[3] ^ k1;
+  c[3] = (uint32_t)p;
 }
 
 // What a call's dropout needs: a word below `threshold` drops its value, the others scale it.
@@ -42,14 +35,52 @@ struct Drop {
   uint32_t threshold;   // floor(p 2^32)
   float scale;          // 1 / (1 - p)
 };
-// (seed, offset), read once a thread.
+
+// The generator's part that a call's counters share: the offset fills the upper half of each, and
+// the quads' upper word is 0 up to 2^34 values.  Two of the first rounds' four products and most of
+// their xors are then the same for all, and the words of the key schedule too.  Taken from one
+// lane, so that the compiler keeps them in registers that a warp shares.
 struct DropKey {
-  uint64_t seed, offset;
+  uint32_t k0, k1, o0, o1;
+  uint32_t b, c, d, e;  // rounds 1 to 3, for a quad's upper word of 0
 };
+__device__ __forceinline__ DropKey drop_key(const uint64_t* rng) {
+  const uint64_t seed = rng[0], offset = rng[1];
+  DropKey k;
+  k.k0 = __shfl_sync(0xffffffffu, (uint32_t)seed, 0);
+  k.k1 = __shfl_sync(0xffffffffu, (uint32_t)(seed >> 32), 0);
+  k.o0 = __shfl_sync(0xffffffffu, (uint32_t)offset, 0);
+  k.o1 = __shfl_sync(0xffffffffu, (uint32_t)(offset >> 32), 0);
+  const uint64_t q1 = (uint64_t)kM1 * k.o0, p2 = (uint64_t)kM0 * ((uint32_t)(q1 >> 32) ^ k.k0);
+  k.b = k.o1 ^ k.k1;
+  k.c = (uint32_t)q1 ^ (k.k0 + kW0);
+  k.d = (uint32_t)(p2 >> 32) ^ (k.k1 + kW1);
+  k.e = (uint32_t)p2 ^ (k.k1 + 2 * kW1);
+  return k;
+}
+
+__device__ __forceinline__ Words philox(uint64_t quad, const DropKey& k) {
+  uint32_t c[4];
+  if ((uint32_t)(quad >> 32) == 0) {
+    const uint64_t p1 = (uint64_t)kM0 * (uint32_t)quad, q2 = (uint64_t)kM1 * ((uint32_t)(p1 >> 32) ^ k.b);
+    const uint64_t p3 = (uint64_t)kM0 * ((uint32_t)(q2 >> 32) ^ k.c), q3 = (uint64_t)kM1 * ((uint32_t)p1 ^ k.d);
+    c[0] = (uint32_t)(q3 >> 32) ^ (uint32_t)q2 ^ (k.k0 + 2 * kW0);
+    c[1] = (uint32_t)q3;
+    c[2] = (uint32_t)(p3 >> 32) ^ k.e;
+    c[3] = (uint32_t)p3;
+  } else {
+    c[0] = (uint32_t)quad, c[1] = (uint32_t)(quad >> 32), c[2] = k.o0, c[3] = k.o1;
+#pragma unroll
+    for (uint32_t r = 0; r < 3; r++) philox_round(c, k.k0 + r * kW0, k.k1 + r * kW1);
+  }
+#pragma unroll
+  for (uint32_t r = 3; r < 10; r++) philox_round(c, k.k0 + r * kW0, k.k1 + r * kW1);
+  return {{c[0], c[1], c[2], c[3]}};
+}
 
 // A word that drops gives 0 whatever the value is (a NaN or an infinity included).
-__device__ __forceinline__ void keep4(const Drop& d, const DropKey& k, uint64_t quad, float (&v)[4]) {
-  const Words r = philox(quad, k.offset, k.seed);
+__device__ __forceinline__ void keep4(const Drop& d, const DropKey& k, uint64_t quad, float* v) {
+  const Words r = philox(quad, k);
 #pragma unroll
   for (int i = 0; i < 4; i++) v[i] = r.w[i] >= d.threshold ? v[i] * d.scale : 0.f;
 }
@@ -121,22 +152,39 @@ __device__ __forceinline__ float silu_slope(float u) {
   return s * fmaf(b, 1.f - s, 1.f);
 }
 
-template <bool kFast>
-__device__ __forceinline__ void apply4(int act, float (&v)[4]) {
-  if (act == FS_ACT_NONE) return;
+// v = act(v), n values that one loop walks (so that the chains of several are under way at once).
+template <bool kFast, int ACT, int n>
+__device__ __forceinline__ void apply(float (&v)[n]) {
 #pragma unroll
-  for (int i = 0; i < 4; i++)
-    v[i] = act == FS_ACT_GELU ? gelu<kFast>(v[i]) : act == FS_ACT_SILU ? silu<kFast>(v[i]) : (v[i] < 0.f ? 0.f : v[i]);
-}
-// v *= act'(u)
-template <bool kFast>
-__device__ __forceinline__ void slope4(int act, const float (&u)[4], float (&v)[4]) {
-  if (act == FS_ACT_NONE) return;
-#pragma unroll
-  for (int i = 0; i < 4; i++) {
-    if (act == FS_ACT_RELU) v[i] = u[i] > 0.f ? v[i] : u[i] <= 0.f ? 0.f : u[i];
-    else v[i] *= act == FS_ACT_GELU ? gelu_slope<kFast>(u[i]) : silu_slope<kFast>(u[i]);
+  for (int i = 0; i < n; i++) {
+    if (ACT == FS_ACT_GELU) v[i] = gelu<kFast>(v[i]);
+    if (ACT == FS_ACT_SILU) v[i] = silu<kFast>(v[i]);
+    if (ACT == FS_ACT_RELU) v[i] = v[i] < 0.f ? 0.f : v[i];
   }
+}
+// v = g act'(v)
+template <bool kFast, int ACT, int n>
+__device__ __forceinline__ void slope(float (&v)[n], const float* g) {
+#pragma unroll
+  for (int i = 0; i < n; i++) {
+    if (ACT == FS_ACT_GELU) v[i] = gelu_slope<kFast>(v[i]) * g[i];
+    if (ACT == FS_ACT_SILU) v[i] = silu_slope<kFast>(v[i]) * g[i];
+    if (ACT == FS_ACT_RELU) v[i] = v[i] > 0.f ? g[i] : v[i] <= 0.f ? 0.f : v[i];
+    if (ACT == FS_ACT_NONE) v[i] = g[i];
+  }
+}
+template <bool kFast, int n>
+__device__ __forceinline__ void apply(int act, float (&v)[n]) {
+  if (act == FS_ACT_GELU) apply<kFast, FS_ACT_GELU>(v);
+  else if (act == FS_ACT_SILU) apply<kFast, FS_ACT_SILU>(v);
+  else if (act == FS_ACT_RELU) apply<kFast, FS_ACT_RELU>(v);
+}
+template <bool kFast, int n>
+__device__ __forceinline__ void slope(int act, float (&v)[n], const float* g) {
+  if (act == FS_ACT_GELU) slope<kFast, FS_ACT_GELU>(v, g);
+  else if (act == FS_ACT_SILU) slope<kFast, FS_ACT_SILU>(v, g);
+  else if (act == FS_ACT_RELU) slope<kFast, FS_ACT_RELU>(v, g);
+  else slope<kFast, FS_ACT_NONE>(v, g);
 }
 
 // ---- four neighbouring channels in memory --------------------------------------------------

@@ -12,53 +12,72 @@
 namespace fs {
 namespace {
 
-template <typename T>
-__device__ __forceinline__ void drop4(const DropArgs& a, const act::DropKey& key, uint64_t quad, const float (&pre)[4],
-                                      const float (&res)[4], float (&v)[4]) {
+// n values, quad after quad.
+template <typename T, int n>
+__device__ __forceinline__ void drop(const DropArgs& a, const act::DropKey& key, uint64_t quad, float (&pre)[n],
+                                     const float (&res)[n], float (&v)[n]) {
   constexpr bool kFast = sizeof(T) == 2;
-  if (a.backward) act::slope4<kFast>(a.act, pre, v);
-  else act::apply4<kFast>(a.act, v);
-  if (a.rng) act::keep4({a.rng, a.threshold, a.scale}, key, quad, v);
+  if (a.backward) {
+    act::slope<kFast>(a.act, pre, v);
+#pragma unroll
+    for (int i = 0; i < n; i++) v[i] = pre[i];
+  } else {
+    act::apply<kFast>(a.act, v);
+  }
+  if (a.rng)
+#pragma unroll
+    for (int i = 0; i < n; i += 4) act::keep4({a.rng, a.threshold, a.scale}, key, quad + i / 4, v + i);
   if (a.res)
 #pragma unroll
-    for (int i = 0; i < 4; i++) v[i] += res[i];
+    for (int i = 0; i < n; i++) v[i] += res[i];
 }
 
 // Rows of a multiple of four channels: the quads lie one after another, so rows do not matter.
-// A thread takes 16 bytes of each tensor at a time.
-template <typename T>
+// A thread takes kP pieces of 16 bytes of each tensor at a time, a block's width apart, loaded
+// before the first is worked on.
+template <typename T, int kP>
 __global__ void __launch_bounds__(256) k_dropout(DropArgs a) {
   const int64_t zero = grid_begin();
-  constexpr int kQ = 16 / (4 * sizeof(T));  // quads in 16 bytes
-  const int64_t quads = a.rows * (a.C >> 2), step = (int64_t)gridDim.x * 256 * kQ;
+  constexpr int kV = 16 / sizeof(T);  // values of a piece
+  const int64_t values = a.rows * a.C, step = (int64_t)gridDim.x * 256 * kP * kV;
   const T *x = static_cast<const T*>(a.x) + zero, *res = static_cast<const T*>(a.res), *pre = static_cast<const T*>(a.pre);
   T* y = static_cast<T*>(a.y);
-  act::DropKey key{0, 0};
-  if (a.rng) key = {a.rng[zero], a.rng[1 + zero]};
+  act::DropKey key{};
+  if (a.rng) key = act::drop_key(a.rng + zero);
   const bool slope = a.backward && a.act != FS_ACT_NONE;
-  for (int64_t q = ((int64_t)blockIdx.x * 256 + threadIdx.x) * kQ; q < quads; q += step) {
-    if (kQ == 2 && q + 2 <= quads) {
-      const int4 w = *reinterpret_cast<const int4*>(x + 4 * q);
-      int4 r = make_int4(0, 0, 0, 0), u = r, out;
-      if (a.res) r = *reinterpret_cast<const int4*>(res + 4 * q);
-      if (slope) u = *reinterpret_cast<const int4*>(pre + 4 * q);
+  for (int64_t first = ((int64_t)blockIdx.x * 256 * kP + threadIdx.x) * kV; first < values; first += step) {
+    int4 w[kP], r[kP], u[kP];
 #pragma unroll
-      for (int h = 0; h < 2; h++) {
-        float v[4], f[4], g[4];
-        act::load4(reinterpret_cast<const T*>(&w) + 4 * h, 4, true, v);
-        act::load4(reinterpret_cast<const T*>(&u) + 4 * h, 4, true, f);
-        act::load4(reinterpret_cast<const T*>(&r) + 4 * h, 4, true, g);
-        drop4<T>(a, key, (uint64_t)(q + h), f, g, v);
-        act::store4(reinterpret_cast<T*>(&out) + 4 * h, 4, true, v);
+    for (int p = 0; p < kP; p++) {
+      const int64_t at = first + p * 256 * kV;
+      w[p] = r[p] = u[p] = make_int4(0, 0, 0, 0);
+      if (at + kV <= values) {
+        w[p] = *reinterpret_cast<const int4*>(x + at);
+        if (a.res) r[p] = *reinterpret_cast<const int4*>(res + at);
+        if (slope) u[p] = *reinterpret_cast<const int4*>(pre + at);
+      } else if (at < values) {  // a last quad of bf16
+        *reinterpret_cast<int2*>(&w[p]) = *reinterpret_cast<const int2*>(x + at);
+        if (a.res) *reinterpret_cast<int2*>(&r[p]) = *reinterpret_cast<const int2*>(res + at);
+        if (slope) *reinterpret_cast<int2*>(&u[p]) = *reinterpret_cast<const int2*>(pre + at);
       }
-      *reinterpret_cast<int4*>(y + 4 * q) = out;
-    } else {
-      float v[4], f[4] = {}, g[4] = {};
-      act::load4(x + 4 * q, 4, true, v);
-      if (slope) act::load4(pre + 4 * q, 4, true, f);
-      if (a.res) act::load4(res + 4 * q, 4, true, g);
-      drop4<T>(a, key, (uint64_t)q, f, g, v);
-      act::store4(y + 4 * q, 4, true, v);
+    }
+#pragma unroll
+    for (int p = 0; p < kP; p++) {
+      const int64_t at = first + p * 256 * kV;
+      float v[kV], f[kV], g[kV];
+#pragma unroll
+      for (int h = 0; h < kV; h += 4) {
+        act::load4(reinterpret_cast<const T*>(&w[p]) + h, 4, true, *reinterpret_cast<float(*)[4]>(v + h));
+        act::load4(reinterpret_cast<const T*>(&u[p]) + h, 4, true, *reinterpret_cast<float(*)[4]>(f + h));
+        act::load4(reinterpret_cast<const T*>(&r[p]) + h, 4, true, *reinterpret_cast<float(*)[4]>(g + h));
+      }
+      drop<T, kV>(a, key, (uint64_t)at >> 2, f, g, v);
+      int4 out;
+#pragma unroll
+      for (int h = 0; h < kV; h += 4)
+        act::store4(reinterpret_cast<T*>(&out) + h, 4, true, *reinterpret_cast<const float(*)[4]>(v + h));
+      if (at + kV <= values) *reinterpret_cast<int4*>(y + at) = out;
+      else if (at < values) *reinterpret_cast<int2*>(y + at) = *reinterpret_cast<const int2*>(&out);
     }
   }
 }
@@ -71,8 +90,8 @@ __global__ void __launch_bounds__(256) k_dropout_ragged(DropArgs a) {
   const int64_t quads = a.rows * per_row, step = (int64_t)gridDim.x * 256;
   const T *x = static_cast<const T*>(a.x) + zero, *res = static_cast<const T*>(a.res), *pre = static_cast<const T*>(a.pre);
   T* y = static_cast<T*>(a.y);
-  act::DropKey key{0, 0};
-  if (a.rng) key = {a.rng[zero], a.rng[1 + zero]};
+  act::DropKey key{};
+  if (a.rng) key = act::drop_key(a.rng + zero);
   const bool slope = a.backward && a.act != FS_ACT_NONE;
   int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x;
   int64_t row = q / per_row;
@@ -86,7 +105,7 @@ __global__ void __launch_bounds__(256) k_dropout_ragged(DropArgs a) {
     act::load4(x + at, n, false, v);
     if (slope) act::load4(pre + at, n, false, f);
     if (a.res) act::load4(res + at, n, false, g);
-    drop4<T>(a, key, (uint64_t)q, f, g, v);
+    drop<T, 4>(a, key, (uint64_t)q, f, g, v);
     act::store4(y + at, n, false, v);
     row += rows_on, col += cols_on;
     if (col >= per_row) col -= per_row, row++;
@@ -96,9 +115,13 @@ __global__ void __launch_bounds__(256) k_dropout_ragged(DropArgs a) {
 template <typename T>
 cudaError_t run(const DropArgs& a, cudaStream_t st) {
   const bool flat = (a.C & 3) == 0;
-  const int64_t threads = flat ? (a.rows * (a.C >> 2) * 4 * (int64_t)sizeof(T) + 15) / 16 : a.rows * ((a.C + 3) >> 2);
-  const int64_t blocks = std::min<int64_t>((threads + 255) / 256, (int64_t)num_sms() * 8);
-  return launch(flat ? k_dropout<T> : k_dropout_ragged<T>, dim3((unsigned)blocks), dim3(256), 0, st, a);
+  const int64_t pieces = flat ? (a.rows * a.C * (int64_t)sizeof(T) + 15) / 16 : a.rows * ((a.C + 3) >> 2);
+  // Two pieces a thread where that still fills the device.
+  const int64_t most = (int64_t)num_sms() * 8;
+  const bool two = flat && pieces >= most * 512;
+  const int64_t blocks = std::min<int64_t>((pieces + (two ? 511 : 255)) / (two ? 512 : 256), most);
+  return launch(!flat ? k_dropout_ragged<T> : two ? k_dropout<T, 2> : k_dropout<T, 1>, dim3((unsigned)blocks), dim3(256), 0,
+                st, a);
 }
 
 }  // namespace

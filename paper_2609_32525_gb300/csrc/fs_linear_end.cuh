@@ -11,9 +11,10 @@ namespace lin {
 template <typename T>
 constexpr bool kFastAct = sizeof(T) == 2;
 
+// (by a whole warp)
 __device__ __forceinline__ act::DropKey drop_key(const LinearEnd& e) {
-  act::DropKey k{0, 0};
-  if (e.rng) k.seed = e.rng[0], k.offset = e.rng[1];
+  act::DropKey k{};
+  if (e.rng) k = act::drop_key(e.rng);
   return k;
 }
 
@@ -43,11 +44,13 @@ __device__ __forceinline__ void end4(const LinearEnd& e, const act::DropKey& key
       for (int i = 0; i < 4; i++) v[i] += b[i];
     }
     if (e.pre_out) act::store4(static_cast<T*>(e.pre_out) + at, n, whole, v);
-    act::apply4<kFastAct<T>>(e.act, v);
+    act::apply<kFastAct<T>>(e.act, v);
   } else if (e.act != FS_ACT_NONE) {
     float u[4];
     act::load4(static_cast<const T*>(e.pre_in) + at, n, whole, u);
-    act::slope4<kFastAct<T>>(e.act, u, v);
+    act::slope<kFastAct<T>>(e.act, u, v);
+#pragma unroll
+    for (int i = 0; i < 4; i++) v[i] = u[i];
   }
   if (e.rng) {
     const uint64_t quads = (uint64_t)((N + 3) >> 2);

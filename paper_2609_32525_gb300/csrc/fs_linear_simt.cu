@@ -137,6 +137,7 @@ __global__ void __launch_bounds__(256) k_linear_join(int64_t M, int N, int ld, i
   sm[threadIdx.y][threadIdx.x] = s;
   __syncthreads();
   if (threadIdx.y != 0) return;
+  const act::DropKey key = lin::drop_key(e);
 #pragma unroll
   for (int y = 1; y < 8; y++) {
     const float4 v = sm[y][threadIdx.x];
@@ -151,7 +152,7 @@ __global__ void __launch_bounds__(256) k_linear_join(int64_t M, int N, int ld, i
     return;
   }
   const int64_t row = i / (ld >> 2);
-  lin::end4<T, OP>(e, lin::drop_key(e), row, (int)(i - row * (ld >> 2)) * 4, N, v);
+  lin::end4<T, OP>(e, key, row, (int)(i - row * (ld >> 2)) * 4, N, v);
 }
 
 template <typename T, int OP>

@@ -101,87 +101,85 @@ __device__ __forceinline__ uint4 ld_box(uint32_t addr) {
   return v;
 }
 
-// Four columns' biases; N cuts the last ones off.
-__device__ __forceinline__ void bias4(const float* bias, int col, int N, float (&b)[4]) {
-  if (col + 4 <= N) {
-    const float4 x = *reinterpret_cast<const float4*>(bias + col);
-    b[0] = x.x, b[1] = x.y, b[2] = x.z, b[3] = x.w;
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; i++) b[i] = col + i < N ? bias[col + i] : 0.f;
+// 32 neighbouring values of a row (which is the lane's) in a box, from piece piece0 on: piece j of
+// 16 bytes of row r lies at (j ^ r % 8) * 16, TMA's 128-byte swizzle.
+template <typename T>
+struct Line {
+  static constexpr int kPieces = 2 * sizeof(T);
+  __device__ __forceinline__ static uint32_t at(uint32_t box, int piece) {
+    const uint32_t lane = threadIdx.x & 31;
+    return box + lane * 128 + (((uint32_t)piece ^ (lane & 7)) << 4);
   }
-}
+  __device__ __forceinline__ static void load(uint32_t box, int piece0, float (&v)[32]) {
+#pragma unroll
+    for (int j = 0; j < kPieces; j++) {
+      const uint4 w = ld_box(at(box, piece0 + j));
+      const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+      for (int i = 0; i < 4; i++) {
+        if constexpr (sizeof(T) == 2)
+          v[8 * j + 2 * i] = __uint_as_float(x[i] << 16), v[8 * j + 2 * i + 1] = __uint_as_float(x[i] & 0xFFFF0000u);
+        else
+          v[4 * j + i] = __uint_as_float(x[i]);
+      }
+    }
+  }
+  __device__ __forceinline__ static void store(uint32_t box, int piece0, const float (&v)[32]) {
+#pragma unroll
+    for (int j = 0; j < kPieces; j++) {
+      uint32_t x[4];
+#pragma unroll
+      for (int i = 0; i < 4; i++)
+        x[i] = sizeof(T) == 2 ? pack_bf16(v[8 * j + 2 * i], v[8 * j + 2 * i + 1]) : __float_as_uint(v[4 * j + i]);
+      st_shared_v4(at(box, piece0 + j), x[0], x[1], x[2], x[3]);
+    }
+  }
+};
 
-// The end of a map on 32 neighbouring columns of a row (which is the lane's), in pieces of 16 bytes
-// of the box: piece j of row r lies at (j ^ r % 8) * 16, TMA's 128-byte swizzle.
-template <int END, typename T, int ACT>
+// The end of a map on 32 neighbouring columns of a row, step by step for all of them, so that the
+// chains of 32 values (8 counters) are under way at once.
+template <int END, typename T>
 __device__ __forceinline__ void end32(const TcArgs& g, const act::DropKey& key, int64_t row, int col, int piece0,
                                       uint32_t ybox, uint32_t pbox, float (&v)[32]) {
-  constexpr int kV = 16 / sizeof(T);  // values of a piece
   constexpr bool kFast = sizeof(T) == 2;
-  const uint32_t lane = threadIdx.x & 31, line = lane * 128, x = lane & 7;
-  const uint64_t quad0 = (uint64_t)row * (uint64_t)((g.N + 3) >> 2) + (uint64_t)(col >> 2);
-  // (fp32's functions are long: one copy of them, with v in local memory)
-#pragma unroll(kFast || END == kEndRaw ? 32 / kV : 1)
-  for (int j = 0; j < 32 / kV; j++) {
-    const uint32_t at = line + (((uint32_t)(piece0 + j) ^ x) << 4);
-    uint4 res = make_uint4(0, 0, 0, 0), pre = res;
-    if (g.load_res) res = ld_box(ybox + at);
-    if (END == kEndDx && ACT != FS_ACT_NONE) pre = ld_box(pbox + at);
-    uint32_t out[4], out_pre[4];
+  if constexpr (END == kEndFwd) {
+    if (g.e.bias) {
+      if (col + 32 <= g.N) {
 #pragma unroll
-    for (int q = 0; q < kV / 4; q++) {
-      float f[4] = {v[j * kV + 4 * q], v[j * kV + 4 * q + 1], v[j * kV + 4 * q + 2], v[j * kV + 4 * q + 3]};
-      const uint32_t w0 = q ? res.z : res.x, w1 = q ? res.w : res.y;
-      if (END == kEndFwd) {
-        if (g.e.bias) {
-          float b[4];
-          bias4(g.e.bias, col + j * kV + 4 * q, g.N, b);
-#pragma unroll
-          for (int i = 0; i < 4; i++) f[i] += b[i];
+        for (int i = 0; i < 32; i += 4) {
+          const float4 b = *reinterpret_cast<const float4*>(g.e.bias + col + i);
+          v[i] += b.x, v[i + 1] += b.y, v[i + 2] += b.z, v[i + 3] += b.w;
         }
-        if constexpr (kFast) out_pre[2 * q] = pack_bf16(f[0], f[1]), out_pre[2 * q + 1] = pack_bf16(f[2], f[3]);
-        else
+      } else {
 #pragma unroll
-          for (int i = 0; i < 4; i++) out_pre[i] = __float_as_uint(f[i]);
-        act::apply4<kFast>(ACT, f);
-      } else if (END == kEndDx && ACT != FS_ACT_NONE) {
-        const uint32_t p0 = q ? pre.z : pre.x, p1 = q ? pre.w : pre.y;
-        float u[4];
-        if constexpr (kFast)
-          u[0] = __uint_as_float(p0 << 16), u[1] = __uint_as_float(p0 & 0xFFFF0000u), u[2] = __uint_as_float(p1 << 16),
-          u[3] = __uint_as_float(p1 & 0xFFFF0000u);
-        else
-          u[0] = __uint_as_float(pre.x), u[1] = __uint_as_float(pre.y), u[2] = __uint_as_float(pre.z),
-          u[3] = __uint_as_float(pre.w);
-        act::slope4<kFast>(ACT, u, f);
+        for (int i = 0; i < 32; i++)
+          if (col + i < g.N) v[i] += g.e.bias[col + i];
       }
-      if (END != kEndRaw && g.e.rng)
-        act::keep4({g.e.rng, g.e.threshold, g.e.scale}, key, quad0 + (uint64_t)((j * kV) / 4 + q), f);
-      if (g.load_res) {
-        if constexpr (kFast)
-          f[0] += __uint_as_float(w0 << 16), f[1] += __uint_as_float(w0 & 0xFFFF0000u), f[2] += __uint_as_float(w1 << 16),
-          f[3] += __uint_as_float(w1 & 0xFFFF0000u);
-        else
-          f[0] += __uint_as_float(res.x), f[1] += __uint_as_float(res.y), f[2] += __uint_as_float(res.z),
-          f[3] += __uint_as_float(res.w);
-      }
-      if constexpr (kFast) out[2 * q] = pack_bf16(f[0], f[1]), out[2 * q + 1] = pack_bf16(f[2], f[3]);
-      else
-#pragma unroll
-        for (int i = 0; i < 4; i++) out[i] = __float_as_uint(f[i]);
     }
-    if (END == kEndFwd && g.store_pre) st_shared_v4(pbox + at, out_pre[0], out_pre[1], out_pre[2], out_pre[3]);
-    st_shared_v4(ybox + at, out[0], out[1], out[2], out[3]);
+    if (g.store_pre) Line<T>::store(pbox, piece0, v);
+    act::apply<kFast>(g.e.act, v);
   }
-}
-template <int END, typename T>
-__device__ __forceinline__ void end32_by_act(const TcArgs& g, const act::DropKey& key, int64_t row, int col, int piece0,
-                                             uint32_t ybox, uint32_t pbox, float (&v)[32]) {
-  if (END == kEndRaw || g.e.act == FS_ACT_NONE) end32<END, T, FS_ACT_NONE>(g, key, row, col, piece0, ybox, pbox, v);
-  else if (g.e.act == FS_ACT_GELU) end32<END, T, FS_ACT_GELU>(g, key, row, col, piece0, ybox, pbox, v);
-  else if (g.e.act == FS_ACT_SILU) end32<END, T, FS_ACT_SILU>(g, key, row, col, piece0, ybox, pbox, v);
-  else end32<END, T, FS_ACT_RELU>(g, key, row, col, piece0, ybox, pbox, v);
+  if constexpr (END == kEndDx) {
+    if (g.load_pre) {
+      float u[32];
+      Line<T>::load(pbox, piece0, u);
+      act::slope<kFast>(g.e.act, u, v);
+#pragma unroll
+      for (int i = 0; i < 32; i++) v[i] = u[i];
+    }
+  }
+  if (END != kEndRaw && g.e.rng) {
+    const uint64_t quad = (uint64_t)row * (uint64_t)((g.N + 3) >> 2) + (uint64_t)(col >> 2);
+#pragma unroll
+    for (int i = 0; i < 8; i++) act::keep4({g.e.rng, g.e.threshold, g.e.scale}, key, quad + i, v + 4 * i);
+  }
+  if (g.load_res) {
+    float r[32];
+    Line<T>::load(ybox, piece0, r);
+#pragma unroll
+    for (int i = 0; i < 32; i++) v[i] += r[i];
+  }
+  Line<T>::store(ybox, piece0, v);
 }
 
 // A box between shared memory and rows that TMA cannot address, by a warp.
@@ -456,8 +454,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_linea
     const int e = warp - 2, wg = e >> 2, sub = warp & 3;
     const uint32_t lanes = tmem + ((uint32_t)(sub * 32) << 16), free0 = leader_addr(&acc_empty[0]);
     Boxes<END, T> box(g, boxes + e * 2 * kBox, in_full[e]);
-    act::DropKey key{0, 0};
-    if (END != kEndRaw && g.e.rng) key = lin::drop_key(g.e);
+    const act::DropKey key = lin::drop_key(g.e);
     Halves h;
     bool ok = true;
     auto row_of = [&](const Unit& w) { return (int64_t)w.m0 + rank * 128 + sub * 32; };
@@ -507,7 +504,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_linea
             float v[32];
 #pragma unroll
             for (int i = 0; i < 32; i++) v[i] = __uint_as_float(r[p][i]);
-            end32_by_act<END, T>(g, key, row0 + lane, col + 32 * p, 4 * p, box.ybox(), box.pbox(), v);
+            end32<END, T>(g, key, row0 + lane, col + 32 * p, 4 * p, box.ybox(), box.pbox(), v);
           }
           box.send(row0, col, w.split);
           if (box.both && nu < g.units) {
@@ -577,7 +574,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_linea
           if (!box.both && i + 1 < chunks) box.start(1, row0, col + (i + 1) * 32);
           ok = box.ready(row0, col + i * 32, ab, status);
           if (!ok) continue;
-          end32_by_act<END, T>(g, key, row0 + lane, col + i * 32, 0, box.ybox(), box.pbox(), acc[i]);
+          end32<END, T>(g, key, row0 + lane, col + i * 32, 0, box.ybox(), box.pbox(), acc[i]);
           box.send(row0, col + i * 32, w.split);
           if (box.both && i + 1 < chunks) box.start(1, row0, col + (i + 1) * 32);
         }
