@@ -11,13 +11,10 @@
 #include <cstdint>
 
 #include "flashslice.h"
+#include "fs_tc_ptx.cuh"
 
 namespace fs {
 namespace act {
-
-struct Words {
-  uint32_t w[4];
-};
 
 constexpr uint32_t kM0 = 0xD2511F53u, kM1 = 0xCD9E8D57u, kW0 = 0x9E3779B9u, kW1 = 0xBB67AE85u;
 
@@ -59,30 +56,56 @@ __device__ __forceinline__ DropKey drop_key(const uint64_t* rng) {
   return k;
 }
 
-__device__ __forceinline__ Words philox(uint64_t quad, const DropKey& k) {
-  uint32_t c[4];
-  if ((uint32_t)(quad >> 32) == 0) {
-    const uint64_t p1 = (uint64_t)kM0 * (uint32_t)quad, q2 = (uint64_t)kM1 * ((uint32_t)(p1 >> 32) ^ k.b);
-    const uint64_t p3 = (uint64_t)kM0 * ((uint32_t)(q2 >> 32) ^ k.c), q3 = (uint64_t)kM1 * ((uint32_t)p1 ^ k.d);
-    c[0] = (uint32_t)(q3 >> 32) ^ (uint32_t)q2 ^ (k.k0 + 2 * kW0);
-    c[1] = (uint32_t)q3;
-    c[2] = (uint32_t)(p3 >> 32) ^ k.e;
-    c[3] = (uint32_t)p3;
-  } else {
-    c[0] = (uint32_t)quad, c[1] = (uint32_t)(quad >> 32), c[2] = k.o0, c[3] = k.o1;
+// n neighbouring quads, round by round for all of them: the chains of n counters are under way at
+// once and share the key schedule's additions.  A quad of 32 bits has an upper word of 0.
+template <int n, typename Q>
+__device__ __forceinline__ void philox(Q quad, const DropKey& k, uint32_t (&c)[n][4]) {
+  constexpr bool kLow = sizeof(Q) == 4;
+  uint32_t k0 = k.k0, k1 = k.k1;
+  if constexpr (kLow) {
+    k0 += 2 * kW0;
 #pragma unroll
-    for (uint32_t r = 0; r < 3; r++) philox_round(c, k.k0 + r * kW0, k.k1 + r * kW1);
+    for (int i = 0; i < n; i++) {
+      const uint64_t p1 = (uint64_t)kM0 * (quad + i), q2 = (uint64_t)kM1 * ((uint32_t)(p1 >> 32) ^ k.b);
+      const uint64_t p3 = (uint64_t)kM0 * ((uint32_t)(q2 >> 32) ^ k.c), q3 = (uint64_t)kM1 * ((uint32_t)p1 ^ k.d);
+      c[i][0] = (uint32_t)(q3 >> 32) ^ (uint32_t)q2 ^ k0;
+      c[i][1] = (uint32_t)q3;
+      c[i][2] = (uint32_t)(p3 >> 32) ^ k.e;
+      c[i][3] = (uint32_t)p3;
+    }
+    k0 += kW0;
+    k1 += 3 * kW1;
+  } else {
+#pragma unroll
+    for (int i = 0; i < n; i++)
+      c[i][0] = (uint32_t)(quad + i), c[i][1] = (uint32_t)((uint64_t)(quad + i) >> 32), c[i][2] = k.o0, c[i][3] = k.o1;
   }
 #pragma unroll
-  for (uint32_t r = 3; r < 10; r++) philox_round(c, k.k0 + r * kW0, k.k1 + r * kW1);
-  return {{c[0], c[1], c[2], c[3]}};
+  for (int r = kLow ? 3 : 0; r < 10; r++) {
+#pragma unroll
+    for (int i = 0; i < n; i++) philox_round(c[i], k0, k1);
+    k0 += kW0;
+    k1 += kW1;
+  }
 }
 
-// A word that drops gives 0 whatever the value is (a NaN or an infinity included).
-__device__ __forceinline__ void keep4(const Drop& d, const DropKey& k, uint64_t quad, float* v) {
-  const Words r = philox(quad, k);
+// r += drop(v), n values from a quad on (a 32-bit one where all of them have an upper word of 0).  A word that
+// drops leaves r as it is, whatever the value is (a NaN or an infinity included); else product and sum are one
+// instruction under the comparison's predicate.
+template <int n, typename Q>
+__device__ __forceinline__ void keep_by(const Drop& d, const DropKey& k, Q quad, const float* v, float* r) {
+  uint32_t w[n / 4][4];
+  philox<n / 4>(quad, k, w);
 #pragma unroll
-  for (int i = 0; i < 4; i++) v[i] = r.w[i] >= d.threshold ? v[i] * d.scale : 0.f;
+  for (int i = 0; i < n; i++)
+    asm("{\n .reg .pred p;\n setp.ge.u32 p, %1, %2;\n @p fma.rn.f32 %0, %3, %4, %0;\n}"
+        : "+f"(r[i])
+        : "r"(w[i / 4][i % 4]), "r"(d.threshold), "f"(v[i]), "f"(d.scale));
+}
+template <int n>
+__device__ __forceinline__ void keep(const Drop& d, const DropKey& k, uint64_t quad, const float* v, float* r) {
+  if (((quad + n / 4 - 1) >> 32) == 0) keep_by<n>(d, k, (uint32_t)quad, v, r);
+  else keep_by<n>(d, k, quad, v, r);
 }
 
 // ---- activations ---------------------------------------------------------------------------
@@ -94,22 +117,25 @@ __device__ __forceinline__ void keep4(const Drop& d, const DropKey& k, uint64_t 
 // least squares, reweighted towards the minimax fit) is within 1.6e-4 of itself there, and past
 // a = 5, where gelu(-a) is below 1.5e-6, Q stays at Q(5) and the Gaussian goes on falling.  One
 // exponential and eight fused multiply-adds, and the exponential serves the derivative
-// Phi(u) + u e^(-u^2/2) / sqrt(2 pi) too.
-__device__ __forceinline__ float gauss_tail(float a, float& e) {
-  constexpr float kHalfLog2e = 0.7213475204f;
-  float q;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(-kHalfLog2e * a * a));
-  const float b = fminf(a, 5.f);
-  q = 5.7904302e-06f;
-  q = fmaf(q, b, -0.00014531538f);
-  q = fmaf(q, b, 0.0015831057f);
-  q = fmaf(q, b, -0.0099215629f);
-  q = fmaf(q, b, 0.040258871f);
-  q = fmaf(q, b, -0.11416839f);
-  q = fmaf(q, b, 0.24129194f);
-  q = fmaf(q, b, -0.39726451f);
-  q = fmaf(q, b, 0.49994163f);
-  return e * q;
+// Phi(u) + u e^(-u^2/2) / sqrt(2 pi) too.  Two values share the instructions (f32x2).
+//
+// e: e^(-a^2/2); the result is Phi(-a).  a <= kGaussEnd.
+__device__ __forceinline__ uint64_t twice(float x) { return tc::pack2(__float_as_uint(x), __float_as_uint(x)); }
+__device__ __forceinline__ uint64_t pair(float x, float y) { return tc::pack2(__float_as_uint(x), __float_as_uint(y)); }
+__device__ __forceinline__ uint64_t gauss_tail2(float a0, float a1, uint64_t& e) {
+  const uint64_t a = pair(a0, a1), s = tc::mul2(tc::mul2(a, twice(-0.7213475204f)), a);  // log2(e) / 2
+  e = pair(tc::ex2(tc::lo_f(s)), tc::ex2(tc::hi_f(s)));
+  const uint64_t b = pair(fminf(a0, 5.f), fminf(a1, 5.f));
+  uint64_t q = twice(5.7904302e-06f);
+  q = tc::fma2(q, b, twice(-0.00014531538f));
+  q = tc::fma2(q, b, twice(0.0015831057f));
+  q = tc::fma2(q, b, twice(-0.0099215629f));
+  q = tc::fma2(q, b, twice(0.040258871f));
+  q = tc::fma2(q, b, twice(-0.11416839f));
+  q = tc::fma2(q, b, twice(0.24129194f));
+  q = tc::fma2(q, b, twice(-0.39726451f));
+  q = tc::fma2(q, b, twice(0.49994163f));
+  return tc::mul2(e, q);
 }
 constexpr float kInvSqrt2Pi = 0.3989422804014327f;
 // Past this a the Gaussian is 0 in fp32; a product of it with an infinite u would be NaN.
@@ -117,21 +143,39 @@ constexpr float kGaussEnd = 15.f;
 // Past this u the sigmoid is 1 (or 0) in fp32, and with u held there no infinity meets a 0.
 constexpr float kSigmoidEnd = 110.f;
 
-template <bool kFast>
-__device__ __forceinline__ float gelu(float u) {
-  if (u < -kGaussEnd) return 0.f;
-  if (!kFast) return u * normcdff(u);
-  float e;
-  const float a = fabsf(u), t = a * gauss_tail(a, e);  // |u| Phi(-|u|)
-  return a > kGaussEnd ? u : fmaxf(u, 0.f) - t;  // a NaN is one in t
+// The larger (smaller) of two; NaN where one is.
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float d;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+  return d;
 }
-template <bool kFast>
+__device__ __forceinline__ float min_nan(float a, float b) {
+  float d;
+  asm("min.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+  return d;
+}
+
+__device__ __forceinline__ float gelu(float u) { return u < -kGaussEnd ? 0.f : u * normcdff(u); }
 __device__ __forceinline__ float gelu_slope(float u) {
-  if (fabsf(u) > kGaussEnd) return u > 0.f ? 1.f : 0.f;
-  if (!kFast) return fmaf(u * kInvSqrt2Pi, expf(-0.5f * u * u), normcdff(u));
-  float e;
-  const float t = gauss_tail(fabsf(u), e);
-  return fmaf(u * kInvSqrt2Pi, e, u > 0.f ? 1.f - t : t);
+  const float v = max_nan(min_nan(u, kGaussEnd), -kGaussEnd);
+  return fmaf(v * kInvSqrt2Pi, expf(-0.5f * v * v), normcdff(v));
+}
+// max(u, 0) - a Phi(-a)
+__device__ __forceinline__ void gelu2(float& u0, float& u1) {
+  const float a0 = fminf(fabsf(u0), kGaussEnd), a1 = fminf(fabsf(u1), kGaussEnd);
+  uint64_t e;
+  const uint64_t t = gauss_tail2(a0, a1, e);
+  const uint64_t y = tc::fma2(t, pair(-a0, -a1), pair(max_nan(u0, 0.f), max_nan(u1, 0.f)));
+  u0 = tc::lo_f(y), u1 = tc::hi_f(y);
+}
+__device__ __forceinline__ void gelu_slope2(float& u0, float& u1) {
+  const float v0 = max_nan(min_nan(u0, kGaussEnd), -kGaussEnd), v1 = max_nan(min_nan(u1, kGaussEnd), -kGaussEnd);
+  uint64_t e;
+  const uint64_t t = gauss_tail2(fabsf(v0), fabsf(v1), e);
+  const float t0 = tc::lo_f(t), t1 = tc::hi_f(t);
+  const uint64_t cdf = pair(v0 > 0.f ? 1.f - t0 : t0, v1 > 0.f ? 1.f - t1 : t1);
+  const uint64_t y = tc::fma2(tc::mul2(pair(v0, v1), twice(kInvSqrt2Pi)), e, cdf);
+  u0 = tc::lo_f(y), u1 = tc::hi_f(y);
 }
 
 // By e^-|u|, which never overflows, so that the left tail keeps its values.
@@ -152,14 +196,15 @@ __device__ __forceinline__ float silu_slope(float u) {
   return s * fmaf(b, 1.f - s, 1.f);
 }
 
-// v = act(v), n values that one loop walks (so that the chains of several are under way at once).
+// v = act(v), n values (an even number) that one loop walks, so that the chains of several are under way at once.
 template <bool kFast, int ACT, int n>
 __device__ __forceinline__ void apply(float (&v)[n]) {
 #pragma unroll
   for (int i = 0; i < n; i++) {
-    if (ACT == FS_ACT_GELU) v[i] = gelu<kFast>(v[i]);
+    if (ACT == FS_ACT_GELU && !kFast) v[i] = gelu(v[i]);
+    if (ACT == FS_ACT_GELU && kFast && i % 2 == 0) gelu2(v[i], v[i + 1]);
     if (ACT == FS_ACT_SILU) v[i] = silu<kFast>(v[i]);
-    if (ACT == FS_ACT_RELU) v[i] = v[i] < 0.f ? 0.f : v[i];
+    if (ACT == FS_ACT_RELU) v[i] = max_nan(v[i], 0.f);
   }
 }
 // v = g act'(v)
@@ -167,11 +212,15 @@ template <bool kFast, int ACT, int n>
 __device__ __forceinline__ void slope(float (&v)[n], const float* g) {
 #pragma unroll
   for (int i = 0; i < n; i++) {
-    if (ACT == FS_ACT_GELU) v[i] = gelu_slope<kFast>(v[i]) * g[i];
-    if (ACT == FS_ACT_SILU) v[i] = silu_slope<kFast>(v[i]) * g[i];
+    if (ACT == FS_ACT_GELU && !kFast) v[i] = gelu_slope(v[i]);
+    if (ACT == FS_ACT_GELU && kFast && i % 2 == 0) gelu_slope2(v[i], v[i + 1]);
+    if (ACT == FS_ACT_SILU) v[i] = silu_slope<kFast>(v[i]);
     if (ACT == FS_ACT_RELU) v[i] = v[i] > 0.f ? g[i] : v[i] <= 0.f ? 0.f : v[i];
     if (ACT == FS_ACT_NONE) v[i] = g[i];
   }
+  if (ACT == FS_ACT_GELU || ACT == FS_ACT_SILU)
+#pragma unroll
+    for (int i = 0; i < n; i++) v[i] *= g[i];
 }
 template <bool kFast, int n>
 __device__ __forceinline__ void apply(int act, float (&v)[n]) {

@@ -15,7 +15,7 @@ namespace {
 // n values, quad after quad.
 template <typename T, int n>
 __device__ __forceinline__ void drop(const DropArgs& a, const act::DropKey& key, uint64_t quad, float (&pre)[n],
-                                     const float (&res)[n], float (&v)[n]) {
+                                     float (&res)[n], float (&v)[n]) {
   constexpr bool kFast = sizeof(T) == 2;
   if (a.backward) {
     act::slope<kFast>(a.act, pre, v);
@@ -24,12 +24,14 @@ __device__ __forceinline__ void drop(const DropArgs& a, const act::DropKey& key,
   } else {
     act::apply<kFast>(a.act, v);
   }
-  if (a.rng)
+  if (a.rng) {
+    act::keep<n>({a.rng, a.threshold, a.scale}, key, quad, v, res);
 #pragma unroll
-    for (int i = 0; i < n; i += 4) act::keep4({a.rng, a.threshold, a.scale}, key, quad + i / 4, v + i);
-  if (a.res)
+    for (int i = 0; i < n; i++) v[i] = res[i];
+  } else {
 #pragma unroll
     for (int i = 0; i < n; i++) v[i] += res[i];
+  }
 }
 
 // Rows of a multiple of four channels: the quads lie one after another, so rows do not matter.

@@ -52,13 +52,14 @@ __device__ __forceinline__ void end4(const LinearEnd& e, const act::DropKey& key
 #pragma unroll
     for (int i = 0; i < 4; i++) v[i] = u[i];
   }
+  float r[4] = {};
+  if (e.res) act::load4(static_cast<const T*>(e.res) + at, n, whole, r);
   if (e.rng) {
     const uint64_t quads = (uint64_t)((N + 3) >> 2);
-    act::keep4({e.rng, e.threshold, e.scale}, key, (uint64_t)row * quads + (uint64_t)(col >> 2), v);
-  }
-  if (e.res) {
-    float r[4];
-    act::load4(static_cast<const T*>(e.res) + at, n, whole, r);
+    act::keep<4>({e.rng, e.threshold, e.scale}, key, (uint64_t)row * quads + (uint64_t)(col >> 2), v, r);
+#pragma unroll
+    for (int i = 0; i < 4; i++) v[i] = r[i];
+  } else {
 #pragma unroll
     for (int i = 0; i < 4; i++) v[i] += r[i];
   }

@@ -8,7 +8,7 @@
 // go to the other half of TMEM.
 //   warp 0       TMA loads of A and B, 64 terms at a time, into a ring of 128-byte-swizzled stages
 //   warp 1       TMEM, products (leader)
-//   warps 2..9   epilogue: 32 rows each, columns shared between two warpgroups; a residual or
+//   warps 2 on   epilogue: 32 rows each, columns shared between two or three warpgroups; a residual or
 //                pre-activation comes by TMA into the 32 x 128 byte box that the result leaves
 //                from, so all traffic with HBM is in whole 128-byte lines
 // x and W lie with their terms next to each other (K-major), W in dx and both operands of dW with
@@ -37,13 +37,22 @@ namespace {
 
 using namespace tc;
 
-constexpr int kThreads = 320, kMaxStages = 12;
+constexpr int kMaxStages = 12;
 constexpr uint32_t kABytes = 128 * 128;          // 128 rows (or 64 terms x 128) of 64 values
 constexpr uint32_t kBox = 32 * 128;              // an epilogue warp's box
-constexpr uint32_t kBoxes = 8 * 2 * kBox, kOnes = 1024;
+constexpr uint32_t kOnes = 1024;
 constexpr size_t kSmem = 231424;                 // with the barriers below the limit of a block
-constexpr uint32_t kStageRoom = kSmem - 1024 - kOnes - kBoxes;
 constexpr uint32_t kSumCol = 256;                // dbias' accumulator
+// Epilogue warpgroups and boxes of a warp; what the boxes leave for the stages.
+template <int kGroups, int kPer>
+struct Block {
+  static constexpr int kThreads = 64 + 128 * kGroups;
+  static constexpr uint32_t kBoxes = kGroups * 4 * kPer * kBox, kStageRoom = kSmem - 1024 - kOnes - kBoxes;
+};
+// Where sums are short the epilogue is the work: five warpgroups with one box each.  Where they are long, or a
+// chunk has two inputs or results, three with two boxes.  (1,048,576 x 256 x 256 with dropout and residual:
+// 361 us against 404 with three groups; 32,768 x 1024 x 4096 173 us with three against 183 with five.)
+constexpr int kManyGroups = 5, kShortK = 512;
 
 enum { kEndFwd = 0, kEndDx = 1, kEndRaw = 2 };
 
@@ -51,32 +60,43 @@ struct TcArgs {
   CUtensorMap a, b, y, pre, res;
   LinearEnd e;
   int64_t M, K, per;
-  int N, ldy, n_tiles, units, bn, splits, stages, seg;  // ldy: pitch of y; seg: blocks of 64 terms taken out at a time
+  int N, ldy, n_tiles, m_tiles, tiles, units, bn, splits, stages, seg;  // ldy: pitch of y; seg: blocks of 64 terms taken out at a time
+  int step_n, step_m, step_split;                       // from a pair's unit to its next one
   uint32_t stage_bytes, idesc, idesc_sum, a_step, b_step;  // steps: 16 terms on in a stage, in 16-byte units
   int a_mn, b_mn;
   int load_res, load_pre, store_pre, plain;             // plain: y, res and pre by plain accesses
+  const char* ahead;                                    // null, or A to prefetch to L2 a tile ahead, in whole rows
   int sums;                                             // dbias is wanted
   float* part_sums;                                     // split: [splits][M]
   uint32_t* status;
   int reset;
 };
 
+// The units of a pair, number `pair` and every pairs-th one after it; stepped, not divided, since an epilogue
+// warp's few hundred instructions a chunk run one after another.
 struct Unit {
-  int m0, n, split, blocks;
-  int64_t k0;
+  int m, n, split;
+  int left;  // units from this one on, 0 or less: none
+  __device__ __forceinline__ Unit(const TcArgs& g, int u) : left(g.units - u) {
+    split = u / g.tiles;
+    const int t = u - split * g.tiles;
+    m = t / g.n_tiles;
+    n = t - m * g.n_tiles;
+  }
+  __device__ __forceinline__ void next(const TcArgs& g, int pairs) {
+    left -= pairs;
+    n += g.step_n;
+    m += g.step_m;
+    split += g.step_split;
+    if (n >= g.n_tiles) n -= g.n_tiles, m++;
+    if (m >= g.m_tiles) m -= g.m_tiles, split++;
+  }
+  __device__ __forceinline__ int64_t k0(const TcArgs& g) const { return split * g.per; }
+  __device__ __forceinline__ int blocks(const TcArgs& g) const {
+    const int64_t k = g.K - k0(g) < g.per ? g.K - k0(g) : g.per;
+    return (int)((k + 63) >> 6);
+  }
 };
-__device__ __forceinline__ Unit unit_of(const TcArgs& g, int u) {
-  Unit w;
-  const int tiles = g.units / g.splits;
-  w.split = u / tiles;
-  const int t = u - w.split * tiles, m = t / g.n_tiles;
-  w.n = t - m * g.n_tiles;
-  w.m0 = m * 256;
-  w.k0 = w.split * g.per;
-  const int64_t k1 = w.k0 + g.per < g.K ? w.k0 + g.per : g.K;
-  w.blocks = (int)((k1 - w.k0 + 63) >> 6);
-  return w;
-}
 
 // Which half of TMEM a segment's products go to.  Units with dbias use the first half for all and
 // columns of the second one for the sums; the others take turns.
@@ -101,19 +121,18 @@ __device__ __forceinline__ uint4 ld_box(uint32_t addr) {
   return v;
 }
 
-// 32 neighbouring values of a row (which is the lane's) in a box, from piece piece0 on: piece j of
-// 16 bytes of row r lies at (j ^ r % 8) * 16, TMA's 128-byte swizzle.
+// 16 neighbouring values of a row in a box, from piece piece0 on: piece j of 16 bytes of row r lies
+// at (j ^ r % 8) * 16, TMA's 128-byte swizzle.  line: the box's address + 128 r.
 template <typename T>
 struct Line {
-  static constexpr int kPieces = 2 * sizeof(T);
-  __device__ __forceinline__ static uint32_t at(uint32_t box, int piece) {
-    const uint32_t lane = threadIdx.x & 31;
-    return box + lane * 128 + (((uint32_t)piece ^ (lane & 7)) << 4);
+  static constexpr int kPieces = sizeof(T);
+  __device__ __forceinline__ static uint32_t at(uint32_t line, int piece) {
+    return line + (((uint32_t)piece ^ ((line >> 7) & 7)) << 4);
   }
-  __device__ __forceinline__ static void load(uint32_t box, int piece0, float (&v)[32]) {
+  __device__ __forceinline__ static void load(uint32_t line, int piece0, float (&v)[16]) {
 #pragma unroll
     for (int j = 0; j < kPieces; j++) {
-      const uint4 w = ld_box(at(box, piece0 + j));
+      const uint4 w = ld_box(at(line, piece0 + j));
       const uint32_t x[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
       for (int i = 0; i < 4; i++) {
@@ -124,62 +143,101 @@ struct Line {
       }
     }
   }
-  __device__ __forceinline__ static void store(uint32_t box, int piece0, const float (&v)[32]) {
+  __device__ __forceinline__ static void store(uint32_t line, int piece0, const float (&v)[16]) {
 #pragma unroll
     for (int j = 0; j < kPieces; j++) {
       uint32_t x[4];
 #pragma unroll
       for (int i = 0; i < 4; i++)
         x[i] = sizeof(T) == 2 ? pack_bf16(v[8 * j + 2 * i], v[8 * j + 2 * i + 1]) : __float_as_uint(v[4 * j + i]);
-      st_shared_v4(at(box, piece0 + j), x[0], x[1], x[2], x[3]);
+      st_shared_v4(at(line, piece0 + j), x[0], x[1], x[2], x[3]);
     }
   }
 };
 
-// The end of a map on 32 neighbouring columns of a row, step by step for all of them, so that the
-// chains of 32 values (8 counters) are under way at once.
-template <int END, typename T>
-__device__ __forceinline__ void end32(const TcArgs& g, const act::DropKey& key, int64_t row, int col, int piece0,
-                                      uint32_t ybox, uint32_t pbox, float (&v)[32]) {
+// What the end of a map does: dropout (counters of 32 or of 64 bits) and a residual.
+enum { kNoDrop = 0, kDrop32 = 1, kDrop64 = 2 };
+
+// The end of a map on 16 neighbouring columns of a row, step by step for all of them, so that the
+// chains of 16 values (4 counters) are under way at once.  quad: the first one's counter.
+template <int END, typename T, int DROP, bool kRes, typename Q>
+__device__ __forceinline__ void end16(const TcArgs& g, const act::DropKey& key, Q quad, int col, int piece0, uint32_t yline,
+                                      uint32_t pline, float (&v)[16]) {
   constexpr bool kFast = sizeof(T) == 2;
   if constexpr (END == kEndFwd) {
     if (g.e.bias) {
-      if (col + 32 <= g.N) {
+      if ((g.N & 3) == 0) {  // (four columns past the last ones get biases that nobody looks at)
 #pragma unroll
-        for (int i = 0; i < 32; i += 4) {
-          const float4 b = *reinterpret_cast<const float4*>(g.e.bias + col + i);
+        for (int i = 0; i < 16; i += 4) {
+          const float4 b = *reinterpret_cast<const float4*>(g.e.bias + min(col + i, g.N - 4));
           v[i] += b.x, v[i + 1] += b.y, v[i + 2] += b.z, v[i + 3] += b.w;
         }
       } else {
 #pragma unroll
-        for (int i = 0; i < 32; i++)
-          if (col + i < g.N) v[i] += g.e.bias[col + i];
+        for (int i = 0; i < 16; i++) v[i] += g.e.bias[min(col + i, g.N - 1)];
       }
     }
-    if (g.store_pre) Line<T>::store(pbox, piece0, v);
+    if (g.store_pre) Line<T>::store(pline, piece0, v);
     act::apply<kFast>(g.e.act, v);
   }
   if constexpr (END == kEndDx) {
     if (g.load_pre) {
-      float u[32];
-      Line<T>::load(pbox, piece0, u);
+      float u[16];
+      Line<T>::load(pline, piece0, u);
       act::slope<kFast>(g.e.act, u, v);
 #pragma unroll
-      for (int i = 0; i < 32; i++) v[i] = u[i];
+      for (int i = 0; i < 16; i++) v[i] = u[i];
     }
   }
+  if constexpr (DROP != kNoDrop || kRes) {
+    float r[16];
+    if constexpr (kRes) {
+      Line<T>::load(yline, piece0, r);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; i++) r[i] = 0.f;
+    }
+    if constexpr (DROP != kNoDrop) {
+      act::keep_by<16>({g.e.rng, g.e.threshold, g.e.scale}, key, quad, v, r);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; i++) r[i] += v[i];
+    }
+    Line<T>::store(yline, piece0, r);
+  } else {
+    Line<T>::store(yline, piece0, v);
+  }
+}
+// f(v, i) fills the i-th 16 of n * 16 values.
+template <int END, typename T, int DROP, bool kRes, int n, typename Q, typename F>
+__device__ __forceinline__ void end_loop(const TcArgs& g, const act::DropKey& key, Q quad, int col, uint32_t yline,
+                                         uint32_t pline, F&& f) {
+  // (results that are in registers already need constant indexes)
+#pragma unroll(sizeof(T) == 2 ? 1 : n)
+  for (int i = 0; i < n; i++) {
+    float v[16];
+    f(v, i);
+    end16<END, T, DROP, kRes>(g, key, (Q)(quad + 4 * i), col + 16 * i, Line<T>::kPieces * i, yline, pline, v);
+  }
+}
+template <int END, typename T, int n, typename F>
+__device__ __forceinline__ void end_chunk(const TcArgs& g, const act::DropKey& key, int64_t row, int col, uint32_t yline,
+                                          uint32_t pline, F&& f) {
   if (END != kEndRaw && g.e.rng) {
     const uint64_t quad = (uint64_t)row * (uint64_t)((g.N + 3) >> 2) + (uint64_t)(col >> 2);
-#pragma unroll
-    for (int i = 0; i < 8; i++) act::keep4({g.e.rng, g.e.threshold, g.e.scale}, key, quad + i, v + 4 * i);
+    // one branch for a warp
+    if (__all_sync(0xffffffffu, ((quad + 4 * n) >> 32) == 0)) {
+      const uint32_t q = (uint32_t)quad;
+      if (g.load_res) end_loop<END, T, END != kEndRaw ? kDrop32 : 0, true, n>(g, key, q, col, yline, pline, f);
+      else end_loop<END, T, END != kEndRaw ? kDrop32 : 0, false, n>(g, key, q, col, yline, pline, f);
+    } else {
+      if (g.load_res) end_loop<END, T, END != kEndRaw ? kDrop64 : 0, true, n>(g, key, quad, col, yline, pline, f);
+      else end_loop<END, T, END != kEndRaw ? kDrop64 : 0, false, n>(g, key, quad, col, yline, pline, f);
+    }
+  } else {
+    if (g.load_res) end_loop<END, T, kNoDrop, true, n>(g, key, 0u, col, yline, pline, f);
+    else end_loop<END, T, kNoDrop, false, n>(g, key, 0u, col, yline, pline, f);
   }
-  if (g.load_res) {
-    float r[32];
-    Line<T>::load(ybox, piece0, r);
-#pragma unroll
-    for (int i = 0; i < 32; i++) v[i] += r[i];
-  }
-  Line<T>::store(ybox, piece0, v);
 }
 
 // A box between shared memory and rows that TMA cannot address, by a warp.
@@ -221,21 +279,27 @@ __device__ __forceinline__ void box_by_lanes(T* rows, int64_t ld, int64_t M, int
 
 // An epilogue warp's boxes.  A box is filled by loads that were issued one chunk earlier (two boxes
 // take turns), or both serve one chunk where it has two inputs or two results.
-template <int END, typename T>
+template <int END, typename T, int kPer>
 struct Boxes {
   const TcArgs& g;
   uint32_t base;       // shared address of the warp's two boxes
   uint64_t* bar;       // two barriers
   uint32_t phases = 0; // one bit a barrier
   int turn = 0;
-  const bool both;
+  const bool both;     // both boxes serve one chunk
+  const bool serial;   // a chunk's loads start after the one before has left
   const int loads;
   static constexpr int kCols = 128 / sizeof(T);
   __device__ __forceinline__ Boxes(const TcArgs& g_, uint32_t base_, uint64_t* bar_)
-      : g(g_), base(base_), bar(bar_), both(g_.store_pre || (g_.load_res && g_.load_pre)), loads(g_.load_res + g_.load_pre) {}
+      : g(g_),
+        base(base_),
+        bar(bar_),
+        both(kPer == 2 && (g_.store_pre || (g_.load_res && g_.load_pre))),
+        serial(kPer == 1 || both),
+        loads(g_.load_res + g_.load_pre) {}
 
   // Where y and the residual, and the pre-activations lie for the next chunk processed.
-  __device__ __forceinline__ uint32_t ybox() const { return base + (both ? 0 : turn * kBox); }
+  __device__ __forceinline__ uint32_t ybox() const { return base + (serial ? 0 : turn * kBox); }
   __device__ __forceinline__ uint32_t pbox() const { return both ? base + kBox : ybox(); }
 
   // Starts the loads of a chunk, `ahead` chunks after the next one processed; its box's last store
@@ -244,7 +308,7 @@ struct Boxes {
     if (!loads || g.plain) return;
     if ((threadIdx.x & 31) == 0) {
       bulk_wait_read<0>();
-      const int b = both ? 0 : (turn + ahead) & 1;
+      const int b = serial ? 0 : (turn + ahead) & 1;
       mbar_expect_tx(&bar[b], loads * kBox);
       const uint32_t box = base + b * kBox;
       if (g.load_res) load(box, &g.res, col, (int)row, &bar[b]);
@@ -269,13 +333,13 @@ struct Boxes {
       return true;
     }
     if (loads) {
-      const int b = both ? 0 : turn;
+      const int b = serial ? 0 : turn;
       const bool ok = mbar_wait_w(&bar[b], (phases >> b) & 1u, ab, status);
       phases ^= 1u << b;
       return ok;
     }
     if ((threadIdx.x & 31) == 0) {
-      if (both) bulk_wait_read<0>();
+      if (serial) bulk_wait_read<0>();
       else bulk_wait_read<1>();
     }
     __syncwarp();
@@ -304,15 +368,16 @@ struct Boxes {
   }
 };
 
-template <int END, typename T, int PARTS>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_linear_tc(const __grid_constant__ TcArgs g) {
+template <int END, typename T, int PARTS, int kGroups, int kPer>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Block<kGroups, kPer>::kThreads, 1) k_linear_tc(const __grid_constant__ TcArgs g) {
   constexpr bool kFlush = sizeof(T) == 4;  // fp32 results
+  using B = Block<kGroups, kPer>;
   extern __shared__ __align__(1024) uint8_t raw[];
-  __shared__ uint64_t full[kMaxStages], empty[kMaxStages], acc_full[2], acc_empty[2], drain, in_full[8][2];
+  __shared__ uint64_t full[kMaxStages], empty[kMaxStages], acc_full[2], acc_empty[2], drain, in_full[4 * kGroups][2];
   __shared__ uint32_t tmem_slot;
   __shared__ Abort abort_;
   uint8_t* smem = raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u);
-  const uint32_t stage0 = smem_u32(smem), boxes = stage0 + kStageRoom, ones = boxes + kBoxes;
+  const uint32_t stage0 = smem_u32(smem), boxes = stage0 + B::kStageRoom, ones = boxes + B::kBoxes;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t rank = cluster_rank();
   const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
@@ -321,8 +386,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_linea
   if (tid == 0) {
     abort_.flag = 0;
     for (int i = 0; i < kMaxStages; i++) mbar_init(&full[i], 1), mbar_init(&empty[i], 1);
-    for (int i = 0; i < 2; i++) mbar_init(&acc_full[i], 1), mbar_init(&acc_empty[i], 16);
-    for (int i = 0; i < 16; i++) mbar_init(&in_full[i >> 1][i & 1], 1);
+    for (int i = 0; i < 2; i++) mbar_init(&acc_full[i], 1), mbar_init(&acc_empty[i], 8 * kGroups);
+    for (int i = 0; i < 8 * kGroups; i++) mbar_init(&in_full[i >> 1][i & 1], 1);
     mbar_init(&drain, 1);
     fence_mbar_init();
   }
@@ -348,10 +413,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_linea
       const int bhalf = g.bn >> 1;
       uint32_t issued = 0;
       bool ok = true;
-      for (int u = pair; u < g.units && ok; u += pairs) {
-        const Unit w = unit_of(g, u);
-        const int m = w.m0 + (int)rank * 128, n = w.n * g.bn + (int)rank * bhalf;
-        for (int s = 0; s < w.blocks * PARTS; s++) {
+      for (Unit w(g, pair); w.left > 0 && ok; w.next(g, pairs)) {
+        const int m = w.m * 256 + (int)rank * 128, n = w.n * g.bn + (int)rank * bhalf, blocks = w.blocks(g);
+        const int64_t k0 = w.k0(g);
+        Unit nw = w;
+        nw.next(g, pairs);
+        if (g.ahead && nw.left > 0) {
+          // A's rows lie next to each other: they come from HBM in one piece, not in the 128-byte columns that the
+          // stages take.
+          const int64_t row = (int64_t)nw.m * 256 + rank * 128, rows = g.M - row < 128 ? g.M - row : 128;
+          if (rows > 0) bulk_prefetch(g.ahead + zero + row * g.K * 2, (uint32_t)(rows * g.K * 2));
+        }
+        for (int s = 0; s < blocks * PARTS; s++) {
           const int kb = s / PARTS, part = s - kb * PARTS;
           if (!mbar_wait(&empty[ring.i], ring.pass ^ 1u, ab, status)) {
             ok = false;
@@ -359,7 +432,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_linea
           }
           if (rank == 0) mbar_expect_tx(&full[ring.i], 2 * g.stage_bytes);
           const uint32_t bar = bar0 + 8 * ring.i, a = stage0 + ring.i * g.stage_bytes, b = a + kABytes;
-          const int k = (int)(w.k0 + (int64_t)kb * 64);
+          const int k = (int)(k0 + (int64_t)kb * 64);
           if (g.a_mn) {
             tma_load_pair(a, &g.a, m, k, part, bar);
             tma_load_pair(a + 8192, &g.a, m + 64, k, part, bar);
@@ -387,11 +460,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_linea
       bool ok = true, last_sums = false;
       const uint32_t a_lo0 = sdesc_lo(stage0, g.a_mn ? 8192 : 16), b_lo0 = sdesc_lo(stage0 + kABytes, g.b_mn ? 8192 : 16);
       const uint32_t ones_lo = sdesc_lo(ones, 128), stage_step = g.stage_bytes >> 4;
-      for (int u = pair; u < g.units && ok; u += pairs) {
-        const Unit w = unit_of(g, u);
+      for (Unit w(g, pair); w.left > 0 && ok; w.next(g, pairs)) {
         const bool sums = g.sums && w.n == 0;
-        for (int kb = 0; kb < w.blocks && ok; kb += g.seg) {
-          const int half = h.pick(sums), end = min(kb + g.seg, w.blocks);
+        const int blocks = w.blocks(g);
+        for (int kb = 0; kb < blocks && ok; kb += g.seg) {
+          const int half = h.pick(sums), end = min(kb + g.seg, blocks);
           ok = mbar_wait_pair_w(&acc_empty[half], (h.uses(half) & 1u) ^ 1u, ab, status);
           // Into or out of a unit with sums, the other half has to be read out as well.
           if (ok && sums != last_sums && h.uses(half ^ 1))
@@ -453,32 +526,32 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_linea
   } else {
     const int e = warp - 2, wg = e >> 2, sub = warp & 3;
     const uint32_t lanes = tmem + ((uint32_t)(sub * 32) << 16), free0 = leader_addr(&acc_empty[0]);
-    Boxes<END, T> box(g, boxes + e * 2 * kBox, in_full[e]);
+    Boxes<END, T, kPer> box(g, boxes + e * kPer * kBox, in_full[e]);
     const act::DropKey key = lin::drop_key(g.e);
     Halves h;
     bool ok = true;
-    auto row_of = [&](const Unit& w) { return (int64_t)w.m0 + rank * 128 + sub * 32; };
+    auto row_of = [&](const Unit& w) { return (int64_t)w.m * 256 + rank * 128 + sub * 32; };
     auto release = [&](int half) {
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive_leader(free0 + 8 * half);
     };
     if constexpr (!kFlush) {
-      // The pair's tiles as one sequence of chunks of 64 columns, of which the warpgroups take every other one.
+      // The pair's tiles as one sequence of chunks of 64 columns, which the warpgroups take in turn.
       const int chunks = g.bn >> 6;
-      auto later = [&](int& u, int& c) {  // this warpgroup's next chunk
-        c += 2;
-        while (c >= chunks) c -= chunks, u += pairs;
+      auto place = [&](Unit& w, int& c) {  // from a chunk number past the unit's to the unit that it is in
+        while (c >= chunks) c -= chunks, w.next(g, pairs);
       };
-      int c = wg, nu = pair, nc = wg;  // (nu, nc): the chunk whose loads start next
-      while (nc >= chunks) nc -= chunks, nu += pairs;
-      if (nu < g.units) {
-        const Unit w = unit_of(g, nu);
-        box.start(0, row_of(w), w.n * g.bn + nc * 64);
-      }
-      later(nu, nc);
-      for (int u = pair; u < g.units && ok; u += pairs) {
-        const Unit w = unit_of(g, u);
+      int c = wg, nc = wg;
+      Unit nw(g, pair);  // (nw, nc): the chunk whose loads start next
+      place(nw, nc);
+      auto start_next = [&](int ahead) {
+        if (nw.left > 0) box.start(ahead, row_of(nw), nw.n * g.bn + nc * 64);
+        nc += kGroups;
+        place(nw, nc);
+      };
+      if (box.loads) start_next(0);
+      for (Unit w(g, pair); w.left > 0 && ok; w.next(g, pairs)) {
         const int64_t row0 = row_of(w);
         const int half = h.pick(false);
         ok = mbar_wait_w(&acc_full[half], h.uses(half) & 1u, ab, status);
@@ -486,32 +559,23 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_linea
         h.use(half);
         tc_fence_after();
         if (c >= chunks) release(half);
-        for (; c < chunks && ok; c += 2) {
+        for (; c < chunks && ok; c += kGroups) {
           const int col = w.n * g.bn + c * 64;
-          if (!box.both && nu < g.units) {
-            const Unit x = unit_of(g, nu);
-            box.start(1, row_of(x), x.n * g.bn + nc * 64);
-          }
-          uint32_t r[2][32];
-          tmem_ld32(lanes + half * 256 + c * 64, r[0]);
-          tmem_ld32(lanes + half * 256 + c * 64 + 32, r[1]);
+          if (box.loads && !box.serial) start_next(1);
           ok = box.ready(row0, col, ab, status);
-          tmem_wait_ld2(r[0], r[1]);
-          if (c + 2 >= chunks) release(half);
           if (!ok) break;
+          const uint32_t from = lanes + half * 256 + c * 64;
+          end_chunk<END, T, 4>(g, key, row0 + lane, col, box.ybox() + lane * 128, box.pbox() + lane * 128,
+                               [&](float(&v)[16], int i) {
+                                 uint32_t r[16];
+                                 tmem_ld16(from + 16 * i, r);
+                                 tmem_wait_ld(r);
+                                 if (i == 3 && c + kGroups >= chunks) release(half);
 #pragma unroll
-          for (int p = 0; p < 2; p++) {
-            float v[32];
-#pragma unroll
-            for (int i = 0; i < 32; i++) v[i] = __uint_as_float(r[p][i]);
-            end32<END, T>(g, key, row0 + lane, col + 32 * p, 4 * p, box.ybox(), box.pbox(), v);
-          }
+                                 for (int j = 0; j < 16; j++) v[j] = __uint_as_float(r[j]);
+                               });
           box.send(row0, col, w.split);
-          if (box.both && nu < g.units) {
-            const Unit x = unit_of(g, nu);
-            box.start(1, row_of(x), x.n * g.bn + nc * 64);
-          }
-          later(nu, nc);
+          if (box.loads && box.serial) start_next(1);
         }
         c -= chunks;
       }
@@ -519,14 +583,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_linea
       // The warpgroups take half of a tile's columns each and add its segments up in registers.
       constexpr int kMost = PARTS == 1 ? 4 : 2;
       const int chunks = g.bn >> 6, first = wg * (g.bn >> 1);
-      for (int u = pair; u < g.units && ok; u += pairs) {
-        const Unit w = unit_of(g, u);
+      for (Unit w(g, pair); w.left > 0 && ok; w.next(g, pairs)) {
         const int64_t row0 = row_of(w);
-        const int col = w.n * g.bn + first;
+        const int col = w.n * g.bn + first, blocks = w.blocks(g);
         const bool sums = g.sums && w.n == 0;
         float acc[kMost][32], sum = 0.f;
         box.start(0, row0, col);
-        for (int kb = 0; kb < w.blocks && ok; kb += g.seg) {
+        for (int kb = 0; kb < blocks && ok; kb += g.seg) {
           const int half = h.pick(sums);
           ok = mbar_wait_w(&acc_full[half], h.uses(half) & 1u, ab, status);
           if (!ok) break;
@@ -571,12 +634,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_linea
 #pragma unroll
         for (int i = 0; i < kMost; i++) {
           if (i >= chunks || !ok) continue;
-          if (!box.both && i + 1 < chunks) box.start(1, row0, col + (i + 1) * 32);
+          if (!box.serial && i + 1 < chunks) box.start(1, row0, col + (i + 1) * 32);
           ok = box.ready(row0, col + i * 32, ab, status);
           if (!ok) continue;
-          end32<END, T>(g, key, row0 + lane, col + i * 32, 0, box.ybox(), box.pbox(), acc[i]);
+          end_chunk<END, T, 2>(g, key, row0 + lane, col + i * 32, box.ybox() + lane * 128, box.pbox() + lane * 128,
+                               [&](float(&v)[16], int h) {
+#pragma unroll
+                                 for (int j = 0; j < 16; j++) v[j] = acc[i][16 * h + j];
+                               });
           box.send(row0, col + i * 32, w.split);
-          if (box.both && i + 1 < chunks) box.start(1, row0, col + (i + 1) * 32);
+          if (box.serial && i + 1 < chunks) box.start(1, row0, col + (i + 1) * 32);
         }
       }
     }
@@ -691,13 +758,15 @@ bool make_map(CUtensorMap* map, const void* p, int size, int64_t cols, int64_t r
             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int END, typename T, int PARTS>
-cudaError_t run(const TcArgs& g, cudaStream_t st) {
-  const auto k_tc = k_linear_tc<END, T, PARTS>;
+template <int END, typename T, int PARTS, int kGroups, int kPer>
+cudaError_t run(TcArgs& g, cudaStream_t st) {
+  using B = Block<kGroups, kPer>;
+  const auto k_tc = k_linear_tc<END, T, PARTS, kGroups, kPer>;
+  g.stages = std::min<int>(kMaxStages, (int)(B::kStageRoom / g.stage_bytes));
   cudaError_t e = allow_smem<kSmem>(k_tc);
   if (e != cudaSuccess) return e;
   const int pairs = std::min(g.units, num_sms() / 2);
-  return launch(k_tc, dim3((unsigned)(2 * pairs)), dim3(kThreads), kSmem, st, g);
+  return launch(k_tc, dim3((unsigned)(2 * pairs)), dim3(B::kThreads), kSmem, st, g);
 }
 
 }  // namespace
@@ -735,9 +804,13 @@ cudaError_t linear_tc(const LinearProblem& p, const LinearPlan& plan, const Line
   g.a_mn = dw, g.b_mn = p.op != kLinFwd;
   g.bn = linear_tile_n(p.N, g.b_mn, f32);
   g.n_tiles = (p.N + g.bn - 1) / g.bn;
-  g.units = (int)((p.M + 255) / 256) * g.n_tiles * plan.splits;
+  g.m_tiles = (int)((p.M + 255) / 256);
+  g.tiles = g.m_tiles * g.n_tiles;
+  g.units = g.tiles * plan.splits;
+  const int pairs = std::min(g.units, num_sms() / 2);
+  g.step_n = pairs % g.n_tiles, g.step_m = pairs / g.n_tiles % g.m_tiles, g.step_split = pairs / g.tiles;
   g.stage_bytes = kABytes + (uint32_t)g.bn / 2 * 128;
-  g.stages = std::min<int>(kMaxStages, (int)(kStageRoom / g.stage_bytes));
+  const bool raw = split || dw;
   // Segments: where results are fp32, 256 terms of three parts, 512 of one.
   g.seg = split || dw || f32 ? (f32 ? 4 : 8) : 1 << 30;
   g.idesc = idesc_bf16(256, g.bn, g.a_mn, g.b_mn);
@@ -747,7 +820,6 @@ cudaError_t linear_tc(const LinearProblem& p, const LinearPlan& plan, const Line
   const int lda = linear_pitch((int)(g.a_mn ? p.M : p.K)), ldb = linear_pitch((int)(g.b_mn ? p.N : p.K));
   bool ok = g.a_mn ? make_map(&g.a, p.a, 2, p.M, p.K, parts, lda, 64) : make_map(&g.a, p.a, 2, p.K, p.M, parts, lda, 128);
   ok = ok && (g.b_mn ? make_map(&g.b, p.b, 2, p.N, p.K, parts, ldb, 64) : make_map(&g.b, p.b, 2, p.K, p.N, parts, ldb, g.bn / 2));
-  const bool raw = split || dw;
   const int size = raw || f32 ? 4 : 2;
   float* part = static_cast<float*>(scratch);
   g.ldy = p.N;
@@ -762,6 +834,7 @@ cudaError_t linear_tc(const LinearProblem& p, const LinearPlan& plan, const Line
     g.store_pre = e.pre_out != nullptr;
   }
   g.sums = dw && e.sums;
+  if (g.n_tiles == 1 && !split && !dw && !f32 && p.K % 8 == 0) g.ahead = static_cast<const char*>(p.a);
   g.plain = g.ldy * size % 16 != 0;
   if (!g.plain) {
     ok = ok && make_map(&g.y, g.e.y, size, g.ldy, p.M, plan.splits, g.ldy, 32);
@@ -772,9 +845,16 @@ cudaError_t linear_tc(const LinearProblem& p, const LinearPlan& plan, const Line
   if (!ok) return cudaErrorInvalidValue;
   cudaError_t err;
   using B = __nv_bfloat16;
-  if (raw) err = f32 ? run<kEndRaw, float, 3>(g, st) : run<kEndRaw, float, 1>(g, st);
-  else if (p.op == kLinFwd) err = f32 ? run<kEndFwd, float, 3>(g, st) : run<kEndFwd, B, 1>(g, st);
-  else err = f32 ? run<kEndDx, float, 3>(g, st) : run<kEndDx, B, 1>(g, st);
+  const bool few = g.store_pre || (g.load_res && g.load_pre) || p.K > kShortK;
+  if (raw) err = f32 ? run<kEndRaw, float, 3, 2, 2>(g, st) : run<kEndRaw, float, 1, 2, 2>(g, st);
+  else if (p.op == kLinFwd)
+    err = f32    ? run<kEndFwd, float, 3, 2, 2>(g, st)
+          : few  ? run<kEndFwd, B, 1, 3, 2>(g, st)
+                 : run<kEndFwd, B, 1, kManyGroups, 1>(g, st);
+  else
+    err = f32    ? run<kEndDx, float, 3, 2, 2>(g, st)
+          : few  ? run<kEndDx, B, 1, 3, 2>(g, st)
+                 : run<kEndDx, B, 1, kManyGroups, 1>(g, st);
   if (err != cudaSuccess || !split) return err;
   return linear_join(p, plan.splits, part, g.part_sums, e, st);
 }

@@ -72,6 +72,10 @@ __device__ __forceinline__ void tma_store(const CUtensorMap* map, int c0, int c1
                "r"(c0), "r"(c1), "r"(c2), "r"(src)
                : "memory");
 }
+// To L2 (16-byte aligned, a multiple of 16 bytes).
+__device__ __forceinline__ void bulk_prefetch(const void* p, uint32_t bytes) {
+  asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(p), "r"(bytes) : "memory");
+}
 __device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
 // All but the newest kPending groups of this thread's stores have read their shared memory.
 template <int kPending>
