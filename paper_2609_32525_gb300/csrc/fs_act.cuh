@@ -112,37 +112,36 @@ __device__ __forceinline__ void keep(const Drop& d, const DropKey& k, uint64_t q
 //
 // kFast: for values that are rounded to bf16 afterwards (half a step is 2^-9 of the value).
 //
-// GELU is u Phi(u).  For a = |u|, Phi(-a) = e^(-a^2/2) Q(a) with Q(a) = erfcx(a / sqrt 2) / 2, a
-// smooth function that falls from 1/2 to 0.077 over [0, 5]: a polynomial of degree 8 (weighted
-// least squares, reweighted towards the minimax fit) is within 1.6e-4 of itself there, and past
-// a = 5, where gelu(-a) is below 1.5e-6, Q stays at Q(5) and the Gaussian goes on falling.  One
-// exponential and eight fused multiply-adds, and the exponential serves the derivative
-// Phi(u) + u e^(-u^2/2) / sqrt(2 pi) too.  Two values share the instructions (f32x2).
+// All of them two values at a time (f32x2 instructions).
 //
-// e: e^(-a^2/2); the result is Phi(-a).  a <= kGaussEnd.
-__device__ __forceinline__ uint64_t twice(float x) { return tc::pack2(__float_as_uint(x), __float_as_uint(x)); }
-__device__ __forceinline__ uint64_t pair(float x, float y) { return tc::pack2(__float_as_uint(x), __float_as_uint(y)); }
-__device__ __forceinline__ uint64_t gauss_tail2(float a0, float a1, uint64_t& e) {
-  const uint64_t a = pair(a0, a1), s = tc::mul2(tc::mul2(a, twice(-0.7213475204f)), a);  // log2(e) / 2
-  e = pair(tc::ex2(tc::lo_f(s)), tc::ex2(tc::hi_f(s)));
-  const uint64_t b = pair(fminf(a0, 5.f), fminf(a1, 5.f));
-  uint64_t q = twice(5.7904302e-06f);
-  q = tc::fma2(q, b, twice(-0.00014531538f));
-  q = tc::fma2(q, b, twice(0.0015831057f));
-  q = tc::fma2(q, b, twice(-0.0099215629f));
-  q = tc::fma2(q, b, twice(0.040258871f));
-  q = tc::fma2(q, b, twice(-0.11416839f));
-  q = tc::fma2(q, b, twice(0.24129194f));
-  q = tc::fma2(q, b, twice(-0.39726451f));
-  q = tc::fma2(q, b, twice(0.49994163f));
-  return tc::mul2(e, q);
-}
+// GELU is u Phi(u).  For a = |u|, Phi(-a) = e^(-a^2/2) Q(a) with Q(a) = erfcx(a / sqrt 2) / 2, a smooth function
+// that falls slowly; the exponential serves the derivative Phi(u) + u e^(-u^2/2) / sqrt(2 pi) too.
+//   kFast: a polynomial of degree 8 on [0, 5], within 1.6e-4 of Q; past 5, where gelu(-a) is below 1.5e-6, Q stays
+//   at Q(5) and the Gaussian goes on falling.
+//   else: Q(a) (1 + 2 a) as a polynomial of degree 9 in (a - k) / (a + k) on [0, 15], within 1.3e-8 (the form of
+//   Shepherd and Laframboise, "Chebyshev approximation of (1 + 2x) exp(x^2) erfc x in 0 <= x < inf", 1981).
+//   Quotients get one Newton step, and the exponent's rounding is put back after the exponential.
+// Both polynomials are weighted least-squares fits, reweighted towards the minimax one.
 constexpr float kInvSqrt2Pi = 0.3989422804014327f;
 // Past this a the Gaussian is 0 in fp32; a product of it with an infinite u would be NaN.
 constexpr float kGaussEnd = 15.f;
 // Past this u the sigmoid is 1 (or 0) in fp32, and with u held there no infinity meets a 0.
 constexpr float kSigmoidEnd = 110.f;
+constexpr float kLog2eHi = 1.442695041f, kLog2eLo = 1.925963033e-08f, kLn2 = 0.6931471806f;
 
+__device__ __forceinline__ uint64_t twice(float x) { return tc::pack2(__float_as_uint(x), __float_as_uint(x)); }
+__device__ __forceinline__ uint64_t pair(float x, float y) { return tc::pack2(__float_as_uint(x), __float_as_uint(y)); }
+__device__ __forceinline__ float rcp(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// 2^x, with subnormal results.
+__device__ __forceinline__ float ex2_full(float x) {
+  float y;
+  asm("ex2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
 // The larger (smaller) of two; NaN where one is.
 __device__ __forceinline__ float max_nan(float a, float b) {
   float d;
@@ -155,45 +154,94 @@ __device__ __forceinline__ float min_nan(float a, float b) {
   return d;
 }
 
-__device__ __forceinline__ float gelu(float u) { return u < -kGaussEnd ? 0.f : u * normcdff(u); }
-__device__ __forceinline__ float gelu_slope(float u) {
-  const float v = max_nan(min_nan(u, kGaussEnd), -kGaussEnd);
-  return fmaf(v * kInvSqrt2Pi, expf(-0.5f * v * v), normcdff(v));
+template <int n>
+__device__ __forceinline__ uint64_t poly2(const float (&c)[n], uint64_t x) {
+  uint64_t q = twice(c[n - 1]);
+#pragma unroll
+  for (int i = n - 2; i >= 0; i--) q = tc::fma2(q, x, twice(c[i]));
+  return q;
+}
+// Phi(-a) for 0 <= a <= kGaussEnd; e: e^(-a^2/2).
+template <bool kFast>
+__device__ __forceinline__ uint64_t gauss_tail2(float a0, float a1, uint64_t& e) {
+  const uint64_t a = pair(a0, a1);
+  if constexpr (kFast) {
+    constexpr float c[9] = {0.49994163f,   -0.39726451f,  0.24129194f,    -0.11416839f,  0.040258871f,
+                            -0.0099215629f, 0.0015831057f, -0.00014531538f, 5.7904302e-06f};
+    const uint64_t s = tc::mul2(tc::mul2(a, twice(-0.5f * kLog2eHi)), a);
+    e = pair(tc::ex2(tc::lo_f(s)), tc::ex2(tc::hi_f(s)));
+    return tc::mul2(e, poly2(c, pair(fminf(a0, 5.f), fminf(a1, 5.f))));
+  } else {
+    constexpr float k = 2.8125f;
+    constexpr float c[10] = {0.849999964f,     0.0238276552f,  -0.168504149f,   0.131846741f,    -0.0378766023f,
+                             -0.00768018235f, 0.00614848454f, 0.00123171532f, -0.000851653749f, -0.000309873198f};
+    const uint64_t up = tc::add2(a, twice(k)), down = tc::add2(a, twice(-k)), den = tc::fma2(a, twice(2.f), twice(1.f));
+    const uint64_t both = tc::mul2(up, den), minus = twice(-1.f);
+    const uint64_t r = pair(rcp(tc::lo_f(both)), rcp(tc::hi_f(both)));
+    const uint64_t up_r = tc::mul2(r, den);
+    uint64_t t = tc::mul2(down, up_r), s = tc::mul2(r, up);
+    t = tc::fma2(tc::fma2(tc::mul2(t, minus), up, down), up_r, t);
+    s = tc::fma2(s, tc::fma2(tc::mul2(s, minus), den, twice(1.f)), s);
+    // a^2 = h + l; the exponent y = -h log2(e) / 2 and what it leaves out
+    const uint64_t h = tc::mul2(a, a), l = tc::fma2(a, a, tc::mul2(h, minus));
+    const uint64_t y = tc::mul2(h, twice(-0.5f * kLog2eHi));
+    uint64_t left = tc::fma2(h, twice(-0.5f * kLog2eHi), tc::mul2(y, minus));
+    left = tc::fma2(h, twice(-0.5f * kLog2eLo), left);
+    left = tc::fma2(l, twice(-0.5f * kLog2eHi), left);
+    e = pair(tc::ex2(tc::lo_f(y)), tc::ex2(tc::hi_f(y)));
+    e = tc::fma2(tc::mul2(e, twice(kLn2)), left, e);
+    return tc::mul2(tc::mul2(e, s), poly2(c, t));
+  }
 }
 // max(u, 0) - a Phi(-a)
+template <bool kFast>
 __device__ __forceinline__ void gelu2(float& u0, float& u1) {
   const float a0 = fminf(fabsf(u0), kGaussEnd), a1 = fminf(fabsf(u1), kGaussEnd);
   uint64_t e;
-  const uint64_t t = gauss_tail2(a0, a1, e);
+  const uint64_t t = gauss_tail2<kFast>(a0, a1, e);
   const uint64_t y = tc::fma2(t, pair(-a0, -a1), pair(max_nan(u0, 0.f), max_nan(u1, 0.f)));
   u0 = tc::lo_f(y), u1 = tc::hi_f(y);
 }
+template <bool kFast>
 __device__ __forceinline__ void gelu_slope2(float& u0, float& u1) {
   const float v0 = max_nan(min_nan(u0, kGaussEnd), -kGaussEnd), v1 = max_nan(min_nan(u1, kGaussEnd), -kGaussEnd);
   uint64_t e;
-  const uint64_t t = gauss_tail2(fabsf(v0), fabsf(v1), e);
+  const uint64_t t = gauss_tail2<kFast>(fabsf(v0), fabsf(v1), e);
   const float t0 = tc::lo_f(t), t1 = tc::hi_f(t);
   const uint64_t cdf = pair(v0 > 0.f ? 1.f - t0 : t0, v1 > 0.f ? 1.f - t1 : t1);
   const uint64_t y = tc::fma2(tc::mul2(pair(v0, v1), twice(kInvSqrt2Pi)), e, cdf);
   u0 = tc::lo_f(y), u1 = tc::hi_f(y);
 }
 
-// By e^-|u|, which never overflows, so that the left tail keeps its values.
+// SILU by e^-|u|, which never overflows, so that the left tail keeps its values; |u| <= kSigmoidEnd.
 template <bool kFast>
-__device__ __forceinline__ float sigmoid(float u) {
-  const float e = kFast ? __expf(-fabsf(u)) : expf(-fabsf(u)), top = u < 0.f ? e : 1.f;
-  return kFast ? __fdividef(top, 1.f + e) : top / (1.f + e);
+__device__ __forceinline__ uint64_t sigmoid2(float u0, float u1) {
+  const uint64_t a = pair(fabsf(u0), fabsf(u1)), y = tc::mul2(a, twice(-kLog2eHi));
+  uint64_t e;
+  if constexpr (kFast) {
+    e = pair(tc::ex2(tc::lo_f(y)), tc::ex2(tc::hi_f(y)));
+  } else {
+    uint64_t left = tc::fma2(a, twice(-kLog2eHi), tc::mul2(y, twice(-1.f)));
+    left = tc::fma2(a, twice(-kLog2eLo), left);
+    e = pair(ex2_full(tc::lo_f(y)), ex2_full(tc::hi_f(y)));
+    e = tc::fma2(tc::mul2(e, twice(kLn2)), left, e);
+  }
+  const float e0 = tc::lo_f(e), e1 = tc::hi_f(e);
+  return tc::mul2(pair(u0 < 0.f ? e0 : 1.f, u1 < 0.f ? e1 : 1.f), pair(rcp(1.f + e0), rcp(1.f + e1)));
 }
 template <bool kFast>
-__device__ __forceinline__ float silu(float u) {
-  const float b = u < -kSigmoidEnd ? -kSigmoidEnd : u;
-  return b * sigmoid<kFast>(b);
+__device__ __forceinline__ void silu2(float& u0, float& u1) {
+  const float b0 = max_nan(u0, -kSigmoidEnd), b1 = max_nan(u1, -kSigmoidEnd);
+  // (a large u's own sigmoid is 1)
+  const uint64_t y = tc::mul2(pair(b0, b1), sigmoid2<kFast>(min_nan(b0, kSigmoidEnd), min_nan(b1, kSigmoidEnd)));
+  u0 = tc::lo_f(y), u1 = tc::hi_f(y);
 }
 template <bool kFast>
-__device__ __forceinline__ float silu_slope(float u) {
-  const float b = u > kSigmoidEnd ? kSigmoidEnd : u < -kSigmoidEnd ? -kSigmoidEnd : u;
-  const float s = sigmoid<kFast>(b);
-  return s * fmaf(b, 1.f - s, 1.f);
+__device__ __forceinline__ void silu_slope2(float& u0, float& u1) {
+  const float b0 = max_nan(min_nan(u0, kSigmoidEnd), -kSigmoidEnd), b1 = max_nan(min_nan(u1, kSigmoidEnd), -kSigmoidEnd);
+  const uint64_t s = sigmoid2<kFast>(b0, b1), rest = tc::fma2(s, twice(-1.f), twice(1.f));
+  const uint64_t y = tc::mul2(s, tc::fma2(pair(b0, b1), rest, twice(1.f)));
+  u0 = tc::lo_f(y), u1 = tc::hi_f(y);
 }
 
 // v = act(v), n values (an even number) that one loop walks, so that the chains of several are under way at once.
@@ -201,9 +249,8 @@ template <bool kFast, int ACT, int n>
 __device__ __forceinline__ void apply(float (&v)[n]) {
 #pragma unroll
   for (int i = 0; i < n; i++) {
-    if (ACT == FS_ACT_GELU && !kFast) v[i] = gelu(v[i]);
-    if (ACT == FS_ACT_GELU && kFast && i % 2 == 0) gelu2(v[i], v[i + 1]);
-    if (ACT == FS_ACT_SILU) v[i] = silu<kFast>(v[i]);
+    if (ACT == FS_ACT_GELU && i % 2 == 0) gelu2<kFast>(v[i], v[i + 1]);
+    if (ACT == FS_ACT_SILU && i % 2 == 0) silu2<kFast>(v[i], v[i + 1]);
     if (ACT == FS_ACT_RELU) v[i] = max_nan(v[i], 0.f);
   }
 }
@@ -212,9 +259,8 @@ template <bool kFast, int ACT, int n>
 __device__ __forceinline__ void slope(float (&v)[n], const float* g) {
 #pragma unroll
   for (int i = 0; i < n; i++) {
-    if (ACT == FS_ACT_GELU && !kFast) v[i] = gelu_slope(v[i]);
-    if (ACT == FS_ACT_GELU && kFast && i % 2 == 0) gelu_slope2(v[i], v[i + 1]);
-    if (ACT == FS_ACT_SILU) v[i] = silu_slope<kFast>(v[i]);
+    if (ACT == FS_ACT_GELU && i % 2 == 0) gelu_slope2<kFast>(v[i], v[i + 1]);
+    if (ACT == FS_ACT_SILU && i % 2 == 0) silu_slope2<kFast>(v[i], v[i + 1]);
     if (ACT == FS_ACT_RELU) v[i] = v[i] > 0.f ? g[i] : v[i] <= 0.f ? 0.f : v[i];
     if (ACT == FS_ACT_NONE) v[i] = g[i];
   }

@@ -12,8 +12,8 @@ Bounds, elementwise, with u = 2^-24 (fp32's half step) and h the rows' half step
 So fp32 results are within (180 + K / 128) u S and bf16 rows before their rounding (180 + K / 8) u S.
 
 Past the sum a value goes through the activation, whose slope is at most 1.13, and 1 / (1 - p).  The
-activation itself is off by at most 8 u of the larger of itself and its argument in fp32 (the functions of
-CUDA are good to 5 u, argument and product round once each), 2^-12 of itself and 2e-7 in bf16, where a
+activation itself is off by at most 8 u of the larger of itself and its argument in fp32 (what a GELU or SILU
+takes from its argument is at most half of it, and good to 16 u), 2^-12 of itself and 2e-7 in bf16, where a
 slope is off by at most 1.2e-4; in fp32 by 32 u (1 - sigmoid is off by u, times an argument below 17
 where it is not exactly 0).  The residual's addition rounds once more."""
 import numpy as np

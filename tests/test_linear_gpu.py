@@ -121,8 +121,9 @@ def test_activations_everywhere(lib, dtype, act):
     lib.fs_dropout_bwd(lib.rows_of(x.view(-1, 1)), torch.ones_like(x), t.ACTS.index(act), 0.0, None, x, dx)
     tiny = 2.0 ** -126
     if dtype == "f32":
-        # the Gaussian's argument u^2 / 2 rounds: u^2 u of the tail where it is small
-        assert (np.abs(t.host(y) - a) <= 8 * t.U * np.abs(a) * (1 + (t.host(x) < 0) * np.abs(t.host(x))) + tiny).all()
+        # Phi(-a): quotients 2 u each, the polynomial with its argument 4, the exponential 4 (2 units in the last
+        # place), four products; the sigmoid: exponential 4, reciprocal 2, two products
+        assert (np.abs(t.host(y) - a) <= 16 * t.U * np.abs(a) + tiny).all()
         assert (np.abs(t.host(dx) - s) <= 32 * t.U + tiny).all()
     else:
         assert (np.abs(t.host(y) - a) <= (2.0 ** -12 + 1.01 * 2.0 ** -8) * np.abs(a) + 2e-7).all()
