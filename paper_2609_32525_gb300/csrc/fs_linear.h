@@ -54,16 +54,14 @@ LinearPlan linear_plan(int op, int dtype, int64_t M, int N, int64_t K);
 
 cudaError_t linear_simt(const LinearProblem& p, const LinearPlan& plan, const LinearEnd& e, void* scratch,
                         cudaStream_t st);
-// p.a and p.b as the tensor cores take them: bf16 with a pitch of whole 16 bytes, fp32 as three bf16 parts
-// (linear_pack) of [rows][pitch] each.
+// bf16 operands with a pitch of whole 16 bytes (linear_pack), fp32 ones as they are.
 cudaError_t linear_tc(const LinearProblem& p, const LinearPlan& plan, const LinearEnd& e, void* scratch, cudaStream_t st);
+cudaError_t linear_tc_f32(const LinearProblem& p, const LinearPlan& plan, const LinearEnd& e, void* scratch, cudaStream_t st);
 // Columns of D in one of its tiles (fp32 operands take half the columns for two accumulators).
 int linear_tile_n(int N, bool b_mn, bool f32);
 inline int linear_pitch(int C) { return (C + 7) & ~7; }
-inline bool linear_packed(int dtype, int C) { return dtype == FS_F32 || (C & 7) != 0; }
-inline size_t linear_pack_bytes(int dtype, int64_t rows, int C) {
-  return linear_packed(dtype, C) ? (size_t)rows * linear_pitch(C) * (dtype == FS_F32 ? 6 : 2) : 0;
-}
+inline bool linear_packed(int dtype, int C) { return dtype == FS_BF16 && (C & 7) != 0; }
+inline size_t linear_pack_bytes(int64_t rows, int C) { return (size_t)rows * linear_pitch(C) * 2; }
 struct LinearPack {
   const void* src;
   void* dst;
@@ -71,7 +69,7 @@ struct LinearPack {
   int C;
 };
 // Up to three tensors in one launch, which also clears the status word.
-cudaError_t linear_pack(const LinearPack* packs, int n, int dtype, uint32_t* status, cudaStream_t st);
+cudaError_t linear_pack(const LinearPack* packs, int n, uint32_t* status, cudaStream_t st);
 // Adds up the parts of a product and ends it: part [splits][M][ld], ld the columns rounded up to a
 // multiple of 4; sums [splits][M] behind it for dW.
 cudaError_t linear_join(const LinearProblem& p, int splits, const float* part, const float* sums, const LinearEnd& e,

@@ -69,7 +69,7 @@ struct Scratch {
   void pack(bool tc, const void* p, int64_t rows, int C) {
     if (!tc || !linear_packed(dtype, C)) return;
     packs[n++] = {p, reinterpret_cast<void*>(need), rows, C};
-    need += align_up(linear_pack_bytes(dtype, rows, C), kAlign);
+    need += align_up(linear_pack_bytes(rows, C), kAlign);
   }
   size_t add(size_t bytes) {
     need += bytes;
@@ -77,7 +77,7 @@ struct Scratch {
   }
   cudaError_t launch(void* ws, cudaStream_t st) {
     for (int i = 0; i < n; i++) packs[i].dst = static_cast<char*>(ws) + reinterpret_cast<size_t>(packs[i].dst);
-    return n ? linear_pack(packs, n, dtype, static_cast<uint32_t*>(ws), st) : cudaSuccess;
+    return n ? linear_pack(packs, n, static_cast<uint32_t*>(ws), st) : cudaSuccess;
   }
   const void* at(bool tc, const void* p, int64_t rows, int C) const {
     for (int i = 0; tc && i < n; i++)
