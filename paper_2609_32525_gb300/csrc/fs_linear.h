@@ -10,6 +10,7 @@
 namespace fs {
 
 constexpr int kLinearMaxC = 8192;
+constexpr int kLinearFew = 8;   // rows of a forward that a kernel of its own takes
 
 // The three products of a linear map, each D[m, n] = sum_k A[m, k] B[n, k]:
 //   forward  D = u  [rows, Cout], A = x, B = W

@@ -117,7 +117,7 @@ Span unless(const void* p, size_t n, const void* same) { return {p == same ? nul
 LinearPlan linear_plan(int op, int dtype, int64_t M, int N, int64_t K) {
   LinearPlan p{};
   const double work = (double)M * N * (double)K;
-  p.path = work >= 4194304.0 && M >= 64 && N >= 16 && K >= 16 && std::max(M, K) < (1LL << 31) - 512;
+  p.path = work >= 4194304.0 && M > kLinearFew && N >= 16 && K >= 16 && std::max(M, K) < (1LL << 31) - 512;
   int64_t splits;
   if (p.path) {
     // Pairs of CTAs take tiles; where there are fewer than half as many tiles, sums are split into parts of
@@ -130,6 +130,7 @@ LinearPlan linear_plan(int op, int dtype, int64_t M, int N, int64_t K) {
     // Sums are split until the blocks fill the device twice, into parts of at least 64 terms.
     const int64_t tiles = ((M + 63) / 64) * ((N + 63) / 64);
     splits = std::max<int64_t>(1, std::min<int64_t>(2LL * num_sms() / tiles, (K + 63) / 64));
+    if (op == kLinFwd && M <= kLinearFew) splits = 1;
     p.per = ((K + splits - 1) / splits + 15) / 16 * 16;
   }
   p.splits = (int)((K + p.per - 1) / p.per);

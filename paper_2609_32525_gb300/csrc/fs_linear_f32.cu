@@ -27,14 +27,6 @@ constexpr uint32_t kRaw = kPieces * 2 * kLoaders * 32 * 16;  // a block's values
 constexpr size_t kSmemF32 = 1024 + kStagesF32 * kStageF32 + kBoxesF32 + kRaw + kOnes;
 static_assert(kSmemF32 + 1024 <= 232448);
 
-template <int kBytes>
-__device__ __forceinline__ void copy_async(uint32_t dst, const void* src, int have) {
-  if constexpr (kBytes == 16)
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(have) : "memory");
-  else
-    asm volatile("cp.async.ca.shared.global [%0], [%1], %3, %2;" ::"r"(dst), "l"(src), "r"(have), "n"(kBytes) : "memory");
-}
-
 // A matrix in memory.
 struct Source {
   const float* p;

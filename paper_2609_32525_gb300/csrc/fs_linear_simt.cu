@@ -110,6 +110,61 @@ __global__ void __launch_bounds__(256) k_linear_simt(SimtArgs a) {
   }
 }
 
+// Few rows through the forward: what counts is W, which is read once for four rows.  A warp owns four columns (a
+// dropout counter) and has the loads of 32 x 16 bytes of each on their way at a time; its lanes' sums are added by
+// shuffles.
+// One row, 1024 -> 4096 channels, bf16 with GELU: FS_TIME_FEW us, 31.5 with the tiles above.
+template <typename T, bool kVec>
+__global__ void __launch_bounds__(128) k_linear_few(SimtArgs a) {
+  const int64_t zero = grid_begin();
+  constexpr int kV = kVec ? 16 / (int)sizeof(T) : 1;
+  const T* x = static_cast<const T*>(a.a) + zero;
+  const T* W = static_cast<const T*>(a.b) + zero;
+  if (a.status && threadIdx.x == 0 && blockIdx.x == 0) *a.status = 0;
+  const int lane = threadIdx.x & 31, col = (blockIdx.x * 4 + (threadIdx.x >> 5)) * 4, K = (int)a.K, M = (int)a.M;
+  const act::DropKey key = lin::drop_key(a.e);
+  if (col >= a.N) return;
+  auto load = [&](const T* p, float(&v)[kV]) {
+    if constexpr (!kVec) {
+      v[0] = (float)p[0];
+    } else {
+      const uint4 w = *reinterpret_cast<const uint4*>(p);
+      const T* t = reinterpret_cast<const T*>(&w);
+#pragma unroll
+      for (int i = 0; i < kV; i++) v[i] = (float)t[i];
+    }
+  };
+  for (int r0 = 0; r0 < M; r0 += 4) {
+    float acc[4][4][2] = {};
+#pragma unroll 4
+    for (int k = lane * kV; k < K; k += 32 * kV) {
+      float w[4][kV], v[kV];
+#pragma unroll
+      for (int j = 0; j < 4; j++) load(W + (int64_t)min(col + j, a.N - 1) * K + k, w[j]);
+#pragma unroll
+      for (int r = 0; r < 4; r++) {
+        if (r0 + r >= M) break;
+        load(x + (int64_t)(r0 + r) * K + k, v);
+#pragma unroll
+        for (int j = 0; j < 4; j++)
+#pragma unroll
+          for (int i = 0; i < kV; i++) acc[r][j][i & 1] = fmaf(v[i], w[j][i], acc[r][j][i & 1]);
+      }
+    }
+    float mine[4] = {};
+#pragma unroll
+    for (int r = 0; r < 4; r++)
+#pragma unroll
+      for (int j = 0; j < 4; j++) {
+        float s = acc[r][j][0] + acc[r][j][1];
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+        if (lane == r) mine[j] = s;
+      }
+    if (lane < 4 && r0 + lane < M) lin::end4<T, kLinFwd>(a.e, key, r0 + lane, col, a.N, mine);
+  }
+}
+
 // 32 quads of columns a block; eight threads share a quad's parts (thread y takes parts y, y + 8, ...),
 // and their sums are added in order.  What counts is how many loads are on their way.
 template <typename T, int OP>
@@ -164,6 +219,10 @@ cudaError_t run_simt(const LinearProblem& p, const LinearPlan& plan, const Linea
   a.part_sums = a.part + (int64_t)plan.splits * p.M * a.ld;
   a.status = p.reset ? p.status : nullptr;
   a.e = e;
+  if (OP == kLinFwd && p.M <= kLinearFew) {
+    const bool vec = p.K % (16 / (int)sizeof(T)) == 0;
+    return launch(vec ? k_linear_few<T, true> : k_linear_few<T, false>, dim3((unsigned)((p.N + 15) / 16)), dim3(128), 0, st, a);
+  }
   const dim3 grid((unsigned)((p.M + kT - 1) / kT), (unsigned)((p.N + kT - 1) / kT), (unsigned)plan.splits);
   cudaError_t err = launch(k_linear_simt<T, OP>, grid, dim3(256), 0, st, a);
   if (err == cudaSuccess && plan.splits > 1) err = linear_join(p, plan.splits, a.part, a.part_sums, e, st);

@@ -296,6 +296,28 @@ __device__ __forceinline__ void box_by_lanes(T* rows, int64_t ld, int64_t M, int
   }
 }
 
+template <int kBytes>
+__device__ __forceinline__ void copy_async(uint32_t dst, const void* src, int have) {
+  if constexpr (kBytes == 16)
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(have) : "memory");
+  else
+    asm volatile("cp.async.ca.shared.global [%0], [%1], %3, %2;" ::"r"(dst), "l"(src), "r"(have), "n"(kBytes) : "memory");
+}
+// fp32 rows into a box by asynchronous copies, which copies_wait ends.
+__device__ __forceinline__ void box_copy(const float* rows, int64_t ld, int64_t M, int N, int64_t row0, int col0, uint32_t box) {
+  const int lane = threadIdx.x & 31, n_rows = col0 + lane < N ? (int)min(M - row0, (int64_t)32) : 0;
+  const float* p = rows + row0 * ld + col0 + lane;
+#pragma unroll 8
+  for (int r = 0; r < 32; r++) {
+    copy_async<4>(box + r * 128 + (((lane >> 2) ^ (r & 7)) << 4) + (lane & 3) * 4, r < n_rows ? p : rows, r < n_rows ? 4 : 0);
+    p += ld;
+  }
+}
+__device__ __forceinline__ void copies_wait() {
+  asm volatile("cp.async.wait_all;" ::: "memory");
+  __syncwarp();
+}
+
 // An epilogue warp's boxes.  A box is filled by loads that were issued one chunk earlier (two boxes
 // take turns), or both serve one chunk where it has two inputs or two results.
 template <int END, typename T, int kPer>
@@ -324,7 +346,18 @@ struct Boxes {
   // Starts the loads of a chunk, `ahead` chunks after the next one processed; its box's last store
   // has to be read out first.
   __device__ __forceinline__ void start(int ahead, int64_t row, int col) {
-    if (!loads || g.plain) return;
+    if (!loads) return;
+    if (g.plain) {
+      const uint32_t to = base + (serial ? 0 : (turn + ahead) & 1) * kBox;
+      auto one = [&](const void* from, uint32_t box) {
+        if constexpr (sizeof(T) == 4) box_copy(static_cast<const float*>(from), g.ldy, g.M, g.N, row, col, box);
+        else box_by_lanes<T>(const_cast<T*>(static_cast<const T*>(from)), g.ldy, g.M, g.N, row, col, box, true);
+      };
+      if (g.load_res) one(g.e.res, to);
+      if (g.load_pre) one(g.e.pre_in, both ? to + kBox : to);
+      __syncwarp();
+      return;
+    }
     if ((threadIdx.x & 31) == 0) {
       bulk_wait_read<0>();
       const int b = serial ? 0 : (turn + ahead) & 1;
@@ -338,10 +371,7 @@ struct Boxes {
   // Before the chunk's box is read and written.
   __device__ __forceinline__ bool ready(int64_t row, int col, Abort* ab, uint32_t* status) {
     if (g.plain) {
-      const LinearEnd& e = g.e;
-      if (g.load_res) box_by_lanes<T>(const_cast<T*>(static_cast<const T*>(e.res)), g.ldy, g.M, g.N, row, col, ybox(), true);
-      if (g.load_pre) box_by_lanes<T>(const_cast<T*>(static_cast<const T*>(e.pre_in)), g.ldy, g.M, g.N, row, col, pbox(), true);
-      __syncwarp();
+      if (sizeof(T) == 4 && loads) copies_wait();
       return true;
     }
     if (loads) {
