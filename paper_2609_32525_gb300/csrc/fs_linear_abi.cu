@@ -136,7 +136,8 @@ LinearPlan linear_plan(int op, int dtype, int64_t M, int N, int64_t K) {
   p.splits = (int)((K + p.per - 1) / p.per);
   if (p.splits > 1)
     p.part = ((size_t)p.splits * M * (((size_t)N + 3) & ~(size_t)3) + (op == kLinDw ? (size_t)p.splits * M : 0)) * 4;
-  p.total = align_up(p.part, kAlign);
+  // dW: the parts of dbias behind them
+  p.total = align_up(p.part, kAlign) + (op == kLinDw && p.path ? align_up((size_t)M * kLinearSumParts * 4, kAlign) : 0);
   return p;
 }
 

@@ -347,8 +347,7 @@ cudaError_t linear_tc_f32(const LinearProblem& p, const LinearPlan& plan, const 
   const cudaError_t err = raw                ? (tma ? run<kEndRaw, true>(g, a, b, st) : run<kEndRaw, false>(g, a, b, st))
                           : p.op == kLinFwd ? (tma ? run<kEndFwd, true>(g, a, b, st) : run<kEndFwd, false>(g, a, b, st))
                                             : (tma ? run<kEndDx, true>(g, a, b, st) : run<kEndDx, false>(g, a, b, st));
-  if (err != cudaSuccess || !split) return err;
-  return linear_join(p, plan.splits, static_cast<const float*>(scratch), g.part_sums, e, st);
+  return err != cudaSuccess ? err : finish(g, p, plan, e, scratch, a.ld, st);
 }
 
 }  // namespace fs

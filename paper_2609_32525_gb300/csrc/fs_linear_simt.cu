@@ -210,6 +210,57 @@ __global__ void __launch_bounds__(256) k_linear_join(int64_t M, int N, int ld, i
   lin::end4<T, OP>(e, key, row, (int)(i - row * (ld >> 2)) * 4, N, v);
 }
 
+// The sums of g's columns over ranges of rows, 16 bytes of columns a thread and 8 rows a block at a time, and
+// their sum in order.
+template <typename T, int kV>
+__global__ void __launch_bounds__(256) k_linear_sums(const T* __restrict__ g, int64_t rows, int C, int ld, float* __restrict__ part) {
+  __shared__ float sm[8][32 * kV];
+  grid_begin(g, part);
+  const int c = (blockIdx.x * 32 + threadIdx.x) * kV;
+  const int64_t per = ((rows + gridDim.y - 1) / gridDim.y + 7) & ~(int64_t)7, r0 = blockIdx.y * per;
+  const int64_t r1 = min(r0 + per, rows);
+  float s[kV] = {};
+  if (c < C) {
+#pragma unroll 8
+    for (int64_t r = r0 + threadIdx.y; r < r1; r += 8) {
+      if constexpr (kV == 1) {
+        s[0] += (float)g[r * ld + c];
+      } else {
+        const uint4 w = *reinterpret_cast<const uint4*>(g + r * ld + c);
+        const T* t = reinterpret_cast<const T*>(&w);
+#pragma unroll
+        for (int i = 0; i < kV; i++) s[i] += (float)t[i];
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kV; i++) sm[threadIdx.y][threadIdx.x * kV + i] = s[i];
+  __syncthreads();
+  for (int i = threadIdx.y * 32 + threadIdx.x; i < 32 * kV; i += 256) {
+    float t = 0.f;
+#pragma unroll
+    for (int y = 0; y < 8; y++) t += sm[y][i];
+    if (blockIdx.x * 32 * kV + i < C) part[(int64_t)blockIdx.y * C + blockIdx.x * 32 * kV + i] = t;
+  }
+}
+__global__ void __launch_bounds__(128) k_linear_sums_join(const float* __restrict__ part, int C, int parts, LinearEnd e) {
+  grid_begin(part);
+  const int c = blockIdx.x * 128 + threadIdx.x;
+  if (c >= C) return;
+  float s = 0.f;
+#pragma unroll 8
+  for (int p = 0; p < parts; p++) s += part[(int64_t)p * C + c];
+  lin::end_sum(e, c, s);
+}
+template <typename T, int kV>
+cudaError_t run_sums(const LinearProblem& p, int ld, float* part, const LinearEnd& e, cudaStream_t st) {
+  const int C = (int)p.M;
+  cudaError_t err = launch(k_linear_sums<T, kV>, dim3((unsigned)((C + 32 * kV - 1) / (32 * kV)), kLinearSumParts), dim3(32, 8), 0,
+                           st, static_cast<const T*>(p.a), p.K, C, ld, part);
+  if (err != cudaSuccess) return err;
+  return launch(k_linear_sums_join, dim3((unsigned)((C + 127) / 128)), dim3(128), 0, st, part, C, kLinearSumParts, e);
+}
+
 template <typename T, int OP>
 cudaError_t run_simt(const LinearProblem& p, const LinearPlan& plan, const LinearEnd& e, void* scratch, cudaStream_t st) {
   SimtArgs a{};
@@ -247,6 +298,11 @@ cudaError_t linear_simt(const LinearProblem& p, const LinearPlan& plan, const Li
   if (p.op == kLinFwd) return b ? run_simt<B, kLinFwd>(p, plan, e, scratch, st) : run_simt<float, kLinFwd>(p, plan, e, scratch, st);
   if (p.op == kLinDx) return b ? run_simt<B, kLinDx>(p, plan, e, scratch, st) : run_simt<float, kLinDx>(p, plan, e, scratch, st);
   return b ? run_simt<B, kLinDw>(p, plan, e, scratch, st) : run_simt<float, kLinDw>(p, plan, e, scratch, st);
+}
+
+cudaError_t linear_sums(const LinearProblem& p, int ld, float* part, const LinearEnd& e, cudaStream_t st) {
+  if (p.dtype == FS_BF16) return run_sums<__nv_bfloat16, 8>(p, ld, part, e, st);
+  return ld % 4 == 0 ? run_sums<float, 4>(p, ld, part, e, st) : run_sums<float, 1>(p, ld, part, e, st);
 }
 
 cudaError_t linear_join(const LinearProblem& p, int splits, const float* part, const float* sums, const LinearEnd& e,

@@ -235,8 +235,7 @@ cudaError_t linear_tc(const LinearProblem& p, const LinearPlan& plan, const Line
   const cudaError_t err = raw                ? run<kEndRaw, float, 2, 2>(g, st)
                           : p.op == kLinFwd ? (few ? run<kEndFwd, B, 3, 2>(g, st) : run<kEndFwd, B, kManyGroups, 1>(g, st))
                                             : (few ? run<kEndDx, B, 3, 2>(g, st) : run<kEndDx, B, kManyGroups, 1>(g, st));
-  if (err != cudaSuccess || !split) return err;
-  return linear_join(p, plan.splits, static_cast<const float*>(scratch), g.part_sums, e, st);
+  return err != cudaSuccess ? err : finish(g, p, plan, e, scratch, lda, st);
 }
 
 }  // namespace fs

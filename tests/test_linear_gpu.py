@@ -13,7 +13,7 @@ pytestmark = pytest.mark.gpu
 # rows, Cin, Cout: one of each, odd ones, both sides of tiles of 64, 128 and 256, few rows and many
 SIZES = [(1, 1, 1), (1, 7, 5), (1, 1024, 100), (3, 130, 1), (4, 256, 1030), (5, 64, 33), (17, 8, 8), (63, 31, 65), (64, 64, 64),
          (100, 64, 66), (127, 100, 101), (129, 256, 128), (200, 72, 136), (255, 136, 264), (257, 200, 72), (300, 330, 198),
-         (513, 96, 320), (1000, 33, 257), (1030, 520, 40), (2051, 64, 264), (70, 2049, 130), (30000, 24, 40), (4100, 520, 1032), (9000, 328, 600),
+         (513, 96, 320), (1000, 33, 257), (1030, 520, 40), (600, 700, 72), (3000, 601, 131), (2051, 64, 264), (70, 2049, 130), (30000, 24, 40), (4100, 520, 1032), (9000, 328, 600),
          (20000, 256, 256), (3000, 1100, 72)]
 
 
