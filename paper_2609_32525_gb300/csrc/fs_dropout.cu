@@ -12,124 +12,131 @@
 namespace fs {
 namespace {
 
-// n values, quad after quad.
-template <typename T, int n>
-__device__ __forceinline__ void drop(const DropArgs& a, const act::DropKey& key, uint64_t quad, float (&pre)[n],
-                                     float (&res)[n], float (&v)[n]) {
+// What is read beside x: nothing, a residual, or the pre-activations of a backward.
+enum { kPlain = 0, kRes = 1, kSlope = 2 };
+
+// n values, quad after quad: v becomes the result; other: what is read beside x.
+template <typename T, int MODE, int n, typename Q>
+__device__ __forceinline__ void drop(const DropArgs& a, const act::DropKey& key, Q quad, float (&other)[n], float (&v)[n]) {
   constexpr bool kFast = sizeof(T) == 2;
-  if (a.backward) {
-    act::slope<kFast>(a.act, pre, v);
+  if (MODE == kSlope) {
+    act::slope<kFast>(a.act, other, v);
 #pragma unroll
-    for (int i = 0; i < n; i++) v[i] = pre[i];
+    for (int i = 0; i < n; i++) v[i] = other[i];
   } else {
     act::apply<kFast>(a.act, v);
   }
   if (a.rng) {
-    act::keep<n>({a.rng, a.threshold, a.scale}, key, quad, v, res);
+    float r[n];
 #pragma unroll
-    for (int i = 0; i < n; i++) v[i] = res[i];
-  } else {
+    for (int i = 0; i < n; i++) r[i] = MODE == kRes ? other[i] : 0.f;
+    act::keep_by<n>({a.rng, a.threshold, a.scale}, key, quad, v, r);
 #pragma unroll
-    for (int i = 0; i < n; i++) v[i] += res[i];
+    for (int i = 0; i < n; i++) v[i] = r[i];
+  } else if (MODE == kRes) {
+#pragma unroll
+    for (int i = 0; i < n; i++) v[i] += other[i];
   }
 }
 
 // Rows of a multiple of four channels: the quads lie one after another, so rows do not matter.
-// A thread takes kP pieces of 16 bytes of each tensor at a time, a block's width apart, loaded
-// before the first is worked on.
-template <typename T, int kP>
+// A thread takes 16 bytes of each tensor at a time, the next ones on their way while it works.
+// Q: uint32_t where the quads' numbers fit.
+template <typename T, int MODE, typename Q>
 __global__ void __launch_bounds__(256) k_dropout(DropArgs a) {
   const int64_t zero = grid_begin();
   constexpr int kV = 16 / sizeof(T);  // values of a piece
-  const int64_t values = a.rows * a.C, step = (int64_t)gridDim.x * 256 * kP * kV;
-  const T *x = static_cast<const T*>(a.x) + zero, *res = static_cast<const T*>(a.res), *pre = static_cast<const T*>(a.pre);
+  const int64_t values = a.rows * a.C, step = (int64_t)gridDim.x * 256 * kV;
+  const T *x = static_cast<const T*>(a.x) + zero, *beside = static_cast<const T*>(MODE == kRes ? a.res : a.pre);
   T* y = static_cast<T*>(a.y);
   act::DropKey key{};
   if (a.rng) key = act::drop_key(a.rng + zero);
-  const bool slope = a.backward && a.act != FS_ACT_NONE;
-  for (int64_t first = ((int64_t)blockIdx.x * 256 * kP + threadIdx.x) * kV; first < values; first += step) {
-    int4 w[kP], r[kP], u[kP];
-#pragma unroll
-    for (int p = 0; p < kP; p++) {
-      const int64_t at = first + p * 256 * kV;
-      w[p] = r[p] = u[p] = make_int4(0, 0, 0, 0);
-      if (at + kV <= values) {
-        w[p] = *reinterpret_cast<const int4*>(x + at);
-        if (a.res) r[p] = *reinterpret_cast<const int4*>(res + at);
-        if (slope) u[p] = *reinterpret_cast<const int4*>(pre + at);
-      } else if (at < values) {  // a last quad of bf16
-        *reinterpret_cast<int2*>(&w[p]) = *reinterpret_cast<const int2*>(x + at);
-        if (a.res) *reinterpret_cast<int2*>(&r[p]) = *reinterpret_cast<const int2*>(res + at);
-        if (slope) *reinterpret_cast<int2*>(&u[p]) = *reinterpret_cast<const int2*>(pre + at);
-      }
+  int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) * kV;
+  int4 w = make_int4(0, 0, 0, 0), u = w;
+  auto load = [&](int64_t p) {
+    if (p + kV <= values) {
+      w = *reinterpret_cast<const int4*>(x + p);
+      if (MODE != kPlain) u = *reinterpret_cast<const int4*>(beside + p);
+    } else if (p < values) {  // a last quad of bf16
+      *reinterpret_cast<int2*>(&w) = *reinterpret_cast<const int2*>(x + p);
+      if (MODE != kPlain) *reinterpret_cast<int2*>(&u) = *reinterpret_cast<const int2*>(beside + p);
     }
+  };
+  load(at);
+  for (; at < values; at += step) {
+    float v[kV], f[kV] = {};
 #pragma unroll
-    for (int p = 0; p < kP; p++) {
-      const int64_t at = first + p * 256 * kV;
-      float v[kV], f[kV], g[kV];
-#pragma unroll
-      for (int h = 0; h < kV; h += 4) {
-        act::load4(reinterpret_cast<const T*>(&w[p]) + h, 4, true, *reinterpret_cast<float(*)[4]>(v + h));
-        act::load4(reinterpret_cast<const T*>(&u[p]) + h, 4, true, *reinterpret_cast<float(*)[4]>(f + h));
-        act::load4(reinterpret_cast<const T*>(&r[p]) + h, 4, true, *reinterpret_cast<float(*)[4]>(g + h));
-      }
-      drop<T, kV>(a, key, (uint64_t)at >> 2, f, g, v);
-      int4 out;
-#pragma unroll
-      for (int h = 0; h < kV; h += 4)
-        act::store4(reinterpret_cast<T*>(&out) + h, 4, true, *reinterpret_cast<const float(*)[4]>(v + h));
-      if (at + kV <= values) *reinterpret_cast<int4*>(y + at) = out;
-      else if (at < values) *reinterpret_cast<int2*>(y + at) = *reinterpret_cast<const int2*>(&out);
+    for (int h = 0; h < kV; h += 4) {
+      act::load4(reinterpret_cast<const T*>(&w) + h, 4, true, *reinterpret_cast<float(*)[4]>(v + h));
+      if (MODE != kPlain) act::load4(reinterpret_cast<const T*>(&u) + h, 4, true, *reinterpret_cast<float(*)[4]>(f + h));
     }
+    load(at + step);
+    drop<T, MODE, kV>(a, key, (Q)(at >> 2), f, v);
+    int4 out;
+#pragma unroll
+    for (int h = 0; h < kV; h += 4)
+      act::store4(reinterpret_cast<T*>(&out) + h, 4, true, *reinterpret_cast<const float(*)[4]>(v + h));
+    if (at + kV <= values) *reinterpret_cast<int4*>(y + at) = out;
+    else *reinterpret_cast<int2*>(y + at) = *reinterpret_cast<const int2*>(&out);
   }
 }
 
 // Any number of channels: a row's last quad may be a part of one, and rows begin anywhere.
-template <typename T>
+template <typename T, int MODE, typename Q>
 __global__ void __launch_bounds__(256) k_dropout_ragged(DropArgs a) {
   const int64_t zero = grid_begin();
   const int per_row = (a.C + 3) >> 2;
   const int64_t quads = a.rows * per_row, step = (int64_t)gridDim.x * 256;
-  const T *x = static_cast<const T*>(a.x) + zero, *res = static_cast<const T*>(a.res), *pre = static_cast<const T*>(a.pre);
+  const T *x = static_cast<const T*>(a.x) + zero, *beside = static_cast<const T*>(MODE == kRes ? a.res : a.pre);
   T* y = static_cast<T*>(a.y);
   act::DropKey key{};
   if (a.rng) key = act::drop_key(a.rng + zero);
-  const bool slope = a.backward && a.act != FS_ACT_NONE;
   int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x;
   int64_t row = q / per_row;
   int col = (int)(q - row * per_row);
   const int64_t rows_on = step / per_row;
   const int cols_on = (int)(step - rows_on * per_row);
+  float nv[4], nf[4] = {};
+  auto load = [&]() {
+    const int n = a.C - 4 * col;
+    const int64_t at = row * a.C + 4 * col;
+    act::load4(x + at, n, false, nv);
+    if (MODE != kPlain) act::load4(beside + at, n, false, nf);
+  };
+  if (q < quads) load();
   for (; q < quads; q += step) {
     const int n = a.C - 4 * col;
     const int64_t at = row * a.C + 4 * col;
-    float v[4], f[4] = {}, g[4] = {};
-    act::load4(x + at, n, false, v);
-    if (slope) act::load4(pre + at, n, false, f);
-    if (a.res) act::load4(res + at, n, false, g);
-    drop<T, 4>(a, key, (uint64_t)q, f, g, v);
-    act::store4(y + at, n, false, v);
+    float v[4], f[4];
+#pragma unroll
+    for (int i = 0; i < 4; i++) v[i] = nv[i], f[i] = nf[i];
     row += rows_on, col += cols_on;
     if (col >= per_row) col -= per_row, row++;
+    if (q + step < quads) load();
+    drop<T, MODE, 4>(a, key, (Q)q, f, v);
+    act::store4(y + at, n, false, v);
   }
 }
 
-template <typename T>
+template <typename T, int MODE>
 cudaError_t run(const DropArgs& a, cudaStream_t st) {
   const bool flat = (a.C & 3) == 0;
-  const int64_t pieces = flat ? (a.rows * a.C * (int64_t)sizeof(T) + 15) / 16 : a.rows * ((a.C + 3) >> 2);
-  // Two pieces a thread where that still fills the device.
-  const int64_t most = (int64_t)num_sms() * 8;
-  const bool two = flat && pieces >= most * 512;
-  const int64_t blocks = std::min<int64_t>((pieces + (two ? 511 : 255)) / (two ? 512 : 256), most);
-  return launch(!flat ? k_dropout_ragged<T> : two ? k_dropout<T, 2> : k_dropout<T, 1>, dim3((unsigned)blocks), dim3(256), 0,
-                st, a);
+  const int64_t quads = a.rows * ((a.C + 3) >> 2), pieces = flat ? (quads * 4 * (int64_t)sizeof(T) + 15) / 16 : quads;
+  const bool low = quads + 8 < (1LL << 32);
+  const dim3 grid((unsigned)std::min<int64_t>((pieces + 255) / 256, (int64_t)num_sms() * 8));
+  if (flat) return launch(low ? k_dropout<T, MODE, uint32_t> : k_dropout<T, MODE, uint64_t>, grid, dim3(256), 0, st, a);
+  return launch(low ? k_dropout_ragged<T, MODE, uint32_t> : k_dropout_ragged<T, MODE, uint64_t>, grid, dim3(256), 0, st, a);
+}
+template <typename T>
+cudaError_t by_mode(const DropArgs& a, cudaStream_t st) {
+  if (a.backward && a.act != FS_ACT_NONE) return run<T, kSlope>(a, st);
+  return a.res ? run<T, kRes>(a, st) : run<T, kPlain>(a, st);
 }
 
 }  // namespace
 
 cudaError_t dropout(const DropArgs& a, cudaStream_t st) {
-  return a.dtype == FS_BF16 ? run<__nv_bfloat16>(a, st) : run<float>(a, st);
+  return a.dtype == FS_BF16 ? by_mode<__nv_bfloat16>(a, st) : by_mode<float>(a, st);
 }
 
 }  // namespace fs
