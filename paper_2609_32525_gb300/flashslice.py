@@ -815,3 +815,44 @@ class ShardedCoupling:
         fs_slice_bwd(c.shape, self.x, self.fx, self.W, self.bias, self.tau, c.tokens, c.wsum, c.lse, d_tokens,
                      c.dx_mid, c.dfx, c.dW, c.dbias, c.dtau, True, c.ws_sbwd)
         return c.dW, c.dbias, c.dtau
+
+
+class FeedForward:
+    """The second half of a layer, behind its norm: y = res + drop(W2 drop(act(W1 x + b1)) + b2), on rows of C
+    channels with `hidden` between, with its buffers allocated once.
+
+    p: both dropouts' rate; rng_hidden, rng_out: their words (dropout_rng), which differ from each other and
+    from other layers' and steps', and which the backward gets again.  backward: the buffers of the gradients,
+    too; the forward then keeps x (a reference), the pre-activations and the hidden rows."""
+
+    def __init__(self, rows, C, hidden, dtype=torch.bfloat16, act=FS_ACT_GELU, p=0.0, backward=False, device="cuda"):
+        self.first, self.second = make_linear(rows, C, hidden, dtype), make_linear(rows, hidden, C, dtype)
+        self.rows, self.act, self.p = make_rows(rows, C, dtype), act, p
+        own = dict(dtype=dtype, device=device)
+        self.h, self.y = torch.empty(rows, hidden, **own), torch.empty(rows, C, **own)
+        self.pre, self.x = (torch.empty(rows, hidden, **own) if backward else None), None
+        self.ws = [linear_workspace(s, False, device) for s in (self.first, self.second)]
+        if backward:
+            f32 = dict(dtype=torch.float32, device=device)
+            self.g, self.dh, self.dx = torch.empty(rows, C, **own), torch.empty(rows, hidden, **own), torch.empty(rows, C, **own)
+            self.dW1, self.db1 = torch.empty(hidden, C, **f32), torch.empty(hidden, **f32)
+            self.dW2, self.db2 = torch.empty(C, hidden, **f32), torch.empty(C, **f32)
+            self.ws_bwd = [linear_workspace(s, True, device) for s in (self.first, self.second)]
+
+    def forward(self, x, W1, b1, W2, b2, res=None, rng_hidden=None, rng_out=None, stream=None):
+        self.x = x
+        fs_linear_fwd(self.first, x, W1, b1, self.act, self.p, rng_hidden, None, self.h, self.pre, self.ws[0], stream)
+        fs_linear_fwd(self.second, self.h, W2, b2, FS_ACT_NONE, self.p, rng_out, res, self.y, None, self.ws[1], stream)
+        return self.y
+
+    def backward(self, W1, W2, dy, dres=None, rng_hidden=None, rng_out=None, accumulate=False, stream=None):
+        """dy: the gradient of y (the residual's own gradient, too); dres: added to that of x."""
+        g = dy
+        if self.p > 0:
+            fs_dropout_bwd(self.rows, dy, FS_ACT_NONE, self.p, rng_out, None, self.g, stream)
+            g = self.g
+        fs_linear_bwd(self.second, self.h, W2, g, self.act, self.p, rng_hidden, self.pre, None, self.dh, self.dW2, self.db2,
+                      accumulate, self.ws_bwd[1], stream)
+        fs_linear_bwd(self.first, self.x, W1, self.dh, FS_ACT_NONE, 0.0, None, None, dres, self.dx, self.dW1, self.db1,
+                      accumulate, self.ws_bwd[0], stream)
+        return {"dx": self.dx, "dW1": self.dW1, "db1": self.db1, "dW2": self.dW2, "db2": self.db2}
