@@ -192,7 +192,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreadsF32, 1)
         infinite = lanes_with_infinity(v);
         fetch(w, kb, infinite & none);
       }
-      ok = mbar_wait_pair_w(&empty[ring.i], ring.pass ^ 1u, ab, status);
+      ok = mbar_wait_w(&empty[ring.i], ring.pass ^ 1u, ab, status);
       if (!ok) break;
       const uint32_t stage = stage0 + ring.i * kStageF32;
 #pragma unroll
@@ -261,7 +261,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreadsF32, 1)
           ok = issue.take(half, sums, acc_empty, ab, status);
           const uint32_t d = tmem + half * 256;
           for (int blk = kb; blk < end && ok; blk++) {
-            ok = mbar_wait_pair_w(&full[ring.i], ring.pass, ab, status);
+            ok = mbar_wait_w(&full[ring.i], ring.pass, ab, status);
             if (!ok) break;
             tc_fence_after();
             const uint32_t a_lo = a_lo0 + ring.i * (kStageF32 >> 4), b_lo = b_lo0 + ring.i * (kStageF32 >> 4);

@@ -577,9 +577,9 @@ struct Issuer {
   Halves h;
   bool last_sums = false;
   __device__ __forceinline__ bool take(int half, bool sums, uint64_t* acc_empty, Abort* ab, uint32_t* status) {
-    bool ok = mbar_wait_pair_w(&acc_empty[half], (h.uses(half) & 1u) ^ 1u, ab, status);
+    bool ok = mbar_wait_w(&acc_empty[half], (h.uses(half) & 1u) ^ 1u, ab, status);
     if (ok && sums != last_sums && h.uses(half ^ 1))
-      ok = mbar_wait_pair_w(&acc_empty[half ^ 1], (h.uses(half ^ 1) - 1) & 1u, ab, status);
+      ok = mbar_wait_w(&acc_empty[half ^ 1], (h.uses(half ^ 1) - 1) & 1u, ab, status);
     last_sums = sums;
     h.use(half);
     tc_fence_after();
