@@ -55,6 +55,9 @@ LinearPlan linear_plan(int op, int dtype, int64_t M, int N, int64_t K);
 
 cudaError_t linear_simt(const LinearProblem& p, const LinearPlan& plan, const LinearEnd& e, void* scratch,
                         cudaStream_t st);
+// dx and dW, both by fp32 multiply-adds, in one launch (and their joins).  Fewer than 2^31 blocks together.
+cudaError_t linear_simt_bwd(const LinearProblem& px, const LinearPlan& lx, const LinearEnd& ex, void* sx, const LinearProblem& pw,
+                            const LinearPlan& lw, const LinearEnd& ew, void* sw, cudaStream_t st);
 // bf16 operands with a pitch of whole 16 bytes (linear_pack), fp32 ones as they are.
 cudaError_t linear_tc(const LinearProblem& p, const LinearPlan& plan, const LinearEnd& e, void* scratch, cudaStream_t st);
 cudaError_t linear_tc_f32(const LinearProblem& p, const LinearPlan& plan, const LinearEnd& e, void* scratch, cudaStream_t st);

@@ -127,9 +127,10 @@ LinearPlan linear_plan(int op, int dtype, int64_t M, int N, int64_t K) {
     splits = std::max<int64_t>(1, std::min<int64_t>(pairs / tiles, K / 512));
     p.per = ((K + splits - 1) / splits + 63) / 64 * 64;
   } else {
-    // Sums are split until the blocks fill the device twice, into parts of at least 64 terms.
+    // Sums are split until the blocks fill the device twice, into parts of at least 128 terms: below, a launch for the
+    // join takes longer than the terms (backward of 100 x 64 x 66: FS_TIME_SPLIT).
     const int64_t tiles = ((M + 63) / 64) * ((N + 63) / 64);
-    splits = std::max<int64_t>(1, std::min<int64_t>(2LL * num_sms() / tiles, (K + 63) / 64));
+    splits = std::max<int64_t>(1, std::min<int64_t>(2LL * num_sms() / tiles, (K + 127) / 128));
     if (op == kLinFwd && M <= kLinearFew) splits = 1;
     p.per = ((K + splits - 1) / splits + 15) / 16 * 16;
   }
@@ -215,21 +216,19 @@ fs_status fs_linear_bwd(const fs_linear* s, const void* x, const void* W, const 
   Plans plan = plan_bwd(s, dx != nullptr, dW != nullptr, x, W, g);
   char* w = static_cast<char*>(ws);
   FS_CUDA(plan.scratch.launch(ws, st));
-  bool reset = plan.scratch.n == 0;
-  if (dx) {
-    LinearEnd e{};
-    e.act = act; e.rng = p > 0.f ? rng : nullptr; e.threshold = threshold_of(p); e.scale = scale_of(p);
-    e.pre_in = pre; e.res = dres; e.y = dx;
-    const bool tc = plan.dx.path;
-    FS_CUDA(run(problem(s, kLinDx, plan.scratch.at(tc, g, s->rows, s->Cout), plan.scratch.at(tc, W, s->Cout, s->Cin), ws, reset), plan.dx, e, w + plan.at_dx, st));
-    reset = false;
-  }
-  if (dW) {
-    LinearEnd e{};
-    e.y = dW; e.sums = dbias; e.accumulate = accumulate;
-    const bool tc = plan.dw.path;
-    FS_CUDA(run(problem(s, kLinDw, plan.scratch.at(tc, g, s->rows, s->Cout), plan.scratch.at(tc, x, s->rows, s->Cin), ws, reset), plan.dw, e, w + plan.at_dw, st));
-  }
+  LinearEnd ex{}, ew{};
+  ex.act = act; ex.rng = p > 0.f ? rng : nullptr; ex.threshold = threshold_of(p); ex.scale = scale_of(p);
+  ex.pre_in = pre; ex.res = dres; ex.y = dx;
+  ew.y = dW; ew.sums = dbias; ew.accumulate = accumulate;
+  const bool tx = plan.dx.path, tw = plan.dw.path, reset = plan.scratch.n == 0;
+  const LinearProblem px = problem(s, kLinDx, plan.scratch.at(tx, g, s->rows, s->Cout), plan.scratch.at(tx, W, s->Cout, s->Cin), ws, reset);
+  const LinearProblem pw = problem(s, kLinDw, plan.scratch.at(tw, g, s->rows, s->Cout), plan.scratch.at(tw, x, s->rows, s->Cin), ws,
+                                   reset && !dx);
+  // (the tiles of a product by multiply-adds are below 2^26, except where rows are more than those of any memory)
+  if (dx && dW && !tx && !tw && s->rows < (1LL << 30))
+    return cuda_status(linear_simt_bwd(px, plan.dx, ex, w + plan.at_dx, pw, plan.dw, ew, w + plan.at_dw, st));
+  if (dx) FS_CUDA(run(px, plan.dx, ex, w + plan.at_dx, st));
+  if (dW) FS_CUDA(run(pw, plan.dw, ew, w + plan.at_dw, st));
   return FS_OK;
 }
 

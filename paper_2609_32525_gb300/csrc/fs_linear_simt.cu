@@ -24,17 +24,21 @@ struct SimtArgs {
   LinearEnd e;
 };
 
+struct Tiles {
+  float a[2][kK][kPitch], b[2][kK][kPitch];
+};
+
+// block: of the grid of D's tiles (rows, columns) and the sum's parts.
 template <typename T, int OP>
-__global__ void __launch_bounds__(256) k_linear_simt(SimtArgs a) {
-  __shared__ __align__(16) float As[2][kK][kPitch], Bs[2][kK][kPitch];
-  const int64_t zero = grid_begin();
+__device__ __forceinline__ void simt_block(const SimtArgs& a, int64_t zero, Tiles& tiles, uint3 block) {
+  auto &As = tiles.a, &Bs = tiles.b;
   const T* A = static_cast<const T*>(a.a) + zero;
   const T* B = static_cast<const T*>(a.b) + zero;
   const int t = threadIdx.x, tx = t & 15, ty = t >> 4;
-  if (a.status && t == 0 && (blockIdx.x | blockIdx.y | blockIdx.z) == 0) *a.status = 0;
-  const int64_t m0 = (int64_t)blockIdx.x * kT;
-  const int n0 = blockIdx.y * kT;
-  const int64_t k0 = (int64_t)blockIdx.z * a.per, k1 = k0 + a.per < a.K ? k0 + a.per : a.K;
+  if (a.status && t == 0 && (block.x | block.y | block.z) == 0) *a.status = 0;
+  const int64_t m0 = (int64_t)block.x * kT;
+  const int n0 = block.y * kT;
+  const int64_t k0 = (int64_t)block.z * a.per, k1 = k0 + a.per < a.K ? k0 + a.per : a.K;
   // A: x and g have their channels (k) next to each other, g transposed its m; B: W has its k next
   // to each other in the forward product, its n in dx, and x transposed its n.
   constexpr bool kAk = OP != kLinDw, kBk = OP == kLinFwd;
@@ -97,17 +101,37 @@ __global__ void __launch_bounds__(256) k_linear_simt(SimtArgs a) {
   for (int i = 0; i < 4; i++) {
     const int64_t m = m0 + ty * 4 + i;
     if (m >= a.M) break;
-    if (OP == kLinDw && a.e.sums && blockIdx.y == 0 && tx == 0) {
-      if (a.splits > 1) a.part_sums[(int64_t)blockIdx.z * a.M + m] = sum[i];
+    if (OP == kLinDw && a.e.sums && block.y == 0 && tx == 0) {
+      if (a.splits > 1) a.part_sums[(int64_t)block.z * a.M + m] = sum[i];
       else lin::end_sum(a.e, m, sum[i]);
     }
     if (col >= a.N) continue;
     if (a.splits > 1)
-      *reinterpret_cast<float4*>(a.part + ((int64_t)blockIdx.z * a.M + m) * a.ld + col) =
+      *reinterpret_cast<float4*>(a.part + ((int64_t)block.z * a.M + m) * a.ld + col) =
           make_float4(acc[i][0], acc[i][1], acc[i][2], acc[i][3]);
     else
       lin::end4<T, OP>(a.e, key, m, col, a.N, acc[i]);
   }
+}
+
+template <typename T, int OP>
+__global__ void __launch_bounds__(256) k_linear_simt(SimtArgs a) {
+  __shared__ __align__(16) Tiles tiles;
+  const int64_t zero = grid_begin();
+  simt_block<T, OP>(a, zero, tiles, blockIdx);
+}
+// dx and dW in one launch: small backward calls are mostly launches.
+template <typename T>
+__global__ void __launch_bounds__(256) k_linear_simt_bwd(SimtArgs x, SimtArgs w, dim3 grid_x, dim3 grid_w) {
+  __shared__ __align__(16) Tiles tiles;
+  const int64_t zero = grid_begin();
+  const unsigned nx = grid_x.x * grid_x.y * grid_x.z;
+  unsigned b = blockIdx.x;
+  const dim3 g = b < nx ? grid_x : grid_w;
+  if (b >= nx) b -= nx;
+  const uint3 block = make_uint3(b % g.x, b / g.x % g.y, b / (g.x * g.y));
+  if (blockIdx.x < nx) simt_block<T, kLinDx>(x, zero, tiles, block);
+  else simt_block<T, kLinDw>(w, zero, tiles, block);
 }
 
 // Few rows through the forward: what counts is W, which is read once for four rows.  A warp owns four columns (a
@@ -261,8 +285,7 @@ cudaError_t run_sums(const LinearProblem& p, int ld, float* part, const LinearEn
   return launch(k_linear_sums_join, dim3((unsigned)((C + 127) / 128)), dim3(128), 0, st, part, C, kLinearSumParts, e);
 }
 
-template <typename T, int OP>
-cudaError_t run_simt(const LinearProblem& p, const LinearPlan& plan, const LinearEnd& e, void* scratch, cudaStream_t st) {
+SimtArgs simt_args(const LinearProblem& p, const LinearPlan& plan, const LinearEnd& e, void* scratch) {
   SimtArgs a{};
   a.a = p.a; a.b = p.b; a.M = p.M; a.N = p.N; a.K = p.K; a.per = plan.per; a.splits = plan.splits;
   a.ld = (p.N + 3) & ~3;
@@ -270,12 +293,20 @@ cudaError_t run_simt(const LinearProblem& p, const LinearPlan& plan, const Linea
   a.part_sums = a.part + (int64_t)plan.splits * p.M * a.ld;
   a.status = p.reset ? p.status : nullptr;
   a.e = e;
+  return a;
+}
+dim3 simt_grid(const SimtArgs& a) {
+  return dim3((unsigned)((a.M + kT - 1) / kT), (unsigned)((a.N + kT - 1) / kT), (unsigned)a.splits);
+}
+
+template <typename T, int OP>
+cudaError_t run_simt(const LinearProblem& p, const LinearPlan& plan, const LinearEnd& e, void* scratch, cudaStream_t st) {
+  const SimtArgs a = simt_args(p, plan, e, scratch);
   if (OP == kLinFwd && p.M <= kLinearFew) {
     const bool vec = p.K % (16 / (int)sizeof(T)) == 0;
     return launch(vec ? k_linear_few<T, true> : k_linear_few<T, false>, dim3((unsigned)((p.N + 15) / 16)), dim3(128), 0, st, a);
   }
-  const dim3 grid((unsigned)((p.M + kT - 1) / kT), (unsigned)((p.N + kT - 1) / kT), (unsigned)plan.splits);
-  cudaError_t err = launch(k_linear_simt<T, OP>, grid, dim3(256), 0, st, a);
+  cudaError_t err = launch(k_linear_simt<T, OP>, simt_grid(a), dim3(256), 0, st, a);
   if (err == cudaSuccess && plan.splits > 1) err = linear_join(p, plan.splits, a.part, a.part_sums, e, st);
   return err;
 }
@@ -298,6 +329,18 @@ cudaError_t linear_simt(const LinearProblem& p, const LinearPlan& plan, const Li
   if (p.op == kLinFwd) return b ? run_simt<B, kLinFwd>(p, plan, e, scratch, st) : run_simt<float, kLinFwd>(p, plan, e, scratch, st);
   if (p.op == kLinDx) return b ? run_simt<B, kLinDx>(p, plan, e, scratch, st) : run_simt<float, kLinDx>(p, plan, e, scratch, st);
   return b ? run_simt<B, kLinDw>(p, plan, e, scratch, st) : run_simt<float, kLinDw>(p, plan, e, scratch, st);
+}
+
+cudaError_t linear_simt_bwd(const LinearProblem& px, const LinearPlan& lx, const LinearEnd& ex, void* sx, const LinearProblem& pw,
+                            const LinearPlan& lw, const LinearEnd& ew, void* sw, cudaStream_t st) {
+  const SimtArgs x = simt_args(px, lx, ex, sx), w = simt_args(pw, lw, ew, sw);
+  const dim3 gx = simt_grid(x), gw = simt_grid(w);
+  const dim3 grid(gx.x * gx.y * gx.z + gw.x * gw.y * gw.z);
+  cudaError_t err = px.dtype == FS_BF16 ? launch(k_linear_simt_bwd<__nv_bfloat16>, grid, dim3(256), 0, st, x, w, gx, gw)
+                                        : launch(k_linear_simt_bwd<float>, grid, dim3(256), 0, st, x, w, gx, gw);
+  if (err == cudaSuccess && lx.splits > 1) err = linear_join(px, lx.splits, x.part, x.part_sums, ex, st);
+  if (err == cudaSuccess && lw.splits > 1) err = linear_join(pw, lw.splits, w.part, w.part_sums, ew, st);
+  return err;
 }
 
 cudaError_t linear_sums(const LinearProblem& p, int ld, float* part, const LinearEnd& e, cudaStream_t st) {
