@@ -128,7 +128,7 @@ LinearPlan linear_plan(int op, int dtype, int64_t M, int N, int64_t K) {
     p.per = ((K + splits - 1) / splits + 63) / 64 * 64;
   } else {
     // Sums are split until the blocks fill the device twice, into parts of at least 128 terms: below, a launch for the
-    // join takes longer than the terms (backward of 100 x 64 x 66: FS_TIME_SPLIT).
+    // join takes longer than the terms (backward of 100 x 64 x 66: 14.4 us with a split of its 100 rows and two launches more, 10.1 without).
     const int64_t tiles = ((M + 63) / 64) * ((N + 63) / 64);
     splits = std::max<int64_t>(1, std::min<int64_t>(2LL * num_sms() / tiles, (K + 127) / 128));
     if (op == kLinFwd && M <= kLinearFew) splits = 1;
@@ -224,7 +224,7 @@ fs_status fs_linear_bwd(const fs_linear* s, const void* x, const void* W, const 
   const LinearProblem px = problem(s, kLinDx, plan.scratch.at(tx, g, s->rows, s->Cout), plan.scratch.at(tx, W, s->Cout, s->Cin), ws, reset);
   const LinearProblem pw = problem(s, kLinDw, plan.scratch.at(tw, g, s->rows, s->Cout), plan.scratch.at(tw, x, s->rows, s->Cin), ws,
                                    reset && !dx);
-  // (the tiles of a product by multiply-adds are below 2^26, except where rows are more than those of any memory)
+  // (a grid of both products' tiles has to stay below 2^31 blocks)
   if (dx && dW && !tx && !tw && s->rows < (1LL << 30))
     return cuda_status(linear_simt_bwd(px, plan.dx, ex, w + plan.at_dx, pw, plan.dw, ew, w + plan.at_dw, st));
   if (dx) FS_CUDA(run(px, plan.dx, ex, w + plan.at_dx, st));

@@ -229,7 +229,8 @@ cudaError_t linear_tc(const LinearProblem& p, const LinearPlan& plan, const Line
   ok = ok && (g.a_mn ? make_map(&g.a, p.a, 2, p.M, p.K, 1, lda, 64) : make_map(&g.a, p.a, 2, p.K, p.M, 1, lda, 128));
   ok = ok && (g.b_mn ? make_map(&g.b, p.b, 2, p.N, p.K, 1, ldb, 64) : make_map(&g.b, p.b, 2, p.K, p.N, 1, ldb, g.bn / 2));
   if (!ok) return cudaErrorInvalidValue;
-  if (g.n_tiles == 1 && !raw && p.K % 8 == 0) g.ahead = static_cast<const char*>(p.a);
+  // (a tile of long rows would be more than L2 keeps)
+  if (g.n_tiles == 1 && !raw && p.K % 8 == 0 && p.K <= kShortK) g.ahead = static_cast<const char*>(p.a);
   using B = __nv_bfloat16;
   const bool few = g.store_pre || (g.load_res && g.load_pre) || p.K > kShortK;
   const cudaError_t err = raw                ? run<kEndRaw, float, 2, 2>(g, st)
