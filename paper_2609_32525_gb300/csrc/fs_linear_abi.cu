@@ -117,7 +117,10 @@ Span unless(const void* p, size_t n, const void* same) { return {p == same ? nul
 LinearPlan linear_plan(int op, int dtype, int64_t M, int N, int64_t K) {
   LinearPlan p{};
   const double work = (double)M * N * (double)K;
-  p.path = work >= 4194304.0 && M > kLinearFew && N >= 16 && K >= 16 && std::max(M, K) < (1LL << 31) - 512;
+  // Below this many products of terms a block's start and the two CTAs' hand-overs cost more than multiply-adds (1024
+  // rows of 64 -> 64 bf16: 17 us against 13, of 256 -> 256 fp32: 23 against 17, backward 49 against 25).
+  const double least = dtype == FS_BF16 ? 16777216.0 : 134217728.0;
+  p.path = work >= least && M > kLinearFew && N >= 16 && K >= 16 && std::max(M, K) < (1LL << 31) - 512;
   int64_t splits;
   if (p.path) {
     // Pairs of CTAs take tiles; where there are fewer than half as many tiles, sums are split into parts of
@@ -128,7 +131,8 @@ LinearPlan linear_plan(int op, int dtype, int64_t M, int N, int64_t K) {
     p.per = ((K + splits - 1) / splits + 63) / 64 * 64;
   } else {
     // Sums are split until the blocks fill the device twice, into parts of at least 128 terms: below, a launch for the
-    // join takes longer than the terms (backward of 100 x 64 x 66: 14.4 us with a split of its 100 rows and two launches more, 10.1 without).
+    // join takes longer than the terms (backward of 100 x 64 x 66: 14.4 us with a split of its 100 rows and two
+    // launches more, 10.1 without).
     const int64_t tiles = ((M + 63) / 64) * ((N + 63) / 64);
     splits = std::max<int64_t>(1, std::min<int64_t>(2LL * num_sms() / tiles, (K + 127) / 128));
     if (op == kLinFwd && M <= kLinearFew) splits = 1;

@@ -259,43 +259,6 @@ __device__ __forceinline__ void end_chunk(const TcArgs& g, const act::DropKey& k
   }
 }
 
-// A box between shared memory and rows that TMA cannot address, by a warp: a row at a time, all rows under way
-// at once.
-template <typename T>
-__device__ __forceinline__ void box_by_lanes(T* rows, int64_t ld, int64_t M, int N, int64_t row0, int col0, uint32_t box,
-                                             bool load) {
-  constexpr int kCols = 128 / sizeof(T), kV = 16 / sizeof(T);
-  using W = typename std::conditional<sizeof(T) == 2, unsigned short, uint32_t>::type;
-  const int lane = threadIdx.x & 31, n_rows = (int)min(M - row0, (int64_t)32);
-#pragma unroll 1
-  for (int c = lane; c < kCols; c += 32) {
-    const bool in = col0 + c < N;
-    W* p = reinterpret_cast<W*>(rows) + row0 * ld + col0 + c;
-    const uint32_t at = box + (c % kV) * (int)sizeof(T);
-    W w[32];
-    if (load) {
-#pragma unroll
-      for (int r = 0; r < 32; r++) w[r] = in && r < n_rows ? p[r * ld] : W(0);
-    }
-#pragma unroll
-    for (int r = 0; r < 32; r++) {
-      const uint32_t q = at + r * 128 + (((c / kV) ^ (r & 7)) << 4);
-      if constexpr (sizeof(T) == 2) {
-        if (load) asm volatile("st.shared.u16 [%0], %1;" ::"r"(q), "h"(w[r]) : "memory");
-        else asm volatile("ld.shared.u16 %0, [%1];" : "=h"(w[r]) : "r"(q) : "memory");
-      } else {
-        if (load) asm volatile("st.shared.u32 [%0], %1;" ::"r"(q), "r"(w[r]) : "memory");
-        else asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w[r]) : "r"(q) : "memory");
-      }
-    }
-    if (!load) {
-#pragma unroll
-      for (int r = 0; r < 32; r++)
-        if (in && r < n_rows) p[r * ld] = w[r];
-    }
-  }
-}
-
 template <int kBytes>
 __device__ __forceinline__ void copy_async(uint32_t dst, const void* src, int have) {
   if constexpr (kBytes == 16)
@@ -303,14 +266,88 @@ __device__ __forceinline__ void copy_async(uint32_t dst, const void* src, int ha
   else
     asm volatile("cp.async.ca.shared.global [%0], [%1], %3, %2;" ::"r"(dst), "l"(src), "r"(have), "n"(kBytes) : "memory");
 }
-// fp32 rows into a box by asynchronous copies, which copies_wait ends.
-__device__ __forceinline__ void box_copy(const float* rows, int64_t ld, int64_t M, int N, int64_t row0, int col0, uint32_t box) {
-  const int lane = threadIdx.x & 31, n_rows = col0 + lane < N ? (int)min(M - row0, (int64_t)32) : 0;
-  const float* p = rows + row0 * ld + col0 + lane;
-#pragma unroll 8
-  for (int r = 0; r < 32; r++) {
-    copy_async<4>(box + r * 128 + (((lane >> 2) ^ (r & 7)) << 4) + (lane & 3) * 4, r < n_rows ? p : rows, r < n_rows ? 4 : 0);
-    p += ld;
+// A box between shared memory and rows that TMA cannot address, by a warp.  Rows of bf16 with an even pitch are rows
+// of half as many words; with an odd one they go value by value.  kWords: neighbouring words of an access (two
+// where the pitch in words is even).
+template <int kWords>
+__device__ __forceinline__ void box_in(const uint32_t* rows, int64_t ld, int64_t M, int N, int64_t row0, int col0, uint32_t box) {
+  constexpr int kLanes = 32 / kWords;
+  const int lane = threadIdx.x & 31, c = lane % kLanes * kWords, first = lane / kLanes;
+  const int n_rows = col0 + c < N ? (int)min(M - row0, (int64_t)32) : 0;
+  const uint32_t* p = rows + (row0 + first) * ld + col0 + c;
+#pragma unroll 4
+  for (int r = first; r < 32; r += kWords) {
+    copy_async<4 * kWords>(box + r * 128 + (((c >> 2) ^ (r & 7)) << 4) + (c & 3) * 4, r < n_rows ? p : rows, r < n_rows ? 4 * kWords : 0);
+    p += kWords * ld;
+  }
+}
+// (eight accesses at a time: more would take registers from the paths that have no use for this one)
+template <int kWords>
+__device__ __forceinline__ void box_out(uint32_t* rows, int64_t ld, int64_t M, int N, int64_t row0, int col0, uint32_t box) {
+  constexpr int kLanes = 32 / kWords;
+  const int lane = threadIdx.x & 31, c = lane % kLanes * kWords, first = lane / kLanes;
+  const int n_rows = col0 + c < N ? (int)min(M - row0, (int64_t)32) : 0;
+  uint32_t* p = rows + (row0 + first) * ld + col0 + c;
+#pragma unroll 1
+  for (int r0 = first; r0 < 32; r0 += 8 * kWords) {
+    uint2 w[8];
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+      const int r = r0 + i * kWords;
+      const uint32_t at = box + r * 128 + (((c >> 2) ^ (r & 7)) << 4) + (c & 3) * 4;
+      if constexpr (kWords == 2) asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(w[i].x), "=r"(w[i].y) : "r"(at) : "memory");
+      else asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w[i].x) : "r"(at) : "memory");
+    }
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+      if (r0 + i * kWords < n_rows) {
+        if constexpr (kWords == 2) *reinterpret_cast<uint2*>(p) = w[i];
+        else *p = w[i].x;
+      }
+      p += kWords * ld;
+    }
+  }
+}
+__device__ __forceinline__ void box_of_bf16(unsigned short* rows, int64_t ld, int64_t M, int N, int64_t row0, int col0, uint32_t box,
+                                            bool load) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll 1
+  for (int j = 0; j < 8; j++) {  // 32 columns of 8 rows
+    const int c = lane + 32 * (j & 1), r0 = 8 * (j >> 1), n_rows = col0 + c < N ? (int)min(M - row0 - r0, (int64_t)8) : 0;
+    unsigned short *p = rows + (row0 + r0) * ld + col0 + c, w[8];
+    if (load) {
+#pragma unroll
+      for (int r = 0; r < 8; r++) w[r] = r < n_rows ? p[r * ld] : (unsigned short)0;
+    }
+#pragma unroll
+    for (int r = 0; r < 8; r++) {
+      const uint32_t q = box + (r0 + r) * 128 + (((c >> 3) ^ r) << 4) + (c & 7) * 2;
+      if (load) asm volatile("st.shared.u16 [%0], %1;" ::"r"(q), "h"(w[r]) : "memory");
+      else asm volatile("ld.shared.u16 %0, [%1];" : "=h"(w[r]) : "r"(q) : "memory");
+    }
+    if (!load) {
+#pragma unroll
+      for (int r = 0; r < 8; r++)
+        if (r < n_rows) p[r * ld] = w[r];
+    }
+  }
+}
+// Columns of T; loads are under way until copies_wait.
+template <typename T>
+__device__ __forceinline__ void box_by_lanes(T* rows, int64_t ld, int64_t M, int N, int64_t row0, int col0, uint32_t box, bool load) {
+  if (sizeof(T) == 2 && (ld & 1)) {
+    box_of_bf16(reinterpret_cast<unsigned short*>(rows), ld, M, N, row0, col0, box, load);
+    return;
+  }
+  constexpr int kPer = 4 / sizeof(T);
+  uint32_t* w = reinterpret_cast<uint32_t*>(rows);
+  ld /= kPer, N /= kPer, col0 /= kPer;
+  if ((ld & 1) == 0) {
+    if (load) box_in<2>(w, ld, M, N, row0, col0, box);
+    else box_out<2>(w, ld, M, N, row0, col0, box);
+  } else {
+    if (load) box_in<1>(w, ld, M, N, row0, col0, box);
+    else box_out<1>(w, ld, M, N, row0, col0, box);
   }
 }
 __device__ __forceinline__ void copies_wait() {
@@ -350,8 +387,7 @@ struct Boxes {
     if (g.plain) {
       const uint32_t to = base + (serial ? 0 : (turn + ahead) & 1) * kBox;
       auto one = [&](const void* from, uint32_t box) {
-        if constexpr (sizeof(T) == 4) box_copy(static_cast<const float*>(from), g.ldy, g.M, g.N, row, col, box);
-        else box_by_lanes<T>(const_cast<T*>(static_cast<const T*>(from)), g.ldy, g.M, g.N, row, col, box, true);
+        box_by_lanes<T>(const_cast<T*>(static_cast<const T*>(from)), g.ldy, g.M, g.N, row, col, box, true);
       };
       if (g.load_res) one(g.e.res, to);
       if (g.load_pre) one(g.e.pre_in, both ? to + kBox : to);
@@ -371,7 +407,7 @@ struct Boxes {
   // Before the chunk's box is read and written.
   __device__ __forceinline__ bool ready(int64_t row, int col, Abort* ab, uint32_t* status) {
     if (g.plain) {
-      if (sizeof(T) == 4 && loads) copies_wait();
+      if (loads) copies_wait();
       return true;
     }
     if (loads) {
@@ -661,8 +697,6 @@ inline bool fill_args(TcArgs& g, const LinearProblem& p, const LinearPlan& plan,
   g.units = g.tiles * plan.splits;
   const int pairs = std::min(g.units, num_sms() / 2);
   g.step_n = pairs % g.n_tiles, g.step_m = pairs / g.n_tiles % g.m_tiles, g.step_split = pairs / g.tiles;
-  // Segments: where results are fp32, 256 terms of three parts, 512 of one.
-  g.seg = split || dw || f32 ? (f32 ? 4 : 8) : 1 << 30;
   g.idesc = idesc_bf16(256, g.bn, g.a_mn, g.b_mn);
   g.idesc_sum = idesc_bf16(256, 32, g.a_mn, false);
   g.a_step = g.a_mn ? 128 : 2, g.b_step = g.b_mn ? 128 : 2;
@@ -685,6 +719,9 @@ inline bool fill_args(TcArgs& g, const LinearProblem& p, const LinearPlan& plan,
     g.load_pre = g.store_pre = 0;
   }
   g.sums = dw && e.sums && !sums_apart(g);
+  // Segments: where results are fp32, 256 terms of three parts; 512 of one, 1024 where dbias keeps the products
+  // waiting while a segment is taken out.
+  g.seg = split || dw || f32 ? (f32 ? 4 : g.sums ? 16 : 8) : 1 << 30;
   g.plain = g.ldy * size % 16 != 0;
   if (g.plain) return true;
   bool ok = make_map(&g.y, g.e.y, size, g.ldy, p.M, plan.splits, g.ldy, 32);

@@ -6,8 +6,8 @@ Bounds, elementwise, with u = 2^-24 (fp32's half step) and h the rows' half step
 * fp32 multiply-adds run over at most 128 terms, these sums over K / 128 in each part, and at most
   304 parts, eight at a time (38) and these eight in turn, are added: (128 + K / 128 + 46) u S.
 * Tensor cores add 16 products a step and cut their accumulator towards zero, 2 u of it each time.
-  Sums with fp32 results are taken out after at most 512 terms (32 steps, 64 u) and added in fp32, K / 512
-  times over all parts; fp32 operands come in three bf16 parts, which leave out at most 5 u of a
+  Sums with fp32 results are taken out after at most 1024 terms (64 steps, 128 u) and added in fp32, K / 256
+  times over all parts at most, in as many chains as there are parts; fp32 operands come in three bf16 parts, which leave out at most 5 u of a
   product.  bf16 results are rounded to 2^-9, and their sums run through: K / 16 steps, K / 8 u.
 So fp32 results are within (180 + K / 128) u S and bf16 rows before their rounding (180 + K / 8) u S.
 

@@ -14,7 +14,8 @@ pytestmark = pytest.mark.gpu
 SIZES = [(1, 1, 1), (1, 7, 5), (1, 1024, 100), (3, 130, 1), (4, 256, 1030), (5, 64, 33), (17, 8, 8), (63, 31, 65), (64, 64, 64),
          (100, 64, 66), (127, 100, 101), (129, 256, 128), (200, 72, 136), (255, 136, 264), (257, 200, 72), (300, 330, 198),
          (513, 96, 320), (1000, 33, 257), (1030, 520, 40), (600, 700, 72), (3000, 601, 131), (2051, 64, 264), (70, 2049, 130), (30000, 24, 40), (4100, 520, 1032), (9000, 328, 600),
-         (20000, 256, 256), (3000, 1100, 72)]
+         (20000, 256, 256), (3000, 1100, 72), (4100, 518, 1030),
+         (1300, 301, 555)]
 
 
 @pytest.mark.parametrize("R, K, N", SIZES)
@@ -37,7 +38,7 @@ def test_backward(lib, dtype, R, K, N):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("R, K, N", [(5, 40, 24), (700, 264, 328), (700, 331, 263)])
+@pytest.mark.parametrize("R, K, N", [(5, 40, 24), (700, 264, 328), (700, 331, 263), (1700, 264, 328), (1700, 331, 263)])
 def test_non_finite_values_stay_where_they_enter(lib, dtype, R, K, N):
     rng = np.random.default_rng(5)
     x, W, g = (t.tensor(rng, s, dtype) for s in ((R, K), (N, K), (R, N)))
@@ -160,7 +161,8 @@ def test_the_product_and_the_dropout_call_draw_the_same_mask(lib):
         assert torch.equal(y != 0, z != 0)
 
 
-@pytest.mark.parametrize("R, K, N, dtype", [(9, 40, 24, "bf16"), (3000, 256, 264, "bf16"), (3000, 100, 66, "f32"), (700, 33, 65, "bf16")])
+@pytest.mark.parametrize("R, K, N, dtype", [(9, 40, 24, "bf16"), (3000, 256, 264, "bf16"), (3000, 100, 66, "f32"), (3000, 300, 200, "f32"), (3000, 201, 301, "f32"),
+                                           (700, 33, 65, "bf16"), (700, 333, 165, "bf16")])
 def test_calls_repeat_to_the_bit_and_graphs_draw_anew(lib, R, K, N, dtype):
     rng = np.random.default_rng(1)
     x, W, g, pre = (t.tensor(rng, s, dtype) for s in ((R, K), (N, K), (R, N), (R, K)))
