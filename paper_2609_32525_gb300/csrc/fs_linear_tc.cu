@@ -13,7 +13,8 @@ namespace {
 
 // Where sums are short the epilogue is the work: five warpgroups with one box each.  Where they are long, or a
 // chunk has two inputs or results, three with two boxes.  (1,048,576 x 256 x 256 with dropout and residual:
-// 361 us against 404 with three groups; 32,768 x 1024 x 4096 173 us with three against 183 with five.)
+// 353 us; with four groups 384, with six 359, with three and their two boxes 383 before the others had a box fewer.
+// 32,768 x 1024 x 4096: 173 us with three against 183 with five.)
 constexpr int kManyGroups = 5, kShortK = 512;
 
 // T: float for dW and split sums.
