@@ -161,8 +161,10 @@ __device__ __forceinline__ uint64_t poly2(const float (&c)[n], uint64_t x) {
   for (int i = n - 2; i >= 0; i--) q = tc::fma2(q, x, twice(c[i]));
   return q;
 }
-// Phi(-a) for 0 <= a <= kGaussEnd; e: e^(-a^2/2).
-template <bool kFast>
+// Phi(-a) for 0 <= a <= kGaussEnd; e: e^(-a^2/2).  kTail: small values are good to their own size; without it (a
+// derivative adds them to others) the Newton steps and the exponent's remainder are left out, and fp32's absolute
+// error is 2^-21 at most: quotients and polynomial 8 u of 1/2, and a^2/2 e^(-a^2/2) u from the exponent.
+template <bool kFast, bool kTail>
 __device__ __forceinline__ uint64_t gauss_tail2(float a0, float a1, uint64_t& e) {
   const uint64_t a = pair(a0, a1);
   if constexpr (kFast) {
@@ -180,16 +182,20 @@ __device__ __forceinline__ uint64_t gauss_tail2(float a0, float a1, uint64_t& e)
     const uint64_t r = pair(rcp(tc::lo_f(both)), rcp(tc::hi_f(both)));
     const uint64_t up_r = tc::mul2(r, den);
     uint64_t t = tc::mul2(down, up_r), s = tc::mul2(r, up);
-    t = tc::fma2(tc::fma2(tc::mul2(t, minus), up, down), up_r, t);
-    s = tc::fma2(s, tc::fma2(tc::mul2(s, minus), den, twice(1.f)), s);
+    if (kTail) {
+      t = tc::fma2(tc::fma2(tc::mul2(t, minus), up, down), up_r, t);
+      s = tc::fma2(s, tc::fma2(tc::mul2(s, minus), den, twice(1.f)), s);
+    }
     // a^2 = h + l; the exponent y = -h log2(e) / 2 and what it leaves out
-    const uint64_t h = tc::mul2(a, a), l = tc::fma2(a, a, tc::mul2(h, minus));
-    const uint64_t y = tc::mul2(h, twice(-0.5f * kLog2eHi));
-    uint64_t left = tc::fma2(h, twice(-0.5f * kLog2eHi), tc::mul2(y, minus));
-    left = tc::fma2(h, twice(-0.5f * kLog2eLo), left);
-    left = tc::fma2(l, twice(-0.5f * kLog2eHi), left);
+    const uint64_t h = tc::mul2(a, a), y = tc::mul2(h, twice(-0.5f * kLog2eHi));
     e = pair(tc::ex2(tc::lo_f(y)), tc::ex2(tc::hi_f(y)));
-    e = tc::fma2(tc::mul2(e, twice(kLn2)), left, e);
+    if (kTail) {
+      const uint64_t l = tc::fma2(a, a, tc::mul2(h, minus));
+      uint64_t left = tc::fma2(h, twice(-0.5f * kLog2eHi), tc::mul2(y, minus));
+      left = tc::fma2(h, twice(-0.5f * kLog2eLo), left);
+      left = tc::fma2(l, twice(-0.5f * kLog2eHi), left);
+      e = tc::fma2(tc::mul2(e, twice(kLn2)), left, e);
+    }
     return tc::mul2(tc::mul2(e, s), poly2(c, t));
   }
 }
@@ -198,7 +204,7 @@ template <bool kFast>
 __device__ __forceinline__ void gelu2(float& u0, float& u1) {
   const float a0 = fminf(fabsf(u0), kGaussEnd), a1 = fminf(fabsf(u1), kGaussEnd);
   uint64_t e;
-  const uint64_t t = gauss_tail2<kFast>(a0, a1, e);
+  const uint64_t t = gauss_tail2<kFast, true>(a0, a1, e);
   const uint64_t y = tc::fma2(t, pair(-a0, -a1), pair(max_nan(u0, 0.f), max_nan(u1, 0.f)));
   u0 = tc::lo_f(y), u1 = tc::hi_f(y);
 }
@@ -206,7 +212,7 @@ template <bool kFast>
 __device__ __forceinline__ void gelu_slope2(float& u0, float& u1) {
   const float v0 = max_nan(min_nan(u0, kGaussEnd), -kGaussEnd), v1 = max_nan(min_nan(u1, kGaussEnd), -kGaussEnd);
   uint64_t e;
-  const uint64_t t = gauss_tail2<kFast>(fabsf(v0), fabsf(v1), e);
+  const uint64_t t = gauss_tail2<kFast, false>(fabsf(v0), fabsf(v1), e);
   const float t0 = tc::lo_f(t), t1 = tc::hi_f(t);
   const uint64_t cdf = pair(v0 > 0.f ? 1.f - t0 : t0, v1 > 0.f ? 1.f - t1 : t1);
   const uint64_t y = tc::fma2(tc::mul2(pair(v0, v1), twice(kInvSqrt2Pi)), e, cdf);
