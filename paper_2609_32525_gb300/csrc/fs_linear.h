@@ -76,7 +76,7 @@ struct LinearPack {
 cudaError_t linear_pack(const LinearPack* packs, int n, uint32_t* status, cudaStream_t st);
 // dbias alone: the sums of a (rows of pitch ld, a multiple of 16 bytes in bf16) over its K rows; part
 // [kLinearSumParts][M].
-constexpr int kLinearSumParts = 64;
+constexpr int kLinearSumParts = 128;
 cudaError_t linear_sums(const LinearProblem& p, int ld, float* part, const LinearEnd& e, cudaStream_t st);
 // Adds up the parts of a product and ends it: part [splits][M][ld], ld the columns rounded up to a
 // multiple of 4; sums [splits][M] behind it for dW.

@@ -668,7 +668,7 @@ bool make_map(CUtensorMap* map, const void* p, int size, int64_t cols, int64_t r
 
 // dbias as a product with ones takes the second half of TMEM, so that the unit that does it does nothing else
 // meanwhile.  Where a tile's columns are a small part of dW the other units would wait for that one: then two
-// kernels add g up (dW of 32,768 rows, 1024 x 4096: 328 us with the product, 205 without, 241 with the kernels).
+// kernels add g up (dW of 32,768 rows, 1024 x 4096: 328 us with the product, 205 without, 229 with the kernels).
 inline bool sums_apart(const TcArgs& g) { return g.n_tiles > 2; }
 // After the product: dbias by the kernels, and the join of split sums.
 inline cudaError_t finish(const TcArgs& g, const LinearProblem& p, const LinearPlan& plan, const LinearEnd& e, void* scratch,
