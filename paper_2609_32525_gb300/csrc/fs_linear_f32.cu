@@ -21,11 +21,13 @@ namespace fs {
 namespace {
 
 constexpr int kLoaders = 12, kFirstLoader = 4, kFirstEpilogue = 16, kThreadsF32 = 768;
-constexpr int kPieces = 1536 / (kLoaders * 32), kLines = kLoaders * 4;  // of a loader; image rows that all of them take at a time
+// Pieces of a loader in a block; image rows that all loaders take at a time.
+constexpr int kPieces = 1536 / (kLoaders * 32), kLines = kLoaders * 4;
 constexpr uint32_t kPartA = kABytes, kPartB = kABytes / 2, kStageF32 = 3 * (kPartA + kPartB);
 constexpr int kStagesF32 = 2;
 constexpr uint32_t kBoxesF32 = 8 * kBox;
-constexpr uint32_t kRaw = kPieces * 2 * kLoaders * 32 * 16;  // a block's values as they come: [piece][half][loader] of 16 bytes
+// A block's values as they come: [piece][half][loader] of 16 bytes.
+constexpr uint32_t kRaw = kPieces * 2 * kLoaders * 32 * 16;
 constexpr size_t kSmemF32 = 1024 + kStagesF32 * kStageF32 + kBoxesF32 + kRaw + kOnes;
 static_assert(kSmemF32 + 1024 <= 232448);
 
@@ -73,7 +75,8 @@ __device__ __forceinline__ void split8(const float (&v)[8], bool infinite, uint4
 
 // The lanes with an infinity among their values.  The vote takes every value, so that all of them have come from
 // shared memory when it is over: only then may the next copies go there.  What releases the memory has to use the
-// vote's result, in a way that no compiler can leave out (& g.none): nothing else keeps the compiler, or the load unit, from releasing it earlier.
+// vote's result, in a way that no compiler can leave out (& g.none): nothing else keeps the compiler, or the load
+// unit, from releasing it earlier.
 __device__ __forceinline__ uint32_t lanes_with_infinity(const float (&v)[kPieces][8]) {
   float top = 0.f;
 #pragma unroll

@@ -72,6 +72,23 @@ def test_non_finite_values_stay_where_they_enter(lib, dtype, R, K, N):
     assert torch.isfinite(y[:, ok]).all() and torch.isnan(y[:, ~ok]).all()
 
 
+@pytest.mark.parametrize("R", [64, 2048])
+def test_fp32_values_up_to_the_largest(lib, R):
+    """Rows of fp32's largest values and weights that bring them back: nothing on the way is infinite."""
+    rng = np.random.default_rng(6)
+    K = N = 256
+    top = np.float32(np.finfo(np.float32).max)
+    x = (top * rng.uniform(0.97, 1.0, (R, K)).astype(np.float32) * rng.choice(np.float32([-1, 1]), (R, K))).astype(np.float32)
+    x[:, 0] = top
+    W = (rng.standard_normal((N, K)) * 2.0 ** -30).astype(np.float32)
+    s = lib.make_linear(R, K, N, torch.float32)
+    assert lib.linear_path_for_shape(s) == (R == 2048)
+    y = torch.empty(R, N, device="cuda")
+    lib.fs_linear_fwd(s, torch.from_numpy(x).cuda(), torch.from_numpy(W).cuda(), None, 0, 0.0, None, None, y, None, lib.linear_workspace(s))
+    x, W = x.astype(np.float64), W.astype(np.float64)
+    assert (np.abs(t.host(y) - x @ W.T) <= t.sum_bound(K, np.abs(x) @ np.abs(W).T, "f32")).all()
+
+
 WIDTHS = [1, 2, 3, 4, 5, 6, 8, 12, 30, 31, 32, 64, 66, 100, 198, 255, 256, 1000, 8192]
 
 
