@@ -119,8 +119,10 @@ LinearPlan linear_plan(int op, int dtype, int64_t M, int N, int64_t K) {
   const double work = (double)M * N * (double)K;
   // Below this many products of terms a block's start and the two CTAs' hand-overs cost more than multiply-adds (1024
   // rows of 64 -> 64 bf16: 17 us against 13, of 256 -> 256 fp32: 23 against 17, backward 49 against 25).
+  // Few channels fill a tile badly, but those calls are bound by HBM (1,048,576 x 256 -> 4 bf16: forward 1093 us in
+  // multiply-adds and 132 here, backward 2551 and 278).
   const double least = dtype == FS_BF16 ? 16777216.0 : 134217728.0;
-  p.path = work >= least && M > kLinearFew && N >= 16 && K >= 16 && std::max(M, K) < (1LL << 31) - 512;
+  p.path = work >= least && (M > kLinearFew || op == kLinDw) && std::max(M, K) < (1LL << 31) - 512;
   int64_t splits;
   if (p.path) {
     // Pairs of CTAs take tiles; where there are fewer than half as many tiles, sums are split into parts of

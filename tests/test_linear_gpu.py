@@ -15,7 +15,8 @@ SIZES = [(1, 1, 1), (1, 7, 5), (1, 1024, 100), (3, 130, 1), (4, 256, 1030), (5, 
          (100, 64, 66), (127, 100, 101), (129, 256, 128), (200, 72, 136), (255, 136, 264), (257, 200, 72), (300, 330, 198),
          (513, 96, 320), (1000, 33, 257), (1030, 520, 40), (600, 700, 72), (3000, 601, 131), (2051, 64, 264), (70, 2049, 130), (30000, 24, 40), (4100, 520, 1032), (9000, 328, 600),
          (20000, 256, 256), (3000, 1100, 72), (4100, 518, 1030),
-         (1300, 301, 555), (40, 8192, 300), (40, 300, 8192)]
+         (1300, 301, 555), (40, 8192, 300), (40, 300, 8192), (70000, 256, 1),
+         (70000, 3, 100), (140000, 320, 3), (140000, 4, 240)]
 
 
 @pytest.mark.parametrize("R, K, N", SIZES)
