@@ -285,9 +285,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreadsF32, 1)
               mul(d, 0, 0, more);
               if (sums)
 #pragma unroll
-                for (int i = 2; i >= 0; i--)
-                  mma_pair_w<kHi128, kHi32>(tmem + kSumCol, a_lo + i * (kPartA >> 4) + k * g.a_step, ones_lo, g.idesc_sum,
-                                            more || i < 2);
+                for (int i = 2; i >= 0; i--)  // lo and mid apart from hi, as the products
+                  mma_pair_w<kHi128, kHi32>(tmem + kSumCol + (i ? kSumSmall : 0), a_lo + i * (kPartA >> 4) + k * g.a_step, ones_lo,
+                                            g.idesc_sum, more || i == 1);
             }
             mma_commit_pair_w(&empty[ring.i]);
             ring.next();
