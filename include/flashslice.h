@@ -425,8 +425,8 @@ fs_status fs_ckpt_unpack(const fs_rows* s, const int8_t* q8, const uint8_t* e8, 
  * shall see its mask gets the same two words there; calls that shall not share a mask (another
  * layer, another step) get different offsets.
  *
- * Sums are fp32.  FS_BF16: products of bf16 values, exact; GELU and SILU to 2^-12 of themselves
- * (for u > -5; below, where |gelu| < 2e-6, to 2e-7), y, pre and dx rounded to bf16.  FS_F32: fp32
+ * Sums are fp32.  FS_BF16: products of bf16 values, exact; GELU and SILU to 2^-16 of themselves (where
+ * they are below 2^-119: to 2^-119), their derivatives to 2^-19; y, pre and dx rounded to bf16.  FS_F32: fp32
  * throughout, sums of products to a few 2^-24 of their terms' magnitudes.  An infinity or NaN in
  * x, W or g makes results that it enters non-finite, and no others.
  *

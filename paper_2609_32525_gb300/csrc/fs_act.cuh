@@ -110,16 +110,18 @@ __device__ __forceinline__ void keep(const Drop& d, const DropKey& k, uint64_t q
 
 // ---- activations ---------------------------------------------------------------------------
 //
-// kFast: for values that are rounded to bf16 afterwards (half a step is 2^-9 of the value).
+// kFast: for values that are rounded to bf16 afterwards, by half a step of 2^-9 to 2^-8 of the value.  GELU and SILU are
+// good to 2^-16 of themselves over the whole range, their derivatives to 2^-19.
 //
 // All of them two values at a time (f32x2 instructions).
 //
 // GELU is u Phi(u).  For a = |u|, Phi(-a) = e^(-a^2/2) Q(a) with Q(a) = erfcx(a / sqrt 2) / 2, a smooth function
 // that falls slowly; the exponential serves the derivative Phi(u) + u e^(-u^2/2) / sqrt(2 pi) too.
-//   kFast: a polynomial of degree 8 on [0, 5], within 1.6e-4 of Q; past 5, where gelu(-a) is below 1.5e-6, Q stays
-//   at Q(5) and the Gaussian goes on falling.
-//   else: Q(a) (1 + 2 a) as a polynomial of degree 9 in (a - k) / (a + k) on [0, 15], within 1.3e-8 (the form of
-//   Shepherd and Laframboise, "Chebyshev approximation of (1 + 2x) exp(x^2) erfc x in 0 <= x < inf", 1981).
+//   kFast: Q(a) (a + k) as a polynomial of degree 6 in (a - k) / (a + k) on [0, 15], within 1.4e-6 of itself.  (A
+//   polynomial of degree 8 in a on [0, 5], Q held past 5, has as many instructions but the reciprocal; it was off by
+//   1.6e-4, and past 5 by up to the value itself.)
+//   else: Q(a) (1 + 2 a) as a polynomial of degree 9 in (a - k) / (a + k) on [0, 15], within 2.7e-8 of itself (the
+//   form of Shepherd and Laframboise, "Chebyshev approximation of (1 + 2x) exp(x^2) erfc x in 0 <= x < inf", 1981).
 //   Quotients get one Newton step, and the exponent's rounding is put back after the exponential.
 // Both polynomials are weighted least-squares fits, reweighted towards the minimax one.
 constexpr float kInvSqrt2Pi = 0.3989422804014327f;
@@ -168,11 +170,12 @@ template <bool kFast, bool kTail>
 __device__ __forceinline__ uint64_t gauss_tail2(float a0, float a1, uint64_t& e) {
   const uint64_t a = pair(a0, a1);
   if constexpr (kFast) {
-    constexpr float c[9] = {0.49994163f,   -0.39726451f,  0.24129194f,    -0.11416839f,  0.040258871f,
-                            -0.0099215629f, 0.0015831057f, -0.00014531538f, 5.7904302e-06f};
-    const uint64_t s = tc::mul2(tc::mul2(a, twice(-0.5f * kLog2eHi)), a);
-    e = pair(tc::ex2(tc::lo_f(s)), tc::ex2(tc::hi_f(s)));
-    return tc::mul2(e, poly2(c, pair(fminf(a0, 5.f), fminf(a1, 5.f))));
+    constexpr float k = 5.f;
+    constexpr float c[7] = {0.769192398f, -0.665391624f, 0.495357752f, -0.313332379f, 0.164524734f, -0.070451133f, 0.0217513554f};
+    const uint64_t up = tc::add2(a, twice(k)), r = pair(rcp(tc::lo_f(up)), rcp(tc::hi_f(up)));
+    const uint64_t y = tc::mul2(tc::mul2(a, twice(-0.5f * kLog2eHi)), a);
+    e = pair(tc::ex2(tc::lo_f(y)), tc::ex2(tc::hi_f(y)));
+    return tc::mul2(tc::mul2(e, r), poly2(c, tc::fma2(r, twice(-2.f * k), twice(1.f))));
   } else {
     constexpr float k = 2.8125f;
     constexpr float c[10] = {0.849999964f,     0.0238276552f,  -0.168504149f,   0.131846741f,    -0.0378766023f,

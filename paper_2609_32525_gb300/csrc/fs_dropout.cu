@@ -1,9 +1,8 @@
 // Dropout of rows with an activation and a residual, forward and backward.  Each value is read and
-// written once (a mask is computed, not stored).  1,048,576 x 256 bf16 with a residual: 259 us, 92% of this
-// card's copy rate; without the residual 246 us, which is the generator: 18 products of 32 x 32 bits for
-// four values at 32 a clock and SM are 129 us of it, its xors, comparisons and selections at 64 as many, and
-// the two pipes overlap by half.  All launches have eight blocks an SM: fewer, all resident at once, were
-// slower (five 287 us, four 271).
+// written once (a mask is computed, not stored).  1,048,576 x 256 bf16 with a residual: 253 us, 94% of this
+// card's copy rate; without the residual 223 us, which is the generator: 18 products of 32 x 32 bits for
+// four values at 32 a clock and SM are 129 us of it, beside its xors, comparisons and selections at 64 as many.  Blocks walk
+// over the rows, 16 an SM (8 for ragged rows), more than are resident: 8 take 10 us longer there, 32 up to 1 us for 60,033 rows.
 #include "fs_act.cuh"
 #include "fs_internal.h"
 #include "fs_launch.h"
@@ -17,16 +16,19 @@ namespace {
 // What is read beside x: nothing, a residual, or the pre-activations of a backward.
 enum { kPlain = 0, kRes = 1, kSlope = 2 };
 
-// n values, quad after quad: v becomes the result; other: what is read beside x.
-template <typename T, int MODE, int n, typename Q>
+// n values, quad after quad: v becomes the result; other: what is read beside x.  ACT: the activation, or kAnyAct.
+constexpr int kAnyAct = -1;
+template <typename T, int MODE, int ACT, int n, typename Q>
 __device__ __forceinline__ void drop(const DropArgs& a, const act::DropKey& key, Q quad, float (&other)[n], float (&v)[n]) {
   constexpr bool kFast = sizeof(T) == 2;
   if (MODE == kSlope) {
-    act::slope<kFast>(a.act, other, v);
+    if constexpr (ACT == kAnyAct) act::slope<kFast>(a.act, other, v);
+    else act::slope<kFast, ACT>(other, v);
 #pragma unroll
     for (int i = 0; i < n; i++) v[i] = other[i];
   } else {
-    act::apply<kFast>(a.act, v);
+    if constexpr (ACT == kAnyAct) act::apply<kFast>(a.act, v);
+    else act::apply<kFast, ACT>(v);
   }
   if (a.rng) {
     float r[n];
@@ -43,9 +45,11 @@ __device__ __forceinline__ void drop(const DropArgs& a, const act::DropKey& key,
 
 // Rows of a multiple of four channels: the quads lie one after another, so rows do not matter.
 // A thread takes 16 bytes of each tensor at a time, the next ones on their way while it works.
-// Q: uint32_t where the quads' numbers fit.
-template <typename T, int MODE, typename Q>
-__global__ void __launch_bounds__(256) k_dropout(DropArgs a) {
+// Q: uint32_t where the quads' numbers fit.  A kernel an activation: behind one branch the loop of each has the registers
+// of all.  bf16: at most 48 registers (five blocks an SM; 264 us above with the compiler's choice, 253 with this one);
+// fp32 is left to the compiler (323 us for 1,048,576 x 256, 409 with the bound).
+template <typename T, int MODE, int ACT, typename Q>
+__global__ void __launch_bounds__(256, sizeof(T) == 2 ? 5 : 0) k_dropout(DropArgs a) {
   const int64_t zero = grid_begin();
   constexpr int kV = 16 / sizeof(T);  // values of a piece
   const int64_t values = a.rows * a.C, step = (int64_t)gridDim.x * 256 * kV;
@@ -73,7 +77,7 @@ __global__ void __launch_bounds__(256) k_dropout(DropArgs a) {
       if (MODE != kPlain) act::load4(reinterpret_cast<const T*>(&u) + h, 4, true, *reinterpret_cast<float(*)[4]>(f + h));
     }
     load(at + step);
-    drop<T, MODE, kV>(a, key, (Q)(at >> 2), f, v);
+    drop<T, MODE, ACT, kV>(a, key, (Q)(at >> 2), f, v);
     int4 out;
 #pragma unroll
     for (int h = 0; h < kV; h += 4)
@@ -115,19 +119,27 @@ __global__ void __launch_bounds__(256) k_dropout_ragged(DropArgs a) {
     row += rows_on, col += cols_on;
     if (col >= per_row) col -= per_row, row++;
     if (q + step < quads) load();
-    drop<T, MODE, 4>(a, key, (Q)q, f, v);
+    drop<T, MODE, kAnyAct, 4>(a, key, (Q)q, f, v);
     act::store4(y + at, n, false, v);
   }
 }
 
+template <typename T, int MODE, int ACT>
+cudaError_t run_flat(const DropArgs& a, bool low, dim3 grid, cudaStream_t st) {
+  return launch(low ? k_dropout<T, MODE, ACT, uint32_t> : k_dropout<T, MODE, ACT, uint64_t>, grid, dim3(256), 0, st, a);
+}
 template <typename T, int MODE>
 cudaError_t run(const DropArgs& a, cudaStream_t st) {
   const bool flat = (a.C & 3) == 0;
   const int64_t quads = a.rows * ((a.C + 3) >> 2), pieces = flat ? (quads * 4 * (int64_t)sizeof(T) + 15) / 16 : quads;
   const bool low = quads + 8 < (1LL << 32);
-  const dim3 grid((unsigned)std::min<int64_t>((pieces + 255) / 256, (int64_t)num_sms() * 8));
-  if (flat) return launch(low ? k_dropout<T, MODE, uint32_t> : k_dropout<T, MODE, uint64_t>, grid, dim3(256), 0, st, a);
-  return launch(low ? k_dropout_ragged<T, MODE, uint32_t> : k_dropout_ragged<T, MODE, uint64_t>, grid, dim3(256), 0, st, a);
+  const dim3 grid((unsigned)std::min<int64_t>((pieces + 255) / 256, (int64_t)num_sms() * (flat ? 16 : 8)));
+  if (!flat) return launch(low ? k_dropout_ragged<T, MODE, uint32_t> : k_dropout_ragged<T, MODE, uint64_t>, grid, dim3(256), 0, st, a);
+  if (a.act == FS_ACT_GELU) return run_flat<T, MODE, FS_ACT_GELU>(a, low, grid, st);
+  if (a.act == FS_ACT_SILU) return run_flat<T, MODE, FS_ACT_SILU>(a, low, grid, st);
+  if (a.act == FS_ACT_RELU) return run_flat<T, MODE, FS_ACT_RELU>(a, low, grid, st);
+  if constexpr (MODE != kSlope) return run_flat<T, MODE, FS_ACT_NONE>(a, low, grid, st);
+  else return cudaErrorInvalidValue;  // (a backward without an activation reads nothing beside x)
 }
 template <typename T>
 cudaError_t by_mode(const DropArgs& a, cudaStream_t st) {
