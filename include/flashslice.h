@@ -427,8 +427,9 @@ fs_status fs_ckpt_unpack(const fs_rows* s, const int8_t* q8, const uint8_t* e8, 
  *
  * Sums are fp32.  FS_BF16: products of bf16 values, exact; GELU and SILU to 2^-16 of themselves (where
  * they are below 2^-119: to 2^-119), their derivatives to 2^-19; y, pre and dx rounded to bf16.  FS_F32: fp32
- * throughout, sums of products to a few 2^-24 of their terms' magnitudes.  An infinity or NaN in
- * x, W or g makes results that it enters non-finite, and no others.
+ * throughout, sums of products to a few 2^-24 of their terms' magnitudes.  Infinities and NaN
+ * in x, W, g or a bias go through sums, activations and residuals as in fp32 arithmetic, and to no
+ * results that they do not enter; a dropped value is 0 whatever it was.
  *
  * Supported: rows >= 1; Cin, Cout in [1, 8192]; rows*max(Cin, Cout) < 2^40.  No output may share a
  * byte with an input or another output, except where a call says so (FS_ERR_INVALID). */

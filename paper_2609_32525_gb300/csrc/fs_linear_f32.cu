@@ -53,21 +53,31 @@ __device__ __forceinline__ void copy8(const float* p, int n, int vec, uint32_t t
   }
 }
 
-// The three parts of 8 values, 16 bytes each.  infinite: some value of the warp is; an infinity has no further parts.
-__device__ __forceinline__ void split8(const float (&v)[8], bool infinite, uint4 (&p)[3]) {
+// The three parts of 8 values, 16 bytes each.  kInfinite: some value of the warp is.  An infinity has the parts (+-1, 0, +-inf):
+// it then meets the other operand's hi alone, which has that value's sign and is 0 only where the value is, and sums are
+// infinite or NaN as in fp32.  (As hi it would meet mid and lo, too, which are 0 or of either sign: NaN.)  The 1 is for an
+// infinity in both operands.
+template <bool kInfinite>
+__device__ __forceinline__ void split8(const float (&v)[8], uint4 (&p)[3]) {
   uint32_t w[3][4];
 #pragma unroll
   for (int i = 0; i < 4; i++) {
     const uint32_t x0 = __float_as_uint(v[2 * i]), x1 = __float_as_uint(v[2 * i + 1]);
-    float r0 = v[2 * i] - __uint_as_float(x0 & 0xFFFF0000u), r1 = v[2 * i + 1] - __uint_as_float(x1 & 0xFFFF0000u);
-    if (infinite) {
-      if (fabsf(v[2 * i]) == INFINITY) r0 = 0.f;
-      if (fabsf(v[2 * i + 1]) == INFINITY) r1 = 0.f;
-    }
+    const float r0 = v[2 * i] - __uint_as_float(x0 & 0xFFFF0000u), r1 = v[2 * i + 1] - __uint_as_float(x1 & 0xFFFF0000u);
     const uint32_t mid = pack_bf16(r0, r1);
     w[0][i] = __byte_perm(x0, x1, 0x7632);
     w[1][i] = mid;
     w[2][i] = pack_bf16(r0 - __uint_as_float(mid << 16), r1 - __uint_as_float(mid & 0xFFFF0000u));
+  }
+  if (kInfinite) {
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+      const uint32_t half = i & 1 ? 0xFFFF0000u : 0x0000FFFFu, x = __byte_perm(__float_as_uint(v[i]), 0, 0x3232) & half;
+      if (fabsf(v[i]) != INFINITY) continue;
+      w[0][i >> 1] ^= 0x40004000u & half;  // 0x7F80 to 0x3F80, which is 1
+      w[1][i >> 1] &= ~half;
+      w[2][i >> 1] = (w[2][i >> 1] & ~half) | x;
+    }
   }
 #pragma unroll
   for (int i = 0; i < 3; i++) p[i] = make_uint4(w[i][0], w[i][1], w[i][2], w[i][3]);
@@ -200,17 +210,21 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreadsF32, 1)
       ok = mbar_wait_w(&empty[ring.i], ring.pass ^ 1u, ab, status);
       if (!ok) break;
       const uint32_t stage = stage0 + ring.i * kStageF32;
+      auto store = [&](auto is_infinite) {
 #pragma unroll
-      for (int i = 0; i < kPieces; i++) {
-        const int r = line + kLines * i;
-        uint4 p[3];
-        split8(v[i], infinite != 0, p);
-        const bool of_a = r < 128;
-        const uint32_t at = stage + (of_a ? r : r - 128 + 3 * 128) * 128 + ((uint32_t)(piece ^ (r & 7)) << 4);
-        const uint32_t step = of_a ? kPartA : kPartB;
+        for (int i = 0; i < kPieces; i++) {
+          const int r = line + kLines * i;
+          uint4 p[3];
+          split8<decltype(is_infinite)::value>(v[i], p);
+          const bool of_a = r < 128;
+          const uint32_t at = stage + (of_a ? r : r - 128 + 3 * 128) * 128 + ((uint32_t)(piece ^ (r & 7)) << 4);
+          const uint32_t step = of_a ? kPartA : kPartB;
 #pragma unroll
-        for (int q = 0; q < 3; q++) st_shared_v4(at + q * step, p[q].x, p[q].y, p[q].z, p[q].w);
-      }
+          for (int q = 0; q < 3; q++) st_shared_v4(at + q * step, p[q].x, p[q].y, p[q].z, p[q].w);
+        }
+      };
+      if (infinite) store(std::true_type{});
+      else store(std::false_type{});
       fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive_leader(full0 + 8 * ring.i);
