@@ -10,7 +10,7 @@
 namespace fs {
 
 constexpr int kLinearMaxC = 8192;
-constexpr int kLinearFew = 8;   // rows of a forward that a kernel of its own takes
+constexpr int kLinearFew = 8;   // rows of a forward that a kernel of its own can take
 
 // The three products of a linear map, each D[m, n] = sum_k A[m, k] B[n, k]:
 //   forward  D = u  [rows, Cout], A = x, B = W
@@ -46,6 +46,7 @@ struct LinearProblem {
 // How a product runs; a function of its sizes and the device alone.
 struct LinearPlan {
   int path;         // 0: fp32 multiply-adds, 1: tcgen05
+  int few;          // path 0: by the kernel for few rows
   int splits;       // parts of the sum, added in order by k_linear_join
   int64_t per;      // terms of a part
   size_t part;      // bytes of scratch for parts

@@ -122,9 +122,16 @@ LinearPlan linear_plan(int op, int dtype, int64_t M, int N, int64_t K) {
   // Few channels fill a tile badly, but those calls are bound by HBM (1,048,576 x 256 -> 4 bf16: forward 1093 us in
   // multiply-adds and 132 here, backward 2551 and 278).
   const double least = dtype == FS_BF16 ? 16777216.0 : 134217728.0;
+  const bool large = work >= least && std::max(M, K) < (1LL << 31) - 512;
+  // Few rows of a forward have a kernel that reads W once for four of them, 16 columns a block.  Where that is a block an SM or
+  // more it is taken up to kLinearFew rows; with fewer, its time is the rows times the terms, and past a limit the
+  // other path is faster (us here, there): bf16 2048 -> 2048, 4 rows 9.1, 11.4, 5 rows 12.2, 11.4; 4096 -> 1024, 2 rows
+  // 9.6, 11.5, 3 rows 12.7, 11.6, 8 rows 29, 11.7; where the other path are multiply-adds: fp32 4096 -> 1024, 4 rows 20, 27, 6 rows
+  // 33, 27; bf16 8192 -> 256, 2 rows 17, 18, 7 rows 50, 18.
+  p.few = op == kLinFwd && M <= kLinearFew && (N >= 16 * num_sms() || M * K <= (large ? 8192 : 16384));
   // (dx of 4 rows of 1024, 4096 channels of g: 29 us in multiply-adds and 11 here, of 8 rows of 8192, 8192: 530 and 36;
   // fp32 437 and 238.)
-  p.path = work >= least && (M > kLinearFew || op != kLinFwd) && std::max(M, K) < (1LL << 31) - 512;
+  p.path = large && !p.few;
   int64_t splits;
   if (p.path) {
     // Pairs of CTAs take tiles; where there are fewer than half as many tiles, sums are split into parts of
@@ -139,7 +146,7 @@ LinearPlan linear_plan(int op, int dtype, int64_t M, int N, int64_t K) {
     // launches more, 10.1 without).
     const int64_t tiles = ((M + 63) / 64) * ((N + 63) / 64);
     splits = std::max<int64_t>(1, std::min<int64_t>(2LL * num_sms() / tiles, (K + 127) / 128));
-    if (op == kLinFwd && M <= kLinearFew) splits = 1;
+    if (p.few) splits = 1;
     p.per = ((K + splits - 1) / splits + 15) / 16 * 16;
   }
   p.splits = (int)((K + p.per - 1) / p.per);

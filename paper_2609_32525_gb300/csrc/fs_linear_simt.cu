@@ -137,8 +137,9 @@ __global__ void __launch_bounds__(256) k_linear_simt_bwd(SimtArgs x, SimtArgs w,
 // Few rows through the forward: what counts is W, which is read once for four rows.  A warp owns four columns (a
 // dropout counter) and has the loads of 32 x 16 bytes of each on their way at a time; its lanes' sums are added by
 // shuffles.
-// One row, 1024 -> 4096 channels, bf16 with GELU: 7 us, 31 with the tiles above; eight rows 21, against 33, and
-// past eight the tensor cores take 18.
+// One row, 1024 -> 4096 channels, bf16 with GELU: 7 us, 31 with the tiles above; eight rows 11, 12 on the tensor cores.  From
+// five rows on W is read twice, and terms past a few thousand wait for one another: 4096 -> 4096, four rows 17 us against
+// 17, eight 32 against 19.
 template <typename T, bool kVec>
 __global__ void __launch_bounds__(128) k_linear_few(SimtArgs a) {
   const int64_t zero = grid_begin();
@@ -303,7 +304,7 @@ dim3 simt_grid(const SimtArgs& a) {
 template <typename T, int OP>
 cudaError_t run_simt(const LinearProblem& p, const LinearPlan& plan, const LinearEnd& e, void* scratch, cudaStream_t st) {
   const SimtArgs a = simt_args(p, plan, e, scratch);
-  if (OP == kLinFwd && p.M <= kLinearFew) {
+  if (OP == kLinFwd && plan.few) {
     const bool vec = p.K % (16 / (int)sizeof(T)) == 0;
     return launch(vec ? k_linear_few<T, true> : k_linear_few<T, false>, dim3((unsigned)((p.N + 15) / 16)), dim3(128), 0, st, a);
   }

@@ -21,3 +21,25 @@ def test_backward(lib, R, K, N, dtype):
     assert lib.linear_path_for_shape(lib.make_linear(R, K, N, t.DTYPES[dtype]), True) == (R * K * N >= (1 << 24 if dtype == "bf16" else 1 << 27))
     t.check_backward(lib, R, K, N, dtype, seed=R)
     t.check_backward(lib, R, K, N, dtype, "gelu", 0.25, dres=True, inplace=True, want_dw=False, seed=R + 1)
+
+
+@pytest.mark.gpu
+def test_narrow_forwards_go_by_rows_and_terms(lib):
+    """Fewer columns than 16 an SM: both sides of 8192 rows times terms, 16,384 where the other path are multiply-adds."""
+    assert lib.linear_path_for_shape(lib.make_linear(4, 2048, 2048, lib.FS_BF16)) == 0
+    assert lib.linear_path_for_shape(lib.make_linear(5, 2048, 2048, lib.FS_BF16)) == 1
+    assert lib.linear_path_for_shape(lib.make_linear(8, 2048, 8192, lib.FS_BF16)) == 0
+    assert lib.linear_path_for_shape(lib.make_linear(8, 4096, 2048, lib.FS_F32)) == 0
+    # a split sum has parts in the workspace
+    size = lambda R, K, N: lib.linear_workspace_bytes(lib.make_linear(R, K, N, lib.FS_F32))  # noqa: E731
+    assert size(4, 4096, 1024) == 256 and size(5, 4096, 1024) > 256
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("R, K, N, dtype", [(8, 4096, 1024, "bf16"), (3, 8192, 1024, "bf16"), (4, 8192, 256, "bf16"), (7, 8189, 250, "bf16"), (5, 2049, 2047, "bf16"),
+                                            (5, 4096, 1024, "f32"), (8, 8191, 130, "f32"), (2, 8192, 1024, "bf16"), (8, 1024, 2048, "f32"), (1, 8192, 16, "f32"),
+                                            (8, 2048, 2500, "bf16")])
+def test_forward(lib, R, K, N, dtype):
+    t.check_forward(lib, R, K, N, dtype, seed=R)
+    t.check_forward(lib, R, K, N, dtype, "gelu", 0.25, res=True, pre=True, seed=R + 1)
+    t.check_forward(lib, R, K, N, dtype, "relu", 0.1, res=True, inplace=True, seed=R + 2)
