@@ -119,10 +119,16 @@ LinearPlan linear_plan(int op, int dtype, int64_t M, int N, int64_t K) {
   const double work = (double)M * N * (double)K;
   // Below this many products of terms a block's start and the two CTAs' hand-overs cost more than multiply-adds (1024
   // rows of 64 -> 64 bf16: 17 us against 13, of 256 -> 256 fp32: 23 against 17, backward 49 against 25).
-  // Few channels fill a tile badly, but those calls are bound by HBM (1,048,576 x 256 -> 4 bf16: forward 1093 us in
-  // multiply-adds and 132 here, backward 2551 and 278).
+  // Few channels fill a tile badly, but bf16 calls of them are bound by HBM (1,048,576 x 256 -> 4: forward 1093 us in
+  // multiply-adds and 123 here, dx 481 and 145, dW 1968 and 130).
   const double least = dtype == FS_BF16 ? 16777216.0 : 134217728.0;
-  const bool large = work >= least && std::max(M, K) < (1LL << 31) - 512;
+  // fp32 rows are split into parts by 64 terms and multiplied by 128 columns, however few there are.  What one tile of
+  // multiply-adds holds, 64 columns and short sums (dW: 64 columns and 64 rows), takes less in those (1,048,576 rows, us
+  // there, here: forward 2 -> 64 135, 244, 32 -> 64 183, 249, 64 -> 64 291, 249; dx of 64 from 3 119, 197, from 64 293, 181; dW of 64 x 64
+  // 306, 473, of 128 x 64 598, 477), and a first map of few channels as much or less: 3 -> 256 527, 528, with GELU 725, 848; 2 -> 128 266,
+  // 246 and 365, 424.
+  const bool narrow = dtype == FS_F32 && (op == kLinDw ? M <= 64 && N <= 64 : (N <= 64 && K <= 32) || (op == kLinFwd && K < 16));
+  const bool large = work >= least && !narrow && std::max(M, K) < (1LL << 31) - 512;
   // Few rows of a forward have a kernel that reads W once for four of them, 16 columns a block.  Where that is a block an SM or
   // more it is taken up to kLinearFew rows; with fewer, its time is the rows times the terms, and past a limit the
   // other path is faster (us here, there): bf16 2048 -> 2048, 4 rows 9.1, 11.4, 5 rows 12.2, 11.4; 4096 -> 1024, 2 rows
