@@ -1,5 +1,5 @@
-// Linear maps in fp32 multiply-adds, for sizes that fill no tensor-core tiles and for rows that TMA
-// cannot address, and the fixed-order join of products whose sums were split.
+// Linear maps in fp32 multiply-adds, for sizes that fill no tensor-core tiles and for rows past TMA's coordinates, and the
+// fixed-order join of products whose sums were split.
 //
 // A block owns 64 x 64 values of D and runs over the sum in steps of 16, which it stages in shared
 // memory two deep; a thread owns 4 x 4 values, so that four neighbouring channels, which share a

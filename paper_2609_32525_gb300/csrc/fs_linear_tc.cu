@@ -114,7 +114,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Block<kGroups, kPer>
         const int blocks = w.blocks(g);
         for (int kb = 0; kb < blocks && ok; kb += g.seg) {
           const int half = issue.h.pick(sums), end = min(kb + g.seg, blocks);
-          ok = issue.take(half, sums, acc_empty, ab, status);
+          ok = issue.take(half, acc_empty, ab, status);
           const uint32_t d = tmem + half * 256;
           for (int b = kb; b < end && ok; b++) {
             ok = mbar_wait_w(&full[ring.i], ring.pass, ab, status);

@@ -49,8 +49,8 @@ struct TcArgs {
   CUtensorMap a, b, y, pre, res;
   LinearEnd e;
   int64_t M, K, per;
-  int N, ldy, n_tiles, m_tiles, tiles, units, bn, splits, stages, seg;  // ldy: pitch of y; seg: blocks of 64 terms taken out at a time
-  int step_n, step_m, step_split;                       // from a pair's unit to its next one
+  int N, ldy, n_tiles, tiles, units, bn, splits, stages, seg;  // ldy: pitch of y; seg: blocks of 64 terms taken out at a time
+  int step_n, step_m;                                   // from a pair's unit to its next one
   uint32_t stage_bytes, idesc, idesc_sum, a_step, b_step;  // steps: 16 terms on in a stage, in 16-byte units
   int a_mn, b_mn;
   int load_res, load_pre, store_pre, plain;             // plain: y, res and pre by plain accesses
@@ -64,7 +64,8 @@ struct TcArgs {
 };
 
 // The units of a pair, number `pair` and every pairs-th one after it; stepped, not divided, since an epilogue
-// warp's few hundred instructions a chunk run one after another.
+// warp's few hundred instructions a chunk run one after another.  Where sums are split there are no more units than pairs,
+// so that a step stays within its part.
 struct Unit {
   int m, n, split;
   int left;  // units from this one on, 0 or less: none
@@ -78,9 +79,7 @@ struct Unit {
     left -= pairs;
     n += g.step_n;
     m += g.step_m;
-    split += g.step_split;
     if (n >= g.n_tiles) n -= g.n_tiles, m++;
-    if (m >= g.m_tiles) m -= g.m_tiles, split++;
   }
   __device__ __forceinline__ int64_t k0(const TcArgs& g) const { return split * g.per; }
   __device__ __forceinline__ int blocks(const TcArgs& g) const {
@@ -89,8 +88,8 @@ struct Unit {
   }
 };
 
-// Which half of TMEM a segment's products go to.  Units with dbias use the first half for all and
-// columns of the second one for the sums; the others take turns.
+// Which half of TMEM a segment's products go to.  A unit with dbias, its pair's only one, uses the first half for all
+// and columns of the second one for the sums; the others take turns.
 struct Halves {
   uint32_t uses0 = 0, uses1 = 0;
   int turn = 0;
@@ -609,16 +608,11 @@ __device__ __forceinline__ void sum_epilogue(const Place& at, Boxes<END, float, 
 
 // ---- the products' issue -----------------------------------------------------------------------
 
-// Waits until a half of TMEM is free for a segment; into or out of a unit with dbias the other half has to be
-// read out as well.  By the leader's issuing warp.
+// Waits until a half of TMEM is free for a segment.  By the leader's issuing warp.
 struct Issuer {
   Halves h;
-  bool last_sums = false;
-  __device__ __forceinline__ bool take(int half, bool sums, uint64_t* acc_empty, Abort* ab, uint32_t* status) {
-    bool ok = mbar_wait_w(&acc_empty[half], (h.uses(half) & 1u) ^ 1u, ab, status);
-    if (ok && sums != last_sums && h.uses(half ^ 1))
-      ok = mbar_wait_w(&acc_empty[half ^ 1], (h.uses(half ^ 1) - 1) & 1u, ab, status);
-    last_sums = sums;
+  __device__ __forceinline__ bool take(int half, uint64_t* acc_empty, Abort* ab, uint32_t* status) {
+    const bool ok = mbar_wait_w(&acc_empty[half], (h.uses(half) & 1u) ^ 1u, ab, status);
     h.use(half);
     tc_fence_after();
     return ok;
@@ -671,7 +665,8 @@ bool make_map(CUtensorMap* map, const void* p, int size, int64_t cols, int64_t r
 // dbias as a product with ones takes the second half of TMEM, so that the unit that does it does nothing else
 // meanwhile.  Where a tile's columns are a small part of dW the other units would wait for that one: then two
 // kernels add g up (dW of 32,768 rows, 1024 x 4096: 328 us with the product, 205 without, 229 with the kernels).
-inline bool sums_apart(const TcArgs& g) { return g.n_tiles > 2; }
+// Up to two tiles of columns are at most 64 tiles (8192 rows of dW): one unit a pair, on all but small parts of a device.
+inline bool sums_apart(const TcArgs& g) { return g.n_tiles > 2 || g.units > num_sms() / 2; }
 // After the product: dbias by the kernels, and the join of split sums.
 inline cudaError_t finish(const TcArgs& g, const LinearProblem& p, const LinearPlan& plan, const LinearEnd& e, void* scratch,
                           int ld, cudaStream_t st) {
@@ -686,7 +681,7 @@ inline cudaError_t finish(const TcArgs& g, const LinearProblem& p, const LinearP
   return linear_join(p, plan.splits, static_cast<const float*>(scratch), g.part_sums, end, st);
 }
 
-// What both kinds of product need from their problem.  false: no tensor map.
+// What both kinds of product need from their problem.  false: no tensor map, or a plan that is not for this device.
 inline bool fill_args(TcArgs& g, const LinearProblem& p, const LinearPlan& plan, const LinearEnd& e, void* scratch) {
   const bool f32 = p.dtype == FS_F32, split = plan.splits > 1, dw = p.op == kLinDw;
   g.e = e;
@@ -694,11 +689,11 @@ inline bool fill_args(TcArgs& g, const LinearProblem& p, const LinearPlan& plan,
   g.a_mn = dw, g.b_mn = p.op != kLinFwd;
   g.bn = linear_tile_n(p.N, g.b_mn, f32);
   g.n_tiles = (p.N + g.bn - 1) / g.bn;
-  g.m_tiles = (int)((p.M + 255) / 256);
-  g.tiles = g.m_tiles * g.n_tiles;
+  g.tiles = (int)((p.M + 255) / 256) * g.n_tiles;
   g.units = g.tiles * plan.splits;
+  if (split && g.units > num_sms() / 2) return false;  // Unit::next does not step from part to part
   const int pairs = std::min(g.units, num_sms() / 2);
-  g.step_n = pairs % g.n_tiles, g.step_m = pairs / g.n_tiles % g.m_tiles, g.step_split = pairs / g.tiles;
+  g.step_n = pairs % g.n_tiles, g.step_m = pairs / g.n_tiles;
   g.idesc = idesc_bf16(256, g.bn, g.a_mn, g.b_mn);
   g.idesc_sum = idesc_bf16(256, 32, g.a_mn, false);
   g.a_step = g.a_mn ? 128 : 2, g.b_step = g.b_mn ? 128 : 2;
