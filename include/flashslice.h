@@ -426,8 +426,11 @@ fs_status fs_ckpt_unpack(const fs_rows* s, const int8_t* q8, const uint8_t* e8, 
  * layer, another step) get different offsets.
  *
  * Sums are fp32.  FS_BF16: products of bf16 values, exact; GELU and SILU to 2^-16 of themselves (where
- * they are below 2^-119: to 2^-119), their derivatives to 2^-19; y, pre and dx rounded to bf16.  FS_F32: fp32
- * throughout, sums of products to a few 2^-24 of their terms' magnitudes.  Infinities and NaN
+ * they are below 2^-119: to 2^-119), their derivatives to 2^-19; y, pre and dx rounded to bf16.  FS_F32:
+ * fp32 throughout; on tensor cores operands in three bf16 parts, which leave out at most 2^-25 of a value, or
+ * 2^-134 where that is more.  A sum of K products whose magnitudes add up to S is off by at most
+ * (180 + K / 128) 2^-24 S where the result is fp32 (dW and dbias always), and (180 + K / 8) 2^-24 S before it is
+ * rounded to bf16; terms of random sign give fp32 results within 3e-7 of their norm.  Infinities and NaN
  * in x, W, g or a bias go through sums, activations and residuals as in fp32 arithmetic, and to no
  * results that they do not enter; a dropped value is 0 whatever it was.
  *
