@@ -237,7 +237,8 @@ __global__ void __launch_bounds__(256) k_linear_join(int64_t M, int N, int ld, i
 }
 
 // The sums of g's columns over ranges of rows, 16 bytes of columns a thread and 8 rows a block at a time, and
-// their sum in order.
+// their sum in order.  A thread adds up eight rows in pairs and these sums in turn, the parts go to eight chains: of a
+// million rows a value is rounded some 150 times, not 1200 (of N(0, 1) 2.4e-7 of the norm, 5.8e-7 in one chain each).
 template <typename T, int kV>
 __global__ void __launch_bounds__(256) k_linear_sums(const T* g, int64_t rows, int C, int ld, float* part) {
   __shared__ float sm[8][32 * kV];
@@ -247,15 +248,19 @@ __global__ void __launch_bounds__(256) k_linear_sums(const T* g, int64_t rows, i
   const int64_t r1 = min(r0 + per, rows);
   float s[kV] = {};
   if (c < C) {
-#pragma unroll 8
-    for (int64_t r = r0 + threadIdx.y; r < r1; r += 8) {
-      if constexpr (kV == 1) {
-        s[0] += (float)g[r * ld + c];
-      } else {
-        const uint4 w = *reinterpret_cast<const uint4*>(g + r * ld + c);
-        const T* t = reinterpret_cast<const T*>(&w);
+    for (int64_t r = r0 + threadIdx.y; r < r1; r += 64) {
+      struct alignas(sizeof(T) * kV) {
+        T v[kV];
+      } w[8];
 #pragma unroll
-        for (int i = 0; i < kV; i++) s[i] += (float)t[i];
+      for (int j = 0; j < 8; j++) {
+        if constexpr (kV == 1) w[j].v[0] = r + 8 * j < r1 ? g[(r + 8 * j) * ld + c] : T(0.f);
+        else *reinterpret_cast<uint4*>(&w[j]) = r + 8 * j < r1 ? *reinterpret_cast<const uint4*>(g + (r + 8 * j) * ld + c) : make_uint4(0, 0, 0, 0);
+      }
+#pragma unroll
+      for (int i = 0; i < kV; i++) {
+        auto two = [&](int j) { return (float)w[j].v[i] + (float)w[j + 1].v[i]; };
+        s[i] += (two(0) + two(2)) + (two(4) + two(6));
       }
     }
   }
@@ -269,15 +274,18 @@ __global__ void __launch_bounds__(256) k_linear_sums(const T* g, int64_t rows, i
     if (blockIdx.x * 32 * kV + i < C) part[(int64_t)blockIdx.y * C + blockIdx.x * 32 * kV + i] = t;
   }
 }
+// parts: a multiple of 8.
 __global__ void __launch_bounds__(128) k_linear_sums_join(const float* part, int C, int parts, LinearEnd e) {
   grid_begin(part);
   const int c = blockIdx.x * 128 + threadIdx.x;
   if (c >= C) return;
-  float s = 0.f;
-#pragma unroll 8
-  for (int p = 0; p < parts; p++) s += part[(int64_t)p * C + c];
-  lin::end_sum(e, c, s);
+  float s[8] = {};
+  for (int p = 0; p < parts; p += 8)
+#pragma unroll
+    for (int i = 0; i < 8; i++) s[i] += part[(int64_t)(p + i) * C + c];
+  lin::end_sum(e, c, ((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7])));
 }
+static_assert(kLinearSumParts % 8 == 0);
 template <typename T, int kV>
 cudaError_t run_sums(const LinearProblem& p, int ld, float* part, const LinearEnd& e, cudaStream_t st) {
   const int C = (int)p.M;

@@ -48,3 +48,19 @@ def test_dbias(lib, R, K, N, shift, accumulate):
     off = tc.off(t.host(db), g.astype(np.float64).sum(0))
     print(R, K, N, accumulate, off)
     assert off < BOUND
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("R, K, N", [(1 << 20, 300, 64), (1 << 20, 258, 65), (300001, 2048, 40)])
+def test_dbias_of_many_rows(lib, R, K, N):
+    """By kernels of their own (Cin above 256): 128 sums of eight rows in turn, 3 additions in pairs, 8 threads, 16 parts and
+    3 additions of the chains are about 160 roundings by u / 2 at most, of running sums whose squares are half of the
+    result's on average: sqrt(160 / 2) u / 2 = 4.5 u."""
+    gen = torch.Generator(device="cuda").manual_seed(23)
+    x, g = (torch.randn(s, generator=gen, device="cuda") for s in ((R, K), (R, N)))
+    s = lib.make_linear(R, K, N, torch.float32)
+    dW, db = torch.empty(N, K, device="cuda"), torch.empty(N, device="cuda")
+    lib.fs_linear_bwd(s, x, None, g, 0, 0.0, None, None, None, None, dW, db, False, lib.linear_workspace(s, True))
+    off = tc.off(t.host(db), t.host(g.double().sum(0)))
+    print(R, K, N, off)
+    assert off < BOUND
