@@ -12,7 +12,7 @@
 //                  copy too, 16, 8 or 4 bytes at a time.
 //   warps 16..23   epilogue
 // An earlier form wrote the parts to memory first (a kernel of its own, 6 bytes written and read for 4):
-// 131,072 x 256 x 256 forward 155 us, here 128, 2.1 TB/s of what it cannot do without.  What bounds it: 2.0 us a block
+// 131,072 x 256 x 256 forward 155 us, here 120, 2.2 TB/s of what it cannot do without.  What bounds it: 2.0 us a block
 // of 64 terms in the loaders, whose products take 0.8, and behind an activation the epilogue, 2000 clocks for
 // a SILU of 32 x 16 values and more for the derivative of a GELU.
 #include "fs_linear_tc.cuh"

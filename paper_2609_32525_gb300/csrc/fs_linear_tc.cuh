@@ -717,7 +717,8 @@ inline bool fill_args(TcArgs& g, const LinearProblem& p, const LinearPlan& plan,
   }
   g.sums = dw && e.sums && !sums_apart(g);
   // Segments: where results are fp32, 256 terms of three parts; 512 of one, 1024 where dbias keeps the products
-  // waiting while a segment is taken out.
+  // waiting while a segment is taken out (bwd of 1,048,576 x 256 x 256 444 -> 430 us; by norm, terms of random sign are off
+  // by 9.9e-7 then, 4.9e-7 in segments of 512).
   g.seg = split || dw || f32 ? (f32 ? 4 : g.sums ? 16 : 8) : 1 << 30;
   g.plain = g.ldy * size % 16 != 0;
   if (g.plain) return true;
