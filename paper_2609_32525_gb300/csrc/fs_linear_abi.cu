@@ -134,7 +134,7 @@ LinearPlan linear_plan(int op, int dtype, int64_t M, int N, int64_t K) {
   // other path is faster (us here, there): bf16 2048 -> 2048, 4 rows 9.1, 11.4, 5 rows 12.2, 11.4; 4096 -> 1024, 2 rows
   // 9.6, 11.5, 3 rows 12.7, 11.6, 8 rows 29, 11.7; where the other path are multiply-adds: fp32 4096 -> 1024, 4 rows 20, 27, 6 rows
   // 33, 27; bf16 8192 -> 256, 2 rows 17, 18, 7 rows 50, 18.
-  p.few = op == kLinFwd && M <= kLinearFew && (N >= 16 * num_sms() || M * K <= (large ? 8192 : 16384));
+  p.few = op == kLinFwd && M <= kLinearFew && (M * K <= (large ? 8192 : 16384) || N >= 16 * num_sms());
   // (dx of 4 rows of 1024, 4096 channels of g: 29 us in multiply-adds and 11 here, of 8 rows of 8192, 8192: 530 and 36;
   // fp32 437 and 238.)
   p.path = large && !p.few;

@@ -145,7 +145,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreadsF32, 1)
     Ring<kStagesF32> ring;
     auto fetch = [&](const Unit& w, int kb, uint32_t after) {
       if (w.left <= 0) return;
-      const int64_t k = w.k0(g) + (int64_t)kb * 64, m = (int64_t)w.m * 256 + rank * 128;
+      const int64_t k = w.k0() + (int64_t)kb * 64, m = (int64_t)w.m * 256 + rank * 128;
       const int n = w.n * 128 + (int)rank * 64, col = 8 * piece;
       // the first piece's row and column, and where rows and columns end from there
       const int64_t row_a = g.a_mn ? k : m, row_b = g.b_mn ? k : n;
@@ -247,7 +247,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreadsF32, 1)
       for (Unit w(g, pair); w.left > 0 && ok; w.next(g, pairs)) {
         const int blocks = w.blocks(g), m = w.m * 256 + (int)rank * 128, n = w.n * 128 + (int)rank * 64;
         for (int kb = 0; kb < blocks; kb++) {
-          const int k = (int)(w.k0(g) + (int64_t)kb * 64);
+          const int k = (int)(w.k0() + (int64_t)kb * 64);
           ok = mbar_wait(&raw_empty, (issued & 1u) ^ 1u, ab, status);
           if (!ok) break;
           mbar_expect_tx(&raw_full, kRaw);

@@ -65,7 +65,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Block<kGroups, kPer>
       bool ok = true;
       for (Unit w(g, pair); w.left > 0 && ok; w.next(g, pairs)) {
         const int m = w.m * 256 + (int)rank * 128, n = w.n * g.bn + (int)rank * bhalf, blocks = w.blocks(g);
-        const int64_t k0 = w.k0(g);
+        const int64_t k0 = w.k0();
         Unit nw = w;
         nw.next(g, pairs);
         if (g.ahead && nw.left > 0) {

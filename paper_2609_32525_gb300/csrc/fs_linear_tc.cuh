@@ -64,13 +64,15 @@ struct TcArgs {
 };
 
 // The units of a pair, number `pair` and every pairs-th one after it; stepped, not divided, since an epilogue
-// warp's few hundred instructions a chunk run one after another.  Where sums are split there are no more units than pairs,
-// so that a step stays within its part.
+// warp's few hundred instructions a chunk run one after another.  Where sums are split a pair has one unit, so that no
+// step leaves its part.
 struct Unit {
-  int m, n, split;
+  int m, n;
   int left;  // units from this one on, 0 or less: none
+  int64_t first;
   __device__ __forceinline__ Unit(const TcArgs& g, int u) : left(g.units - u) {
-    split = u / g.tiles;
+    const int split = u / g.tiles;
+    first = split * g.per;
     const int t = u - split * g.tiles;
     m = t / g.n_tiles;
     n = t - m * g.n_tiles;
@@ -81,9 +83,11 @@ struct Unit {
     m += g.step_m;
     if (n >= g.n_tiles) n -= g.n_tiles, m++;
   }
-  __device__ __forceinline__ int64_t k0(const TcArgs& g) const { return split * g.per; }
+  // Its part of the sum, and the part's first term.
+  __device__ __forceinline__ int split(const TcArgs& g) const { return g.splits > 1 ? (int)(first / g.per) : 0; }
+  __device__ __forceinline__ int64_t k0() const { return first; }
   __device__ __forceinline__ int blocks(const TcArgs& g) const {
-    const int64_t k = g.K - k0(g) < g.per ? g.K - k0(g) : g.per;
+    const int64_t k = g.K - first < g.per ? g.K - first : g.per;
     return (int)((k + 63) >> 6);
   }
 };
@@ -512,7 +516,7 @@ __device__ __forceinline__ void row_epilogue(const Place& at, Boxes<END, T, kPer
 #pragma unroll
                              for (int j = 0; j < 16; j++) v[j] = __uint_as_float(r[j]);
                            });
-      box.send(row0, col, w.split);
+      box.send(row0, col, 0);  // (split sums are fp32)
       if (box.loads && box.serial) start_next(1);
     }
     c -= chunks;
@@ -548,7 +552,7 @@ __device__ __forceinline__ void sum_epilogue(const Place& at, Boxes<END, float, 
   };
   for (Unit w(g, at.pair); w.left > 0 && ok; w.next(g, at.pairs)) {
     const int64_t row0 = at.row(w);
-    const int col = w.n * g.bn + first, blocks = w.blocks(g);
+    const int col = w.n * g.bn + first, blocks = w.blocks(g), part = w.split(g);
     const bool sums = g.sums && w.n == 0, many = blocks > g.seg;
     float acc[kMost][16], sum = 0.f;
     box.start(0, row0, col);
@@ -586,7 +590,7 @@ __device__ __forceinline__ void sum_epilogue(const Place& at, Boxes<END, float, 
     if (!ok) break;
     if (many) tmem_wait_st();
     if (END == kEndRaw && sums && at.wg == 0 && row0 + at.lane < g.M) {
-      if (g.splits > 1) g.part_sums[(int64_t)w.split * g.M + row0 + at.lane] = sum;
+      if (g.splits > 1) g.part_sums[(int64_t)part * g.M + row0 + at.lane] = sum;
       else lin::end_sum(g.e, row0 + at.lane, sum);
     }
 #pragma unroll 1
@@ -600,7 +604,7 @@ __device__ __forceinline__ void sum_epilogue(const Place& at, Boxes<END, float, 
                                  piece(t + 32 * i + 16 * p, many ? 0 : 128, v);
                                  if (p == 1 && !more) at.release(half);
                                });
-      box.send(row0, col + i * 32, w.split);
+      box.send(row0, col + i * 32, part);
       if (box.serial && more) box.start(1, row0, col + (i + 1) * 32);
     }
   }
